@@ -69,13 +69,15 @@ typedef enum {
     DFA_ERR_SHAPE = -2,     /* B, H, N <= 0; D != 64; w < 1; r < 1; head offset outside      */
                             /* [0, r); scale not finite or <= 0; for the index map, gather   */
                             /* and placement also w > N, N % w != 0, w % r != 0; for the     */
-                            /* projections sizes that the tiles do not divide                */
+                            /* projections sizes that the tiles do not divide; for 8-bit     */
+                            /* operands also pitches below the rows they hold, and blocks    */
+                            /* and pages of other sizes than the entry point names           */
     DFA_ERR_BRANCHES = -3,  /* nb < 1 or nb > DFA_MAX_BRANCHES                               */
     DFA_ERR_DTYPE = -4,     /* unknown dfa_dtype_t                                           */
     DFA_ERR_ALIGN = -5,     /* a base pointer or stride breaks the 16-byte row alignment     */
     DFA_ERR_LAUNCH = -6,    /* the HIP runtime refused an allocation, copy or launch         */
     DFA_ERR_TOO_LARGE = -7, /* index arithmetic would overflow the kernel's 32-bit counters  */
-    DFA_ERR_WORKSPACE = -8  /* a workspace was passed that is smaller than dfa_workspace_bytes() */
+    DFA_ERR_WORKSPACE = -8  /* a workspace was passed that is smaller than the entry point's ..._workspace_bytes() */
 } dfa_status_t;
 
 typedef enum { DFA_BF16 = 0, DFA_F32 = 1 } dfa_dtype_t;
@@ -314,6 +316,62 @@ int dfa_encoder_stack(const void *x, const void *w_qkv, const void *w_o, int32_t
                       const dfa_branch_t *branches, int32_t nb, const int32_t *head_offsets,
                       void *qkv_ws, void *attn_ws, void *y, void *workspace, size_t workspace_bytes,
                       void *stream);
+
+/*
+ * ---- Products of 8-bit operands --------------------------------------------------------------------------------------------
+ * A quantised matrix of `rows` rows of `cols` elements: OCP e4m3 values in blocks that share a power of two, 2^e with the smallest
+ * e >= -126 for which the block's largest finite |x| is at most 448 * 2^e.  A value is the e4m3 number nearest to x / 2^e (ties to even); x that is
+ * not finite is NaN.  A block is 128 elements of a row (block_rows = 1), or 128 rows by 128 columns (block_rows = 128: the same
+ * values for the matrix and its transpose, the form for weights that a backward pass reads too).
+ *   values  device, bytes [rows][ld], ld (a multiple of 128) at least cols; columns from cols to the next multiple of 128 hold 0
+ *   scales  device, bytes [ld / 128][ld_scales], e + 127 of the block that holds row r and columns 128 c .. 128 c + 127 at
+ *           [c][r] (128 equal ones for a 128 x 128 block); ld_scales (a multiple of 16) at least rows
+ * Both 16-byte aligned; ld < 2^23.
+ */
+typedef struct { void *values; void *scales; int64_t ld; int64_t ld_scales; } dfa_quantized_t;
+
+/*
+ * Quantises x (device, dtype dt, [rows][cols] with row pitch ldx, any alignment; rows on 16-byte boundaries are read faster).
+ *   q    (host struct or NULL)  receives x: blocks along its columns
+ *   q_t  (host struct or NULL)  receives x transposed, [cols][rows]: blocks along x's rows (what a product that contracts over
+ *        x's rows reads)
+ * Writes values up to the next multiple of 128 columns and scales up to the next multiple of 16 rows.  Asynchronous on `stream`.
+ */
+int dfa_quantize(const void *x, dfa_dtype_t dt, int64_t rows, int64_t cols, int64_t ldx, int32_t block_rows,
+                 const dfa_quantized_t *q, const dfa_quantized_t *q_t, void *stream);
+
+/*
+ * y[m][n] = sum_k a[m][k] * b[n][k] of the values that a [M][K] and b [N][K] hold: exact products, fp32 sums, rounded once to dt.
+ *   y          device, dtype dt, [M][N] with row pitch ldy (elements); must not overlap a or b
+ *   workspace  device, 16-byte aligned, dfa_quantized_product_workspace_bytes(M, N, K) (0 = none, NULL allowed): partial sums of
+ *              products whose k-steps are shared out over workgroups.  Written and read by this call only: calls that may
+ *              overlap need one each.
+ * The sums are in a fixed order: equal calls give equal results.  Asynchronous on `stream`; allocates nothing.
+ */
+size_t dfa_quantized_product_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int dfa_quantized_product(dfa_quantized_t a, dfa_quantized_t b, void *y, dfa_dtype_t dt, int64_t M, int64_t N, int64_t K, int64_t ldy,
+                          void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The projection dfa_linear with a quantised weight: x (device, dtype dt, [M][K] with row pitch ldx) is quantised by the call in blocks
+ * of 1 x 128, y[m][n] = sum_k x[m][k] * w[n][k] as above, y of x's dtype.  Any M, N, K >= 1.  Up to 64 rows take one launch and
+ * no workspace; others quantise into the workspace first.
+ */
+size_t dfa_quantized_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int dfa_quantized_linear(const void *x, dfa_dtype_t dt, int64_t ldx, dfa_quantized_t w, void *y, int64_t M, int64_t N, int64_t K, int64_t ldy,
+                         void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Gradients of y = x . w^T for a gradient dy [M][N] of y (the quantisation of x and w is passed through as the identity):
+ *   dx [M][K] = dy . w    dy in 1 x 128 blocks along N; w_t: w transposed, [K][N] (quantised with block_rows = 128 it holds the forward's
+ *                         values)
+ *   dw [N][K] = dy^T . x  dy and x in blocks of 128 along M, each column on its own; fp32
+ * dy, x and dx have dtype dt.  dx or dw may be NULL (not wanted): x is read for dw only, w_t for dx only.
+ */
+size_t dfa_quantized_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int dfa_quantized_linear_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx, dfa_dtype_t dt, dfa_quantized_t w_t, void *dx,
+                                  int64_t lddx, float *dw, int64_t lddw, int64_t M, int64_t N, int64_t K, void *workspace, size_t workspace_bytes,
+                                  void *stream);
 
 /* Empties the plan cache of every device; a plan is freed (its device synchronised) as soon as no
  * call is using it any more. */

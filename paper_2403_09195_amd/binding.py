@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 from .build import LIB_PATH, TORCH_MODULE_PATH
 
@@ -22,6 +23,8 @@ EXPORTS = [
     "dfa_forward_alloc", "dfa_forward_static",
     "dfa_forward_branch", "dfa_merge", "dfa_gather", "dfa_scatter", "dfa_plan_describe", "dfa_plan_describe_forward",
     "dfa_release_plans", "dfa_linear", "dfa_encoder_stack", "dfa_backward",
+    "dfa_quantize", "dfa_quantized_product", "dfa_quantized_product_workspace_bytes", "dfa_quantized_linear",
+    "dfa_quantized_linear_workspace_bytes", "dfa_quantized_linear_backward", "dfa_quantized_linear_backward_workspace_bytes",
 ]
 BENCH_EXPORTS = ["dfa_launch_describe", "dfa_launch_image", "dfa_forward_timed", "dfa_mfma_peak", "dfa_dense_unfused", "dfa_dense_unfused_workspace_bytes"]
 
@@ -35,6 +38,10 @@ class Strides(ctypes.Structure):
 
 
 FORM_TILES, FORM_SHORT, FORM_SPLIT = 0, 1, 2
+
+
+class Quantized(ctypes.Structure):
+    _fields_ = [("values", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("ld", ctypes.c_int64), ("ld_scales", ctypes.c_int64)]
 
 
 class Launch(ctypes.Structure):
@@ -112,15 +119,20 @@ def lib():
         L.dfa_dense_unfused_workspace_bytes.argtypes = [i32, i32, i32, i32]
         L.dfa_dense_unfused.argtypes = [vp, vp, vp, Strides, Strides, Strides, i32, i32, i32, i32, f32, vp, vp, vp,
                                         ctypes.c_size_t, vp]
+        qm, st = Quantized, ctypes.c_size_t
+        L.dfa_quantize.argtypes = [vp, ctypes.c_int, i64, i64, i64, i32, ctypes.POINTER(qm), ctypes.POINTER(qm), vp]
+        L.dfa_quantized_product.argtypes = [qm, qm, vp, ctypes.c_int, i64, i64, i64, i64, vp, st, vp]
+        L.dfa_quantized_linear.argtypes = [vp, ctypes.c_int, i64, qm, vp, i64, i64, i64, i64, vp, st, vp]
+        L.dfa_quantized_linear_backward.argtypes = [vp, i64, vp, i64, ctypes.c_int, qm, vp, i64, vp, i64, i64, i64, i64, vp, st, vp]
+        for name in ("dfa_quantized_product", "dfa_quantized_linear", "dfa_quantized_linear_backward"):
+            getattr(L, name + "_workspace_bytes").argtypes = [i64, i64, i64]
         for name in EXPORTS + BENCH_EXPORTS:
-            if name not in ("dfa_error_string", "dfa_workspace_bytes", "dfa_dense_unfused_workspace_bytes"):
-                getattr(L, name).restype = ctypes.c_int
+            if name != "dfa_error_string":
+                getattr(L, name).restype = ctypes.c_size_t if name.endswith("_workspace_bytes") else ctypes.c_int
         from . import _dfa_torch
         _dfa_torch.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.dfa_forward_alloc, L.dfa_backward)))
         global _native_forward, _native_backward
         _native_forward, _native_backward = _dfa_torch.forward, _dfa_torch.backward
-        L.dfa_workspace_bytes.restype = ctypes.c_size_t
-        L.dfa_dense_unfused_workspace_bytes.restype = ctypes.c_size_t
         _lib = L
     return _lib
 
@@ -595,3 +607,176 @@ def launch_image(B, H, N, branches, head_offsets=None, dtype_code=DFA_BF16, back
 
 def release_plans():
     _check(lib().dfa_release_plans(), "dfa_release_plans")
+
+
+# ---- 8-bit operands ----------------------------------------------------------------------------------------------------------
+
+class QuantizedMatrix(NamedTuple):
+    """A matrix [rows, cols] in e4m3 with a power of two for each block (include/dfa.h): values float8_e4m3fn [rows, ld >= cols], scales
+    uint8 [ld // 128, >= rows] (exponent + 127; entry [c, r] is that of row r, columns 128 c .. 128 c + 127)."""
+    values: "torch.Tensor"
+    scales: "torch.Tensor"
+    cols: int
+
+
+def _up(n, of):
+    return -(-n // of) * of
+
+
+def _device(*tensors):
+    """The one GPU that all these (name, tensor) live on."""
+    dev = None
+    for name, t in tensors:
+        _gpu(t, name)
+        if dev is not None and t.get_device() != dev:
+            raise RuntimeError(f"{name} lives on another GPU than {tensors[0][0]}")
+        dev = t.get_device()
+    return dev
+
+
+def _elsewhere(dev):
+    """Whether `dev` is not the current device: calls then run again with it current (launches go to the current device's stream)."""
+    import torch
+    return dev != torch.cuda.current_device()
+
+
+def _quantized(m, name):
+    """The C struct of a QuantizedMatrix, whose arrays hold what its shape says."""
+    import torch
+    v, s = m.values, m.scales
+    if v.dtype != torch.float8_e4m3fn or s.dtype != torch.uint8:
+        raise TypeError(f"{name}: float8_e4m3fn values and uint8 scales expected")
+    if v.dim() != 2 or s.dim() != 2 or v.stride(1) != 1 or s.stride(1) != 1:
+        raise ValueError(f"{name}: values and scales must be two-dimensional with contiguous rows")
+    rows, need = v.shape[0], _up(m.cols, 128)
+    if m.cols < 1 or v.shape[1] < need or s.shape[0] < need // 128 or s.shape[1] < _up(rows, 16):
+        raise DfaError(-2, f"{name} holds less than its {rows} x {m.cols} elements")
+    return Quantized(v.data_ptr(), s.data_ptr(), v.stride(0) if rows > 1 else v.shape[1], s.stride(0) if s.shape[0] > 1 else s.shape[1])
+
+
+def _rows_of(t, name):
+    """(rows, row pitch) of a tensor read as a matrix of its last dimension: contiguous, or two-dimensional with contiguous rows."""
+    cols = t.shape[-1] if t.dim() else 0
+    if cols and t.dim() == 2 and (t.stride(1) == 1 or cols == 1) and (t.stride(0) >= cols or t.shape[0] == 1):
+        return t.shape[0], max(t.stride(0), cols)
+    if not cols or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous, or two-dimensional with contiguous rows")
+    return t.numel() // cols, cols
+
+
+def _call_workspace(workspace, need, like):
+    """(pointer, bytes, tensor to record) of a call's workspace argument, as in _workspace()."""
+    import torch
+    if isinstance(workspace, str) and workspace == "auto":
+        if not need:
+            return None, 0, None
+        t = torch.empty((need,), dtype=torch.uint8, device=like.device)
+        return t.data_ptr(), need, None          # allocated on this stream: later work of this stream only gets its memory
+    if workspace is None:
+        return None, 0, None
+    _device(("x", like), ("workspace", workspace))
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+
+
+def _keep(workspace):
+    """A workspace of the caller's is read after the call returns."""
+    import torch
+    if workspace is not None:
+        workspace.record_stream(torch.cuda.current_stream())
+
+
+def _empty_quantized(rows, cols, like):
+    import torch
+    ld = _up(cols, 128)
+    return QuantizedMatrix(torch.empty((rows, ld), dtype=torch.float8_e4m3fn, device=like.device),
+                           torch.empty((ld // 128, _up(rows, 16)), dtype=torch.uint8, device=like.device), cols)
+
+
+def quantize(x, block_rows=1, transpose=False):
+    """x [R, C] (bf16 or fp32, contiguous rows) -> QuantizedMatrix of x, of its transpose (transpose=True), or both (transpose="both").
+    block_rows: 1 for blocks of 128 along the result's rows, 128 for 128 x 128 blocks."""
+    import torch
+    dev = _device(("x", x))
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return quantize(x, block_rows, transpose)
+    if x.dim() != 2:
+        raise ValueError("quantize: x must be a matrix")
+    code, (R, ld), C = _dtype_code(x), _rows_of(x, "x"), x.shape[1]
+    q = _empty_quantized(R, C, x) if transpose in (False, "both") else None
+    qt = _empty_quantized(C, R, x) if transpose else None
+    _check(lib().dfa_quantize(x.data_ptr(), code, R, C, ld, block_rows, ctypes.byref(_quantized(q, "q")) if q else None,
+                              ctypes.byref(_quantized(qt, "q_t")) if qt else None, _stream()), "dfa_quantize")
+    return (q, qt) if q and qt else q or qt
+
+
+def _result(out, shape, dtype, like, name):
+    """A result tensor: the caller's, if it is what the call writes, or a new one.  Returns (tensor, row pitch)."""
+    import torch
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=like.device), shape[-1]
+    _device(("x", like), (name, out))
+    if out.dtype != dtype or tuple(out.shape) != tuple(shape):
+        raise DfaError(-2, f"{name} must be {dtype} {tuple(shape)}")
+    return out, _rows_of(out, name)[1]
+
+
+def quantized_product(a, b, dtype, out=None, workspace="auto"):
+    """y [M, N] of `dtype` (bf16 or fp32): y[m][n] = sum_k a[m][k] b[n][k] of QuantizedMatrix a [M, K] and b [N, K]."""
+    import torch
+    dev = _device(("a", a.values), ("a.scales", a.scales), ("b", b.values), ("b.scales", b.scales))
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return quantized_product(a, b, dtype, out, workspace)
+    qa, qb, M, N = _quantized(a, "a"), _quantized(b, "b"), a.values.shape[0], b.values.shape[0]
+    if a.cols != b.cols:
+        raise DfaError(-2, f"a has {a.cols} columns, b {b.cols}")
+    y, ldy = _result(out, (M, N), dtype, a.values, "out")
+    need = lib().dfa_quantized_product_workspace_bytes(M, N, a.cols) if M and N else 0
+    ptr, size, keep = _call_workspace(workspace, need, a.values)
+    _check(lib().dfa_quantized_product(qa, qb, y.data_ptr(), _dtype_code(y), M, N, a.cols, ldy, ptr, size, _stream()), "dfa_quantized_product")
+    _keep(keep)
+    return y
+
+
+def quantized_linear(x, w, out=None, workspace="auto"):
+    """y = x . w^T of x's dtype (bf16 or fp32): x [..., K], quantised by the call in 1 x 128 blocks, w a QuantizedMatrix [N, K]."""
+    import torch
+    dev = _device(("x", x), ("w", w.values), ("w.scales", w.scales))
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return quantized_linear(x, w, out, workspace)
+    code, (M, ldx), N, K = _dtype_code(x), _rows_of(x, "x"), w.values.shape[0], w.cols
+    if x.shape[-1] != K:
+        raise DfaError(-2, f"x has {x.shape[-1]} columns, w {K}")
+    qw = _quantized(w, "w")
+    y, ldy = _result(out, x.shape[:-1] + (N,), x.dtype, x, "out")
+    need = lib().dfa_quantized_linear_workspace_bytes(M, N, K) if M > 64 else 0
+    ptr, size, keep = _call_workspace(workspace, need, x)
+    _check(lib().dfa_quantized_linear(x.data_ptr(), code, ldx, qw, y.data_ptr(), M, N, K, ldy, ptr, size, _stream()), "dfa_quantized_linear")
+    _keep(keep)
+    return y
+
+
+def quantized_linear_backward(dy, x, w_t, want_dx=True, want_dw=True, workspace="auto"):
+    """(dx, dw) of quantized_linear for a gradient dy [..., N] of y: dx [..., K] of dy's dtype, dw fp32 [N, K]; None for what is not wanted.
+    w_t: QuantizedMatrix [K, N] of the transposed weight (quantize(w, 128, transpose=True) holds the forward's values)."""
+    import torch
+    dev = _device(("dy", dy), ("x", x), ("w_t", w_t.values), ("w_t.scales", w_t.scales))
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return quantized_linear_backward(dy, x, w_t, want_dx, want_dw, workspace)
+    code, (M, lddy), (Mx, ldx), N, K = _dtype_code(dy), _rows_of(dy, "dy"), _rows_of(x, "x"), w_t.cols, w_t.values.shape[0]
+    if x.dtype != dy.dtype:
+        raise DfaError(-4, "x must have dy's dtype")
+    if Mx != M or dy.shape[-1] != N or x.shape[-1] != K:
+        raise DfaError(-2, f"dy {tuple(dy.shape)}, x {tuple(x.shape)} and w_t {K} x {N} do not belong together")
+    qw = _quantized(w_t, "w_t")
+    dx = torch.empty(dy.shape[:-1] + (K,), dtype=dy.dtype, device=dy.device) if want_dx else None
+    dw = torch.empty((N, K), dtype=torch.float32, device=dy.device) if want_dw else None
+    need = lib().dfa_quantized_linear_backward_workspace_bytes(M, N, K) if M else 0
+    ptr, size, keep = _call_workspace(workspace, need, dy)
+    _check(lib().dfa_quantized_linear_backward(dy.data_ptr(), lddy, x.data_ptr(), ldx, code, qw, dx.data_ptr() if want_dx else None, K,
+                                               dw.data_ptr() if want_dw else None, K, M, N, K, ptr, size, _stream()), "dfa_quantized_linear_backward")
+    _keep(keep)
+    return dx, dw

@@ -245,10 +245,14 @@ int chip_of(int device, ChipShape* out) {
     return DFA_OK;
 }
 
-int current_chip(int* device, ChipShape* chip) {
+}  // namespace
+
+int dfa::current_chip(int* device, ChipShape* chip) {
     if (hipGetDevice(device) != hipSuccess) return DFA_ERR_LAUNCH;
     return chip_of(*device, chip);
 }
+
+namespace {
 
 // Looks the plan of the current device up, building and uploading it on first use (the only device
 // allocation the library makes).  Plans pushed out of the cache are freed once no call holds them.
@@ -443,13 +447,13 @@ const char* dfa_error_string(int code) {
     switch (code) {
         case DFA_OK: return "ok";
         case DFA_ERR_NULL: return "a required pointer is NULL";
-        case DFA_ERR_SHAPE: return "bad shape, branch (w, r), head offset or scale";
+        case DFA_ERR_SHAPE: return "bad shape, branch (w, r), head offset, block, page or scale";
         case DFA_ERR_BRANCHES: return "number of branches outside 1..DFA_MAX_BRANCHES";
         case DFA_ERR_DTYPE: return "unknown dtype";
         case DFA_ERR_ALIGN: return "pointer or stride breaks 16-byte row alignment";
         case DFA_ERR_LAUNCH: return "HIP runtime error (allocation, copy or launch)";
         case DFA_ERR_TOO_LARGE: return "problem too large for the kernel's index arithmetic";
-        case DFA_ERR_WORKSPACE: return "workspace smaller than dfa_workspace_bytes() asks for";
+        case DFA_ERR_WORKSPACE: return "workspace smaller than the call's ..._workspace_bytes() asks for";
         default: return "unknown error code";
     }
 }

@@ -62,6 +62,9 @@ struct ChipShape {
     int32_t fwd_slots_per_die() const { return fwd_slots() / (dies > 0 ? dies : 1); }
 };
 
+// The current device and its shape (dfa_api.hip); a dfa_status_t.
+int current_chip(int* device, ChipShape* chip);
+
 // Split launches (few workgroups, see split_plan): workgroup g of the launch walks share `part` of `nparts` of the
 // 64-key steps of launch item `item` and leaves its partial result in block `block` of the workspace
 // (kSplitBlockBytes: out [256 rows][64] in fp16, each row divided by its largest magnitude, then lse [256] and

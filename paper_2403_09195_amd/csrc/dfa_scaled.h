@@ -1,0 +1,129 @@
+// What the operators on 8-bit operands share (gfx950): e4m3 values in blocks with a power of two each.
+//
+// A block's scale is 2^e with the smallest e >= -126 for which its largest finite |x| is at most 448 * 2^e (448 is the largest
+// e4m3 number), held as the byte e + 127.  A value is the e4m3 number nearest to x / 2^e, ties to even; what is not finite is NaN.
+// Powers of two, because x / 2^e is then exact in fp32 (one rounding, to e4m3, in all), because a value times its scale is
+// exact in bf16, because moving held values to a larger scale changes only those that fall below e4m3's normal range, and
+// because the matrix instruction multiplies by them on its way (its scale operands are these bytes).
+#pragma once
+#include "dfa_device.h"
+
+namespace dfa {
+
+constexpr int kScaleBlock = 128;            // elements of a row that share a scale
+constexpr uint32_t kLeastScaleByte = 1;     // 2^-126
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4s __attribute__((ext_vector_type(4)));
+typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+// |x| as an ordered integer, 0 for what is not finite.
+__device__ __forceinline__ uint32_t finite_magnitude(float x) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x) & 0x7fffffffu;
+    return u < 0x7f800000u ? u : 0u;
+}
+
+// The scale byte of a block whose largest magnitude is `amax`: with amax = m * 2^E, 1 <= m < 2, e = E - 8 where m <= 1.75 (448 = 1.75 * 2^8)
+// and E - 7 above.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
+    const int32_t byte = (int32_t)(amax >> 23) - 8 + ((amax & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return byte > (int32_t)kLeastScaleByte ? (uint32_t)byte : kLeastScaleByte;
+}
+
+// 2^e and 2^-e of a scale byte in 1 .. 253.
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+__device__ __forceinline__ float inverse_scale(uint32_t byte) { return __builtin_bit_cast(float, (254u - byte) << 23); }
+
+// Four values, |x * inv| <= 448 or not finite, as e4m3 (the conversion makes NaN of infinities).
+__device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d, float inv) {
+    int v = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, v, true);
+}
+
+// Eight e4m3 values as bf16 numbers times their scale: exact (a value has 4 significant bits).
+__device__ __forceinline__ bf16x8 scaled_bf16(uint32_t lo, uint32_t hi, float scale) {
+    typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
+    const bf16x2v a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+    const bf16x2v c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// N consecutive elements as fp32, in loads of 16 bytes (`vec`: p is aligned for them and all N exist) or one by one, 0 behind `have`.
+template <typename T, int N>
+__device__ __forceinline__ void load_row(const T* p, int64_t have, bool vec, float (&x)[N]) {
+    constexpr int kPer = 16 / (int)sizeof(T);
+    static_assert(N % kPer == 0, "whole 16-byte loads");
+    if (vec && have >= N) {
+#pragma unroll
+        for (int i = 0; i < N / kPer; ++i) {
+            const u32x4s v = reinterpret_cast<const u32x4s*>(p)[i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t u = v[j];         // (a bit cast of the element itself takes element 0)
+                if constexpr (sizeof(T) == 4) {
+                    x[4 * i + j] = __builtin_bit_cast(float, u);
+                } else {
+                    x[8 * i + 2 * j] = __builtin_bit_cast(float, u << 16);
+                    x[8 * i + 2 * j + 1] = __builtin_bit_cast(float, u & 0xffff0000u);
+                }
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = i < have ? (float)p[i] : 0.f;
+    }
+}
+
+// Largest value over the 16 lanes of a row of lanes, left in all of them.
+__device__ __forceinline__ uint32_t row16_max(uint32_t x) {
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, true));     // quad_perm [1, 0, 3, 2]
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, true));     // quad_perm [2, 3, 0, 1]
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x124, 0xF, 0xF, true));    // row_ror 4
+    return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xF, 0xF, true)); // row_ror 8
+}
+
+// Arguments of the quantisation: x [rows][cols] -> values [rows][ldv] with bytes [ldv / 128][lds], and / or the transposed matrix
+// values_t [cols][ldv_t] with bytes [ldv_t / 128][lds_t].
+struct QuantizeParams {
+    const void* x;
+    int64_t ldx, rows, cols;
+    uint8_t *values, *scales, *values_t, *scales_t;
+    int64_t ldv, lds, ldv_t, lds_t;
+    bool vec;                               // rows of x start on 16-byte boundaries
+};
+hipError_t launch_quantize(const QuantizeParams& p, bool f32, bool square, hipStream_t st);
+
+// y[m][n] = sum_k a[m][k] b[n][k] with a [M][K], b [N][K] quantised along k.
+struct ProductParams {
+    const uint8_t *a, *a_scales, *b, *b_scales;
+    int64_t lda, lds_a, ldb, lds_b;
+    void* y;
+    int64_t ldy, M, N;
+    int32_t n_k;                            // 128-k steps
+    float* parts;                           // [splits][M][N] partial sums where splits > 1
+    int32_t splits;
+    bool vec;                               // rows of y start on 16-byte boundaries
+};
+// How a product is cut into tiles, and its k-steps over workgroups.
+struct ProductShape {
+    int32_t tile;                           // rows and features of a tile
+    int32_t splits;
+};
+ProductShape product_shape(int64_t M, int64_t N, int32_t n_k, const ChipShape& chip);
+hipError_t launch_product(const ProductParams& p, const ProductShape& shape, const ChipShape& chip, bool f32, hipStream_t st);
+
+// The product for few rows, a being the unquantised x [M][K], K elements of each row.
+constexpr int64_t kFewRows = 64;
+struct FewRowsParams {
+    const void* x;
+    int64_t ldx, M, N, K;
+    const uint8_t *b, *b_scales;
+    int64_t ldb, lds_b;
+    void* y;
+    int64_t ldy;
+    bool vec_x, vec_y;                      // rows start on 16-byte boundaries
+};
+hipError_t launch_few_rows(const FewRowsParams& p, bool f32, hipStream_t st);
+
+}  // namespace dfa
