@@ -373,6 +373,53 @@ int dfa_quantized_linear_backward(const void *dy, int64_t lddy, const void *x, i
                                   int64_t lddx, float *dw, int64_t lddw, int64_t M, int64_t N, int64_t K, void *workspace, size_t workspace_bytes,
                                   void *stream);
 
+/*
+ * ---- Attention over keys and values held in 8 bits -------------------------------------------------------------------------
+ * A cache of `pages` pages of `page` tokens (16, 32, 64 or 128) of `heads` heads of D (64 or 128) channels, in e4m3 with one
+ * power of two per page and head for the keys and one for the values (format as above: the block is the tokens that the page holds):
+ *   k       device, [pages][heads][page][D]       16-byte aligned
+ *   v       device, [pages][heads][D][page]       16-byte aligned; a channel's tokens lie side by side
+ *   scales  device, bytes [pages][heads][2]       exponent + 127 of the keys and of the values
+ * It needs no initialisation.  Sequence b of a call has token n in slot n % page of page table[b * ld_table + n / page]:
+ *   table   device, int32 [B][width], width * page tokens at most; entries behind the last token are not used.  A page outside
+ *           0 .. pages - 1 is skipped: nothing is written to it, its tokens are attended to by no row.
+ *   lengths device, int32 [B]: tokens that sequence b holds, those of this step included
+ *   counts  device, int32 [B], or NULL for all: how many of the call's T (or M) rows of sequence b there are, the first ones; the last of
+ *           them is token lengths[b] - 1
+ */
+typedef struct { void *k; void *v; void *scales; int32_t pages; int32_t heads; int32_t page; int32_t D; } dfa_cache_t;
+
+/*
+ * Writes rows 0 .. n - 1 (n = counts[b], T without counts) of k and v as tokens lengths[b] - n .. lengths[b] - 1 of every sequence.
+ *   k, v   device, dtype dt, [B, T, heads, D] through strides (every row 16-byte aligned)
+ * A page's scale holds its new tokens and is not below what its earlier tokens (of this sequence, slots before the first new one) have;
+ * where it grows, those move to it: values are rounded to the new scale, a change only below e4m3's normal range.  Slots behind the last new token
+ * and pages without new tokens are left as they were.  Tokens before 0 or behind the table's last page are dropped.  No two sequences of a call may
+ * write to one page.  Asynchronous on `stream`; allocates nothing.
+ */
+int dfa_cache_append(const void *k, const void *v, dfa_strides_t sk, dfa_strides_t sv, dfa_dtype_t dt, int32_t B, int32_t T, dfa_cache_t cache,
+                     const int32_t *table, int32_t width, int64_t ld_table, const int32_t *lengths, const int32_t *counts, void *stream);
+
+/*
+ * out[b, i, h] = softmax(scale * q[b, i, h] . k) v over tokens of head h / (H / heads) of sequence b, and its lse.
+ *   q       device, dtype dt, [B, M, H, D] through strides (every row 16-byte aligned); H a multiple of cache.heads
+ *   causal  0: a row attends to all lengths[b] tokens; otherwise row i of the n = counts[b] (M) attends to the first
+ *           lengths[b] - (n - 1 - i): the rows are the sequence's last tokens.
+ *   out     device, dtype dt, contiguous [B, M, H, D];  lse device, fp32 [B, H, M], or NULL
+ *           rows that attend to nothing (no tokens, i >= counts[b]) are 0 and -inf; lengths outside 0 .. width * page count as the
+ *           nearest of them
+ *   max_length  host: no sequence is expected to be longer (longer ones are right, but slower).  It decides how the walk is shared out.
+ *   workspace   device, 16-byte aligned, dfa_cache_attention_workspace_bytes() of the same arguments (0 = none, NULL allowed); written and
+ *           read by this call only: calls that may overlap, captured ones among them, need one each.
+ * dt = DFA_BF16: bf16 operands, probabilities rounded to bf16 before the second product, fp32 sums and statistics; dt = DFA_F32: 24-bit
+ * operands throughout.  Keys, values and rows that are not finite reach only the rows that attend to them.  One launch, two where the walk is shared
+ * out over workgroups; equal calls give equal results.  Asynchronous on `stream`; allocates nothing.
+ */
+size_t dfa_cache_attention_workspace_bytes(int32_t B, int32_t M, int32_t H, int32_t heads, int32_t D, dfa_dtype_t dt, int64_t max_length);
+int dfa_cache_attention(const void *q, dfa_strides_t sq, dfa_dtype_t dt, int32_t B, int32_t M, int32_t H, dfa_cache_t cache, const int32_t *table,
+                        int32_t width, int64_t ld_table, const int32_t *lengths, const int32_t *counts, int32_t causal, float scale, int64_t max_length,
+                        void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Empties the plan cache of every device; a plan is freed (its device synchronised) as soon as no
  * call is using it any more. */
 int dfa_release_plans(void);

@@ -25,6 +25,7 @@ EXPORTS = [
     "dfa_release_plans", "dfa_linear", "dfa_encoder_stack", "dfa_backward",
     "dfa_quantize", "dfa_quantized_product", "dfa_quantized_product_workspace_bytes", "dfa_quantized_linear",
     "dfa_quantized_linear_workspace_bytes", "dfa_quantized_linear_backward", "dfa_quantized_linear_backward_workspace_bytes",
+    "dfa_cache_append", "dfa_cache_attention", "dfa_cache_attention_workspace_bytes",
 ]
 BENCH_EXPORTS = ["dfa_launch_describe", "dfa_launch_image", "dfa_forward_timed", "dfa_mfma_peak", "dfa_dense_unfused", "dfa_dense_unfused_workspace_bytes"]
 
@@ -42,6 +43,10 @@ FORM_TILES, FORM_SHORT, FORM_SPLIT = 0, 1, 2
 
 class Quantized(ctypes.Structure):
     _fields_ = [("values", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("ld", ctypes.c_int64), ("ld_scales", ctypes.c_int64)]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "scales")] + [(n, ctypes.c_int32) for n in ("pages", "heads", "page", "D")]
 
 
 class Launch(ctypes.Structure):
@@ -126,6 +131,9 @@ def lib():
         L.dfa_quantized_linear_backward.argtypes = [vp, i64, vp, i64, ctypes.c_int, qm, vp, i64, vp, i64, i64, i64, i64, vp, st, vp]
         for name in ("dfa_quantized_product", "dfa_quantized_linear", "dfa_quantized_linear_backward"):
             getattr(L, name + "_workspace_bytes").argtypes = [i64, i64, i64]
+        L.dfa_cache_append.argtypes = [vp, vp, Strides, Strides, ctypes.c_int, i32, i32, Cache, vp, i32, i64, vp, vp, vp]
+        L.dfa_cache_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, ctypes.c_int, i64]
+        L.dfa_cache_attention.argtypes = [vp, Strides, ctypes.c_int, i32, i32, i32, Cache, vp, i32, i64, vp, vp, i32, f32, i64, vp, vp, vp, st, vp]
         for name in EXPORTS + BENCH_EXPORTS:
             if name != "dfa_error_string":
                 getattr(L, name).restype = ctypes.c_size_t if name.endswith("_workspace_bytes") else ctypes.c_int
@@ -780,3 +788,101 @@ def quantized_linear_backward(dy, x, w_t, want_dx=True, want_dw=True, workspace=
                                                dw.data_ptr() if want_dw else None, K, M, N, K, ptr, size, _stream()), "dfa_quantized_linear_backward")
     _keep(keep)
     return dx, dw
+
+
+class KvCache(NamedTuple):
+    """Keys and values in e4m3 with a power of two per page and head (include/dfa.h): k float8_e4m3fn [pages, heads, page, D], v float8_e4m3fn
+    [pages, heads, D, page], scales uint8 [pages, heads, 2] (keys, values; exponent + 127)."""
+    k: "torch.Tensor"
+    v: "torch.Tensor"
+    scales: "torch.Tensor"
+
+
+def kv_cache(pages, heads, page=64, D=64, device="cuda"):
+    """An empty KvCache."""
+    import torch
+    return KvCache(torch.zeros((pages, heads, page, D), dtype=torch.float8_e4m3fn, device=device),
+                   torch.zeros((pages, heads, D, page), dtype=torch.float8_e4m3fn, device=device),
+                   torch.zeros((pages, heads, 2), dtype=torch.uint8, device=device))
+
+
+def _cache(cache):
+    """The C struct of a KvCache, whose arrays are what its shape says."""
+    import torch
+    k, v, s = cache.k, cache.v, cache.scales
+    if k.dtype != torch.float8_e4m3fn or v.dtype != torch.float8_e4m3fn or s.dtype != torch.uint8:
+        raise TypeError("cache: float8_e4m3fn keys and values and uint8 scales expected")
+    if k.dim() != 4 or not (k.is_contiguous() and v.is_contiguous() and s.is_contiguous()):
+        raise ValueError("cache: keys, values and scales must be contiguous")
+    pages, heads, page, D = k.shape
+    if tuple(v.shape) != (pages, heads, D, page) or tuple(s.shape) != (pages, heads, 2):
+        raise DfaError(-2, f"cache: values {tuple(v.shape)} and scales {tuple(s.shape)} do not belong to keys {tuple(k.shape)}")
+    return Cache(k.data_ptr(), v.data_ptr(), s.data_ptr(), pages, heads, page, D)
+
+
+def _sequences(table, lengths, counts, B):
+    """Checks of what names a call's sequences: (table pointer, width, its pitch, lengths pointer, counts pointer)."""
+    import torch
+    for t, name, shape in ((table, "table", None), (lengths, "lengths", (B,)), (counts, "counts", (B,))):
+        if t is None and name == "counts":
+            continue
+        if t.dtype != torch.int32:
+            raise TypeError(f"{name} must be int32")
+        if shape is not None and (tuple(t.shape) != shape or not t.is_contiguous()):
+            raise DfaError(-2, f"{name} must be contiguous and have an entry for each of {B} sequences")
+    if table.dim() != 2 or table.shape[0] != B or table.shape[1] < 1 or table.stride(1) != 1:
+        raise DfaError(-2, f"table must be [{B}, width] with contiguous rows")
+    width = table.shape[1]
+    return table.data_ptr(), width, table.stride(0) if B > 1 else width, lengths.data_ptr(), None if counts is None else counts.data_ptr()
+
+
+def cache_append(k, v, cache, table, lengths, counts=None):
+    """Writes k, v [B, T, heads, D] (bf16 or fp32, may be strided views) into the pages of a KvCache as the last tokens of every sequence.
+    table int32 [B, width]: pages of the sequences; lengths int32 [B]: tokens held, the new ones included; counts int32 [B]: how many of the T
+    rows there are (None: all)."""
+    import torch
+    dev = _device(("k", k), ("v", v), ("cache.k", cache.k), ("cache.v", cache.v), ("cache.scales", cache.scales), ("table", table),
+                  ("lengths", lengths), *(() if counts is None else (("counts", counts),)))
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return cache_append(k, v, cache, table, lengths, counts)
+    c, sk, sv, code = _cache(cache), _strides(k), _strides(v), _dtype_code(k)
+    if v.dtype != k.dtype:
+        raise DfaError(-4, "v must have k's dtype")
+    B, T, heads, D = k.shape
+    if v.shape != k.shape or heads != c.heads or D != c.D:
+        raise DfaError(-2, f"k {tuple(k.shape)} and v {tuple(v.shape)} are not rows of a cache of {c.heads} heads of {c.D}")
+    names = _sequences(table, lengths, counts, B)
+    _check(lib().dfa_cache_append(k.data_ptr(), v.data_ptr(), sk, sv, code, B, T, c, *names, _stream()), "dfa_cache_append")
+
+
+def cache_attention(q, cache, table, lengths, scale, causal=True, counts=None, max_length=None, out=None, want_lse=True, workspace="auto"):
+    """Attention of q [B, M, H, D] (bf16 or fp32, may be a strided view) over the tokens that a KvCache holds -> (out [B, M, H, D], lse fp32
+    [B, H, M] or None).  H is a multiple of the cache's heads.  causal: the rows are each sequence's last tokens and attend to those before
+    them and themselves; otherwise to all `lengths`.  table, lengths, counts as in cache_append.  max_length: no sequence is expected to be longer
+    (None: what the table has room for)."""
+    import torch
+    dev = _device(("q", q), ("cache.k", cache.k), ("cache.v", cache.v), ("cache.scales", cache.scales), ("table", table), ("lengths", lengths),
+                  *(() if counts is None else (("counts", counts),)))
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return cache_attention(q, cache, table, lengths, scale, causal, counts, max_length, out, want_lse, workspace)
+    c, sq, code = _cache(cache), _strides(q), _dtype_code(q)
+    B, M, H, D = q.shape
+    if D != c.D or H % c.heads:
+        raise DfaError(-2, f"q {tuple(q.shape)} does not go with a cache of {c.heads} heads of {c.D}")
+    names = _sequences(table, lengths, counts, B)
+    limit = min(names[1] * c.page, names[1] * c.page if max_length is None else int(max_length))
+    if out is None:
+        out = torch.empty((B, M, H, D), dtype=q.dtype, device=q.device)
+    else:
+        _device(("q", q), ("out", out))
+        if out.dtype != q.dtype or out.shape != q.shape or not out.is_contiguous():
+            raise DfaError(-2, f"out must be a contiguous {q.dtype} {tuple(q.shape)}")
+    lse = torch.empty((B, H, M), dtype=torch.float32, device=q.device) if want_lse else None
+    need = lib().dfa_cache_attention_workspace_bytes(B, M, H, c.heads, D, code, limit)
+    ptr, size, keep = _call_workspace(workspace, need, q)
+    _check(lib().dfa_cache_attention(q.data_ptr(), sq, code, B, M, H, c, *names, int(bool(causal)), scale, limit, out.data_ptr(),
+                                     lse.data_ptr() if want_lse else None, ptr, size, _stream()), "dfa_cache_attention")
+    _keep(keep)
+    return out, lse

@@ -6,7 +6,7 @@
 #include <new>
 
 #include "../../include/dfa.h"
-#include "dfa_scaled.h"
+#include "dfa_cache.h"
 
 namespace {
 
@@ -103,6 +103,34 @@ int run_product(const dfa_quantized_t& a, const dfa_quantized_t& b, void* y, dfa
 // Sizes of a quantisation whose grid is counted in 32 bits.
 bool quantize_fits(int64_t rows, int64_t cols) {
     return rows <= kMaxSize && cols <= kMaxSize && up(rows, 32) / 32 * (up(cols, 128) / 128) <= kMaxSize;
+}
+
+// Sizes of a cache and of what addresses it; lengths and pages themselves are device memory, which the kernels bound.
+int check_cache(const dfa_cache_t& c, int32_t B, const int32_t* table, int32_t width, int64_t ld_table, const int32_t* lengths, int32_t* page_shift) {
+    if (!c.k || !c.v || !c.scales || !table || !lengths) return DFA_ERR_NULL;
+    *page_shift = c.page == 16 ? 4 : c.page == 32 ? 5 : c.page == 64 ? 6 : c.page == 128 ? 7 : 0;
+    if (!*page_shift || (c.D != 64 && c.D != 128) || c.pages < 1 || c.heads < 1 || B < 1 || width < 1 || ld_table < width) return DFA_ERR_SHAPE;
+    if (!aligned16(c.k) || !aligned16(c.v) || !matrix_aligned(table, 4) || !matrix_aligned(lengths, 4)) return DFA_ERR_ALIGN;
+    return (int64_t)width * c.page > kMaxSize - 256 ? DFA_ERR_TOO_LARGE : DFA_OK;
+}
+
+CacheView view(const dfa_cache_t& c, int32_t page_shift, const int32_t* table, int32_t width, int64_t ld_table, const int32_t* lengths, const int32_t* counts) {
+    return CacheView{static_cast<uint8_t*>(c.k), static_cast<uint8_t*>(c.v), static_cast<uint8_t*>(c.scales), c.pages, c.heads, page_shift,
+                     table, ld_table, width, lengths, counts};
+}
+
+bool rows_aligned(const void* p, const dfa_strides_t& s, int64_t es) {
+    return aligned16(p) && s.b * es % 16 == 0 && s.n * es % 16 == 0 && s.h * es % 16 == 0;
+}
+
+int64_t attention_bytes(const CacheAttentionShape& s, int32_t B, int32_t heads) {
+    return s.splits > 1 ? up((int64_t)B * heads * s.row_tiles * s.splits * s.part_floats * 4, 256) : 0;
+}
+
+int check_attention_sizes(int32_t B, int32_t M, int32_t H, int32_t heads, int32_t D, int64_t max_length) {
+    if (B < 1 || M < 1 || heads < 1 || H < heads || H % heads || (D != 64 && D != 128) || max_length < 0) return DFA_ERR_SHAPE;
+    if ((int64_t)M * (H / heads) > kMaxSize - 256 || max_length > kMaxSize - 256) return DFA_ERR_TOO_LARGE;
+    return DFA_OK;
 }
 
 bool room(const void* workspace, size_t have, int64_t need) { return need == 0 || (workspace && have >= (size_t)need); }
@@ -213,6 +241,59 @@ int dfa_quantized_linear_backward(const void* dy, int64_t lddy, const void* x, i
     if (rc == DFA_OK && dw) rc = run_quantize(x, dt, M, K, ldx, false, nullptr, &xq_t, stream);
     if (rc == DFA_OK && dw) rc = run_product(dyq_t, xq_t, dw, DFA_F32, N, K, M, lddw, at, chip, stream);
     return rc;
+}
+
+int dfa_cache_append(const void* k, const void* v, dfa_strides_t sk, dfa_strides_t sv, dfa_dtype_t dt, int32_t B, int32_t T, dfa_cache_t cache,
+                     const int32_t* table, int32_t width, int64_t ld_table, const int32_t* lengths, const int32_t* counts, void* stream) {
+    if (!k || !v) return DFA_ERR_NULL;
+    if (!known(dt)) return DFA_ERR_DTYPE;
+    AppendParams p{};
+    int32_t shift = 0;
+    const int rc = check_cache(cache, B, table, width, ld_table, lengths, &shift);
+    if (rc != DFA_OK) return rc;
+    if (T < 1) return DFA_ERR_SHAPE;
+    if (!rows_aligned(k, sk, size_of(dt)) || !rows_aligned(v, sv, size_of(dt)) || !matrix_aligned(counts, 4)) return DFA_ERR_ALIGN;
+    // tokens start anywhere in a page, and no more pages than the table names are touched
+    const int64_t blocks = std::min(((int64_t)T + cache.page - 2) / cache.page + 1, (int64_t)width);
+    if (T > kMaxSize - 256 || B * blocks * 2 * cache.heads > kMaxSize) return DFA_ERR_TOO_LARGE;
+    p.k = k, p.skb = sk.b, p.skn = sk.n, p.skh = sk.h;
+    p.v = v, p.svb = sv.b, p.svn = sv.n, p.svh = sv.h;
+    p.cache = view(cache, shift, table, width, ld_table, lengths, counts);
+    p.B = B, p.T = T, p.page_blocks = (int32_t)blocks;
+    return launch_cache_append(p, dt == DFA_F32, cache.D, static_cast<hipStream_t>(stream)) == hipSuccess ? DFA_OK : DFA_ERR_LAUNCH;
+}
+
+size_t dfa_cache_attention_workspace_bytes(int32_t B, int32_t M, int32_t H, int32_t heads, int32_t D, dfa_dtype_t dt, int64_t max_length) {
+    if (!known(dt) || check_attention_sizes(B, M, H, heads, D, max_length) != DFA_OK) return 0;
+    return (size_t)attention_bytes(cache_attention_shape(B, M, H, heads, D, dt == DFA_F32, max_length, chip_or_default()), B, heads);
+}
+
+int dfa_cache_attention(const void* q, dfa_strides_t sq, dfa_dtype_t dt, int32_t B, int32_t M, int32_t H, dfa_cache_t cache, const int32_t* table,
+                        int32_t width, int64_t ld_table, const int32_t* lengths, const int32_t* counts, int32_t causal, float scale, int64_t max_length,
+                        void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!q || !out) return DFA_ERR_NULL;
+    if (!known(dt)) return DFA_ERR_DTYPE;
+    int32_t shift = 0;
+    int rc = check_cache(cache, B, table, width, ld_table, lengths, &shift);
+    if (rc == DFA_OK) rc = check_attention_sizes(B, M, H, cache.heads, cache.D, max_length);
+    if (rc != DFA_OK) return rc;
+    if (!std::isfinite(scale) || scale <= 0.f) return DFA_ERR_SHAPE;
+    if (!rows_aligned(q, sq, size_of(dt)) || !aligned16(out) || !matrix_aligned(lse, 4) || !matrix_aligned(counts, 4) || !aligned16(workspace)) return DFA_ERR_ALIGN;
+    ChipShape chip;
+    rc = this_chip(&chip);
+    if (rc != DFA_OK) return rc;
+    const CacheAttentionShape s = cache_attention_shape(B, M, H, cache.heads, cache.D, dt == DFA_F32, max_length, chip);
+    // (the merge takes up to eight workgroups for a tile)
+    if ((int64_t)B * cache.heads * s.row_tiles * std::max(s.splits, 8) > kMaxSize) return DFA_ERR_TOO_LARGE;
+    if (!room(workspace, workspace_bytes, attention_bytes(s, B, cache.heads))) return DFA_ERR_WORKSPACE;
+    CacheAttentionParams p{};
+    p.q = q, p.sqb = sq.b, p.sqn = sq.n, p.sqh = sq.h;
+    p.cache = view(cache, shift, table, width, ld_table, lengths, counts);
+    p.out = out, p.lse = lse, p.parts = static_cast<float*>(workspace);
+    p.scale_log2 = scale * kLog2e;
+    p.B = B, p.M = M, p.H = H, p.group = H / cache.heads, p.causal = causal ? 1 : 0;
+    p.row_tiles = s.row_tiles, p.splits = s.splits, p.split_chunks = s.split_chunks;
+    return launch_cache_attention(p, s, dt == DFA_F32, cache.D, static_cast<hipStream_t>(stream)) == hipSuccess ? DFA_OK : DFA_ERR_LAUNCH;
 }
 
 }  // extern "C"

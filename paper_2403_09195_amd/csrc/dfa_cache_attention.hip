@@ -1,0 +1,456 @@
+// Attention of a few or many query rows over the e4m3 cache (dfa_cache.h): out = softmax(scale q k^T) v over a sequence's tokens.
+//
+// Online softmax over chunks of 64 tokens.  A wave has 16 R query rows (query heads that share a head of the cache count as
+// rows) and walks every fourth chunk of its workgroup's share; the four waves' states are merged in LDS at the end, the workgroups' shares of
+// a long cache by a second launch.
+//
+// Matrix-core mapping (v_mfma_f32_16x16x32_bf16; lane = 16*g4 + r16).  S^T = K Q^T: A operand = 16 keys, B operand = 16 query rows;
+// O^T += V^T P^T: A operand = 16 channels, B operand = 16 query rows, contraction over keys.  Row m of the key block t is key 16*(m/4) + 4*t + m%4 of
+// the chunk, so a lane's scores of the four blocks are those of the 16 consecutive keys 16*g4 .. +15 of its query row, in order,
+// which is what the second product's B operand wants next to 16 bytes of a row of values.  Every operand goes from memory
+// to registers in 16-byte pieces and no score changes lanes.  e4m3 numbers times their scale are exact in bf16; one instruction makes
+// two of them.
+// Precision: scores, statistics and sums in fp32.  bf16 calls round the probabilities to bf16 before the second product (half a step, 2^-9 on
+// average, of each, which the sum over keys averages out; the row sum is taken before that rounding).  fp32 calls carry q and the probabilities as the
+// sum of three bf16 numbers, 24 bits, through both products.
+// Bound: the cache's bytes while there are few query rows (a chunk's conversions and products take a quarter of the time that its 8 or 16 KB take at
+// the rate of memory), the vector ALU (exponentials, conversions) beyond some 64 rows.
+#include <algorithm>
+
+#include "dfa_cache.h"
+#include "dfa_mfma.h"
+
+namespace dfa {
+
+namespace {
+
+constexpr int kShareWaves = 4;
+constexpr int kChunk = 64;                  // tokens
+constexpr float kLowest = -3e38f;           // a running maximum that has seen nothing
+
+// The four lanes of a query row (r16, in every group of 16) combine their values.
+__device__ __forceinline__ void lane_group_pair(float x, float& a, float& b) {
+    a = x;
+    b = x;
+    asm volatile("s_nop 1\n\tv_permlane16_swap_b32 %0, %1\n\ts_nop 1" : "+v"(a), "+v"(b));
+}
+__device__ __forceinline__ float row_max(float x) {
+    float a, b;
+    lane_group_pair(x, a, b);
+    return wave_half_max(fmaxf(a, b));
+}
+__device__ __forceinline__ float row_sum(float x) {
+    float a, b;
+    lane_group_pair(x, a, b);
+    return wave_half_sum(a + b);
+}
+
+// Parts of an operand: bf16 as it is, fp32 as the sum of three bf16 numbers.
+template <typename T> constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
+template <int N>
+__device__ __forceinline__ void split_parts(const float (&x)[8], bf16x8 (&part)[N]) {
+    float rest[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rest[i] = x[i];
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            part[n][i] = (__bf16)rest[i];
+            rest[i] -= (float)part[n][i];
+        }
+}
+
+// A row of a tile: query row i and head of the tile's row rho.
+struct QueryRow {
+    int i, head;
+};
+__device__ __forceinline__ QueryRow query_row(const CacheAttentionParams& p, int kv_head, int rho) {
+    const int i = rho / p.group;
+    return QueryRow{i, kv_head * p.group + (rho - i * p.group)};
+}
+
+// Tokens that query row i of sequence b attends to: the first `end`.
+__device__ __forceinline__ int row_end(const CacheAttentionParams& p, int length, int count, int i) {
+    if (i >= count) return 0;
+    return p.causal ? max(length - (count - 1 - i), 0) : length;
+}
+__device__ __forceinline__ int sequence_length(const CacheView& c, int b) {
+    return min(max(c.lengths[b], 0), c.width << c.page_shift);
+}
+__device__ __forceinline__ int sequence_count(const CacheAttentionParams& p, int b) {
+    return p.cache.counts ? min(max(p.cache.counts[b], 0), p.M) : p.M;
+}
+// Splits that hold some of a sequence's tokens; the last one takes what is behind it too.
+__device__ __forceinline__ int splits_used(const CacheAttentionParams& p, int length) {
+    const int chunks = (length + kChunk - 1) / kChunk;
+    return min(max((chunks + p.split_chunks - 1) / p.split_chunks, 1), p.splits);
+}
+
+template <typename T, int D, int R>
+__global__ __launch_bounds__(64 * kShareWaves) void cache_attention_kernel(CacheAttentionParams p) {
+    constexpr int NJ = D / 32, NB = D / 16, NP = kParts<T>;
+    __shared__ floatx4 merge_acc[kShareWaves / 2][R * NB][64];
+    __shared__ float merge_stat[kShareWaves / 2][2 * R][64];
+
+    const CacheView& c = p.cache;
+    const int tid = threadIdx.x;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r16 = lane & 15, g4 = lane >> 4;
+    uint32_t id = blockIdx.x;
+    const int split = id % p.splits;
+    id /= p.splits;
+    const int tile = id % p.row_tiles;
+    id /= p.row_tiles;
+    const int kv_head = id % c.heads, b = id / c.heads;
+
+    const int length = sequence_length(c, b), count = sequence_count(p, b), used = splits_used(p, length);
+    if (split >= used) return;
+    const int rows = p.M * p.group, row0 = tile * 16 * R;
+
+    // rows of the tile, the tokens they attend to, and the chunks that any of them does
+    int end[R], head[R], qi[R], most = 0, least = 0x7fffffff;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int rho = row0 + 16 * r + r16;
+        const QueryRow at = query_row(p, kv_head, min(rho, rows - 1));
+        qi[r] = at.i;
+        head[r] = at.head;
+        end[r] = rho < rows ? row_end(p, length, count, at.i) : 0;
+    }
+    {   // ends grow with i: the tile's first and last rows bound them, except for rows behind the sequence's count
+        const int last = min(row0 + 16 * R, rows) - 1, i_last = last / p.group, i_first = row0 / p.group;
+        most = i_first < count ? row_end(p, length, count, min(i_last, count - 1)) : 0;
+        least = i_last < count ? row_end(p, length, count, i_first) : 0;
+    }
+    const int chunks = (most + kChunk - 1) / kChunk;
+    const int c_begin = split * p.split_chunks, c_end = split == used - 1 ? chunks : min(chunks, c_begin + p.split_chunks);
+
+    // q: this lane's 8 channels of each product, 16*g4 + 8*(j & 1) + 64*(j / 2)
+    bf16x8 qf[R][NJ][NP];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const T* const src = static_cast<const T*>(p.q) + b * p.sqb + qi[r] * p.sqn + head[r] * p.sqh + 16 * g4;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            float x[8];
+            load_row<T, 8>(src + 8 * (j & 1) + 64 * (j / 2), 8, true, x);
+            split_parts<NP>(x, qf[r][j]);
+        }
+    }
+
+    floatx4 acc[R][NB];
+    float top[R], sum[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        top[r] = kLowest;
+        sum[r] = 0.f;
+#pragma unroll
+        for (int n = 0; n < NB; ++n) acc[r][n] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    // Pages of a chunk: a lane reads keys of 16-token group r16 / 4 and values of group g4 of it.
+    const int32_t* const table = c.table + b * c.ld_table;
+    const int group_shift = c.page_shift - 4, slot_mask = (1 << c.page_shift) - 1;
+    const int last_place = c.width - 1;
+    struct Pages {
+        int32_t k, v;
+    };
+    auto pages_of = [&](int chunk) {
+        const int kg = 4 * chunk + (r16 >> 2), vg = 4 * chunk + g4;
+        return Pages{table[min(kg >> group_shift, last_place)], table[min(vg >> group_shift, last_place)]};
+    };
+    u32x4s kr[4][D / 64], vr[NB];
+    uint32_t k_scale, v_scale;
+    auto load_k = [&](int chunk, int32_t page) {
+        const int64_t block = (int64_t)((uint32_t)page < (uint32_t)c.pages ? page : 0) * c.heads + kv_head;
+        const int slot = (kChunk * chunk + 16 * (r16 >> 2)) & slot_mask;
+        const uint8_t* const at = c.k + ((block << c.page_shift) + slot + (r16 & 3)) * D + 16 * g4;
+        k_scale = c.scales[2 * block];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int d = 0; d < D / 64; ++d) kr[t][d] = *reinterpret_cast<const u32x4s*>(at + 4 * t * D + 64 * d);
+    };
+    auto load_v = [&](int chunk, int32_t page) {
+        const int64_t block = (int64_t)((uint32_t)page < (uint32_t)c.pages ? page : 0) * c.heads + kv_head;
+        const int slot = (kChunk * chunk + 16 * g4) & slot_mask;
+        const uint8_t* const at = c.v + ((block * D + r16) << c.page_shift) + slot;
+        v_scale = c.scales[2 * block + 1];
+#pragma unroll
+        for (int n = 0; n < NB; ++n) vr[n] = *reinterpret_cast<const u32x4s*>(at + ((int64_t)(16 * n) << c.page_shift));
+    };
+
+    int chunk = c_begin + wave;
+    Pages now{0, 0}, next{0, 0};
+    if (chunk < c_end) {
+        now = pages_of(chunk);
+        load_k(chunk, now.k);
+        load_v(chunk, now.v);
+        if (chunk + kShareWaves < c_end) next = pages_of(chunk + kShareWaves);
+    }
+    for (; chunk < c_end; chunk += kShareWaves) {
+        const bool more = chunk + kShareWaves < c_end;
+        // ---- scores: element 4*t + i of s is key 64*chunk + 16*g4 + 4*t + i against query row r16 of block r
+        float s[R][16];
+        {
+            const float scale = scale_of(k_scale);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                floatx4 z[R];
+#pragma unroll
+                for (int r = 0; r < R; ++r) z[r] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    const u32x4s& w = kr[t][j / 2];
+                    const bf16x8 kf = scaled_bf16(w[2 * (j & 1)], w[2 * (j & 1) + 1], scale);
+#pragma unroll
+                    for (int r = 0; r < R; ++r)
+#pragma unroll
+                        for (int n = 0; n < NP; ++n) z[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][j][n], z[r], 0, 0, 0);
+                }
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[r][4 * t + i] = z[r][i] * p.scale_log2;
+            }
+        }
+        const bool v_there = (uint32_t)now.v < (uint32_t)c.pages;
+        if (more) {
+            load_k(chunk + kShareWaves, next.k);
+            now.k = next.k;
+        }
+        // ---- tokens that not every row attends to, pages that do not exist
+        const int key0 = kChunk * chunk + 16 * g4;
+        const bool masked = kChunk * (chunk + 1) > least || __any(!v_there);
+        if (masked) {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (!v_there || key0 + e >= end[r]) s[r][e] = -INFINITY;
+        }
+        // ---- probabilities
+        bf16x8 pf[R][2][NP];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float m = fmaxf(s[r][0], s[r][1]);
+#pragma unroll
+            for (int e = 2; e < 16; ++e) m = fmaxf(m, s[r][e]);
+            m = fmaxf(row_max(m), top[r]);
+            if (__any(m > top[r])) {
+                const float shrink = __builtin_amdgcn_exp2f(top[r] - m);
+                top[r] = m;
+                sum[r] *= shrink;
+#pragma unroll
+                for (int n = 0; n < NB; ++n) acc[r][n] *= shrink;
+            }
+            float w[2][8];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                w[e / 8][e % 8] = __builtin_amdgcn_exp2f(s[r][e] - m);
+                sum[r] += w[e / 8][e % 8];
+            }
+            split_parts<NP>(w[0], pf[r][0]);
+            split_parts<NP>(w[1], pf[r][1]);
+        }
+        // ---- values
+        if (masked) {
+            // A value behind every row's end, or on no page, may be anything: 0.  One that some rows attend to and is not a number must not reach
+            // the others through 0 * NaN: it is taken out as well, and the rows that attend to it are made NaN.
+            bool bad = false;
+            const int have = v_there ? min(max(most - key0, 0), 16) : 0;
+            if (have == 0) v_scale = 127;       // nor need the scale of such a page be one
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int keep = min(max(have - 4 * w, 0), 4);
+                    const uint32_t v = keep == 4 ? vr[n][w] : vr[n][w] & ((1u << (8 * keep)) - 1u);
+                    vr[n][w] = v;
+                    // a byte of 7 ones below its sign: the sum carries into bit 7 of that byte
+                    bad = bad || (((v & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+                }
+            if (__any(bad)) {
+                bf16x8 seen[R][2];
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) seen[r][e / 8][e % 8] = (__bf16)(v_there && key0 + e < end[r] ? 1.f : 0.f);
+#pragma unroll
+                for (int n = 0; n < NB; ++n) {
+                    bf16x8 nans[2];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const uint32_t byte = (vr[n][e / 4] >> (8 * (e % 4))) & 255u;
+                        nans[e / 8][e % 8] = (__bf16)((byte & 127u) == 127u ? 1.f : 0.f);
+                        if ((byte & 127u) == 127u) vr[n][e / 4] &= ~(255u << (8 * (e % 4)));
+                    }
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        floatx4 hits = {0.f, 0.f, 0.f, 0.f};
+                        hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nans[0], seen[r][0], hits, 0, 0, 0);
+                        hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nans[1], seen[r][1], hits, 0, 0, 0);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (hits[i] > 0.f) acc[r][n][i] = __builtin_nanf("");
+                    }
+                }
+            }
+        }
+        {
+            const float scale = scale_of(v_scale);
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const bf16x8 vf = scaled_bf16(vr[n][2 * h], vr[n][2 * h + 1], scale);
+#pragma unroll
+                    for (int r = 0; r < R; ++r)
+#pragma unroll
+                        for (int k = 0; k < NP; ++k) acc[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r][h][k], acc[r][n], 0, 0, 0);
+                }
+        }
+        if (more) {
+            load_v(chunk + kShareWaves, next.v);
+            now.v = next.v;
+            if (chunk + 2 * kShareWaves < c_end) next = pages_of(chunk + 2 * kShareWaves);
+        }
+    }
+
+    // ---- the four waves' states into one: 2 and 3 to 0 and 1, then 1 to 0
+#pragma unroll
+    for (int r = 0; r < R; ++r) sum[r] = row_sum(sum[r]);
+#pragma unroll
+    for (int half = kShareWaves / 2; half >= 1; half /= 2) {
+        if (wave >= half && wave < 2 * half) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                merge_stat[wave - half][2 * r][lane] = top[r];
+                merge_stat[wave - half][2 * r + 1][lane] = sum[r];
+#pragma unroll
+                for (int n = 0; n < NB; ++n) merge_acc[wave - half][r * NB + n][lane] = acc[r][n];
+            }
+        }
+        __syncthreads();
+        if (wave < half) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float other = merge_stat[wave][2 * r][lane], m = fmaxf(top[r], other);
+                const float mine = __builtin_amdgcn_exp2f(top[r] - m), theirs = __builtin_amdgcn_exp2f(other - m);
+                top[r] = m;
+                sum[r] = sum[r] * mine + merge_stat[wave][2 * r + 1][lane] * theirs;
+#pragma unroll
+                for (int n = 0; n < NB; ++n) acc[r][n] = acc[r][n] * mine + merge_acc[wave][r * NB + n][lane] * theirs;
+            }
+        }
+        __syncthreads();
+    }
+    if (wave != 0) return;
+
+    if (p.splits > 1) {
+        constexpr int kRows = 16 * R;
+        float* const part = p.parts + (((int64_t)b * c.heads + kv_head) * p.row_tiles + tile) * p.splits * (kRows * (D + 2)) + (int64_t)split * (kRows * (D + 2));
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+#pragma unroll
+            for (int n = 0; n < NB; ++n) *reinterpret_cast<floatx4*>(part + (16 * r + r16) * D + 16 * n + 4 * g4) = acc[r][n];
+            if (g4 == 0) {
+                part[kRows * D + 16 * r + r16] = top[r];
+                part[kRows * (D + 1) + 16 * r + r16] = sum[r];
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (row0 + 16 * r + r16 >= rows) continue;
+        const float scale = sum[r] == 0.f ? 0.f : 1.f / sum[r];
+        T* const out = static_cast<T*>(p.out) + (((int64_t)b * p.M + qi[r]) * p.H + head[r]) * D + 4 * g4;
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            const floatx4 o = acc[r][n] * scale;
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<floatx4*>(out + 16 * n) = o;
+            else *reinterpret_cast<bf16x4*>(out + 16 * n) = bf16x4{(__bf16)o[0], (__bf16)o[1], (__bf16)o[2], (__bf16)o[3]};
+        }
+        if (p.lse && g4 == 0) p.lse[((int64_t)b * p.H + head[r]) * p.M + qi[r]] = sum[r] == 0.f ? -INFINITY : (top[r] + __builtin_amdgcn_logf(sum[r])) * kLn2;
+    }
+}
+
+// Merges the splits of a tile's rows: D / 4 lanes to a row.
+template <typename T, int D, int R>
+__global__ __launch_bounds__(256) void cache_attention_merge_kernel(CacheAttentionParams p) {
+    constexpr int kRows = 16 * R, kLanes = D / 4, kRowsPerGroup = 256 / kLanes;
+    const CacheView& c = p.cache;
+    const int groups = (kRows + kRowsPerGroup - 1) / kRowsPerGroup;
+    uint32_t id = blockIdx.x;
+    const int in_tile = id % groups * kRowsPerGroup + (int)threadIdx.x / kLanes;
+    id /= groups;
+    const int tile = id % p.row_tiles;
+    const int kv_head = id / p.row_tiles % c.heads, b = id / p.row_tiles / c.heads;
+    const int rho = tile * kRows + in_tile, d = threadIdx.x % kLanes * 4;
+    if (in_tile >= kRows || rho >= p.M * p.group) return;
+    const int used = splits_used(p, sequence_length(c, b));
+    const float* const part = p.parts + (int64_t)id * p.splits * (kRows * (D + 2));
+    float top = kLowest;
+    for (int s = 0; s < used; ++s) top = fmaxf(top, part[s * (kRows * (D + 2)) + kRows * D + in_tile]);
+    float sum = 0.f;
+    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < used; ++s) {
+        const float* const at = part + s * (kRows * (D + 2));
+        const float w = __builtin_amdgcn_exp2f(at[kRows * D + in_tile] - top);
+        sum += w * at[kRows * (D + 1) + in_tile];
+        acc += *reinterpret_cast<const floatx4*>(at + in_tile * D + d) * w;
+    }
+    const QueryRow q = query_row(p, kv_head, rho);
+    const floatx4 o = acc * (sum == 0.f ? 0.f : 1.f / sum);
+    T* const out = static_cast<T*>(p.out) + (((int64_t)b * p.M + q.i) * p.H + q.head) * D + d;
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<floatx4*>(out) = o;
+    else *reinterpret_cast<bf16x4*>(out) = bf16x4{(__bf16)o[0], (__bf16)o[1], (__bf16)o[2], (__bf16)o[3]};
+    if (p.lse && d == 0) p.lse[((int64_t)b * p.H + q.head) * p.M + q.i] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+template <typename T, int D, int R>
+hipError_t launch(const CacheAttentionParams& p, hipStream_t st) {
+    const int64_t tiles = (int64_t)p.B * p.cache.heads * p.row_tiles;
+    hipLaunchKernelGGL((cache_attention_kernel<T, D, R>), dim3((unsigned)(tiles * p.splits)), dim3(64 * kShareWaves), 0, st, p);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && p.splits > 1) {
+        constexpr int kRowsPerGroup = 256 / (D / 4);
+        const int64_t groups = (16 * R + kRowsPerGroup - 1) / kRowsPerGroup;
+        hipLaunchKernelGGL((cache_attention_merge_kernel<T, D, R>), dim3((unsigned)(tiles * groups)), dim3(256), 0, st, p);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+// Most 16-row blocks of a tile: what 256 registers hold.
+int most_blocks(int32_t D, bool f32) { return (f32 ? 2 : 4) / (D / 64); }
+
+}  // namespace
+
+CacheAttentionShape cache_attention_shape(int32_t B, int32_t M, int32_t H, int32_t heads, int32_t D, bool f32, int64_t max_length, const ChipShape& chip) {
+    const int64_t rows = (int64_t)M * (H / heads);
+    CacheAttentionShape s;
+    s.blocks = 1;
+    while (16 * s.blocks < rows && s.blocks < most_blocks(D, f32)) s.blocks *= 2;
+    s.row_tiles = (int32_t)((rows + 16 * s.blocks - 1) / (16 * s.blocks));
+    const int64_t tiles = (int64_t)B * heads * s.row_tiles, chunks = (max_length + kChunk - 1) / kChunk;
+    // workgroups for four to a CU, each with a chunk for every wave at least
+    const int64_t wanted = std::min((4 * (int64_t)chip.cus + tiles - 1) / tiles, (chunks + kShareWaves - 1) / kShareWaves);
+    const int64_t per = (chunks + std::max(wanted, (int64_t)1) - 1) / std::max(wanted, (int64_t)1);
+    s.split_chunks = (int32_t)std::max((per + kShareWaves - 1) / kShareWaves * kShareWaves, (int64_t)kShareWaves);
+    s.splits = (int32_t)std::max((chunks + s.split_chunks - 1) / s.split_chunks, (int64_t)1);
+    s.part_floats = (int64_t)16 * s.blocks * (D + 2);
+    return s;
+}
+
+hipError_t launch_cache_attention(const CacheAttentionParams& p, const CacheAttentionShape& s, bool f32, int32_t D, hipStream_t st) {
+    if (f32) {
+        if (D == 128) return launch<float, 128, 1>(p, st);
+        return s.blocks == 1 ? launch<float, 64, 1>(p, st) : launch<float, 64, 2>(p, st);
+    }
+    if (D == 128) return s.blocks == 1 ? launch<__bf16, 128, 1>(p, st) : launch<__bf16, 128, 2>(p, st);
+    return s.blocks == 1 ? launch<__bf16, 64, 1>(p, st) : s.blocks == 2 ? launch<__bf16, 64, 2>(p, st) : launch<__bf16, 64, 4>(p, st);
+}
+
+}  // namespace dfa
