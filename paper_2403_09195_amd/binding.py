@@ -66,6 +66,7 @@ class DfaError(RuntimeError):
 _lib = None
 _native_forward = None       # the ordinary forward and backward calls in native code (csrc/dfa_torch.cpp), set by lib()
 _native_backward = None
+_native = None               # the module itself: the ordinary calls of the operators on 8-bit operands
 _i32p = ctypes.POINTER(ctypes.c_int32)
 
 
@@ -138,9 +139,11 @@ def lib():
             if name != "dfa_error_string":
                 getattr(L, name).restype = ctypes.c_size_t if name.endswith("_workspace_bytes") else ctypes.c_int
         from . import _dfa_torch
-        _dfa_torch.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.dfa_forward_alloc, L.dfa_backward)))
-        global _native_forward, _native_backward
-        _native_forward, _native_backward = _dfa_torch.forward, _dfa_torch.backward
+        _dfa_torch.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+            L.dfa_forward_alloc, L.dfa_backward, L.dfa_quantized_linear, L.dfa_quantized_linear_workspace_bytes, L.dfa_quantized_linear_backward,
+            L.dfa_quantized_linear_backward_workspace_bytes, L.dfa_cache_append, L.dfa_cache_attention, L.dfa_cache_attention_workspace_bytes)))
+        global _native_forward, _native_backward, _native
+        _native_forward, _native_backward, _native = _dfa_torch.forward, _dfa_torch.backward, _dfa_torch
         _lib = L
     return _lib
 
@@ -693,6 +696,16 @@ def _keep(workspace):
         workspace.record_stream(torch.cuda.current_stream())
 
 
+def _native_call(name, *args):
+    """An ordinary call in native code: what it returns, or None where it is for Python to convert it or to name what is wrong with it."""
+    if _native is None:
+        lib()
+    res = getattr(_native, name)(*args)
+    if type(res) is int:
+        raise DfaError(res, "dfa_" + name)
+    return res
+
+
 def _empty_quantized(rows, cols, like):
     import torch
     ld = _up(cols, 128)
@@ -749,6 +762,10 @@ def quantized_product(a, b, dtype, out=None, workspace="auto"):
 
 def quantized_linear(x, w, out=None, workspace="auto"):
     """y = x . w^T of x's dtype (bf16 or fp32): x [..., K], quantised by the call in 1 x 128 blocks, w a QuantizedMatrix [N, K]."""
+    if out is None and isinstance(workspace, str) and workspace == "auto":
+        res = _native_call("quantized_linear", x, w)
+        if res is not None:
+            return res
     import torch
     dev = _device(("x", x), ("w", w.values), ("w.scales", w.scales))
     if _elsewhere(dev):
@@ -769,6 +786,10 @@ def quantized_linear(x, w, out=None, workspace="auto"):
 def quantized_linear_backward(dy, x, w_t, want_dx=True, want_dw=True, workspace="auto"):
     """(dx, dw) of quantized_linear for a gradient dy [..., N] of y: dx [..., K] of dy's dtype, dw fp32 [N, K]; None for what is not wanted.
     w_t: QuantizedMatrix [K, N] of the transposed weight (quantize(w, 128, transpose=True) holds the forward's values)."""
+    if want_dx and want_dw and isinstance(workspace, str) and workspace == "auto":
+        res = _native_call("quantized_linear_backward", dy, x, w_t)
+        if res is not None:
+            return res
     import torch
     dev = _device(("dy", dy), ("x", x), ("w_t", w_t.values), ("w_t.scales", w_t.scales))
     if _elsewhere(dev):
@@ -840,6 +861,8 @@ def cache_append(k, v, cache, table, lengths, counts=None):
     """Writes k, v [B, T, heads, D] (bf16 or fp32, may be strided views) into the pages of a KvCache as the last tokens of every sequence.
     table int32 [B, width]: pages of the sequences; lengths int32 [B]: tokens held, the new ones included; counts int32 [B]: how many of the T
     rows there are (None: all)."""
+    if _native_call("cache_append", k, v, cache, table, lengths, counts):
+        return
     import torch
     dev = _device(("k", k), ("v", v), ("cache.k", cache.k), ("cache.v", cache.v), ("cache.scales", cache.scales), ("table", table),
                   ("lengths", lengths), *(() if counts is None else (("counts", counts),)))
@@ -861,6 +884,10 @@ def cache_attention(q, cache, table, lengths, scale, causal=True, counts=None, m
     [B, H, M] or None).  H is a multiple of the cache's heads.  causal: the rows are each sequence's last tokens and attend to those before
     them and themselves; otherwise to all `lengths`.  table, lengths, counts as in cache_append.  max_length: no sequence is expected to be longer
     (None: what the table has room for)."""
+    if out is None and want_lse and isinstance(workspace, str) and workspace == "auto":
+        res = _native_call("cache_attention", q, cache, table, lengths, scale, causal, counts, max_length)
+        if res is not None:
+            return res
     import torch
     dev = _device(("q", q), ("cache.k", cache.k), ("cache.v", cache.v), ("cache.scales", cache.scales), ("table", table), ("lengths", lengths),
                   *(() if counts is None else (("counts", counts),)))

@@ -391,15 +391,37 @@ __global__ __launch_bounds__(256) void cache_attention_merge_kernel(CacheAttenti
     if (in_tile >= kRows || rho >= p.M * p.group) return;
     const int used = splits_used(p, sequence_length(c, b));
     const float* const part = p.parts + (int64_t)id * p.splits * (kRows * (D + 2));
-    float top = kLowest;
-    for (int s = 0; s < used; ++s) top = fmaxf(top, part[s * (kRows * (D + 2)) + kRows * D + in_tile]);
-    float sum = 0.f;
+    // The loads of 16 splits at a time, before it is known which of them were used: every trip to memory takes a microsecond or two, of
+    // which an earlier form (eight at a time, behind the length) had three; 7.5 us for one image's row, @MERGE@ now.
+    constexpr int kAtOnce = 16, kPart = kRows * (D + 2);
+    float top = kLowest, sum = 0.f;
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < used; ++s) {
-        const float* const at = part + s * (kRows * (D + 2));
-        const float w = __builtin_amdgcn_exp2f(at[kRows * D + in_tile] - top);
-        sum += w * at[kRows * (D + 1) + in_tile];
-        acc += *reinterpret_cast<const floatx4*>(at + in_tile * D + d) * w;
+    for (int s0 = 0; s0 < p.splits; s0 += kAtOnce) {
+        float t[kAtOnce], l[kAtOnce];
+        floatx4 a[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const float* const at = part + (int64_t)min(s0 + u, p.splits - 1) * kPart;
+            t[u] = at[kRows * D + in_tile];
+            l[u] = at[kRows * (D + 1) + in_tile];
+            a[u] = *reinterpret_cast<const floatx4*>(at + in_tile * D + d);
+        }
+        if (s0 >= used) break;
+        float m = top;
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+            if (s0 + u < used) m = fmaxf(m, t[u]);
+        const float shrink = __builtin_amdgcn_exp2f(top - m);
+        sum *= shrink;
+        acc *= shrink;
+        top = m;
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+            if (s0 + u < used) {
+                const float w = __builtin_amdgcn_exp2f(t[u] - m);
+                sum += w * l[u];
+                acc += a[u] * w;
+            }
     }
     const QueryRow q = query_row(p, kv_head, rho);
     const floatx4 o = acc * (sum == 0.f ? 0.f : 1.f / sum);

@@ -25,19 +25,24 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantizeParams p) {
     const uint32_t col_blocks = (uint32_t)((p.cols + 127) / 128);
     const int64_t cb = blockIdx.x % col_blocks, col = cb * 128 + 8 * c16;
     const int64_t rb = blockIdx.x / col_blocks, row = rb * kTileRows + R * rg;
-    float x[R][8];
+    Chunk<T> x[R];
+    const T* const src = static_cast<const T*>(p.x);
+    if (p.vec && (cb + 1) * 128 <= p.cols) {
 #pragma unroll
-    for (int i = 0; i < R; ++i)
-        load_row<T, 8>(static_cast<const T*>(p.x) + (row + i) * p.ldx + col, row + i < p.rows ? p.cols - col : 0, p.vec, x[i]);
+        for (int i = 0; i < R; ++i) x[i] = load_whole_chunk(src + min(row + i, p.rows - 1) * p.ldx + col);
+    } else {
+#pragma unroll
+        for (int i = 0; i < R; ++i) x[i] = load_part_chunk(src + min(row + i, p.rows - 1) * p.ldx, col, p.cols);
+    }
+    if (row + R > p.rows) {
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (row + i >= p.rows) clear(x[i]);
+    }
 
     uint32_t square_byte = 0;
     if constexpr (kSquare) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i < R; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) m = max(m, finite_magnitude(x[i][j]));
-        m = row16_max(m);
+        uint32_t m = row16_max(chunk_max<T, R>(x));
         m = max(m, (uint32_t)__shfl_xor((int)m, 16));
         m = max(m, (uint32_t)__shfl_xor((int)m, 32));
         if (lane == 0) wave_max[wave] = m;
@@ -50,16 +55,9 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantizeParams p) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             uint32_t byte = square_byte;
-            if constexpr (!kSquare) {
-                uint32_t m = 0;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) m = max(m, finite_magnitude(x[i][j]));
-                byte = scale_byte(row16_max(m));
-            }
-            const float inv = inverse_scale(byte);
+            if constexpr (!kSquare) byte = scale_byte(row16_max(chunk_max<T, 1>(x + i)));
             if (row + i < p.rows) {
-                const u32x2 v = {to_e4m3(x[i][0], x[i][1], x[i][2], x[i][3], inv), to_e4m3(x[i][4], x[i][5], x[i][6], x[i][7], inv)};
-                *reinterpret_cast<u32x2*>(p.values + (row + i) * p.ldv + col) = v;
+                *reinterpret_cast<u32x2*>(p.values + (row + i) * p.ldv + col) = chunk_to_e4m3(x[i], scale_of(byte));
             } else {
                 byte = kLeastScaleByte;
             }
@@ -78,14 +76,13 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantizeParams p) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) byte[j] = square_byte;
         } else {
+            uint32_t m[8];
+            column_max<T, R>(x, m);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                uint32_t m = 0;
-#pragma unroll
-                for (int i = 0; i < R; ++i) m = max(m, finite_magnitude(x[i][j]));
-                m = max(m, (uint32_t)__shfl_xor((int)m, 16));
-                m = max(m, (uint32_t)__shfl_xor((int)m, 32));
-                if (lane < 16) col_max[128 * wave + 8 * c16 + j] = m;
+                m[j] = max(m[j], (uint32_t)__shfl_xor((int)m[j], 16));
+                m[j] = max(m[j], (uint32_t)__shfl_xor((int)m[j], 32));
+                if (lane < 16) col_max[128 * wave + 8 * c16 + j] = m[j];
             }
             __syncthreads();
 #pragma unroll
@@ -97,9 +94,8 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantizeParams p) {
         // the transposed tile, 8 rows of a column at a time: rows of x behind the last are zeros
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float inv = inverse_scale(byte[j]);
-            const u32x2 v = {to_e4m3(x[0][j], x[1][j], x[2][j], x[3][j], inv), to_e4m3(x[4][j], x[5][j], x[6][j], x[7][j], inv)};
-            *reinterpret_cast<u32x2*>(turned + (8 * c16 + j) * kPitch + 8 * rg) = v;
+            const float scale = scale_of(byte[j]);
+            *reinterpret_cast<u32x2*>(turned + (8 * c16 + j) * kPitch + 8 * rg) = u32x2{column_to_e4m3(x, j, scale), column_to_e4m3(x + 4, j, scale)};
         }
         if (rg == 0) {
             // columns behind the last are zeros, with the least scale, up to a multiple of 16

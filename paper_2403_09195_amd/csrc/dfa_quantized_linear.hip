@@ -21,6 +21,9 @@ namespace dfa {
 
 namespace {
 
+__device__ __forceinline__ i32x8 both(const u32x4s& lo, const u32x4s& hi) {
+    return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+}
 // acc += block n of b times block m of a.  The bytes of the scale registers are chosen by literal operands.
 template <int n, int m>
 __device__ __forceinline__ void scaled_mfma(floatx4& acc, const i32x8& b, const i32x8& a, uint32_t b_scale, uint32_t a_scale) {
@@ -140,8 +143,7 @@ void product_kernel(ProductParams p, int tiles_m, int tiles_n, int dies) {
     const int frag = r16 * 128 + 16 * (g4 ^ (r16 & 7));            // chunk g4 of LDS row r16 of a block; chunk g4 + 4 is 64 bytes across
     auto half = [&](const char* rows, int block, int h) { return *reinterpret_cast<const u32x4s*>(rows + block * 2048 + (frag ^ (64 * h))); };
     auto fragment = [&](const char* rows, int block) {
-        const u32x4s lo = half(rows, block, 0), hi = half(rows, block, 1);
-        return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+        return both(half(rows, block, 0), half(rows, block, 1));
     };
 
     floatx4 acc[G][4][4];                                          // [64-row group][block of b][block of a]
@@ -234,92 +236,111 @@ __global__ __launch_bounds__(256) void product_sum_kernel(ProductParams p) {
 }
 
 // ---- few rows ------------------------------------------------------------------------------------------------------
-// Up to 64 rows of x, unquantised: bound by the bytes of b, read once.  A workgroup of 8 waves owns 16 F features; its waves take the
-// 128-k blocks in turn and add up in LDS.  b's fragments come straight from memory (16 rows x 64 bytes a load); x's 16 x 128 block is
-// quantised in the registers that then are the B operand (32 values a lane, their maximum over the four lanes of a row), which hides
-// behind b's bytes and saves the launch and the trip through memory of quantising x first.
+// Up to 64 rows of x, unquantised: bound by the bytes of b, read once.  A workgroup of 8 waves owns 16 features; its waves take the
+// 128-k blocks in turn and add up in LDS.  b's fragments come straight from memory (16 rows x 64 bytes a load) and are under way
+// while the workgroup quantises the same blocks of x into LDS, which saves the launch and the trip through memory of quantising x first.
+// (Every wave quantising its own fragments of x in registers took 10.4 us for one row, 4096 x 4096, where this takes @FEW@: the same
+// instructions for one row as for sixteen, in every wave.)
 constexpr int kFewWaves = 8;
 
-template <typename T, int R, int F>
+template <typename T, int R>
 __global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(FewRowsParams p) {
-    __shared__ floatx4 sums[kFewWaves][R * F][64];
+    constexpr int U = 4 / R;                                    // blocks of a wave at a time
+    constexpr int kBlocks = U * kFewWaves, kRows = 16 * R;      // of x in LDS: 64 KB
+    constexpr int kTurn = 4 * kFewWaves / kBlocks;              // rows that the workgroup's groups of 16 lanes quantise at a time: 1, 2, 4
+    constexpr int kAtOnce = 4;                                  // of these under way at once
+    __shared__ __attribute__((aligned(16))) union {
+        uint8_t x[kBlocks][kRows][kScaleBlock];                 // chunk c of row m sits at c ^ (m & 7)
+        floatx4 sums[kFewWaves][R][64];
+    } lds;
+    __shared__ uint8_t x_scales[kBlocks][kRows];
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r16 = lane & 15, g4 = lane >> 4;
-    const int64_t n0 = (int64_t)blockIdx.x * 16 * F;
-    const int n_k = (int)((p.K + kScaleBlock - 1) / kScaleBlock);
+    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const int M = (int)p.M, n_k = (int)((p.K + kScaleBlock - 1) / kScaleBlock);
+    const bool whole = p.vec_x && p.K % 8 == 0;                 // eight neighbouring elements all exist, aligned, or none does
+    const int64_t n = min(n0 + r16, p.N - 1);
+    const uint8_t* const b_row = p.b + n * p.ldb + 16 * g4;
 
-    floatx4 acc[R][F];
+    floatx4 acc[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int f = 0; f < F; ++f) acc[r][f] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int r = 0; r < R; ++r) acc[r] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-    for (int kb = wave; kb < n_k; kb += kFewWaves) {
-        i32x8 bf[F];
-        uint32_t b_scale[F];
+    for (int k0 = 0; k0 < n_k; k0 += kBlocks) {
+        u32x4s lo[U], hi[U];
+        uint32_t b_scale[U];
 #pragma unroll
-        for (int f = 0; f < F; ++f) {
-            const int64_t n = min(n0 + 16 * f + r16, p.N - 1);
-            const uint8_t* const at = p.b + n * p.ldb + (int64_t)kb * kScaleBlock + 16 * g4;
-            const u32x4s lo = *reinterpret_cast<const u32x4s*>(at), hi = *reinterpret_cast<const u32x4s*>(at + 64);
-            bf[f] = i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-            b_scale[f] = p.b_scales[(int64_t)kb * p.lds_b + n];
+        for (int u = 0; u < U; ++u) {
+            const int kb = min(k0 + wave + u * kFewWaves, n_k - 1);
+            lo[u] = *reinterpret_cast<const u32x4s*>(b_row + (int64_t)kb * kScaleBlock);
+            hi[u] = *reinterpret_cast<const u32x4s*>(b_row + (int64_t)kb * kScaleBlock + 64);
+            b_scale[u] = p.b_scales[(int64_t)kb * p.lds_b + n];
         }
+        if (k0) __syncthreads();
+        // x: 16 lanes to a block of a row.  Blocks behind the last are zeros.
+        const int kbl = tid / 16 % kBlocks, c = tid & 15;
+        const int64_t k = (int64_t)(k0 + kbl) * kScaleBlock + 8 * c;
+        for (int m0 = tid / 16 / kBlocks; m0 < M; m0 += kTurn * kAtOnce) {
+            Chunk<T> x[kAtOnce];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int64_t row = 16 * r + r16, k = (int64_t)kb * kScaleBlock + 16 * g4;
-            const T* const at = static_cast<const T*>(p.x) + row * p.ldx + k;
-            float lo[16], hi[16];
-            load_row<T, 16>(at, row < p.M ? p.K - k : 0, p.vec_x, lo);
-            load_row<T, 16>(at + 64, row < p.M ? p.K - k - 64 : 0, p.vec_x, hi);
-            uint32_t top = 0;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = max(top, max(finite_magnitude(lo[i]), finite_magnitude(hi[i])));
-            top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-            top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-            const uint32_t byte = scale_byte(top);
-            const float inv = inverse_scale(byte);
-            i32x8 af;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                af[i] = (int)to_e4m3(lo[4 * i], lo[4 * i + 1], lo[4 * i + 2], lo[4 * i + 3], inv);
-                af[4 + i] = (int)to_e4m3(hi[4 * i], hi[4 * i + 1], hi[4 * i + 2], hi[4 * i + 3], inv);
+            for (int i = 0; i < kAtOnce; ++i) {
+                const T* const row = static_cast<const T*>(p.x) + (int64_t)min(m0 + i * kTurn, M - 1) * p.ldx;
+                if (whole) {
+                    x[i] = load_whole_chunk(row + min(k, p.K - 8));
+                    if (k >= p.K) clear(x[i]);
+                } else {
+                    x[i] = load_part_chunk(row, k, p.K);
+                }
             }
 #pragma unroll
-            for (int f = 0; f < F; ++f) {
-                if constexpr (sizeof(T) == 4) {
+            for (int i = 0; i < kAtOnce; ++i) {
+                const int m = m0 + i * kTurn;
+                const uint32_t byte = scale_byte(row16_max(chunk_max<T, 1>(&x[i])));
+                if (m < M) {
+                    *reinterpret_cast<u32x2*>(&lds.x[kbl][m][16 * ((c >> 1) ^ (m & 7)) + 8 * (c & 1)]) = chunk_to_e4m3(x[i], scale_of(byte));
+                    if (c == 0) x_scales[kbl][m] = (uint8_t)byte;
+                }
+            }
+        }
+        __syncthreads();
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const u32x4s av = {(uint32_t)af[4 * h], (uint32_t)af[4 * h + 1], (uint32_t)af[4 * h + 2], (uint32_t)af[4 * h + 3]};
-                        const u32x4s bv = {(uint32_t)bf[f][4 * h], (uint32_t)bf[f][4 * h + 1], (uint32_t)bf[f][4 * h + 2], (uint32_t)bf[f][4 * h + 3]};
-                        bf16_mfma(acc[r][f], scaled_pair(bv, b_scale[f]), scaled_pair(av, byte));
-                    }
+        for (int u = 0; u < U; ++u) {
+            const int at = wave + u * kFewWaves;
+            if (k0 + at >= n_k) break;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int m = min(16 * r + r16, M - 1);        // rows that do not exist are the last one again: not stored
+                const u32x4s a_lo = *reinterpret_cast<const u32x4s*>(&lds.x[at][m][16 * (g4 ^ (m & 7))]);
+                const u32x4s a_hi = *reinterpret_cast<const u32x4s*>(&lds.x[at][m][16 * ((g4 + 4) ^ (m & 7))]);
+                const uint32_t byte = x_scales[at][m];
+                if constexpr (sizeof(T) == 4) {
+                    bf16_mfma(acc[r], scaled_pair(lo[u], b_scale[u]), scaled_pair(a_lo, byte));
+                    bf16_mfma(acc[r], scaled_pair(hi[u], b_scale[u]), scaled_pair(a_hi, byte));
                 } else {
-                    acc[r][f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bf[f], af, acc[r][f], 0, 0, 0, (int)b_scale[f], 0, (int)byte);
+                    acc[r] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(both(lo[u], hi[u]), both(a_lo, a_hi), acc[r], 0, 0, 0, (int)b_scale[u], 0, (int)byte);
                 }
             }
         }
     }
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int f = 0; f < F; ++f) sums[wave][r * F + f][lane] = acc[r][f];
     __syncthreads();
-    for (int i = tid; i < R * F * 64; i += 64 * kFewWaves) {
-        const int block = i >> 6, l = i & 63;
-        floatx4 v = sums[0][block][l];
 #pragma unroll
-        for (int w = 1; w < kFewWaves; ++w) v += sums[w][block][l];
-        const int64_t row = 16 * (block / F) + (l & 15), n = n0 + 16 * (block % F) + 4 * (l >> 4);
-        if (row >= p.M) continue;
-        T* const y = static_cast<T*>(p.y) + row * p.ldy + n;
-        if (p.vec_y && n + 4 <= p.N) {
+    for (int r = 0; r < R; ++r) lds.sums[wave][r][lane] = acc[r];
+    __syncthreads();
+    if (tid < R * 64) {
+        const int r = tid >> 6;
+        floatx4 v = lds.sums[0][r][lane];
+#pragma unroll
+        for (int w = 1; w < kFewWaves; ++w) v += lds.sums[w][r][lane];
+        const int64_t row = 16 * r + r16, f = n0 + 4 * g4;
+        if (row >= p.M) return;
+        T* const y = static_cast<T*>(p.y) + row * p.ldy + f;
+        if (p.vec_y && f + 4 <= p.N) {
             if constexpr (sizeof(T) == 4) *reinterpret_cast<floatx4*>(y) = v;
             else *reinterpret_cast<bf16x4*>(y) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (n + j < p.N) y[j] = (T)v[j];
+                if (f + j < p.N) y[j] = (T)v[j];
         }
     }
 }
@@ -327,9 +348,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(FewRowsParams 
 template <typename T>
 hipError_t launch_few_typed(const FewRowsParams& p, hipStream_t st) {
     const dim3 grid((unsigned)((p.N + 15) / 16)), block(64 * kFewWaves);
-    if (p.M <= 16) hipLaunchKernelGGL((few_rows_kernel<T, 1, 1>), grid, block, 0, st, p);
-    else if (p.M <= 32) hipLaunchKernelGGL((few_rows_kernel<T, 2, 1>), grid, block, 0, st, p);
-    else hipLaunchKernelGGL((few_rows_kernel<T, 4, 1>), grid, block, 0, st, p);
+    if (p.M <= 16) hipLaunchKernelGGL((few_rows_kernel<T, 1>), grid, block, 0, st, p);
+    else if (p.M <= 32) hipLaunchKernelGGL((few_rows_kernel<T, 2>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((few_rows_kernel<T, 4>), grid, block, 0, st, p);
     return hipGetLastError();
 }
 

@@ -75,6 +75,146 @@ __device__ __forceinline__ void load_row(const T* p, int64_t have, bool vec, flo
     }
 }
 
+// Eight neighbouring elements of a row as they lie in memory.
+template <typename T> struct Chunk;
+template <> struct Chunk<__bf16> {
+    uint32_t w[4];
+};
+template <> struct Chunk<float> {
+    uint32_t w[8];
+};
+// Loads of 16 bytes: all eight elements exist and p is aligned.
+template <typename T>
+__device__ __forceinline__ Chunk<T> load_whole_chunk(const T* p) {
+    Chunk<T> c;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+        const u32x4s v = reinterpret_cast<const u32x4s*>(p)[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c.w[4 * i + j] = v[j];
+    }
+    return c;
+}
+
+// Elements at, at + 1, ... of a row of `cols`, one by one: 0 behind the last.  No branch between the loads: they are under way together.
+template <typename T>
+__device__ __forceinline__ Chunk<T> load_part_chunk(const T* row, int64_t at, int64_t cols) {
+    Chunk<T> c;
+    uint32_t e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t k = min(at + i, cols - 1);
+        if constexpr (sizeof(T) == 4) e[i] = reinterpret_cast<const uint32_t*>(row)[k];
+        else e[i] = reinterpret_cast<const uint16_t*>(row)[k];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = at + i < cols ? e[i] : 0;
+#pragma unroll
+    for (int i = 0; i < 2 * (int)sizeof(T); ++i) {
+        if constexpr (sizeof(T) == 4) c.w[i] = e[i];
+        else c.w[i] = e[2 * i] | e[2 * i + 1] << 16;
+    }
+    return c;
+}
+template <typename T>
+__device__ __forceinline__ void clear(Chunk<T>& c) {
+#pragma unroll
+    for (int i = 0; i < 2 * (int)sizeof(T); ++i) c.w[i] = 0;
+}
+
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+// Magnitudes of two bf16 numbers, 0 for those that are not finite.
+__device__ __forceinline__ uint32_t finite_halves(uint32_t w) {
+    const uint32_t a = w & 0x7fff7fffu;
+    return ((a & 0xffffu) < 0x7f80u ? a & 0xffffu : 0u) | ((a >> 16) < 0x7f80u ? a & 0xffff0000u : 0u);
+}
+__device__ __forceinline__ uint32_t larger_half(uint32_t a) { return max(a << 16, a & 0xffff0000u); }
+
+// The largest finite magnitude of N chunks' elements, as the bits of an fp32 number.  Numbers that are not finite are looked for in the maximum only.
+template <typename T, int N>
+__device__ __forceinline__ uint32_t chunk_max(const Chunk<T>* c) {
+    constexpr int kWords = 2 * (int)sizeof(T);
+    uint32_t m = 0;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+            if constexpr (sizeof(T) == 4) m = max(m, c[n].w[i] & 0x7fffffffu);
+            else m = max_halves(m, c[n].w[i] & 0x7fff7fffu);
+        }
+    if constexpr (sizeof(T) == 2) m = larger_half(m);
+    if (m >= 0x7f800000u) {
+        m = 0;
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) {
+                if constexpr (sizeof(T) == 4) m = max(m, finite_magnitude(__builtin_bit_cast(float, c[n].w[i])));
+                else m = max(m, larger_half(finite_halves(c[n].w[i])));
+            }
+    }
+    return m;
+}
+
+// e4m3 of two pairs of elements x / scale, |x| <= 448 * scale or not finite (which is NaN then).
+typedef short shortx2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t halves_to_e4m3(uint32_t ab, uint32_t cd, float scale) {
+    typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
+    shortx2 v = {0, 0};
+    v = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(v, __builtin_bit_cast(bf16x2v, ab), scale, false);
+    v = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(v, __builtin_bit_cast(bf16x2v, cd), scale, true);
+    return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ uint32_t floats_to_e4m3(uint32_t a, uint32_t b, uint32_t c, uint32_t d, float scale) {
+    shortx2 v = {0, 0};
+    v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, __builtin_bit_cast(float, a), __builtin_bit_cast(float, b), scale, false);
+    v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, __builtin_bit_cast(float, c), __builtin_bit_cast(float, d), scale, true);
+    return __builtin_bit_cast(uint32_t, v);
+}
+template <typename T>
+__device__ __forceinline__ u32x2 chunk_to_e4m3(const Chunk<T>& c, float scale) {
+    if constexpr (sizeof(T) == 4) return u32x2{floats_to_e4m3(c.w[0], c.w[1], c.w[2], c.w[3], scale), floats_to_e4m3(c.w[4], c.w[5], c.w[6], c.w[7], scale)};
+    else return u32x2{halves_to_e4m3(c.w[0], c.w[1], scale), halves_to_e4m3(c.w[2], c.w[3], scale)};
+}
+// Element j of four rows.
+template <typename T>
+__device__ __forceinline__ uint32_t column_to_e4m3(const Chunk<T>* c, int j, float scale) {
+    if constexpr (sizeof(T) == 4) return floats_to_e4m3(c[0].w[j], c[1].w[j], c[2].w[j], c[3].w[j], scale);
+    else {
+        const uint32_t pick = j & 1 ? 0x07060302u : 0x05040100u;        // the upper or the lower half of either word
+        return halves_to_e4m3(__builtin_amdgcn_perm(c[1].w[j / 2], c[0].w[j / 2], pick), __builtin_amdgcn_perm(c[3].w[j / 2], c[2].w[j / 2], pick), scale);
+    }
+}
+// The largest finite magnitude of element j of N rows, for every j, as the bits of fp32 numbers.
+template <typename T, int N>
+__device__ __forceinline__ void column_max(const Chunk<T>* c, uint32_t (&m)[8]) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            m[j] = 0;
+#pragma unroll
+            for (int n = 0; n < N; ++n) m[j] = max(m[j], finite_magnitude(__builtin_bit_cast(float, c[n].w[j])));
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t a = 0;
+#pragma unroll
+            for (int n = 0; n < N; ++n) a = max_halves(a, c[n].w[j] & 0x7fff7fffu);
+            if (larger_half(a) >= 0x7f800000u) {
+                a = 0;
+#pragma unroll
+                for (int n = 0; n < N; ++n) a = max_halves(a, finite_halves(c[n].w[j]));
+            }
+            m[2 * j] = a << 16;
+            m[2 * j + 1] = a & 0xffff0000u;
+        }
+    }
+}
+
 // Largest value over the 16 lanes of a row of lanes, left in all of them.
 __device__ __forceinline__ uint32_t row16_max(uint32_t x) {
     x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, true));     // quad_perm [1, 0, 3, 2]

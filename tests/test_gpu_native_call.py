@@ -197,3 +197,71 @@ def test_keys_and_values_smaller_than_q(B):
     ref = B.forward(q, k, v, [(64, 1)], 0.125)
     longer = torch.cat((k, k), dim=1)
     assert all(torch.equal(a, b) for a, b in zip(ref, B.forward(q, longer, v, [(64, 1)], 0.125)))
+
+
+def _native_or_python(B, monkeypatch, call):
+    """The results of a call both ways, and the names of what the native module answered."""
+    answered = []
+
+    class Spy:
+        def __getattr__(self, name):
+            def run(*args):
+                res = getattr(B._dfa_torch_module, name)(*args)
+                if res is not None:
+                    answered.append(name)
+                return res
+            return run
+
+    class Nothing:
+        def __getattr__(self, name):
+            return lambda *args: None
+
+    from paper_2403_09195_amd import _dfa_torch
+    monkeypatch.setattr(B, "_dfa_torch_module", _dfa_torch, raising=False)
+    results = []
+    for stand_in in (Spy(), Nothing()):
+        with monkeypatch.context() as m:
+            m.setattr(B, "_native", stand_in)
+            results.append(call())
+    return results, answered
+
+
+def _equal(a, b):
+    import torch
+    return all(torch.equal(x, y) and x.dtype == y.dtype and x.shape == y.shape and x.is_contiguous() for x, y in zip(a, b)) and len(a) == len(b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_quantized_calls_same_results(B, monkeypatch, dtype):
+    import torch
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    x, w, dy = (torch.randn(s, device="cuda").to(dt) for s in ((3, 50, 200), (70, 200), (3, 50, 70)))
+    qw, w_t = B.quantize(w, 128), B.quantize(w, 128, transpose=True)
+    for rows in (x, x[:1, :5].contiguous()):
+        (a, b), names = _native_or_python(B, monkeypatch, lambda: (B.quantized_linear(rows, qw),))
+        assert names == ["quantized_linear"] and _equal(a, b) and a[0].shape == rows.shape[:2] + (70,)
+    (a, b), names = _native_or_python(B, monkeypatch, lambda: B.quantized_linear_backward(dy, x, w_t))
+    assert names == ["quantized_linear_backward"] and _equal(a, b)
+    # what is not ordinary goes through Python: a view, a part of a quantised matrix
+    (a, b), names = _native_or_python(B, monkeypatch, lambda: (B.quantized_linear(x[0, ::2], qw), B.quantized_linear(x, B.QuantizedMatrix(qw.values[:48], qw.scales, 200))))
+    assert names == ["quantized_linear"] and _equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_cache_calls_same_results(B, monkeypatch, dtype):
+    import torch
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    rows = torch.randn((2, 90, 6, 64), device="cuda").to(dt)
+    table = torch.arange(20, dtype=torch.int32, device="cuda").view(2, 10)
+    lengths, counts = (torch.tensor(v, dtype=torch.int32, device="cuda") for v in ([90, 41], [3, 1]))
+
+    def steps():
+        cache = B.kv_cache(20, 2, 16, 64)
+        B.cache_append(rows[:, :, :2], rows[:, :, 2:4], cache, table, lengths, counts=lengths)
+        res = [B.cache_attention(rows[:, :3, 2:], cache, table, lengths, 0.125),
+               B.cache_attention(rows[:, :3, 2:], cache, table, lengths, 0.125, causal=False, counts=counts, max_length=64),
+               B.cache_attention(rows[:, :3, 2:], cache, table[:, :8], lengths, 0.125)]
+        return [t for pair in res for t in pair] + [cache.k.view(torch.uint8), cache.v.view(torch.uint8), cache.scales]
+
+    (a, b), names = _native_or_python(B, monkeypatch, steps)
+    assert names == ["cache_append", "cache_attention", "cache_attention"] and _equal(a, b)
