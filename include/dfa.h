@@ -331,7 +331,7 @@ int dfa_encoder_stack(const void *x, const void *w_qkv, const void *w_o, int32_t
 typedef struct { void *values; void *scales; int64_t ld; int64_t ld_scales; } dfa_quantized_t;
 
 /*
- * Quantises x (device, dtype dt, [rows][cols] with row pitch ldx, any alignment; rows on 16-byte boundaries are read faster).
+ * Quantises x (device, dtype dt, [rows][cols] with row pitch ldx; rows may start at any element).
  *   q    (host struct or NULL)  receives x: blocks along its columns
  *   q_t  (host struct or NULL)  receives x transposed, [cols][rows]: blocks along x's rows (what a product that contracts over
  *        x's rows reads)
@@ -343,12 +343,12 @@ int dfa_quantize(const void *x, dfa_dtype_t dt, int64_t rows, int64_t cols, int6
 /*
  * y[m][n] = sum_k a[m][k] * b[n][k] of the values that a [M][K] and b [N][K] hold: exact products, fp32 sums, rounded once to dt.
  *   y          device, dtype dt, [M][N] with row pitch ldy (elements); must not overlap a or b
- *   workspace  device, 16-byte aligned, dfa_quantized_product_workspace_bytes(M, N, K) (0 = none, NULL allowed): partial sums of
+ *   workspace  device, 16-byte aligned, dfa_quantized_product_workspace_bytes(dt, M, N, K) (0 = none, NULL allowed): partial sums of
  *              products whose k-steps are shared out over workgroups.  Written and read by this call only: calls that may
  *              overlap need one each.
  * The sums are in a fixed order: equal calls give equal results.  Asynchronous on `stream`; allocates nothing.
  */
-size_t dfa_quantized_product_workspace_bytes(int64_t M, int64_t N, int64_t K);
+size_t dfa_quantized_product_workspace_bytes(dfa_dtype_t dt, int64_t M, int64_t N, int64_t K);
 int dfa_quantized_product(dfa_quantized_t a, dfa_quantized_t b, void *y, dfa_dtype_t dt, int64_t M, int64_t N, int64_t K, int64_t ldy,
                           void *workspace, size_t workspace_bytes, void *stream);
 
@@ -357,7 +357,7 @@ int dfa_quantized_product(dfa_quantized_t a, dfa_quantized_t b, void *y, dfa_dty
  * of 1 x 128, y[m][n] = sum_k x[m][k] * w[n][k] as above, y of x's dtype.  Any M, N, K >= 1.  Up to 64 rows take one launch and
  * no workspace; others quantise into the workspace first.
  */
-size_t dfa_quantized_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
+size_t dfa_quantized_linear_workspace_bytes(dfa_dtype_t dt, int64_t M, int64_t N, int64_t K);
 int dfa_quantized_linear(const void *x, dfa_dtype_t dt, int64_t ldx, dfa_quantized_t w, void *y, int64_t M, int64_t N, int64_t K, int64_t ldy,
                          void *workspace, size_t workspace_bytes, void *stream);
 
@@ -368,7 +368,7 @@ int dfa_quantized_linear(const void *x, dfa_dtype_t dt, int64_t ldx, dfa_quantiz
  *   dw [N][K] = dy^T . x  dy and x in blocks of 128 along M, each column on its own; fp32
  * dy, x and dx have dtype dt.  dx or dw may be NULL (not wanted): x is read for dw only, w_t for dx only.
  */
-size_t dfa_quantized_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K);
+size_t dfa_quantized_linear_backward_workspace_bytes(dfa_dtype_t dt, int64_t M, int64_t N, int64_t K);
 int dfa_quantized_linear_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx, dfa_dtype_t dt, dfa_quantized_t w_t, void *dx,
                                   int64_t lddx, float *dw, int64_t lddw, int64_t M, int64_t N, int64_t K, void *workspace, size_t workspace_bytes,
                                   void *stream);

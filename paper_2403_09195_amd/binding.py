@@ -131,7 +131,7 @@ def lib():
         L.dfa_quantized_linear.argtypes = [vp, ctypes.c_int, i64, qm, vp, i64, i64, i64, i64, vp, st, vp]
         L.dfa_quantized_linear_backward.argtypes = [vp, i64, vp, i64, ctypes.c_int, qm, vp, i64, vp, i64, i64, i64, i64, vp, st, vp]
         for name in ("dfa_quantized_product", "dfa_quantized_linear", "dfa_quantized_linear_backward"):
-            getattr(L, name + "_workspace_bytes").argtypes = [i64, i64, i64]
+            getattr(L, name + "_workspace_bytes").argtypes = [ctypes.c_int, i64, i64, i64]
         L.dfa_cache_append.argtypes = [vp, vp, Strides, Strides, ctypes.c_int, i32, i32, Cache, vp, i32, i64, vp, vp, vp]
         L.dfa_cache_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, ctypes.c_int, i64]
         L.dfa_cache_attention.argtypes = [vp, Strides, ctypes.c_int, i32, i32, i32, Cache, vp, i32, i64, vp, vp, i32, f32, i64, vp, vp, vp, st, vp]
@@ -753,7 +753,7 @@ def quantized_product(a, b, dtype, out=None, workspace="auto"):
     if a.cols != b.cols:
         raise DfaError(-2, f"a has {a.cols} columns, b {b.cols}")
     y, ldy = _result(out, (M, N), dtype, a.values, "out")
-    need = lib().dfa_quantized_product_workspace_bytes(M, N, a.cols) if M and N else 0
+    need = lib().dfa_quantized_product_workspace_bytes(_dtype_code(y), M, N, a.cols)
     ptr, size, keep = _call_workspace(workspace, need, a.values)
     _check(lib().dfa_quantized_product(qa, qb, y.data_ptr(), _dtype_code(y), M, N, a.cols, ldy, ptr, size, _stream()), "dfa_quantized_product")
     _keep(keep)
@@ -776,7 +776,7 @@ def quantized_linear(x, w, out=None, workspace="auto"):
         raise DfaError(-2, f"x has {x.shape[-1]} columns, w {K}")
     qw = _quantized(w, "w")
     y, ldy = _result(out, x.shape[:-1] + (N,), x.dtype, x, "out")
-    need = lib().dfa_quantized_linear_workspace_bytes(M, N, K) if M > 64 else 0
+    need = lib().dfa_quantized_linear_workspace_bytes(code, M, N, K)
     ptr, size, keep = _call_workspace(workspace, need, x)
     _check(lib().dfa_quantized_linear(x.data_ptr(), code, ldx, qw, y.data_ptr(), M, N, K, ldy, ptr, size, _stream()), "dfa_quantized_linear")
     _keep(keep)
@@ -803,7 +803,7 @@ def quantized_linear_backward(dy, x, w_t, want_dx=True, want_dw=True, workspace=
     qw = _quantized(w_t, "w_t")
     dx = torch.empty(dy.shape[:-1] + (K,), dtype=dy.dtype, device=dy.device) if want_dx else None
     dw = torch.empty((N, K), dtype=torch.float32, device=dy.device) if want_dw else None
-    need = lib().dfa_quantized_linear_backward_workspace_bytes(M, N, K) if M else 0
+    need = lib().dfa_quantized_linear_backward_workspace_bytes(code, M, N, K)
     ptr, size, keep = _call_workspace(workspace, need, dy)
     _check(lib().dfa_quantized_linear_backward(dy.data_ptr(), lddy, x.data_ptr(), ldx, code, qw, dx.data_ptr() if want_dx else None, K,
                                                dw.data_ptr() if want_dw else None, K, M, N, K, ptr, size, _stream()), "dfa_quantized_linear_backward")

@@ -21,9 +21,7 @@ bool known(dfa_dtype_t dt) { return dt == DFA_BF16 || dt == DFA_F32; }
 int64_t size_of(dfa_dtype_t dt) { return dt == DFA_BF16 ? 2 : 4; }
 bool sizes_ok(int64_t a, int64_t b) { return a > 0 && b > 0; }
 
-// A plain matrix whose rows can be read (or written) 16 bytes at a time.
-bool whole_rows(const void* p, int64_t ld, int64_t es) { return aligned16(p) && ld * es % 16 == 0; }
-// A plain matrix of this type at all.
+// A plain matrix of this type.
 bool matrix_aligned(const void* p, int64_t es) { return reinterpret_cast<uintptr_t>(p) % es == 0; }
 
 // A quantised matrix of `rows` rows of `cols` elements.
@@ -61,8 +59,8 @@ ChipShape chip_or_default() {
     return chip;
 }
 
-int64_t parts_bytes(int64_t M, int64_t N, int64_t K, const ChipShape& chip) {
-    const ProductShape s = product_shape(M, N, k_steps(K), chip);
+int64_t parts_bytes(int64_t M, int64_t N, int64_t K, dfa_dtype_t dt, const ChipShape& chip) {
+    const ProductShape s = product_shape(M, N, k_steps(K), dt == DFA_F32, chip);
     return s.splits > 1 ? up((int64_t)s.splits * M * N * 4, 256) : 0;
 }
 
@@ -82,7 +80,6 @@ int run_quantize(const void* x, dfa_dtype_t dt, int64_t rows, int64_t cols, int6
                  const dfa_quantized_t* qt, void* stream) {
     QuantizeParams p{};
     p.x = x, p.ldx = ldx, p.rows = rows, p.cols = cols;
-    p.vec = whole_rows(x, ldx, size_of(dt));
     if (q) p.values = static_cast<uint8_t*>(q->values), p.scales = static_cast<uint8_t*>(q->scales), p.ldv = q->ld, p.lds = q->ld_scales;
     if (qt) p.values_t = static_cast<uint8_t*>(qt->values), p.scales_t = static_cast<uint8_t*>(qt->scales), p.ldv_t = qt->ld, p.lds_t = qt->ld_scales;
     return launch_quantize(p, dt == DFA_F32, square, static_cast<hipStream_t>(stream)) == hipSuccess ? DFA_OK : DFA_ERR_LAUNCH;
@@ -94,9 +91,8 @@ int run_product(const dfa_quantized_t& a, const dfa_quantized_t& b, void* y, dfa
     p.a = static_cast<const uint8_t*>(a.values), p.a_scales = static_cast<const uint8_t*>(a.scales), p.lda = a.ld, p.lds_a = a.ld_scales;
     p.b = static_cast<const uint8_t*>(b.values), p.b_scales = static_cast<const uint8_t*>(b.scales), p.ldb = b.ld, p.lds_b = b.ld_scales;
     p.y = y, p.ldy = ldy, p.M = M, p.N = N, p.n_k = k_steps(K);
-    const ProductShape s = product_shape(M, N, p.n_k, chip);
+    const ProductShape s = product_shape(M, N, p.n_k, dt == DFA_F32, chip);
     p.parts = static_cast<float*>(parts), p.splits = s.splits;
-    p.vec = whole_rows(y, ldy, size_of(dt));
     return launch_product(p, s, chip, dt == DFA_F32, static_cast<hipStream_t>(stream)) == hipSuccess ? DFA_OK : DFA_ERR_LAUNCH;
 }
 
@@ -154,8 +150,8 @@ int dfa_quantize(const void* x, dfa_dtype_t dt, int64_t rows, int64_t cols, int6
     return run_quantize(x, dt, rows, cols, ldx, block_rows != 1, q, q_t, stream);
 }
 
-size_t dfa_quantized_product_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-    return check_product_sizes(M, N, K) == DFA_OK ? (size_t)parts_bytes(M, N, K, chip_or_default()) : 0;
+size_t dfa_quantized_product_workspace_bytes(dfa_dtype_t dt, int64_t M, int64_t N, int64_t K) {
+    return known(dt) && check_product_sizes(M, N, K) == DFA_OK ? (size_t)parts_bytes(M, N, K, dt, chip_or_default()) : 0;
 }
 
 int dfa_quantized_product(dfa_quantized_t a, dfa_quantized_t b, void* y, dfa_dtype_t dt, int64_t M, int64_t N, int64_t K, int64_t ldy, void* workspace,
@@ -171,13 +167,13 @@ int dfa_quantized_product(dfa_quantized_t a, dfa_quantized_t b, void* y, dfa_dty
     ChipShape chip;
     rc = this_chip(&chip);
     if (rc != DFA_OK) return rc;
-    if (!room(workspace, workspace_bytes, parts_bytes(M, N, K, chip))) return DFA_ERR_WORKSPACE;
+    if (!room(workspace, workspace_bytes, parts_bytes(M, N, K, dt, chip))) return DFA_ERR_WORKSPACE;
     return run_product(a, b, y, dt, M, N, K, ldy, workspace, chip, stream);
 }
 
-size_t dfa_quantized_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-    if (check_product_sizes(M, N, K) != DFA_OK || M <= kFewRows) return 0;
-    return (size_t)(quantized_bytes(M, K) + parts_bytes(M, N, K, chip_or_default()));
+size_t dfa_quantized_linear_workspace_bytes(dfa_dtype_t dt, int64_t M, int64_t N, int64_t K) {
+    if (!known(dt) || check_product_sizes(M, N, K) != DFA_OK || M <= kFewRows) return 0;
+    return (size_t)(quantized_bytes(M, K) + parts_bytes(M, N, K, dt, chip_or_default()));
 }
 
 int dfa_quantized_linear(const void* x, dfa_dtype_t dt, int64_t ldx, dfa_quantized_t w, void* y, int64_t M, int64_t N, int64_t K, int64_t ldy,
@@ -195,25 +191,24 @@ int dfa_quantized_linear(const void* x, dfa_dtype_t dt, int64_t ldx, dfa_quantiz
         p.x = x, p.ldx = ldx, p.M = M, p.N = N, p.K = K;
         p.b = static_cast<const uint8_t*>(w.values), p.b_scales = static_cast<const uint8_t*>(w.scales), p.ldb = w.ld, p.lds_b = w.ld_scales;
         p.y = y, p.ldy = ldy;
-        p.vec_x = whole_rows(x, ldx, es), p.vec_y = whole_rows(y, ldy, es);
         return launch_few_rows(p, dt == DFA_F32, static_cast<hipStream_t>(stream)) == hipSuccess ? DFA_OK : DFA_ERR_LAUNCH;
     }
     if (!quantize_fits(M, K)) return DFA_ERR_TOO_LARGE;
     ChipShape chip;
     rc = this_chip(&chip);
     if (rc != DFA_OK) return rc;
-    if (!room(workspace, workspace_bytes, quantized_bytes(M, K) + parts_bytes(M, N, K, chip))) return DFA_ERR_WORKSPACE;
+    if (!room(workspace, workspace_bytes, quantized_bytes(M, K) + parts_bytes(M, N, K, dt, chip))) return DFA_ERR_WORKSPACE;
     char* at = static_cast<char*>(workspace);
     const dfa_quantized_t xq = take_quantized(&at, M, K);
     rc = run_quantize(x, dt, M, K, ldx, false, &xq, nullptr, stream);
     return rc != DFA_OK ? rc : run_product(xq, w, y, dt, M, N, K, ldy, at, chip, stream);
 }
 
-size_t dfa_quantized_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-    if (check_product_sizes(M, K, N) != DFA_OK || check_product_sizes(N, K, M) != DFA_OK) return 0;
+size_t dfa_quantized_linear_backward_workspace_bytes(dfa_dtype_t dt, int64_t M, int64_t N, int64_t K) {
+    if (!known(dt) || check_product_sizes(M, K, N) != DFA_OK || check_product_sizes(N, K, M) != DFA_OK) return 0;
     const ChipShape chip = chip_or_default();
     return (size_t)(quantized_bytes(M, N) + quantized_bytes(N, M) + quantized_bytes(K, M) +
-                    std::max(parts_bytes(M, K, N, chip), parts_bytes(N, K, M, chip)));
+                    std::max(parts_bytes(M, K, N, dt, chip), parts_bytes(N, K, M, DFA_F32, chip)));
 }
 
 int dfa_quantized_linear_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, dfa_dtype_t dt, dfa_quantized_t w_t, void* dx, int64_t lddx,
@@ -232,7 +227,7 @@ int dfa_quantized_linear_backward(const void* dy, int64_t lddy, const void* x, i
     rc = this_chip(&chip);
     if (rc != DFA_OK) return rc;
     const int64_t need = quantized_bytes(M, N) + quantized_bytes(N, M) + quantized_bytes(K, M) +
-                         std::max(parts_bytes(M, K, N, chip), parts_bytes(N, K, M, chip));
+                         std::max(parts_bytes(M, K, N, dt, chip), parts_bytes(N, K, M, DFA_F32, chip));
     if (!room(workspace, workspace_bytes, need)) return DFA_ERR_WORKSPACE;
     char* at = static_cast<char*>(workspace);
     const dfa_quantized_t dyq = take_quantized(&at, M, N), dyq_t = take_quantized(&at, N, M), xq_t = take_quantized(&at, K, M);

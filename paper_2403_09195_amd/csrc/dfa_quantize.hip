@@ -27,7 +27,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantizeParams p) {
     const int64_t rb = blockIdx.x / col_blocks, row = rb * kTileRows + R * rg;
     Chunk<T> x[R];
     const T* const src = static_cast<const T*>(p.x);
-    if (p.vec && (cb + 1) * 128 <= p.cols) {
+    if ((cb + 1) * 128 <= p.cols) {
 #pragma unroll
         for (int i = 0; i < R; ++i) x[i] = load_whole_chunk(src + min(row + i, p.rows - 1) * p.ldx + col);
     } else {

@@ -14,6 +14,8 @@
 // Four 16-row blocks of an operand interleave: row 4*r + m of 64 is row r of block m.  The scales of a lane's rows of the four blocks are
 // then four neighbouring bytes, one register whose byte m the instruction picks, and a lane ends up with 16 neighbouring
 // features of a row of y (4*g4 + i of block n is feature 16*g4 + 4*i + n), whole 128-byte lines from the registers.
+#include <cmath>
+
 #include "dfa_mfma.h"
 #include "dfa_scaled.h"
 
@@ -50,25 +52,35 @@ __device__ __forceinline__ void bf16_mfma(floatx4& acc, const Bf16Pair& b, const
     acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.second, a.second, acc, 0, 0, 0);
 }
 
-// 16 neighbouring features of row m of y, feature n first; those behind N are left out.
+// Four neighbouring elements of a row of y, features n .. n + 3; those behind N are left out.  (Rows may start anywhere.)
 template <typename Y>
-__device__ __forceinline__ void store16(Y* y, int64_t n, int64_t N, bool vec, const float (&v)[16]) {
-    if (vec && n + 16 <= N) {
+__device__ __forceinline__ void store4(Y* row, int64_t n, int64_t N, const floatx4& v) {
+    if (n + 4 <= N) {
         if constexpr (sizeof(Y) == 4) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) *reinterpret_cast<floatx4*>(y + n + 4 * i) = floatx4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+            *reinterpret_cast<words_anywhere*>(row + n) = __builtin_bit_cast(u32x4s, v);
         } else {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const bf16x8 o = {(__bf16)v[8 * i], (__bf16)v[8 * i + 1], (__bf16)v[8 * i + 2], (__bf16)v[8 * i + 3],
-                                  (__bf16)v[8 * i + 4], (__bf16)v[8 * i + 5], (__bf16)v[8 * i + 6], (__bf16)v[8 * i + 7]};
-                *reinterpret_cast<bf16x8*>(y + n + 8 * i) = o;
-            }
+            const bf16x4 o = {(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+            *reinterpret_cast<pair_anywhere*>(row + n) = __builtin_bit_cast(u32x2, o);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (n + i < N) y[n + i] = (Y)v[i];
+        for (int i = 0; i < 4; ++i)
+            if (n + i < N) row[n + i] = (Y)v[i];
+    }
+}
+// The same for 16.
+template <typename Y>
+__device__ __forceinline__ void store16(Y* row, int64_t n, int64_t N, const floatx4 (&v)[4]) {
+    if (sizeof(Y) == 2 && n + 16 <= N) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const bf16x8 o = {(__bf16)v[2 * i][0], (__bf16)v[2 * i][1], (__bf16)v[2 * i][2], (__bf16)v[2 * i][3],
+                              (__bf16)v[2 * i + 1][0], (__bf16)v[2 * i + 1][1], (__bf16)v[2 * i + 1][2], (__bf16)v[2 * i + 1][3]};
+            *reinterpret_cast<words_anywhere*>(row + n + 8 * i) = __builtin_bit_cast(u32x4s, o);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) store4(row, n + 4 * i, N, v[i]);
     }
 }
 
@@ -204,35 +216,33 @@ void product_kernel(ProductParams p, int tiles_m, int tiles_n, int dies) {
         for (int m = 0; m < 4; ++m) {
             const int64_t row = m0 + (T / WM) * wm + 64 * g + 4 * r16 + m;
             if (row >= p.M) continue;
-            float v[16];
+            floatx4 v[4];                                           // feature n + 4 * i + j is element i of block j
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = acc[g][i & 3][m][i >> 2];
-            if (p.splits > 1) store16(p.parts + ((int64_t)split * p.M + row) * p.N, n, p.N, p.N % 4 == 0, v);
-            else store16(static_cast<Y*>(p.y) + row * p.ldy, n, p.N, p.vec, v);
+            for (int i = 0; i < 4; ++i) v[i] = floatx4{acc[g][0][m][i], acc[g][1][m][i], acc[g][2][m][i], acc[g][3][m][i]};
+            if (p.splits > 1) store16(p.parts + ((int64_t)split * p.M + row) * p.N, n, p.N, v);
+            else store16(static_cast<Y*>(p.y) + row * p.ldy, n, p.N, v);
         }
 }
 
-// y = the sum of the splits' partial results, in their order.
-template <typename Y>
+// y = the sum of the splits' partial results, in their order, W neighbouring elements a thread.  Eight splits' loads are under way at once.
+template <typename Y, int W>
 __global__ __launch_bounds__(256) void product_sum_kernel(ProductParams p) {
-    const int64_t size = p.M * p.N;
-    if (p.N % 4 == 0 && p.ldy % 4 == 0) {
-        for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < size; i += (int64_t)gridDim.x * 1024) {
-            floatx4 sum = *reinterpret_cast<const floatx4*>(p.parts + i);
-            for (int s = 1; s < p.splits; ++s) sum += *reinterpret_cast<const floatx4*>(p.parts + s * size + i);
-            const int64_t row = i / p.N;
-            Y* const y = static_cast<Y*>(p.y) + row * p.ldy + (i - row * p.N);
+    typedef float vec __attribute__((ext_vector_type(W)));
+    const int64_t size = p.M * p.N, i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * W;
+    if (i >= size) return;
+    vec sum = *reinterpret_cast<const vec*>(p.parts + i);
+    for (int s0 = 1; s0 < p.splits; s0 += 8) {
+        vec x[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) y[j] = (Y)sum[j];
-        }
-    } else {
-        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
-            float sum = p.parts[i];
-            for (int s = 1; s < p.splits; ++s) sum += p.parts[s * size + i];
-            const int64_t row = i / p.N;
-            static_cast<Y*>(p.y)[row * p.ldy + (i - row * p.N)] = (Y)sum;
-        }
+        for (int u = 0; u < 8; ++u) x[u] = *reinterpret_cast<const vec*>(p.parts + (int64_t)min(s0 + u, p.splits - 1) * size + i);
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (s0 + u < p.splits) sum += x[u];
     }
+    const int64_t row = i / p.N, n = i - row * p.N;
+    Y* const y = static_cast<Y*>(p.y) + row * p.ldy;
+    if constexpr (W == 4) store4(y, n, p.N, sum);
+    else y[n] = (Y)sum[0];
 }
 
 // ---- few rows ------------------------------------------------------------------------------------------------------
@@ -258,7 +268,6 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(FewRowsParams 
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r16 = lane & 15, g4 = lane >> 4;
     const int64_t n0 = (int64_t)blockIdx.x * 16;
     const int M = (int)p.M, n_k = (int)((p.K + kScaleBlock - 1) / kScaleBlock);
-    const bool whole = p.vec_x && p.K % 8 == 0;                 // eight neighbouring elements all exist, aligned, or none does
     const int64_t n = min(n0 + r16, p.N - 1);
     const uint8_t* const b_row = p.b + n * p.ldb + 16 * g4;
 
@@ -277,6 +286,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(FewRowsParams 
             b_scale[u] = p.b_scales[(int64_t)kb * p.lds_b + n];
         }
         if (k0) __syncthreads();
+        const bool whole = p.K % 8 == 0 || (int64_t)(k0 + kBlocks) * kScaleBlock <= p.K;   // eight neighbouring elements all exist, or none does
         // x: 16 lanes to a block of a row.  Blocks behind the last are zeros.
         const int kbl = tid / 16 % kBlocks, c = tid & 15;
         const int64_t k = (int64_t)(k0 + kbl) * kScaleBlock + 8 * c;
@@ -333,15 +343,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(FewRowsParams 
         for (int w = 1; w < kFewWaves; ++w) v += lds.sums[w][r][lane];
         const int64_t row = 16 * r + r16, f = n0 + 4 * g4;
         if (row >= p.M) return;
-        T* const y = static_cast<T*>(p.y) + row * p.ldy + f;
-        if (p.vec_y && f + 4 <= p.N) {
-            if constexpr (sizeof(T) == 4) *reinterpret_cast<floatx4*>(y) = v;
-            else *reinterpret_cast<bf16x4*>(y) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (f + j < p.N) y[j] = (T)v[j];
-        }
+        store4(static_cast<T*>(p.y) + row * p.ldy, f, p.N, v);
     }
 }
 
@@ -363,8 +365,10 @@ hipError_t launch_product_typed(const ProductParams& p, const ProductShape& shap
     else hipLaunchKernelGGL((product_kernel<Y, 128, 2, 2>), grid, dim3(256), 0, st, p, (int)tiles_m, (int)tiles_n, dies);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && p.splits > 1) {
-        const int64_t blocks = (p.M * p.N + 1023) / 1024;
-        hipLaunchKernelGGL((product_sum_kernel<Y>), dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, p);
+        const bool wide = p.N % 4 == 0;                    // four neighbouring elements lie in one row
+        const unsigned blocks = (unsigned)((p.M * p.N + (wide ? 1023 : 255)) / (wide ? 1024 : 256));
+        if (wide) hipLaunchKernelGGL((product_sum_kernel<Y, 4>), dim3(blocks), dim3(256), 0, st, p);
+        else hipLaunchKernelGGL((product_sum_kernel<Y, 1>), dim3(blocks), dim3(256), 0, st, p);
         e = hipGetLastError();
     }
     return e;
@@ -372,16 +376,28 @@ hipError_t launch_product_typed(const ProductParams& p, const ProductShape& shap
 
 }  // namespace
 
-ProductShape product_shape(int64_t M, int64_t N, int32_t n_k, const ChipShape& chip) {
-    const int64_t cus = chip.cus > 0 ? chip.cus : 1;
-    auto tiles = [&](int64_t t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
-    ProductShape s{tiles(256) >= cus ? 256 : 128, 1};
-    // slots that no tile fills take shares of the k-steps, four at least each
-    const int64_t slots = s.tile == 256 ? cus : 2 * cus;
-    const int64_t most = n_k / 4, wanted = slots / tiles(s.tile);
-    s.splits = (int32_t)(wanted < most ? wanted : most);
-    if (s.splits < 1) s.splits = 1;
-    return s;
+// The estimated time of every form in us, the least taken.  A 128-k step of one workgroup takes 0.5 us with a 128-row tile (0.85 where two share
+// a compute unit: what LDS hands out, 96 KB a step at 128 bytes a clock), 1.48 with a 256-row one; 1.05, 1.75 and 2.8 for fp32 results; results and partial
+// sums go at 4 TB/s, and summing takes a launch of 3 us.  Estimated / measured on M x N x K, the two best forms, bf16 results (tile / splits):
+// 512 x 2304 x 768 128/1 8 / 7.1, 256/1 14 / 14.9; 4096 x 2304 x 768 128/1 14 / 16.1, 256/1 18 / 17.3; 4096 x 4096 x 4096 256/1 60 / 58.2, 128/1 67 / 65.5;
+// 64 x 4096 x 4096 128/4 13 / 13.0, 128/1 20 / 20.3; 512 x 4096 x 4096 128/1 21 / 22.7, 128/2 24 / 25.3; 2304 x 768 x 32768 128/4 76 / 75.7, 128/3 74 / 79.8.
+ProductShape product_shape(int64_t M, int64_t N, int32_t n_k, bool f32, const ChipShape& chip) {
+    const double cus = chip.cus > 0 ? chip.cus : 1, rate = 4e6, out = (double)M * N * (f32 ? 4 : 2) / rate, partial = (double)M * N * 8 / rate;
+    ProductShape best{128, 1};
+    double least = 0;
+    for (const int32_t tile : {128, 256}) {
+        const double tiles = (double)((M + tile - 1) / tile) * (double)((N + tile - 1) / tile);
+        // shares of two k-steps at least, up to where every slot has a workgroup
+        for (int32_t s = 1; s == 1 || (s <= n_k / 2 && tiles * s <= 3 * cus); ++s) {
+            const double wgs = tiles * s / cus;
+            double steps = (n_k + s - 1) / s;
+            if (tile == 128) steps *= wgs <= 1 ? (f32 ? 1.05 : 0.5) : (f32 ? 1.75 : 0.85) * (wgs <= 2 ? 1 : wgs / 2);
+            else steps *= (f32 ? 2.8 : 1.48) * std::ceil(wgs);
+            const double us = steps + out + (s > 1 ? 3 + s * partial : 0);
+            if (least == 0 || us < least) least = us, best = ProductShape{tile, s};
+        }
+    }
+    return best;
 }
 
 hipError_t launch_product(const ProductParams& p, const ProductShape& shape, const ChipShape& chip, bool f32, hipStream_t st) {

@@ -83,13 +83,16 @@ template <> struct Chunk<__bf16> {
 template <> struct Chunk<float> {
     uint32_t w[8];
 };
-// Loads of 16 bytes: all eight elements exist and p is aligned.
+// 16 and 8 bytes anywhere an element may be: memory takes loads and stores of them at any address.
+typedef uint32_t words_anywhere __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t pair_anywhere __attribute__((ext_vector_type(2), aligned(2)));
+// All eight elements exist.
 template <typename T>
 __device__ __forceinline__ Chunk<T> load_whole_chunk(const T* p) {
     Chunk<T> c;
 #pragma unroll
     for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-        const u32x4s v = reinterpret_cast<const u32x4s*>(p)[i];
+        const u32x4s v = reinterpret_cast<const words_anywhere*>(p)[i];
 #pragma unroll
         for (int j = 0; j < 4; ++j) c.w[4 * i + j] = v[j];
     }
@@ -230,7 +233,6 @@ struct QuantizeParams {
     int64_t ldx, rows, cols;
     uint8_t *values, *scales, *values_t, *scales_t;
     int64_t ldv, lds, ldv_t, lds_t;
-    bool vec;                               // rows of x start on 16-byte boundaries
 };
 hipError_t launch_quantize(const QuantizeParams& p, bool f32, bool square, hipStream_t st);
 
@@ -243,14 +245,13 @@ struct ProductParams {
     int32_t n_k;                            // 128-k steps
     float* parts;                           // [splits][M][N] partial sums where splits > 1
     int32_t splits;
-    bool vec;                               // rows of y start on 16-byte boundaries
 };
 // How a product is cut into tiles, and its k-steps over workgroups.
 struct ProductShape {
     int32_t tile;                           // rows and features of a tile
     int32_t splits;
 };
-ProductShape product_shape(int64_t M, int64_t N, int32_t n_k, const ChipShape& chip);
+ProductShape product_shape(int64_t M, int64_t N, int32_t n_k, bool f32, const ChipShape& chip);
 hipError_t launch_product(const ProductParams& p, const ProductShape& shape, const ChipShape& chip, bool f32, hipStream_t st);
 
 // The product for few rows, a being the unquantised x [M][K], K elements of each row.
@@ -262,7 +263,6 @@ struct FewRowsParams {
     int64_t ldb, lds_b;
     void* y;
     int64_t ldy;
-    bool vec_x, vec_y;                      // rows start on 16-byte boundaries
 };
 hipError_t launch_few_rows(const FewRowsParams& p, bool f32, hipStream_t st);
 

@@ -285,7 +285,7 @@ PyObject* quantized_linear(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     const at::Tensor* const x = nargs == 2 ? device_tensor(args[0]) : nullptr;
     if (!x || !g_lib.linear || !float_type(*x, &dt) || !read_rows(*x, &M, &K) || !read_matrix(args[1], &w) || w.cols != K || w.rows < 1) Py_RETURN_NONE;
     at::Tensor y = with_last(*x, w.rows);
-    const size_t bytes = g_lib.linear_bytes(M, w.rows, K);
+    const size_t bytes = g_lib.linear_bytes(dt, M, w.rows, K);
     const Room room(bytes, *x);
     int rc;
     {
@@ -307,7 +307,7 @@ PyObject* quantized_linear_backward(PyObject*, PyObject* const* args, Py_ssize_t
         Py_RETURN_NONE;
     if (rows != M || !read_matrix(args[2], &w) || w.cols != N || w.rows != K) Py_RETURN_NONE;
     at::Tensor res[2] = {with_last(*dy, K), at::empty({N, K}, dy->options().dtype(at::kFloat))};
-    const size_t bytes = g_lib.linear_backward_bytes(M, N, K);
+    const size_t bytes = g_lib.linear_backward_bytes(dt, M, N, K);
     const Room room(bytes, *dy);
     int rc;
     {

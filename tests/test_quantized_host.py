@@ -90,11 +90,11 @@ def test_refusals_of_the_products(B):
 
 def test_workspace_sizes(B):
     L = B.lib()
-    assert L.dfa_quantized_linear_workspace_bytes(64, 512, 512) == 0
-    assert L.dfa_quantized_linear_workspace_bytes(65, 512, 512) >= 65 * 512
-    assert L.dfa_quantized_linear_workspace_bytes(0, 512, 512) == 0
-    assert L.dfa_quantized_linear_backward_workspace_bytes(100, 300, 500) >= 100 * 384 + 300 * 128 + 500 * 128
-    many = L.dfa_quantized_product_workspace_bytes(128, 128, 1 << 16)       # one tile, long k: shared out
+    assert L.dfa_quantized_linear_workspace_bytes(0, 64, 512, 512) == 0
+    assert L.dfa_quantized_linear_workspace_bytes(0, 65, 512, 512) >= 65 * 512
+    assert L.dfa_quantized_linear_workspace_bytes(0, 0, 512, 512) == 0 and L.dfa_quantized_linear_workspace_bytes(2, 65, 512, 512) == 0
+    assert L.dfa_quantized_linear_backward_workspace_bytes(1, 100, 300, 500) >= 100 * 384 + 300 * 128 + 500 * 128
+    many = L.dfa_quantized_product_workspace_bytes(1, 128, 128, 1 << 16)       # one tile, long k: shared out
     assert many >= 2 * 128 * 128 * 4 and many % 256 == 0
 
 
