@@ -76,24 +76,30 @@ dfa_quantized_t take_quantized(char** at, int64_t rows, int64_t cols) {
     return q;
 }
 
-int run_quantize(const void* x, dfa_dtype_t dt, int64_t rows, int64_t cols, int64_t ldx, bool square, const dfa_quantized_t* q,
-                 const dfa_quantized_t* qt, void* stream) {
+QuantizeParams quantize_params(const void* x, int64_t rows, int64_t cols, int64_t ldx, const dfa_quantized_t* q, const dfa_quantized_t* qt) {
     QuantizeParams p{};
     p.x = x, p.ldx = ldx, p.rows = rows, p.cols = cols;
     if (q) p.values = static_cast<uint8_t*>(q->values), p.scales = static_cast<uint8_t*>(q->scales), p.ldv = q->ld, p.lds = q->ld_scales;
     if (qt) p.values_t = static_cast<uint8_t*>(qt->values), p.scales_t = static_cast<uint8_t*>(qt->scales), p.ldv_t = qt->ld, p.lds_t = qt->ld_scales;
-    return launch_quantize(p, dt == DFA_F32, square, static_cast<hipStream_t>(stream)) == hipSuccess ? DFA_OK : DFA_ERR_LAUNCH;
+    return p;
 }
 
-int run_product(const dfa_quantized_t& a, const dfa_quantized_t& b, void* y, dfa_dtype_t dt, int64_t M, int64_t N, int64_t K, int64_t ldy, void* parts,
-                const ChipShape& chip, void* stream) {
+ProductParams product_params(const dfa_quantized_t& a, const dfa_quantized_t& b, void* y, int64_t M, int64_t N, int64_t K, int64_t ldy, const ProductShape& s,
+                             void* parts) {
     ProductParams p{};
     p.a = static_cast<const uint8_t*>(a.values), p.a_scales = static_cast<const uint8_t*>(a.scales), p.lda = a.ld, p.lds_a = a.ld_scales;
     p.b = static_cast<const uint8_t*>(b.values), p.b_scales = static_cast<const uint8_t*>(b.scales), p.ldb = b.ld, p.lds_b = b.ld_scales;
     p.y = y, p.ldy = ldy, p.M = M, p.N = N, p.n_k = k_steps(K);
-    const ProductShape s = product_shape(M, N, p.n_k, dt == DFA_F32, chip);
     p.parts = static_cast<float*>(parts), p.splits = s.splits;
-    return launch_product(p, s, chip, dt == DFA_F32, static_cast<hipStream_t>(stream)) == hipSuccess ? DFA_OK : DFA_ERR_LAUNCH;
+    return p;
+}
+
+int status(hipError_t e) { return e == hipSuccess ? DFA_OK : DFA_ERR_LAUNCH; }
+
+int run_product(const dfa_quantized_t& a, const dfa_quantized_t& b, void* y, dfa_dtype_t dt, int64_t M, int64_t N, int64_t K, int64_t ldy, void* parts,
+                const ChipShape& chip, void* stream) {
+    const ProductShape s = product_shape(M, N, k_steps(K), dt == DFA_F32, chip);
+    return status(launch_product(product_params(a, b, y, M, N, K, ldy, s, parts), s, chip, dt == DFA_F32, static_cast<hipStream_t>(stream)));
 }
 
 // Sizes of a quantisation whose grid is counted in 32 bits.
@@ -147,7 +153,7 @@ int dfa_quantize(const void* x, dfa_dtype_t dt, int64_t rows, int64_t cols, int6
             if (rc != DFA_OK) return rc;
         }
     if (!matrix_aligned(x, size_of(dt))) return DFA_ERR_ALIGN;
-    return run_quantize(x, dt, rows, cols, ldx, block_rows != 1, q, q_t, stream);
+    return status(launch_quantize(quantize_params(x, rows, cols, ldx, q, q_t), dt == DFA_F32, block_rows != 1, static_cast<hipStream_t>(stream)));
 }
 
 size_t dfa_quantized_product_workspace_bytes(dfa_dtype_t dt, int64_t M, int64_t N, int64_t K) {
@@ -191,7 +197,7 @@ int dfa_quantized_linear(const void* x, dfa_dtype_t dt, int64_t ldx, dfa_quantiz
         p.x = x, p.ldx = ldx, p.M = M, p.N = N, p.K = K;
         p.b = static_cast<const uint8_t*>(w.values), p.b_scales = static_cast<const uint8_t*>(w.scales), p.ldb = w.ld, p.lds_b = w.ld_scales;
         p.y = y, p.ldy = ldy;
-        return launch_few_rows(p, dt == DFA_F32, static_cast<hipStream_t>(stream)) == hipSuccess ? DFA_OK : DFA_ERR_LAUNCH;
+        return status(launch_few_rows(p, dt == DFA_F32, static_cast<hipStream_t>(stream)));
     }
     if (!quantize_fits(M, K)) return DFA_ERR_TOO_LARGE;
     ChipShape chip;
@@ -200,7 +206,7 @@ int dfa_quantized_linear(const void* x, dfa_dtype_t dt, int64_t ldx, dfa_quantiz
     if (!room(workspace, workspace_bytes, quantized_bytes(M, K) + parts_bytes(M, N, K, dt, chip))) return DFA_ERR_WORKSPACE;
     char* at = static_cast<char*>(workspace);
     const dfa_quantized_t xq = take_quantized(&at, M, K);
-    rc = run_quantize(x, dt, M, K, ldx, false, &xq, nullptr, stream);
+    rc = status(launch_quantize(quantize_params(x, M, K, ldx, &xq, nullptr), dt == DFA_F32, false, static_cast<hipStream_t>(stream)));
     return rc != DFA_OK ? rc : run_product(xq, w, y, dt, M, N, K, ldy, at, chip, stream);
 }
 
@@ -208,7 +214,7 @@ size_t dfa_quantized_linear_backward_workspace_bytes(dfa_dtype_t dt, int64_t M, 
     if (!known(dt) || check_product_sizes(M, K, N) != DFA_OK || check_product_sizes(N, K, M) != DFA_OK) return 0;
     const ChipShape chip = chip_or_default();
     return (size_t)(quantized_bytes(M, N) + quantized_bytes(N, M) + quantized_bytes(K, M) +
-                    std::max(parts_bytes(M, K, N, dt, chip), parts_bytes(N, K, M, DFA_F32, chip)));
+                    parts_bytes(M, K, N, dt, chip) + parts_bytes(N, K, M, DFA_F32, chip));
 }
 
 int dfa_quantized_linear_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, dfa_dtype_t dt, dfa_quantized_t w_t, void* dx, int64_t lddx,
@@ -222,20 +228,34 @@ int dfa_quantized_linear_backward(const void* dy, int64_t lddy, const void* x, i
     if (lddy < N || (dw && (ldx < K || lddw < K)) || (dx && lddx < K)) return DFA_ERR_SHAPE;
     const int64_t es = size_of(dt);
     if (!matrix_aligned(dy, es) || !matrix_aligned(x, es) || !matrix_aligned(dx, es) || !matrix_aligned(dw, 4) || !aligned16(workspace)) return DFA_ERR_ALIGN;
-    if (!quantize_fits(M, N) || !quantize_fits(M, K)) return DFA_ERR_TOO_LARGE;
+    if (!quantize_fits(M, N) || !quantize_fits(M, K) || up(M, 128) / 128 * (up(N, 128) / 128 + up(K, 128) / 128) > kMaxSize) return DFA_ERR_TOO_LARGE;
     ChipShape chip;
     rc = this_chip(&chip);
     if (rc != DFA_OK) return rc;
     const int64_t need = quantized_bytes(M, N) + quantized_bytes(N, M) + quantized_bytes(K, M) +
-                         std::max(parts_bytes(M, K, N, dt, chip), parts_bytes(N, K, M, DFA_F32, chip));
+                         parts_bytes(M, K, N, dt, chip) + parts_bytes(N, K, M, DFA_F32, chip);
     if (!room(workspace, workspace_bytes, need)) return DFA_ERR_WORKSPACE;
     char* at = static_cast<char*>(workspace);
     const dfa_quantized_t dyq = take_quantized(&at, M, N), dyq_t = take_quantized(&at, N, M), xq_t = take_quantized(&at, K, M);
-    rc = run_quantize(dy, dt, M, N, lddy, false, dx ? &dyq : nullptr, dw ? &dyq_t : nullptr, stream);
-    if (rc == DFA_OK && dx) rc = run_product(dyq, w_t, dx, dt, M, K, N, lddx, at, chip, stream);
-    if (rc == DFA_OK && dw) rc = run_quantize(x, dt, M, K, ldx, false, nullptr, &xq_t, stream);
-    if (rc == DFA_OK && dw) rc = run_product(dyq_t, xq_t, dw, DFA_F32, N, K, M, lddw, at, chip, stream);
-    return rc;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const bool f32 = dt == DFA_F32;
+    const QuantizeParams of_dy = quantize_params(dy, M, N, lddy, dx ? &dyq : nullptr, dw ? &dyq_t : nullptr);
+    const QuantizeParams of_x = quantize_params(x, M, K, ldx, nullptr, &xq_t);
+    if (!dx || !dw) {
+        rc = status(launch_quantize(of_dy, f32, false, st));
+        if (rc == DFA_OK && dw) rc = status(launch_quantize(of_x, f32, false, st));
+        if (rc != DFA_OK) return rc;
+        return dx ? run_product(dyq, w_t, dx, dt, M, K, N, lddx, at, chip, stream) : run_product(dyq_t, xq_t, dw, DFA_F32, N, K, M, lddw, at, chip, stream);
+    }
+    rc = status(launch_quantize_pair(of_dy, of_x, f32, st));
+    if (rc != DFA_OK) return rc;
+    const ProductShape s1 = product_shape(M, K, k_steps(N), f32, chip), s2 = product_shape(N, K, k_steps(M), true, chip);
+    const ProductParams p1 = product_params(dyq, w_t, dx, M, K, N, lddx, s1, at);
+    const ProductParams p2 = product_params(dyq_t, xq_t, dw, N, K, M, lddw, s2, at + parts_bytes(M, K, N, dt, chip));
+    // small ones in one launch (1024 x 384 x 1152: 9 and 13 us one after the other, @PAIR@ together)
+    if (pair_fits(p1, p2, s1, s2, chip)) return status(launch_product_pair(p1, p2, s1, s2, chip, f32, st));
+    rc = status(launch_product(p1, s1, chip, f32, st));
+    return rc != DFA_OK ? rc : status(launch_product(p2, s2, chip, true, st));
 }
 
 int dfa_cache_append(const void* k, const void* v, dfa_strides_t sk, dfa_strides_t sv, dfa_dtype_t dt, int32_t B, int32_t T, dfa_cache_t cache,
@@ -255,7 +275,7 @@ int dfa_cache_append(const void* k, const void* v, dfa_strides_t sk, dfa_strides
     p.v = v, p.svb = sv.b, p.svn = sv.n, p.svh = sv.h;
     p.cache = view(cache, shift, table, width, ld_table, lengths, counts);
     p.B = B, p.T = T, p.page_blocks = (int32_t)blocks;
-    return launch_cache_append(p, dt == DFA_F32, cache.D, static_cast<hipStream_t>(stream)) == hipSuccess ? DFA_OK : DFA_ERR_LAUNCH;
+    return status(launch_cache_append(p, dt == DFA_F32, cache.D, static_cast<hipStream_t>(stream)));
 }
 
 size_t dfa_cache_attention_workspace_bytes(int32_t B, int32_t M, int32_t H, int32_t heads, int32_t D, dfa_dtype_t dt, int64_t max_length) {
@@ -288,7 +308,7 @@ int dfa_cache_attention(const void* q, dfa_strides_t sq, dfa_dtype_t dt, int32_t
     p.scale_log2 = scale * kLog2e;
     p.B = B, p.M = M, p.H = H, p.group = H / cache.heads, p.causal = causal ? 1 : 0;
     p.row_tiles = s.row_tiles, p.splits = s.splits, p.split_chunks = s.split_chunks;
-    return launch_cache_attention(p, s, dt == DFA_F32, cache.D, static_cast<hipStream_t>(stream)) == hipSuccess ? DFA_OK : DFA_ERR_LAUNCH;
+    return status(launch_cache_attention(p, s, dt == DFA_F32, cache.D, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

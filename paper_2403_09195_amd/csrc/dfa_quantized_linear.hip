@@ -92,28 +92,23 @@ __device__ __forceinline__ void store16(Y* row, int64_t n, int64_t N, const floa
 template <int T> constexpr uint32_t kTileBytes = T * kScaleBlock;
 template <int T> constexpr uint32_t kTileStage = 2 * (kTileBytes<T> + T);          // both tiles, both sets of scales
 
+// Piece `item` of a product: share by share of the k-steps, a share's tiles in bands of eight rows of tiles.
 template <typename Y, int T, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void product_kernel(ProductParams p, int tiles_m, int tiles_n, int dies) {
+__device__ __forceinline__ void product_tile(const ProductParams& p, int item, char* lds) {
     constexpr int kWaves = WM * WN, G = T / WM / 64;               // groups of 64 rows per wave
     constexpr int kCopies = T / kWaves / 8;                        // 8-row copies per wave, stage and operand
     constexpr uint32_t kStage = kTileStage<T>;
     static_assert(T / WN == 64, "a wave has 64 features");
-    __shared__ __attribute__((aligned(1024))) char lds[2 * kStage];
 
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r16 = lane & 15, g4 = lane >> 4;
 
-    // Workgroups go to the dies in turn: a die takes a run of the tiles, which are numbered in bands of eight rows of tiles, so that
-    // what runs at once on a die shares operands in its L2.
-    const int tiles = tiles_m * tiles_n, per_die = (tiles + dies - 1) / dies;
-    const int t = (int)(blockIdx.x % dies) * per_die + (int)(blockIdx.x / dies);
-    if ((int)(blockIdx.x / dies) >= per_die || t >= tiles) return;
+    const int tiles_m = (int)((p.M + T - 1) / T), tiles_n = (int)((p.N + T - 1) / T), tiles = tiles_m * tiles_n;
+    const int split = item / tiles, t = item - split * tiles;
     constexpr int kBand = 8;
     const int band = t / (kBand * tiles_n), in_band = t - band * kBand * tiles_n;
     const int band_rows = min(kBand, tiles_m - band * kBand);
     const int64_t m0 = (int64_t)(band * kBand + in_band % band_rows) * T, n0 = (int64_t)(in_band / band_rows) * T;
-    const int split = blockIdx.y;
     const int k_begin = (int)((int64_t)p.n_k * split / p.splits), k_end = (int)((int64_t)p.n_k * (split + 1) / p.splits);
 
     // Byte offsets of this lane's source rows, from the tile's first row: rows behind the matrix are its last row again (their results
@@ -222,6 +217,30 @@ void product_kernel(ProductParams p, int tiles_m, int tiles_n, int dies) {
             if (p.splits > 1) store16(p.parts + ((int64_t)split * p.M + row) * p.N, n, p.N, v);
             else store16(static_cast<Y*>(p.y) + row * p.ldy, n, p.N, v);
         }
+}
+
+// Workgroups go to the dies in turn: a die takes a run of the launch's pieces, so that what runs at once on it has operands in common in its L2.
+template <typename Y, int T, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void product_kernel(ProductParams p, int pieces, int per_die, int dies) {
+    __shared__ __attribute__((aligned(1024))) char lds[2 * kTileStage<T>];
+    const int item = (int)(blockIdx.x % dies) * per_die + (int)(blockIdx.x / dies);
+    if (item < pieces) product_tile<Y, T, WM, WN>(p, item, lds);
+}
+
+// Two products whose 128-row tiles all fit the chip at once, in one launch: every die takes a run of either.
+template <typename Y1, typename Y2>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void product_pair_kernel(ProductParams p1, ProductParams p2, int pieces1, int pieces2, int per_die1, int per_die2, int dies) {
+    __shared__ __attribute__((aligned(1024))) char lds[2 * kTileStage<128>];
+    const int die = blockIdx.x % dies, i = blockIdx.x / dies;
+    if (i < per_die2) {
+        const int item = die * per_die2 + i;
+        if (item < pieces2) product_tile<Y2, 128, 2, 2>(p2, item, lds);
+    } else {
+        const int item = die * per_die1 + i - per_die2;
+        if (item < pieces1) product_tile<Y1, 128, 2, 2>(p1, item, lds);
+    }
 }
 
 // y = the sum of the splits' partial results, in their order, W neighbouring elements a thread.  Eight splits' loads are under way at once.
@@ -356,22 +375,35 @@ hipError_t launch_few_typed(const FewRowsParams& p, hipStream_t st) {
     return hipGetLastError();
 }
 
+int64_t pieces_of(const ProductParams& p, const ProductShape& s) { return ((p.M + s.tile - 1) / s.tile) * ((p.N + s.tile - 1) / s.tile) * p.splits; }
+
 template <typename Y>
-hipError_t launch_product_typed(const ProductParams& p, const ProductShape& shape, const ChipShape& chip, hipStream_t st) {
-    const int64_t tiles_m = (p.M + shape.tile - 1) / shape.tile, tiles_n = (p.N + shape.tile - 1) / shape.tile;
-    const int dies = chip.dies > 0 ? chip.dies : 1;
-    const dim3 grid((unsigned)((tiles_m * tiles_n + dies - 1) / dies * dies), (unsigned)p.splits);
-    if (shape.tile == 256) hipLaunchKernelGGL((product_kernel<Y, 256, 2, 4>), grid, dim3(512), 0, st, p, (int)tiles_m, (int)tiles_n, dies);
-    else hipLaunchKernelGGL((product_kernel<Y, 128, 2, 2>), grid, dim3(256), 0, st, p, (int)tiles_m, (int)tiles_n, dies);
+hipError_t launch_sum(const ProductParams& p, hipStream_t st) {
+    if (p.splits <= 1) return hipSuccess;
+    const bool wide = p.N % 4 == 0;                            // four neighbouring elements lie in one row
+    const unsigned blocks = (unsigned)((p.M * p.N + (wide ? 1023 : 255)) / (wide ? 1024 : 256));
+    if (wide) hipLaunchKernelGGL((product_sum_kernel<Y, 4>), dim3(blocks), dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((product_sum_kernel<Y, 1>), dim3(blocks), dim3(256), 0, st, p);
+    return hipGetLastError();
+}
+
+template <typename Y>
+hipError_t launch_product_typed(const ProductParams& p, const ProductShape& shape, int dies, hipStream_t st) {
+    const int pieces = (int)pieces_of(p, shape), per_die = (pieces + dies - 1) / dies;
+    const dim3 grid((unsigned)(per_die * dies));
+    if (shape.tile == 256) hipLaunchKernelGGL((product_kernel<Y, 256, 2, 4>), grid, dim3(512), 0, st, p, pieces, per_die, dies);
+    else hipLaunchKernelGGL((product_kernel<Y, 128, 2, 2>), grid, dim3(256), 0, st, p, pieces, per_die, dies);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? launch_sum<Y>(p, st) : e;
+}
+
+template <typename Y>
+hipError_t launch_pair_typed(const ProductParams& p1, const ProductParams& p2, const ProductShape& s1, const ProductShape& s2, int dies, hipStream_t st) {
+    const int n1 = (int)pieces_of(p1, s1), n2 = (int)pieces_of(p2, s2), per1 = (n1 + dies - 1) / dies, per2 = (n2 + dies - 1) / dies;
+    hipLaunchKernelGGL((product_pair_kernel<Y, float>), dim3((unsigned)((per1 + per2) * dies)), dim3(256), 0, st, p1, p2, n1, n2, per1, per2, dies);
     hipError_t e = hipGetLastError();
-    if (e == hipSuccess && p.splits > 1) {
-        const bool wide = p.N % 4 == 0;                    // four neighbouring elements lie in one row
-        const unsigned blocks = (unsigned)((p.M * p.N + (wide ? 1023 : 255)) / (wide ? 1024 : 256));
-        if (wide) hipLaunchKernelGGL((product_sum_kernel<Y, 4>), dim3(blocks), dim3(256), 0, st, p);
-        else hipLaunchKernelGGL((product_sum_kernel<Y, 1>), dim3(blocks), dim3(256), 0, st, p);
-        e = hipGetLastError();
-    }
-    return e;
+    if (e == hipSuccess) e = launch_sum<Y>(p1, st);
+    return e == hipSuccess ? launch_sum<float>(p2, st) : e;
 }
 
 }  // namespace
@@ -382,14 +414,14 @@ hipError_t launch_product_typed(const ProductParams& p, const ProductShape& shap
 // 512 x 2304 x 768 128/1 8 / 7.1, 256/1 14 / 14.9; 4096 x 2304 x 768 128/1 14 / 16.1, 256/1 18 / 17.3; 4096 x 4096 x 4096 256/1 60 / 58.2, 128/1 67 / 65.5;
 // 64 x 4096 x 4096 128/4 13 / 13.0, 128/1 20 / 20.3; 512 x 4096 x 4096 128/1 21 / 22.7, 128/2 24 / 25.3; 2304 x 768 x 32768 128/4 76 / 75.7, 128/3 74 / 79.8.
 ProductShape product_shape(int64_t M, int64_t N, int32_t n_k, bool f32, const ChipShape& chip) {
-    const double cus = chip.cus > 0 ? chip.cus : 1, rate = 4e6, out = (double)M * N * (f32 ? 4 : 2) / rate, partial = (double)M * N * 8 / rate;
+    const double cus = chip.cus > 0 ? chip.cus : 1, dies = chip.dies > 0 ? chip.dies : 1, rate = 4e6, out = (double)M * N * (f32 ? 4 : 2) / rate, partial = (double)M * N * 8 / rate;
     ProductShape best{128, 1};
     double least = 0;
     for (const int32_t tile : {128, 256}) {
         const double tiles = (double)((M + tile - 1) / tile) * (double)((N + tile - 1) / tile);
         // shares of two k-steps at least, up to where every slot has a workgroup
         for (int32_t s = 1; s == 1 || (s <= n_k / 2 && tiles * s <= 3 * cus); ++s) {
-            const double wgs = tiles * s / cus;
+            const double wgs = std::ceil(tiles * s / dies) * dies / cus;               // of the die that has most
             double steps = (n_k + s - 1) / s;
             if (tile == 128) steps *= wgs <= 1 ? (f32 ? 1.05 : 0.5) : (f32 ? 1.75 : 0.85) * (wgs <= 2 ? 1 : wgs / 2);
             else steps *= (f32 ? 2.8 : 1.48) * std::ceil(wgs);
@@ -401,7 +433,18 @@ ProductShape product_shape(int64_t M, int64_t N, int32_t n_k, bool f32, const Ch
 }
 
 hipError_t launch_product(const ProductParams& p, const ProductShape& shape, const ChipShape& chip, bool f32, hipStream_t st) {
-    return f32 ? launch_product_typed<float>(p, shape, chip, st) : launch_product_typed<__bf16>(p, shape, chip, st);
+    const int dies = chip.dies > 0 ? chip.dies : 1;
+    return f32 ? launch_product_typed<float>(p, shape, dies, st) : launch_product_typed<__bf16>(p, shape, dies, st);
+}
+
+bool pair_fits(const ProductParams& p1, const ProductParams& p2, const ProductShape& s1, const ProductShape& s2, const ChipShape& chip) {
+    return s1.tile == 128 && s2.tile == 128 && pieces_of(p1, s1) + pieces_of(p2, s2) <= 2 * chip.cus;
+}
+
+hipError_t launch_product_pair(const ProductParams& p1, const ProductParams& p2, const ProductShape& s1, const ProductShape& s2, const ChipShape& chip, bool f32,
+                               hipStream_t st) {
+    const int dies = chip.dies > 0 ? chip.dies : 1;
+    return f32 ? launch_pair_typed<float>(p1, p2, s1, s2, dies, st) : launch_pair_typed<__bf16>(p1, p2, s1, s2, dies, st);
 }
 
 hipError_t launch_few_rows(const FewRowsParams& p, bool f32, hipStream_t st) {

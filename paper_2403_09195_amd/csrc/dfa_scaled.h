@@ -235,6 +235,8 @@ struct QuantizeParams {
     int64_t ldv, lds, ldv_t, lds_t;
 };
 hipError_t launch_quantize(const QuantizeParams& p, bool f32, bool square, hipStream_t st);
+// Two matrices of the same type in one launch, in blocks of 1 x 128 of the rows that are written, both with a transpose.
+hipError_t launch_quantize_pair(const QuantizeParams& p1, const QuantizeParams& p2, bool f32, hipStream_t st);
 
 // y[m][n] = sum_k a[m][k] b[n][k] with a [M][K], b [N][K] quantised along k.
 struct ProductParams {
@@ -253,6 +255,10 @@ struct ProductShape {
 };
 ProductShape product_shape(int64_t M, int64_t N, int32_t n_k, bool f32, const ChipShape& chip);
 hipError_t launch_product(const ProductParams& p, const ProductShape& shape, const ChipShape& chip, bool f32, hipStream_t st);
+// Two products in one launch, the first with results of either type, the second in fp32, where their workgroups all fit the chip at once.
+bool pair_fits(const ProductParams& p1, const ProductParams& p2, const ProductShape& s1, const ProductShape& s2, const ChipShape& chip);
+hipError_t launch_product_pair(const ProductParams& p1, const ProductParams& p2, const ProductShape& s1, const ProductShape& s2, const ChipShape& chip, bool f32,
+                               hipStream_t st);
 
 // The product for few rows, a being the unquantised x [M][K], K elements of each row.
 constexpr int64_t kFewRows = 64;
