@@ -298,8 +298,8 @@ int dfa_cache_attention(const void* q, dfa_strides_t sq, dfa_dtype_t dt, int32_t
     rc = this_chip(&chip);
     if (rc != DFA_OK) return rc;
     const CacheAttentionShape s = cache_attention_shape(B, M, H, cache.heads, cache.D, dt == DFA_F32, max_length, chip);
-    // (the merge takes up to eight workgroups for a tile)
-    if ((int64_t)B * cache.heads * s.row_tiles * std::max(s.splits, 8) > kMaxSize) return DFA_ERR_TOO_LARGE;
+    // (the merge takes up to 64 workgroups for a tile)
+    if ((int64_t)B * cache.heads * s.row_tiles * std::max(s.splits, 64) > kMaxSize) return DFA_ERR_TOO_LARGE;
     if (!room(workspace, workspace_bytes, attention_bytes(s, B, cache.heads))) return DFA_ERR_WORKSPACE;
     CacheAttentionParams p{};
     p.q = q, p.sqb = sq.b, p.sqn = sq.n, p.sqh = sq.h;
@@ -308,6 +308,9 @@ int dfa_cache_attention(const void* q, dfa_strides_t sq, dfa_dtype_t dt, int32_t
     p.scale_log2 = scale * kLog2e;
     p.B = B, p.M = M, p.H = H, p.group = H / cache.heads, p.causal = causal ? 1 : 0;
     p.row_tiles = s.row_tiles, p.splits = s.splits, p.split_chunks = s.split_chunks;
+    p.dies = chip.dies > 0 ? chip.dies : 1;
+    p.pieces = B * cache.heads * s.row_tiles * s.splits;
+    p.per_die = (p.pieces + p.dies - 1) / p.dies;
     return status(launch_cache_attention(p, s, dt == DFA_F32, cache.D, static_cast<hipStream_t>(stream)));
 }
 

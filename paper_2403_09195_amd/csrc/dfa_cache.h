@@ -37,6 +37,7 @@ struct CacheAttentionParams {
     int32_t B, M, H, group;                 // group: query heads per head of the cache
     int32_t causal;
     int32_t row_tiles, splits, split_chunks;// 64-token chunks of a split
+    int32_t dies, per_die, pieces;          // pieces of work: one for every row tile and split of a head
 };
 // How a call is cut into workgroups.
 struct CacheAttentionShape {

@@ -16,6 +16,7 @@
 // Bound: the cache's bytes while there are few query rows (a chunk's conversions and products take a quarter of the time that its 8 or 16 KB take at
 // the rate of memory), the vector ALU (exponentials, conversions) beyond some 64 rows.
 #include <algorithm>
+#include <cmath>
 
 #include "dfa_cache.h"
 #include "dfa_mfma.h"
@@ -26,7 +27,8 @@ namespace {
 
 constexpr int kShareWaves = 4;
 constexpr int kChunk = 64;                  // tokens
-constexpr float kLowest = -3e38f;           // a running maximum that has seen nothing
+constexpr float kNothing = -1e30f;          // a running maximum of scores that has seen none
+constexpr float kLowest = -3e38f;           // the same as an exponent
 
 // The four lanes of a query row (r16, in every group of 16) combine their values.
 __device__ __forceinline__ void lane_group_pair(float x, float& a, float& b) {
@@ -87,35 +89,86 @@ __device__ __forceinline__ int splits_used(const CacheAttentionParams& p, int le
     return min(max((chunks + p.split_chunks - 1) / p.split_chunks, 1), p.splits);
 }
 
+// 1 in every byte of four e4m3 values that is not a number (seven ones below the sign: one more carries into bit 7).
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t v) { return (((v & 0x7f7f7f7fu) + 0x01010101u) >> 7) & 0x01010101u; }
+
+// Four keys' scores of a lane's query row.
+template <int NJ, int NP>
+__device__ __forceinline__ void score_keys(const bf16x8 (&k)[NJ], const bf16x8 (&q)[NJ][NP], float* s) {
+    floatx4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int n = 0; n < NP; ++n) z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[j], q[j][n], z, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = z[i];
+}
+
+// Sixteen channels' share of eight keys' values.
+template <int NP>
+__device__ __forceinline__ void add_values(floatx4& acc, const bf16x8& v, const bf16x8 (&p)[NP]) {
+#pragma unroll
+    for (int n = 0; n < NP; ++n) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[n], acc, 0, 0, 0);
+}
+
 template <typename T, int D, int R>
-__global__ __launch_bounds__(64 * kShareWaves) void cache_attention_kernel(CacheAttentionParams p) {
+__device__ __forceinline__ void attend(const CacheAttentionParams& p) {
     constexpr int NJ = D / 32, NB = D / 16, NP = kParts<T>;
+    constexpr bool kHold = D == 64;          // 256 registers hold a chunk's keys and values as bf16 numbers (values: with more than one block of rows)
+    constexpr bool kHoldV = kHold && (R == 2 || R == 3);
     __shared__ floatx4 merge_acc[kShareWaves / 2][R * NB][64];
     __shared__ float merge_stat[kShareWaves / 2][2 * R][64];
 
     const CacheView& c = p.cache;
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r16 = lane & 15, g4 = lane >> 4;
-    uint32_t id = blockIdx.x;
-    const int split = id % p.splits;
-    id /= p.splits;
-    const int tile = id % p.row_tiles;
-    id /= p.row_tiles;
-    const int kv_head = id % c.heads, b = id / c.heads;
+    // Several row tiles walk the same keys: then a die takes a run of the work, its tiles of a head one after the other, and the keys come
+    // from its L2.  Otherwise all sequences' first splits come first, the later ones, which short sequences do not have, last; workgroups go to the
+    // dies in turn, so that every die has its share of either (two splits next to each other put all the second ones on every other die: 64
+    // sequences of 1 to 8192 tokens 144 us, @SPLIT@ this way).
+    int split, tile, kv_head, b;
+    if (p.row_tiles > 1) {
+        uint32_t id = blockIdx.x % p.dies * p.per_die + blockIdx.x / p.dies;
+        if (id >= (uint32_t)p.pieces) return;
+        split = id % p.splits;
+        id /= p.splits;
+        tile = id % p.row_tiles;
+        id /= p.row_tiles;
+        kv_head = id % c.heads, b = id / c.heads;
+    } else {
+        uint32_t id = blockIdx.x;
+        if (id >= (uint32_t)p.pieces) return;
+        kv_head = id % c.heads;
+        id /= c.heads;
+        b = id % p.B, split = id / p.B, tile = 0;
+    }
+
+    // Pages of a chunk: a lane reads keys of 16-token group r16 / 4 and values of group g4 of it.  (The first ones are asked for before it is known
+    // whether the sequence is that long: a trip to memory less.)
+    const int32_t* const table = c.table + b * c.ld_table;
+    const int group_shift = c.page_shift - 4, slot_mask = (1 << c.page_shift) - 1;
+    const int last_place = c.width - 1;
+    struct Pages {
+        int32_t k, v;
+    };
+    auto pages_of = [&](int chunk) {
+        const int kg = 4 * chunk + (r16 >> 2), vg = 4 * chunk + g4;
+        return Pages{table[min(kg >> group_shift, last_place)], table[min(vg >> group_shift, last_place)]};
+    };
+    const int c_begin = split * p.split_chunks;
+    int chunk = c_begin + wave;
+    Pages now = pages_of(chunk), next = pages_of(chunk + kShareWaves);
 
     const int length = sequence_length(c, b), count = sequence_count(p, b), used = splits_used(p, length);
     if (split >= used) return;
     const int rows = p.M * p.group, row0 = tile * 16 * R;
 
-    // rows of the tile, the tokens they attend to, and the chunks that any of them does
-    int end[R], head[R], qi[R], most = 0, least = 0x7fffffff;
+    // the tokens that the tile's rows attend to, and the chunks that any of them does
+    int end[R], most = 0, least = 0x7fffffff;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int rho = row0 + 16 * r + r16;
-        const QueryRow at = query_row(p, kv_head, min(rho, rows - 1));
-        qi[r] = at.i;
-        head[r] = at.head;
-        end[r] = rho < rows ? row_end(p, length, count, at.i) : 0;
+        end[r] = rho < rows ? row_end(p, length, count, rho / p.group) : 0;
     }
     {   // ends grow with i: the tile's first and last rows bound them, except for rows behind the sequence's count
         const int last = min(row0 + 16 * R, rows) - 1, i_last = last / p.group, i_first = row0 / p.group;
@@ -123,13 +176,14 @@ __global__ __launch_bounds__(64 * kShareWaves) void cache_attention_kernel(Cache
         least = i_last < count ? row_end(p, length, count, i_first) : 0;
     }
     const int chunks = (most + kChunk - 1) / kChunk;
-    const int c_begin = split * p.split_chunks, c_end = split == used - 1 ? chunks : min(chunks, c_begin + p.split_chunks);
+    const int c_end = split == used - 1 ? chunks : min(chunks, c_begin + p.split_chunks);
 
     // q: this lane's 8 channels of each product, 16*g4 + 8*(j & 1) + 64*(j / 2)
     bf16x8 qf[R][NJ][NP];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const T* const src = static_cast<const T*>(p.q) + b * p.sqb + qi[r] * p.sqn + head[r] * p.sqh + 16 * g4;
+        const QueryRow at = query_row(p, kv_head, min(row0 + 16 * r + r16, rows - 1));
+        const T* const src = static_cast<const T*>(p.q) + b * p.sqb + at.i * p.sqn + at.head * p.sqh + 16 * g4;
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
             float x[8];
@@ -142,23 +196,12 @@ __global__ __launch_bounds__(64 * kShareWaves) void cache_attention_kernel(Cache
     float top[R], sum[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        top[r] = kLowest;
+        top[r] = kNothing;
         sum[r] = 0.f;
 #pragma unroll
         for (int n = 0; n < NB; ++n) acc[r][n] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // Pages of a chunk: a lane reads keys of 16-token group r16 / 4 and values of group g4 of it.
-    const int32_t* const table = c.table + b * c.ld_table;
-    const int group_shift = c.page_shift - 4, slot_mask = (1 << c.page_shift) - 1;
-    const int last_place = c.width - 1;
-    struct Pages {
-        int32_t k, v;
-    };
-    auto pages_of = [&](int chunk) {
-        const int kg = 4 * chunk + (r16 >> 2), vg = 4 * chunk + g4;
-        return Pages{table[min(kg >> group_shift, last_place)], table[min(vg >> group_shift, last_place)]};
-    };
     u32x4s kr[4][D / 64], vr[NB];
     uint32_t k_scale, v_scale;
     auto load_k = [&](int chunk, int32_t page) {
@@ -180,84 +223,37 @@ __global__ __launch_bounds__(64 * kShareWaves) void cache_attention_kernel(Cache
         for (int n = 0; n < NB; ++n) vr[n] = *reinterpret_cast<const u32x4s*>(at + ((int64_t)(16 * n) << c.page_shift));
     };
 
-    int chunk = c_begin + wave;
-    Pages now{0, 0}, next{0, 0};
     if (chunk < c_end) {
-        now = pages_of(chunk);
         load_k(chunk, now.k);
         load_v(chunk, now.v);
-        if (chunk + kShareWaves < c_end) next = pages_of(chunk + kShareWaves);
     }
+    uint32_t lost = 0;                      // values that were taken out of the walk
     for (; chunk < c_end; chunk += kShareWaves) {
         const bool more = chunk + kShareWaves < c_end;
-        // ---- scores: element 4*t + i of s is key 64*chunk + 16*g4 + 4*t + i against query row r16 of block r
-        float s[R][16];
+        // ---- keys as bf16 numbers, the next ones asked for at once; or all rows' scores of them, the next ones when the scores are used up
+        bf16x8 kf[kHold ? 4 : 1][NJ];
+        float all[kHold ? 1 : R][16];
         {
             const float scale = scale_of(k_scale);
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                floatx4 z[R];
+                bf16x8(&k)[NJ] = kf[kHold ? t : 0];
 #pragma unroll
-                for (int r = 0; r < R; ++r) z[r] = floatx4{0.f, 0.f, 0.f, 0.f};
+                for (int j = 0; j < NJ; ++j) k[j] = scaled_bf16(kr[t][j / 2][2 * (j & 1)], kr[t][j / 2][2 * (j & 1) + 1], scale);
+                if constexpr (!kHold) {
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) {
-                    const u32x4s& w = kr[t][j / 2];
-                    const bf16x8 kf = scaled_bf16(w[2 * (j & 1)], w[2 * (j & 1) + 1], scale);
-#pragma unroll
-                    for (int r = 0; r < R; ++r)
-#pragma unroll
-                        for (int n = 0; n < NP; ++n) z[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][j][n], z[r], 0, 0, 0);
+                    for (int r = 0; r < R; ++r) score_keys<NJ, NP>(k, qf[r], &all[r][4 * t]);
                 }
-#pragma unroll
-                for (int r = 0; r < R; ++r)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[r][4 * t + i] = z[r][i] * p.scale_log2;
             }
         }
         const bool v_there = (uint32_t)now.v < (uint32_t)c.pages;
-        if (more) {
-            load_k(chunk + kShareWaves, next.k);
-            now.k = next.k;
-        }
+        if (kHold && more) load_k(chunk + kShareWaves, next.k);
         // ---- tokens that not every row attends to, pages that do not exist
         const int key0 = kChunk * chunk + 16 * g4;
         const bool masked = kChunk * (chunk + 1) > least || __any(!v_there);
         if (masked) {
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (!v_there || key0 + e >= end[r]) s[r][e] = -INFINITY;
-        }
-        // ---- probabilities
-        bf16x8 pf[R][2][NP];
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            float m = fmaxf(s[r][0], s[r][1]);
-#pragma unroll
-            for (int e = 2; e < 16; ++e) m = fmaxf(m, s[r][e]);
-            m = fmaxf(row_max(m), top[r]);
-            if (__any(m > top[r])) {
-                const float shrink = __builtin_amdgcn_exp2f(top[r] - m);
-                top[r] = m;
-                sum[r] *= shrink;
-#pragma unroll
-                for (int n = 0; n < NB; ++n) acc[r][n] *= shrink;
-            }
-            float w[2][8];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                w[e / 8][e % 8] = __builtin_amdgcn_exp2f(s[r][e] - m);
-                sum[r] += w[e / 8][e % 8];
-            }
-            split_parts<NP>(w[0], pf[r][0]);
-            split_parts<NP>(w[1], pf[r][1]);
-        }
-        // ---- values
-        if (masked) {
             // A value behind every row's end, or on no page, may be anything: 0.  One that some rows attend to and is not a number must not reach
-            // the others through 0 * NaN: it is taken out as well, and the rows that attend to it are made NaN.
-            bool bad = false;
+            // the others through 0 * NaN: it is taken out here, and the rows that attend to it are made NaN after the walk.
             const int have = v_there ? min(max(most - key0, 0), 16) : 0;
             if (have == 0) v_scale = 127;       // nor need the scale of such a page be one
 #pragma unroll
@@ -266,60 +262,130 @@ __global__ __launch_bounds__(64 * kShareWaves) void cache_attention_kernel(Cache
                 for (int w = 0; w < 4; ++w) {
                     const int keep = min(max(have - 4 * w, 0), 4);
                     const uint32_t v = keep == 4 ? vr[n][w] : vr[n][w] & ((1u << (8 * keep)) - 1u);
-                    vr[n][w] = v;
-                    // a byte of 7 ones below its sign: the sum carries into bit 7 of that byte
-                    bad = bad || (((v & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+                    const uint32_t nan = nan_bytes(v);
+                    vr[n][w] = v & ~(nan * 255u);
+                    lost |= nan;
                 }
-            if (__any(bad)) {
-                bf16x8 seen[R][2];
+        }
+        // ---- values as bf16 numbers, where there is room for all of them, and the next ones
+        bf16x8 vf[kHoldV ? NB : 1][2];
+        const float value_scale = scale_of(v_scale);
+        if constexpr (kHoldV) {
 #pragma unroll
-                for (int r = 0; r < R; ++r)
+            for (int n = 0; n < NB; ++n)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) seen[r][e / 8][e % 8] = (__bf16)(v_there && key0 + e < end[r] ? 1.f : 0.f);
+                for (int h = 0; h < 2; ++h) vf[n][h] = scaled_bf16(vr[n][2 * h], vr[n][2 * h + 1], value_scale);
+            if (more) load_v(chunk + kShareWaves, next.v);
+        }
+        float ahead[2][16];
+        auto score_chunk = [&](int r) {
 #pragma unroll
-                for (int n = 0; n < NB; ++n) {
-                    bf16x8 nans[2];
+            for (int t = 0; t < 4; ++t) score_keys<NJ, NP>(kf[kHold ? t : 0], qf[r], &ahead[r & 1][4 * t]);
+        };
+        bf16x8 probs[kHold ? 1 : R][2][NP];    // of all rows where keys were scored for all rows
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const uint32_t byte = (vr[n][e / 4] >> (8 * (e % 4))) & 255u;
-                        nans[e / 8][e % 8] = (__bf16)((byte & 127u) == 127u ? 1.f : 0.f);
-                        if ((byte & 127u) == 127u) vr[n][e / 4] &= ~(255u << (8 * (e % 4)));
+        for (int r = 0; r < R; ++r) {
+            // ---- scores, unscaled: element 4*t + i of s is key 64*chunk + 16*g4 + 4*t + i against query row r16 of block r.  The next block's
+            // products run under this one's exponentials; further ahead there are no registers.
+            if constexpr (kHold) {
+                if (r == 0) score_chunk(0);
+                if (r + 1 < R) score_chunk(r + 1);
+            }
+            float(&s)[16] = kHold ? ahead[r & 1] : all[kHold ? 0 : r];
+            if (masked) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (!v_there || key0 + e >= end[r]) s[e] = -INFINITY;
+            }
+            // ---- probabilities
+            float m = fmaxf(s[0], s[1]);
+#pragma unroll
+            for (int e = 2; e < 16; ++e) m = fmaxf(m, s[e]);
+            m = fmaxf(row_max(m), top[r]);
+            if (__any(m > top[r])) {
+                const float shrink = __builtin_amdgcn_exp2f((top[r] - m) * p.scale_log2);
+                top[r] = m;
+                sum[r] *= shrink;
+#pragma unroll
+                for (int n = 0; n < NB; ++n) acc[r][n] *= shrink;
+            }
+            const float shift = m > kNothing ? -m * p.scale_log2 : 0.f;
+            float w[2][8];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                w[e / 8][e % 8] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], p.scale_log2, shift));
+                sum[r] += w[e / 8][e % 8];
+            }
+            if constexpr (!kHold) {
+                split_parts<NP>(w[0], probs[r][0]);
+                split_parts<NP>(w[1], probs[r][1]);
+            } else {
+                bf16x8 pf[2][NP];
+                split_parts<NP>(w[0], pf[0]);
+                split_parts<NP>(w[1], pf[1]);
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const bf16x8 v = kHoldV ? vf[kHoldV ? n : 0][h] : scaled_bf16(vr[n][2 * h], vr[n][2 * h + 1], value_scale);
+                        add_values<NP>(acc[r][n], v, pf[h]);
                     }
-#pragma unroll
-                    for (int r = 0; r < R; ++r) {
-                        floatx4 hits = {0.f, 0.f, 0.f, 0.f};
-                        hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nans[0], seen[r][0], hits, 0, 0, 0);
-                        hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nans[1], seen[r][1], hits, 0, 0, 0);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (hits[i] > 0.f) acc[r][n][i] = __builtin_nanf("");
-                    }
-                }
+                if (R > 2) __builtin_amdgcn_sched_barrier(0);
             }
         }
-        {
-            const float scale = scale_of(v_scale);
+        if constexpr (!kHold) {
+            if (more) load_k(chunk + kShareWaves, next.k);
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const bf16x8 vf = scaled_bf16(vr[n][2 * h], vr[n][2 * h + 1], scale);
+                    const bf16x8 v = scaled_bf16(vr[n][2 * h], vr[n][2 * h + 1], value_scale);
 #pragma unroll
-                    for (int r = 0; r < R; ++r)
-#pragma unroll
-                        for (int k = 0; k < NP; ++k) acc[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r][h][k], acc[r][n], 0, 0, 0);
+                    for (int r = 0; r < R; ++r) add_values<NP>(acc[r][n], v, probs[r][h]);
                 }
         }
-        if (more) {
-            load_v(chunk + kShareWaves, next.v);
-            now.v = next.v;
-            if (chunk + 2 * kShareWaves < c_end) next = pages_of(chunk + 2 * kShareWaves);
+        if (!kHoldV && more) load_v(chunk + kShareWaves, next.v);
+        now = next;
+        next = pages_of(chunk + 2 * kShareWaves);
+    }
+
+    // ---- values that are not numbers in chunks that not every row attends to: what the rows that do would have got
+    if (__any(lost != 0)) {
+        for (chunk = c_begin + wave; chunk < c_end; chunk += kShareWaves) {
+            now = pages_of(chunk);
+            const bool v_there = (uint32_t)now.v < (uint32_t)c.pages;
+            if (kChunk * (chunk + 1) <= least && !__any(!v_there)) continue;
+            load_v(chunk, now.v);
+            const int key0 = kChunk * chunk + 16 * g4;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                bf16x8 seen[2];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) seen[e / 8][e % 8] = (__bf16)(v_there && key0 + e < end[r] ? 1.f : 0.f);
+#pragma unroll
+                for (int n = 0; n < NB; ++n) {
+                    floatx4 hits = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        bf16x8 nans;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) nans[e] = (__bf16)((nan_bytes(vr[n][2 * h + e / 4]) >> (8 * (e % 4)) & 1u) ? 1.f : 0.f);
+                        hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nans, seen[h], hits, 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (hits[i] > 0.f) acc[r][n][i] = __builtin_nanf("");
+                }
+            }
         }
     }
 
     // ---- the four waves' states into one: 2 and 3 to 0 and 1, then 1 to 0
 #pragma unroll
-    for (int r = 0; r < R; ++r) sum[r] = row_sum(sum[r]);
+    for (int r = 0; r < R; ++r) {
+        sum[r] = row_sum(sum[r]);
+        top[r] = top[r] > kNothing ? top[r] * p.scale_log2 : kLowest;     // exponents of 2 from here on
+    }
 #pragma unroll
     for (int half = kShareWaves / 2; half >= 1; half /= 2) {
         if (wave >= half && wave < 2 * half) {
@@ -352,6 +418,7 @@ __global__ __launch_bounds__(64 * kShareWaves) void cache_attention_kernel(Cache
         float* const part = p.parts + (((int64_t)b * c.heads + kv_head) * p.row_tiles + tile) * p.splits * (kRows * (D + 2)) + (int64_t)split * (kRows * (D + 2));
 #pragma unroll
         for (int r = 0; r < R; ++r) {
+            if (row0 + 16 * r + r16 >= rows) continue;
 #pragma unroll
             for (int n = 0; n < NB; ++n) *reinterpret_cast<floatx4*>(part + (16 * r + r16) * D + 16 * n + 4 * g4) = acc[r][n];
             if (g4 == 0) {
@@ -363,66 +430,101 @@ __global__ __launch_bounds__(64 * kShareWaves) void cache_attention_kernel(Cache
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        if (row0 + 16 * r + r16 >= rows) continue;
+        const int rho = row0 + 16 * r + r16;
+        if (rho >= rows) continue;
+        const QueryRow at = query_row(p, kv_head, rho);
         const float scale = sum[r] == 0.f ? 0.f : 1.f / sum[r];
-        T* const out = static_cast<T*>(p.out) + (((int64_t)b * p.M + qi[r]) * p.H + head[r]) * D + 4 * g4;
+        T* const out = static_cast<T*>(p.out) + (((int64_t)b * p.M + at.i) * p.H + at.head) * D + 4 * g4;
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
             const floatx4 o = acc[r][n] * scale;
             if constexpr (sizeof(T) == 4) *reinterpret_cast<floatx4*>(out + 16 * n) = o;
             else *reinterpret_cast<bf16x4*>(out + 16 * n) = bf16x4{(__bf16)o[0], (__bf16)o[1], (__bf16)o[2], (__bf16)o[3]};
         }
-        if (p.lse && g4 == 0) p.lse[((int64_t)b * p.H + head[r]) * p.M + qi[r]] = sum[r] == 0.f ? -INFINITY : (top[r] + __builtin_amdgcn_logf(sum[r])) * kLn2;
+        if (p.lse && g4 == 0) p.lse[((int64_t)b * p.H + at.head) * p.M + at.i] = sum[r] == 0.f ? -INFINITY : (top[r] + __builtin_amdgcn_logf(sum[r])) * kLn2;
     }
 }
 
-// Merges the splits of a tile's rows: D / 4 lanes to a row.
+// Two waves to a SIMD, 256 registers each.
 template <typename T, int D, int R>
-__global__ __launch_bounds__(256) void cache_attention_merge_kernel(CacheAttentionParams p) {
-    constexpr int kRows = 16 * R, kLanes = D / 4, kRowsPerGroup = 256 / kLanes;
+__global__ __launch_bounds__(64 * kShareWaves) __attribute__((amdgpu_waves_per_eu(2))) void cache_attention_kernel(CacheAttentionParams p) {
+    attend<T, D, R>(p);
+}
+// Where they do not suffice: as many as it takes.
+template <typename T, int D, int R>
+__global__ __launch_bounds__(64 * kShareWaves) void cache_attention_wide_kernel(CacheAttentionParams p) {
+    attend<T, D, R>(p);
+}
+
+// Merges the splits of a tile's rows: D / 4 lanes to a row and share of its splits, `shares` (a power of two) to a row, each of which
+// takes every `shares`-th split, four at a time.  Their loads do not wait to hear which splits were used: every trip to memory is a microsecond or two,
+// and one after the other (one share, the length first) they were 9.8 us of one image's row, now @MERGE@.
+constexpr int kMergeAtOnce = 4;
+template <typename T, int D, int R>
+__global__ __launch_bounds__(256) void cache_attention_merge_kernel(CacheAttentionParams p, int shares, int groups) {
+    constexpr int kRows = 16 * R, kLanes = D / 4, kPart = kRows * (D + 2);
+    __shared__ floatx4 accs[256];
+    __shared__ float tops[256 / kLanes], sums[256 / kLanes];
     const CacheView& c = p.cache;
-    const int groups = (kRows + kRowsPerGroup - 1) / kRowsPerGroup;
+    const int tid = threadIdx.x, place = tid / kLanes, share = place % shares, d = tid % kLanes * 4;
     uint32_t id = blockIdx.x;
-    const int in_tile = id % groups * kRowsPerGroup + (int)threadIdx.x / kLanes;
+    const int in_tile = id % groups * (256 / kLanes / shares) + place / shares;
     id /= groups;
     const int tile = id % p.row_tiles;
     const int kv_head = id / p.row_tiles % c.heads, b = id / p.row_tiles / c.heads;
-    const int rho = tile * kRows + in_tile, d = threadIdx.x % kLanes * 4;
-    if (in_tile >= kRows || rho >= p.M * p.group) return;
-    const int used = splits_used(p, sequence_length(c, b));
-    const float* const part = p.parts + (int64_t)id * p.splits * (kRows * (D + 2));
-    // The loads of 16 splits at a time, before it is known which of them were used: every trip to memory takes a microsecond or two, of
-    // which an earlier form (eight at a time, behind the length) had three; 7.5 us for one image's row, @MERGE@ now.
-    constexpr int kAtOnce = 16, kPart = kRows * (D + 2);
+    const int rho = tile * kRows + in_tile;
+    const bool live = in_tile < kRows && rho < p.M * p.group;
+    const float* const part = p.parts + (int64_t)id * p.splits * kPart;
+
     float top = kLowest, sum = 0.f;
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < p.splits; s0 += kAtOnce) {
-        float t[kAtOnce], l[kAtOnce];
-        floatx4 a[kAtOnce];
+    const int used = splits_used(p, sequence_length(c, b));
+    if (live) {
+        for (int s0 = share; s0 < p.splits; s0 += shares * kMergeAtOnce) {
+            float t[kMergeAtOnce], l[kMergeAtOnce];
+            floatx4 a[kMergeAtOnce];
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) {
-            const float* const at = part + (int64_t)min(s0 + u, p.splits - 1) * kPart;
-            t[u] = at[kRows * D + in_tile];
-            l[u] = at[kRows * (D + 1) + in_tile];
-            a[u] = *reinterpret_cast<const floatx4*>(at + in_tile * D + d);
-        }
-        if (s0 >= used) break;
-        float m = top;
-#pragma unroll
-        for (int u = 0; u < kAtOnce; ++u)
-            if (s0 + u < used) m = fmaxf(m, t[u]);
-        const float shrink = __builtin_amdgcn_exp2f(top - m);
-        sum *= shrink;
-        acc *= shrink;
-        top = m;
-#pragma unroll
-        for (int u = 0; u < kAtOnce; ++u)
-            if (s0 + u < used) {
-                const float w = __builtin_amdgcn_exp2f(t[u] - m);
-                sum += w * l[u];
-                acc += a[u] * w;
+            for (int u = 0; u < kMergeAtOnce; ++u) {
+                const float* const at = part + (int64_t)min(s0 + u * shares, p.splits - 1) * kPart;
+                t[u] = at[kRows * D + in_tile];
+                l[u] = at[kRows * (D + 1) + in_tile];
+                a[u] = *reinterpret_cast<const floatx4*>(at + in_tile * D + d);
             }
+            float m = top;
+#pragma unroll
+            for (int u = 0; u < kMergeAtOnce; ++u)
+                if (s0 + u * shares < used) m = fmaxf(m, t[u]);
+            const float shrink = __builtin_amdgcn_exp2f(top - m);
+            sum *= shrink;
+            acc *= shrink;
+            top = m;
+#pragma unroll
+            for (int u = 0; u < kMergeAtOnce; ++u)
+                if (s0 + u * shares < used) {
+                    const float w = __builtin_amdgcn_exp2f(t[u] - m);
+                    sum += w * l[u];
+                    acc += a[u] * w;
+                }
+        }
     }
+    if (shares > 1) {
+        accs[tid] = acc;
+        if (d == 0) tops[place] = top, sums[place] = sum;
+        __syncthreads();
+        if (share != 0) return;
+        float m = top;
+        for (int x = 1; x < shares; ++x) m = fmaxf(m, tops[place + x]);
+        const float own = __builtin_amdgcn_exp2f(top - m);
+        sum *= own;
+        acc *= own;
+        for (int x = 1; x < shares; ++x) {
+            const float w = __builtin_amdgcn_exp2f(tops[place + x] - m);
+            sum += sums[place + x] * w;
+            acc += accs[tid + x * kLanes] * w;
+        }
+        top = m;
+    }
+    if (!live) return;
     const QueryRow q = query_row(p, kv_head, rho);
     const floatx4 o = acc * (sum == 0.f ? 0.f : 1.f / sum);
     T* const out = static_cast<T*>(p.out) + (((int64_t)b * p.M + q.i) * p.H + q.head) * D + d;
@@ -434,19 +536,22 @@ __global__ __launch_bounds__(256) void cache_attention_merge_kernel(CacheAttenti
 template <typename T, int D, int R>
 hipError_t launch(const CacheAttentionParams& p, hipStream_t st) {
     const int64_t tiles = (int64_t)p.B * p.cache.heads * p.row_tiles;
-    hipLaunchKernelGGL((cache_attention_kernel<T, D, R>), dim3((unsigned)(tiles * p.splits)), dim3(64 * kShareWaves), 0, st, p);
+    const dim3 grid((unsigned)(p.per_die * p.dies)), block(64 * kShareWaves);
+    if constexpr (D == 128 && R == 2) hipLaunchKernelGGL((cache_attention_wide_kernel<T, D, R>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((cache_attention_kernel<T, D, R>), grid, block, 0, st, p);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && p.splits > 1) {
-        constexpr int kRowsPerGroup = 256 / (D / 4);
-        const int64_t groups = (16 * R + kRowsPerGroup - 1) / kRowsPerGroup;
-        hipLaunchKernelGGL((cache_attention_merge_kernel<T, D, R>), dim3((unsigned)(tiles * groups)), dim3(256), 0, st, p);
+        int shares = 1;
+        while (shares * kMergeAtOnce < p.splits && shares < 256 / (D / 4)) shares *= 2;
+        const int rows = p.M * p.group < 16 * R ? p.M * p.group : 16 * R, at_once = 256 / (D / 4) / shares, groups = (rows + at_once - 1) / at_once;
+        hipLaunchKernelGGL((cache_attention_merge_kernel<T, D, R>), dim3((unsigned)(tiles * groups)), dim3(256), 0, st, p, shares, groups);
         e = hipGetLastError();
     }
     return e;
 }
 
 // Most 16-row blocks of a tile: what 256 registers hold.
-int most_blocks(int32_t D, bool f32) { return (f32 ? 2 : 4) / (D / 64); }
+int most_blocks(int32_t D, bool f32) { return D == 128 ? (f32 ? 1 : 2) : f32 ? 2 : 3; }
 
 }  // namespace
 
@@ -454,13 +559,30 @@ CacheAttentionShape cache_attention_shape(int32_t B, int32_t M, int32_t H, int32
     const int64_t rows = (int64_t)M * (H / heads);
     CacheAttentionShape s;
     s.blocks = 1;
-    while (16 * s.blocks < rows && s.blocks < most_blocks(D, f32)) s.blocks *= 2;
+    while (16 * s.blocks < rows && s.blocks < most_blocks(D, f32)) ++s.blocks;
     s.row_tiles = (int32_t)((rows + 16 * s.blocks - 1) / (16 * s.blocks));
     const int64_t tiles = (int64_t)B * heads * s.row_tiles, chunks = (max_length + kChunk - 1) / kChunk;
-    // workgroups for four to a CU, each with a chunk for every wave at least
-    const int64_t wanted = std::min((4 * (int64_t)chip.cus + tiles - 1) / tiles, (chunks + kShareWaves - 1) / kShareWaves);
-    const int64_t per = (chunks + std::max(wanted, (int64_t)1) - 1) / std::max(wanted, (int64_t)1);
-    s.split_chunks = (int32_t)std::max((per + kShareWaves - 1) / kShareWaves * kShareWaves, (int64_t)kShareWaves);
+    const int64_t cus = chip.cus > 0 ? chip.cus : 1, most = std::max((chunks + kShareWaves - 1) / kShareWaves, (int64_t)1);      // a chunk for every wave
+    int64_t shares = 1;
+    if (s.blocks == 1) {
+        // Bound by the cache's bytes: a workgroup for every compute unit.  Shares beyond that cost more in partial results and their merge than they
+        // shorten the walk.  Us with one / two workgroups to a CU: 1 row, 65536 tokens of 8 heads of 128 28.1 / 28.9; 4 x 12 heads, 16384 tokens
+        // 22.8 / 24.3; with two chunks a wave at least one image's row 8.2 / 8.7 us.
+        shares = std::min((cus + tiles - 1) / tiles, most);
+    } else {
+        // Bound by what the waves compute: the estimated time in us, the least taken.  A step of a workgroup (a chunk for every wave) takes some 0.4 us
+        // for 16 rows of 64 channels (twice that with another workgroup on the compute unit, which two fill), its start and end 3 us,
+        // partial results go at 4 TB/s and their merge takes a launch.
+        double least = 0;
+        for (int64_t n = 1; n <= std::min(most, (int64_t)64); ++n) {
+            const double pieces = (double)tiles * n, full = std::floor(pieces / (2 * cus)), rest = pieces - full * 2 * cus;
+            const double step = 0.4 * s.blocks * (D / 64) * (f32 ? 2 : 1), walk = (double)((most + n - 1) / n) * step;
+            const double us = full * (2 * walk + 3) + (rest > cus ? 2 * walk + 3 : rest > 0 ? walk + 3 : 0) +
+                              (n > 1 ? 4 + pieces * 16 * s.blocks * (D + 2) * 8 / 4e6 : 0);
+            if (n == 1 || us < least) least = us, shares = n;
+        }
+    }
+    s.split_chunks = (int32_t)((most + shares - 1) / shares * kShareWaves);
     s.splits = (int32_t)std::max((chunks + s.split_chunks - 1) / s.split_chunks, (int64_t)1);
     s.part_floats = (int64_t)16 * s.blocks * (D + 2);
     return s;
@@ -472,7 +594,7 @@ hipError_t launch_cache_attention(const CacheAttentionParams& p, const CacheAtte
         return s.blocks == 1 ? launch<float, 64, 1>(p, st) : launch<float, 64, 2>(p, st);
     }
     if (D == 128) return s.blocks == 1 ? launch<__bf16, 128, 1>(p, st) : launch<__bf16, 128, 2>(p, st);
-    return s.blocks == 1 ? launch<__bf16, 64, 1>(p, st) : s.blocks == 2 ? launch<__bf16, 64, 2>(p, st) : launch<__bf16, 64, 4>(p, st);
+    return s.blocks == 1 ? launch<__bf16, 64, 1>(p, st) : s.blocks == 2 ? launch<__bf16, 64, 2>(p, st) : launch<__bf16, 64, 3>(p, st);
 }
 
 }  // namespace dfa
