@@ -354,8 +354,8 @@ int dfa_quantized_product(dfa_quantized_t a, dfa_quantized_t b, void *y, dfa_dty
 
 /*
  * The projection dfa_linear with a quantised weight: x (device, dtype dt, [M][K] with row pitch ldx) is quantised by the call in blocks
- * of 1 x 128, y[m][n] = sum_k x[m][k] * w[n][k] as above, y of x's dtype.  Any M, N, K >= 1.  Up to 64 rows take one launch and
- * no workspace; others quantise into the workspace first.
+ * of 1 x 128, y[m][n] = sum_k x[m][k] * w[n][k] as above, y of x's dtype.  Any M, N, K >= 1.  Few rows (64 at
+ * most, fewer of long ones) take one launch and no workspace; others quantise into the workspace first.
  */
 size_t dfa_quantized_linear_workspace_bytes(dfa_dtype_t dt, int64_t M, int64_t N, int64_t K);
 int dfa_quantized_linear(const void *x, dfa_dtype_t dt, int64_t ldx, dfa_quantized_t w, void *y, int64_t M, int64_t N, int64_t K, int64_t ldy,

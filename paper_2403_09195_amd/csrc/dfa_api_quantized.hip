@@ -178,8 +178,10 @@ int dfa_quantized_product(dfa_quantized_t a, dfa_quantized_t b, void* y, dfa_dty
 }
 
 size_t dfa_quantized_linear_workspace_bytes(dfa_dtype_t dt, int64_t M, int64_t N, int64_t K) {
-    if (!known(dt) || check_product_sizes(M, N, K) != DFA_OK || M <= kFewRows) return 0;
-    return (size_t)(quantized_bytes(M, K) + parts_bytes(M, N, K, dt, chip_or_default()));
+    if (!known(dt) || check_product_sizes(M, N, K) != DFA_OK) return 0;
+    const ChipShape chip = chip_or_default();
+    if (few_rows_blocks(M, N, K, dt == DFA_F32, chip)) return 0;
+    return (size_t)(quantized_bytes(M, K) + parts_bytes(M, N, K, dt, chip));
 }
 
 int dfa_quantized_linear(const void* x, dfa_dtype_t dt, int64_t ldx, dfa_quantized_t w, void* y, int64_t M, int64_t N, int64_t K, int64_t ldy,
@@ -192,17 +194,17 @@ int dfa_quantized_linear(const void* x, dfa_dtype_t dt, int64_t ldx, dfa_quantiz
     if (ldx < K || ldy < N) return DFA_ERR_SHAPE;
     const int64_t es = size_of(dt);
     if (!matrix_aligned(x, es) || !matrix_aligned(y, es) || !aligned16(workspace)) return DFA_ERR_ALIGN;
-    if (M <= kFewRows) {
-        FewRowsParams p{};
-        p.x = x, p.ldx = ldx, p.M = M, p.N = N, p.K = K;
-        p.b = static_cast<const uint8_t*>(w.values), p.b_scales = static_cast<const uint8_t*>(w.scales), p.ldb = w.ld, p.lds_b = w.ld_scales;
-        p.y = y, p.ldy = ldy;
-        return status(launch_few_rows(p, dt == DFA_F32, static_cast<hipStream_t>(stream)));
-    }
     if (!quantize_fits(M, K)) return DFA_ERR_TOO_LARGE;
     ChipShape chip;
     rc = this_chip(&chip);
     if (rc != DFA_OK) return rc;
+    if (const int blocks = few_rows_blocks(M, N, K, dt == DFA_F32, chip)) {
+        FewRowsParams p{};
+        p.x = x, p.ldx = ldx, p.M = M, p.N = N, p.K = K;
+        p.b = static_cast<const uint8_t*>(w.values), p.b_scales = static_cast<const uint8_t*>(w.scales), p.ldb = w.ld, p.lds_b = w.ld_scales;
+        p.y = y, p.ldy = ldy;
+        return status(launch_few_rows(p, blocks, dt == DFA_F32, static_cast<hipStream_t>(stream)));
+    }
     if (!room(workspace, workspace_bytes, quantized_bytes(M, K) + parts_bytes(M, N, K, dt, chip))) return DFA_ERR_WORKSPACE;
     char* at = static_cast<char*>(workspace);
     const dfa_quantized_t xq = take_quantized(&at, M, K);

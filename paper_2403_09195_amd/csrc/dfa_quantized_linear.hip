@@ -367,10 +367,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(FewRowsParams 
 }
 
 template <typename T>
-hipError_t launch_few_typed(const FewRowsParams& p, hipStream_t st) {
+hipError_t launch_few_typed(const FewRowsParams& p, int blocks, hipStream_t st) {
     const dim3 grid((unsigned)((p.N + 15) / 16)), block(64 * kFewWaves);
-    if (p.M <= 16) hipLaunchKernelGGL((few_rows_kernel<T, 1>), grid, block, 0, st, p);
-    else if (p.M <= 32) hipLaunchKernelGGL((few_rows_kernel<T, 2>), grid, block, 0, st, p);
+    if (blocks == 1) hipLaunchKernelGGL((few_rows_kernel<T, 1>), grid, block, 0, st, p);
+    else if (blocks == 2) hipLaunchKernelGGL((few_rows_kernel<T, 2>), grid, block, 0, st, p);
     else hipLaunchKernelGGL((few_rows_kernel<T, 4>), grid, block, 0, st, p);
     return hipGetLastError();
 }
@@ -415,7 +415,7 @@ hipError_t launch_pair_typed(const ProductParams& p1, const ProductParams& p2, c
 // 64 x 4096 x 4096 128/4 13 / 13.0, 128/1 20 / 20.3; 512 x 4096 x 4096 128/1 21 / 22.7, 128/2 24 / 25.3; 2304 x 768 x 32768 128/4 76 / 75.7, 128/3 74 / 79.8.
 ProductShape product_shape(int64_t M, int64_t N, int32_t n_k, bool f32, const ChipShape& chip) {
     const double cus = chip.cus > 0 ? chip.cus : 1, dies = chip.dies > 0 ? chip.dies : 1, rate = 4e6, out = (double)M * N * (f32 ? 4 : 2) / rate, partial = (double)M * N * 8 / rate;
-    ProductShape best{128, 1};
+    ProductShape best{128, 1, 0};
     double least = 0;
     for (const int32_t tile : {128, 256}) {
         const double tiles = (double)((M + tile - 1) / tile) * (double)((N + tile - 1) / tile);
@@ -426,9 +426,10 @@ ProductShape product_shape(int64_t M, int64_t N, int32_t n_k, bool f32, const Ch
             if (tile == 128) steps *= wgs <= 1 ? (f32 ? 1.05 : 0.5) : (f32 ? 1.75 : 0.85) * (wgs <= 2 ? 1 : wgs / 2);
             else steps *= (f32 ? 2.8 : 1.48) * std::ceil(wgs);
             const double us = steps + out + (s > 1 ? 3 + s * partial : 0);
-            if (least == 0 || us < least) least = us, best = ProductShape{tile, s};
+            if (least == 0 || us < least) least = us, best = ProductShape{tile, s, 0};
         }
     }
+    best.us = least;
     return best;
 }
 
@@ -447,8 +448,25 @@ hipError_t launch_product_pair(const ProductParams& p1, const ProductParams& p2,
     return f32 ? launch_pair_typed<float>(p1, p2, s1, s2, dies, st) : launch_pair_typed<__bf16>(p1, p2, s1, s2, dies, st);
 }
 
-hipError_t launch_few_rows(const FewRowsParams& p, bool f32, hipStream_t st) {
-    return f32 ? launch_few_typed<float>(p, st) : launch_few_typed<__bf16>(p, st);
+// Every workgroup quantises x, 0.25 us for each turn of its groups of lanes (R rows of 32 / R blocks, see the kernel), and b comes at 5 TB/s; a launch apart
+// and the tiles' own estimate on the other side.  Us here / in two launches, bf16: 4096 x 4096 (N x K) 16 rows 8.9 / 15, 32 rows 13.4 / 15, 64 rows 22.5 /
+// 15.0; 768 x 768 64 rows 7.8 / 8.5; 4096 x 8192 32 rows 26.1 / 17.4; 16384 x 768 64 rows 18.5 / 8.7.
+int few_rows_blocks(int64_t M, int64_t N, int64_t K, bool f32, const ChipShape& chip) {
+    if (M > kFewRows) return 0;
+    const int64_t n_k = (K + kScaleBlock - 1) / kScaleBlock;
+    int64_t turns = 0;
+    int blocks = 0;
+    for (const int r : {1, 2, 4}) {
+        const int64_t t = ((M + r - 1) / r) * ((n_k * r + 31) / 32);
+        if (16 * r >= M && (!blocks || t <= turns)) turns = t, blocks = r;     // of equals the one that has fewer blocks of b under way
+    }
+    const double cus = chip.cus > 0 ? chip.cus : 1, rounds = std::fmax(1.0, (double)N / (16 * cus));
+    const double here = 4.5 + rounds * 0.25 * (double)turns + (double)N * (double)K / 5e6;
+    return here <= 8.5 + product_shape(M, N, (int32_t)n_k, f32, chip).us ? blocks : 0;
+}
+
+hipError_t launch_few_rows(const FewRowsParams& p, int blocks, bool f32, hipStream_t st) {
+    return f32 ? launch_few_typed<float>(p, blocks, st) : launch_few_typed<__bf16>(p, blocks, st);
 }
 
 }  // namespace dfa

@@ -252,6 +252,7 @@ struct ProductParams {
 struct ProductShape {
     int32_t tile;                           // rows and features of a tile
     int32_t splits;
+    double us;                              // estimated time
 };
 ProductShape product_shape(int64_t M, int64_t N, int32_t n_k, bool f32, const ChipShape& chip);
 hipError_t launch_product(const ProductParams& p, const ProductShape& shape, const ChipShape& chip, bool f32, hipStream_t st);
@@ -270,6 +271,8 @@ struct FewRowsParams {
     void* y;
     int64_t ldy;
 };
-hipError_t launch_few_rows(const FewRowsParams& p, bool f32, hipStream_t st);
+// 16-row blocks that the launch is made for, 0 where quantising x first and multiplying tiles is faster.
+int few_rows_blocks(int64_t M, int64_t N, int64_t K, bool f32, const ChipShape& chip);
+hipError_t launch_few_rows(const FewRowsParams& p, int blocks, bool f32, hipStream_t st);
 
 }  // namespace dfa

@@ -136,7 +136,8 @@ def test_product_selects_rows_and_columns(B):
     np.testing.assert_array_equal(y.double().cpu().numpy(), ref.held(ae)[:, perm.numpy()].T)
 
 
-LINEARS = [(1, 64, 64), (1, 130, 1), (2, 1533, 1000), (16, 48, 4096), (17, 100, 129), (31, 257, 640), (33, 64, 2000), (64, 96, 768), (65, 96, 768), (333, 153, 1000)]
+LINEARS = [(1, 64, 64), (1, 130, 1), (2, 1533, 1000), (16, 48, 4096), (17, 100, 129), (31, 257, 640), (33, 64, 2000), (64, 96, 768), (65, 96, 768), (333, 153, 1000),
+           (9, 40, 8000), (16, 200, 600), (24, 33, 5000), (50, 64, 8192), (64, 1024, 6001)]
 
 
 @pytest.mark.parametrize("M,N,K", LINEARS)

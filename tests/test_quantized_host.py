@@ -90,7 +90,8 @@ def test_refusals_of_the_products(B):
 
 def test_workspace_sizes(B):
     L = B.lib()
-    assert L.dfa_quantized_linear_workspace_bytes(0, 64, 512, 512) == 0
+    assert L.dfa_quantized_linear_workspace_bytes(0, 1, 4096, 4096) == 0 and L.dfa_quantized_linear_workspace_bytes(1, 16, 512, 512) == 0
+    assert L.dfa_quantized_linear_workspace_bytes(0, 64, 4096, 8192) >= 64 * 8192        # every workgroup quantising x would take longer
     assert L.dfa_quantized_linear_workspace_bytes(0, 65, 512, 512) >= 65 * 512
     assert L.dfa_quantized_linear_workspace_bytes(0, 0, 512, 512) == 0 and L.dfa_quantized_linear_workspace_bytes(2, 65, 512, 512) == 0
     assert L.dfa_quantized_linear_backward_workspace_bytes(1, 100, 300, 500) >= 100 * 384 + 300 * 128 + 500 * 128
