@@ -394,8 +394,8 @@ typedef struct { void *k; void *v; void *scales; int32_t pages; int32_t heads; i
  *   k, v   device, dtype dt, [B, T, heads, D] through strides (every row 16-byte aligned)
  * A page's scale holds its new tokens and is not below what its earlier tokens (of this sequence, slots before the first new one) have;
  * where it grows, those move to it: values are rounded to the new scale, a change only below e4m3's normal range.  Slots behind the last new token
- * and pages without new tokens are left as they were.  Tokens before 0 or behind the table's last page are dropped.  No two sequences of a call may
- * write to one page.  Asynchronous on `stream`; allocates nothing.
+ * and pages without new tokens are left as they were.  Tokens before 0 or behind the table's last page are dropped.  No page may
+ * take new tokens at two places of the table.  Asynchronous on `stream`; allocates nothing.
  */
 int dfa_cache_append(const void *k, const void *v, dfa_strides_t sk, dfa_strides_t sv, dfa_dtype_t dt, int32_t B, int32_t T, dfa_cache_t cache,
                      const int32_t *table, int32_t width, int64_t ld_table, const int32_t *lengths, const int32_t *counts, void *stream);

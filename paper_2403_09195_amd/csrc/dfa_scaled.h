@@ -31,15 +31,8 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
     return byte > (int32_t)kLeastScaleByte ? (uint32_t)byte : kLeastScaleByte;
 }
 
-// 2^e and 2^-e of a scale byte in 1 .. 253.
+// 2^e of a scale byte.
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
-__device__ __forceinline__ float inverse_scale(uint32_t byte) { return __builtin_bit_cast(float, (254u - byte) << 23); }
-
-// Four values, |x * inv| <= 448 or not finite, as e4m3 (the conversion makes NaN of infinities).
-__device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d, float inv) {
-    int v = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, v, true);
-}
 
 // Eight e4m3 values as bf16 numbers times their scale: exact (a value has 4 significant bits).
 __device__ __forceinline__ bf16x8 scaled_bf16(uint32_t lo, uint32_t hi, float scale) {
