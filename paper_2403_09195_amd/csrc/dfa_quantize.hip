@@ -3,7 +3,7 @@
 // Bound: memory; a matrix is read once and written once (twice where both it and its transpose are wanted).  A workgroup
 // takes a tile of 128 columns, a thread 8 columns of R consecutive rows, so that every wave-wide load covers whole 256-byte (bf16) pieces
 // of rows, a row's maximum is four exchanges among 16 lanes, and with R = 4 the four rows of a column are the 4 bytes that the thread leaves in
-// LDS for the transpose.
+// LDS for the transpose.  32768 x 2304 and 32768 x 768 in bf16, the one both ways and the other transposed, in one launch: 70 us, the 74 of a copy of as many bytes.
 #include "dfa_scaled.h"
 
 namespace dfa {
