@@ -354,7 +354,7 @@ int dfa_quantized_product(dfa_quantized_t a, dfa_quantized_t b, void *y, dfa_dty
 
 /*
  * The projection dfa_linear with a quantised weight: x (device, dtype dt, [M][K] with row pitch ldx) is quantised by the call in blocks
- * of 1 x 128, y[m][n] = sum_k x[m][k] * w[n][k] as above, y of x's dtype.  Any M, N, K >= 1.  Few rows (64 at
+ * of 1 x 128, y[m][n] = sum_k x[m][k] * w[n][k] as above, y of x's dtype and apart from x and w.  Any M, N, K >= 1.  Few rows (64 at
  * most, fewer of long ones) take one launch and no workspace; others quantise into the workspace first.
  */
 size_t dfa_quantized_linear_workspace_bytes(dfa_dtype_t dt, int64_t M, int64_t N, int64_t K);
@@ -366,7 +366,7 @@ int dfa_quantized_linear(const void *x, dfa_dtype_t dt, int64_t ldx, dfa_quantiz
  *   dx [M][K] = dy . w    dy in 1 x 128 blocks along N; w_t: w transposed, [K][N] (quantised with block_rows = 128 it holds the forward's
  *                         values)
  *   dw [N][K] = dy^T . x  dy and x in blocks of 128 along M, each column on its own; fp32
- * dy, x and dx have dtype dt.  dx or dw may be NULL (not wanted): x is read for dw only, w_t for dx only.
+ * dy, x and dx have dtype dt; dx and dw overlap none of the operands.  dx or dw may be NULL (not wanted): x is read for dw only, w_t for dx only.
  */
 size_t dfa_quantized_linear_backward_workspace_bytes(dfa_dtype_t dt, int64_t M, int64_t N, int64_t K);
 int dfa_quantized_linear_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx, dfa_dtype_t dt, dfa_quantized_t w_t, void *dx,
@@ -405,7 +405,7 @@ int dfa_cache_append(const void *k, const void *v, dfa_strides_t sk, dfa_strides
  *   q       device, dtype dt, [B, M, H, D] through strides (every row 16-byte aligned); H a multiple of cache.heads
  *   causal  0: a row attends to all lengths[b] tokens; otherwise row i of the n = counts[b] (M) attends to the first
  *           lengths[b] - (n - 1 - i): the rows are the sequence's last tokens.
- *   out     device, dtype dt, contiguous [B, M, H, D];  lse device, fp32 [B, H, M], or NULL
+ *   out     device, dtype dt, contiguous [B, M, H, D], apart from q;  lse device, fp32 [B, H, M], or NULL
  *           rows that attend to nothing (no tokens, i >= counts[b]) are 0 and -inf; lengths outside 0 .. width * page count as the
  *           nearest of them
  *   max_length  host: no sequence is expected to be longer (longer ones are right, but slower).  It decides how the walk is shared out.

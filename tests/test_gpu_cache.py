@@ -148,6 +148,39 @@ def test_attention_counts_views_and_missing_pages(B, dtype):
         assert none is None and torch.equal(o2, out)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("power", [10, 40, 100])
+@pytest.mark.parametrize("M,D", [(1, 64), (20, 64), (80, 64), (1, 128), (20, 128)])
+def test_attention_large_scores(B, M, D, power, sign, dtype):
+    """Scores of up to 2^112, of either sign or all of one.  q and k are integers times a power of two, so all scores are exact and two of them are equal or
+    at least 128 exponents apart: the row is the mean of its best tokens' values.  Bars: the division (2^-20) and the rounding of the result; five
+    roundings of lse."""
+    import torch
+    rng = np.random.default_rng(M + D + power)
+    page, T = 32, 700
+    cache = _garbage(B, rng, 24, 1, page, D)
+    table = np.arange(24, dtype=np.int32)[None, :][:, ::-1].copy()
+    k = torch.from_numpy(rng.integers(1 if sign < 0 else -8, 9, (1, T, 1, D)).astype(np.float32)).cuda()
+    v, _ = _tensor(rng, (1, T, 1, D), "bf16")
+    B.cache_append(k, v.float(), cache, _ints(table), _ints([T]))
+    kk, vv, there = cache_ref.Model(cache).sequence(0, table, T)
+    np.testing.assert_array_equal(kk[:, 0], k.double().cpu().numpy()[0, :, 0])
+    assert there.all()
+    qe = rng.integers(-8, 0 if sign < 0 else 9, (1, M, 1, D)) * 2.0 ** power
+    q = torch.from_numpy(qe).to({"bf16": torch.bfloat16, "fp32": torch.float32}[dtype]).cuda()
+    scores = qe[0, :, 0] @ kk[:, 0].T                                          # exact
+    scores[np.arange(T)[None, :] >= T - (M - 1 - np.arange(M))[:, None]] = -np.inf
+    best = scores == scores.max(1, keepdims=True)
+    want = best @ vv[:, 0] / best.sum(1, keepdims=True)
+    want_lse = scores.max(1) * 0.125 + np.log(best.sum(1))
+    bar = (2.0 ** -8 if dtype == "bf16" else 0.0) * np.abs(want) + 2.0 ** -20 * np.abs(vv).max()
+    for limit in (1, 300, None):
+        out, lse = B.cache_attention(q, cache, _ints(table), _ints([T]), 0.125, max_length=limit)
+        assert (np.abs(out.double().cpu().numpy()[0, :, 0] - want) <= bar).all()
+        assert (np.abs(lse.double().cpu().numpy()[0, 0] - want_lse) <= 2.0 ** -21 * np.abs(want_lse)).all()
+
+
 def test_attention_lengths_out_of_range(B):
     rng = np.random.default_rng(9)
     cache, model, table = _filled(B, rng, 3, 1, 16, 64, [40, 48, 10])
