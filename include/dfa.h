@@ -346,6 +346,7 @@ int dfa_quantize(const void *x, dfa_dtype_t dt, int64_t rows, int64_t cols, int6
  *   workspace  device, 16-byte aligned, dfa_quantized_product_workspace_bytes(dt, M, N, K) (0 = none, NULL allowed): partial sums of
  *              products whose k-steps are shared out over workgroups.  Written and read by this call only: calls that may
  *              overlap need one each.
+ * (fp32: values that lie below fp32's normal range, 2^-126, scale included, may count as 0; this holds for the operators below too.)
  * The sums are in a fixed order: equal calls give equal results.  Asynchronous on `stream`; allocates nothing.
  */
 size_t dfa_quantized_product_workspace_bytes(dfa_dtype_t dt, int64_t M, int64_t N, int64_t K);
@@ -412,8 +413,9 @@ int dfa_cache_append(const void *k, const void *v, dfa_strides_t sk, dfa_strides
  *   workspace   device, 16-byte aligned, dfa_cache_attention_workspace_bytes() of the same arguments (0 = none, NULL allowed); written and
  *           read by this call only: calls that may overlap, captured ones among them, need one each.
  * dt = DFA_BF16: bf16 operands, probabilities rounded to bf16 before the second product, fp32 sums and statistics; dt = DFA_F32: 24-bit
- * operands throughout.  Keys, values and rows that are not finite reach only the rows that attend to them.  One launch, two where the walk is shared
- * out over workgroups; equal calls give equal results.  Asynchronous on `stream`; allocates nothing.
+ * operands throughout.  Cached values below 2^-126, scale included, may count as 0.  Keys, values and rows that are not finite reach only the
+ * rows that attend to them.  One launch, two where the walk is shared out over workgroups; equal calls give equal results.
+ * Asynchronous on `stream`; allocates nothing.
  */
 size_t dfa_cache_attention_workspace_bytes(int32_t B, int32_t M, int32_t H, int32_t heads, int32_t D, dfa_dtype_t dt, int64_t max_length);
 int dfa_cache_attention(const void *q, dfa_strides_t sq, dfa_dtype_t dt, int32_t B, int32_t M, int32_t H, dfa_cache_t cache, const int32_t *table,
