@@ -77,9 +77,9 @@ __device__ __forceinline__ void quantize_tile(const QuantizeParams& p, uint32_t 
             if (c16 == 0) bytes[R * rg + i] = (uint8_t)byte;
         }
         __syncthreads();
-        // whole 16 bytes: rows are counted up to a multiple of 16 in the array of scales
+        // whole 16 bytes: rows are counted up to a multiple of 16 in the array of scales, what follows may be another matrix's
         const int64_t first = rb * kTileRows + 16 * tid;
-        if (tid < kTileRows / 16 && first < p.lds)
+        if (tid < kTileRows / 16 && first < p.rows)
             *reinterpret_cast<u32x4s*>(p.scales + cb * p.lds + first) = *reinterpret_cast<const u32x4s*>(bytes + 16 * tid);
     }
 
@@ -113,9 +113,10 @@ __device__ __forceinline__ void quantize_tile(const QuantizeParams& p, uint32_t 
         }
         if (rg == 0) {
             // columns behind the last are zeros, with the least scale, up to a multiple of 16
+            const int64_t cols16 = (p.cols + 15) / 16 * 16;
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (col + j < p.lds_t) p.scales_t[rb * p.lds_t + col + j] = (uint8_t)(col + j < p.cols ? byte[j] : kLeastScaleByte);
+                if (col + j < cols16) p.scales_t[rb * p.lds_t + col + j] = (uint8_t)(col + j < p.cols ? byte[j] : kLeastScaleByte);
         }
         __syncthreads();
 #pragma unroll
