@@ -124,7 +124,7 @@ __device__ __forceinline__ void product_tile(const ProductParams& p, int item, c
         a_off[u] = (uint32_t)(min((int64_t)row, p.M - 1 - m0) * p.lda) + 16u * chunk;
         b_off[u] = (uint32_t)(min((int64_t)row, p.N - 1 - n0) * p.ldb) + 16u * chunk;
     }
-    // scale bytes: four rows per lane, the last four of the array where it ends
+    // scale bytes: four rows per lane, the four that hold the last row behind it (the arrays may go on with other rows, or end there)
     const int srow = 4 * lane;
     const uint32_t lds_addr = (uint32_t)(uintptr_t)DFA_LDS_PTR(void, &lds[0]);
     const uint8_t* const a_tile = p.a + m0 * p.lda;
@@ -142,8 +142,8 @@ __device__ __forceinline__ void product_tile(const ProductParams& p, int item, c
         if (T >= 256 ? wave < 2 : wave == 0) {
             const bool of_b = T >= 256 ? wave == 1 : lane >= T / 4;
             const int r = T >= 256 ? srow : srow & (T - 1);
-            const uint8_t* const src = of_b ? p.b_scales + (int64_t)ks * p.lds_b + min(n0 + r, p.lds_b - 4)
-                                            : p.a_scales + (int64_t)ks * p.lds_a + min(m0 + r, p.lds_a - 4);
+            const uint8_t* const src = of_b ? p.b_scales + (int64_t)ks * p.lds_b + min(n0 + r, (p.N - 1) & ~(int64_t)3)
+                                            : p.a_scales + (int64_t)ks * p.lds_a + min(m0 + r, (p.M - 1) & ~(int64_t)3);
             copy4_to_lds(reinterpret_cast<const float*>(src), at + 2 * kTileBytes<T> + (T >= 256 ? T * wave : 0));
         }
     };

@@ -63,3 +63,23 @@ def test_quantize_into_a_larger_matrix(B, rows, cols, transpose, block_rows, dty
             assert (s[:, at + R:at + R16] == 1).all()
             assert (s[:, :at] == KEPT).all() and (s[:, at + R16:] == KEPT).all()
             assert (v[:at] == KEPT).all() and (v[at + R:] == KEPT).all() and (v[:, ld:] == KEPT).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(10, 40, 300), (70, 300, 130), (130, 17, 5000), (300, 200, 700)])
+def test_products_of_slices(B, M, N, K):
+    """Operands that are the first, middle and last rows of larger matrices: the bits that copies of these rows give."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(M + N + K)
+    normal = lambda *shape: torch.randn(shape, generator=gen, device="cuda").to(torch.bfloat16)
+    rows = lambda m, first, n: B.QuantizedMatrix(m.values[first:first + n], m.scales[:, first:first + -(-n // 16) * 16], m.cols)
+    copy = lambda m: B.QuantizedMatrix(m.values.clone(), m.scales.contiguous().clone(), m.cols)
+    for before, behind in ((0, 48), (32, 16), (112, 0)):
+        a, b = B.quantize(normal(before + M + behind, K)), B.quantize(normal(before + N + behind, K))
+        pa, pb = rows(a, before, M), rows(b, before, N)
+        for dtype in (torch.float32, torch.bfloat16):
+            assert torch.equal(B.quantized_product(pa, pb, dtype), B.quantized_product(copy(pa), copy(pb), dtype))
+        x, dy = normal(M, K), normal(M, N)
+        assert torch.equal(B.quantized_linear(x, pb), B.quantized_linear(x, copy(pb)))
+        wt = rows(B.quantize(normal(before + K + behind, N)), before, K)
+        for got, want in zip(B.quantized_linear_backward(dy, x, wt), B.quantized_linear_backward(dy, x, copy(wt))):
+            assert torch.equal(got, want)
