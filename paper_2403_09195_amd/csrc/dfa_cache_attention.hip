@@ -30,7 +30,7 @@ constexpr int kShareWaves = 4;
 constexpr int kChunk = 64;                  // tokens
 constexpr float kNothing = -3.4e38f;        // a running maximum of scores that has seen none
 constexpr float kLowest = -3e38f;           // the same as an exponent
-constexpr float kLarge = 4096.f;            // exponents beyond which a wave's scores have bases
+constexpr float kLarge = 4096.f;            // exponents beyond which a wave subtracts the maximum before it scales
 
 // The four lanes of a query row (r16, in every group of 16) combine their values.
 __device__ __forceinline__ void lane_group_pair(float x, float& a, float& b) {
@@ -120,7 +120,6 @@ __device__ __forceinline__ void attend(const CacheAttentionParams& p) {
     constexpr bool kHoldV = kHold && (R == 2 || R == 3);
     __shared__ floatx4 merge_acc[kShareWaves / 2][R * NB][64];
     __shared__ float merge_stat[kShareWaves / 2][2 * R][64];
-    __shared__ float bases[kShareWaves][R][64];
 
     const CacheView& c = p.cache;
     const int tid = threadIdx.x;
@@ -231,9 +230,9 @@ __device__ __forceinline__ void attend(const CacheAttentionParams& p) {
         load_v(chunk, now.v);
     }
     // An exponent is one multiply-add of score and maximum, off by the rounding of the scaled maximum: beyond some 2^30 that alone is more than an exponent
-    // can be.  A wave that meets a large maximum takes scores from a base of each row on (in LDS: no registers are left for it).
+    // can be.  A wave that has met a large maximum subtracts each row's maximum from its scores first: off by half a step of the difference only, wherever
+    // the maximum stood before.
     bool large = false;
-    float* const base = &bases[wave][0][lane];
     uint32_t lost = 0;                      // values that were taken out of the walk
     for (; chunk < c_end; chunk += kShareWaves) {
         const bool more = chunk + kShareWaves < c_end;
@@ -299,11 +298,7 @@ __device__ __forceinline__ void attend(const CacheAttentionParams& p) {
                 if (r + 1 < R) score_chunk(r + 1);
             }
             float(&s)[16] = kHold ? ahead[r & 1] : all[kHold ? 0 : r];
-            if (masked || large) {
-                if (large) {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) s[e] -= base[64 * r];
-                }
+            if (masked) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     if (!v_there || key0 + e >= end[r]) s[e] = -INFINITY;
@@ -319,18 +314,12 @@ __device__ __forceinline__ void attend(const CacheAttentionParams& p) {
                 sum[r] *= shrink;
 #pragma unroll
                 for (int n = 0; n < NB; ++n) acc[r][n] *= shrink;
-                if (__any(m > kNothing && fabsf(m) * p.scale_log2 > kLarge)) {
-                    if (!large) {
+                if (__any(m > kNothing && fabsf(m) * p.scale_log2 > kLarge)) large = true;
+            }
+            if (large) {
 #pragma unroll
-                        for (int x = 0; x < R; ++x) base[64 * x] = 0.f;
-                        large = true;
-                    }
-                    const float up = m > kNothing ? m : 0.f;
-                    base[64 * r] += up;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) s[e] -= up;
-                    top[r] = m -= up;
-                }
+                for (int e = 0; e < 16; ++e) s[e] -= m;
+                m = 0.f;
             }
             const float shift = m > kNothing ? -m * p.scale_log2 : 0.f;
             float w[2][8];
@@ -407,7 +396,6 @@ __device__ __forceinline__ void attend(const CacheAttentionParams& p) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         sum[r] = row_sum(sum[r]);
-        if (large && top[r] > kNothing) top[r] += base[64 * r];
         top[r] = top[r] > kNothing ? top[r] * p.scale_log2 : kLowest;     // exponents of 2 from here on
     }
 #pragma unroll
