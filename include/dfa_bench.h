@@ -78,6 +78,29 @@ int dfa_launch_image(int32_t backward, dfa_dtype_t dt, int32_t B, int32_t H, int
                      const dfa_branch_t *branches, int32_t nb, const int32_t *head_offsets, dfa_launch_image_t *image, void *bytes);
 
 /*
+ * Which kernels the operators on 8-bit operands launch for a shape (no GPU needed; without one, the MI355X's).  They go by estimated times, so
+ * this is what tests and benchmarks ask when they mean one form in particular.
+ *   call   DFA_CALL_*; sizes as in dfa_quantized_product, dfa_quantized_linear, dfa_quantized_linear_backward
+ */
+#define DFA_CALL_PRODUCT 0
+#define DFA_CALL_LINEAR 1
+#define DFA_CALL_DX 2
+#define DFA_CALL_DW 3
+typedef struct {
+    int32_t few_rows;       /* 16-row blocks of the launch that quantises x itself; 0: x is quantised first, tiles are multiplied */
+    int32_t tile, splits;   /* rows of a tile, shares of the k-steps (0 with few_rows) */
+    int32_t paired;         /* gradients, both wanted: one launch multiplies for dx and dw */
+} dfa_quantized_form_t;
+int dfa_quantized_describe(int32_t call, dfa_dtype_t dt, int64_t M, int64_t N, int64_t K, dfa_quantized_form_t *form);
+
+typedef struct {
+    int32_t tile_rows, row_tiles;   /* query rows of a tile, tiles of a head of the cache */
+    int32_t splits, split_tokens;   /* shares of a walk, tokens of a share */
+} dfa_cache_attention_form_t;
+int dfa_cache_attention_describe(int32_t B, int32_t M, int32_t H, int32_t heads, int32_t D, dfa_dtype_t dt, int64_t max_length,
+                                 dfa_cache_attention_form_t *form);
+
+/*
  * Measurement aid (no part of the operator): what the matrix cores sustain on their own, the
  * ceiling that the kernels' MFMA rooflines are also quoted against.  Runs a loop of
  * independent v_mfma_f32_32x32x16_bf16 on the whole chip (two waves per SIMD, no memory

@@ -27,7 +27,8 @@ EXPORTS = [
     "dfa_quantized_linear_workspace_bytes", "dfa_quantized_linear_backward", "dfa_quantized_linear_backward_workspace_bytes",
     "dfa_cache_append", "dfa_cache_attention", "dfa_cache_attention_workspace_bytes",
 ]
-BENCH_EXPORTS = ["dfa_launch_describe", "dfa_launch_image", "dfa_forward_timed", "dfa_mfma_peak", "dfa_dense_unfused", "dfa_dense_unfused_workspace_bytes"]
+BENCH_EXPORTS = ["dfa_launch_describe", "dfa_launch_image", "dfa_forward_timed", "dfa_mfma_peak", "dfa_dense_unfused", "dfa_dense_unfused_workspace_bytes",
+                 "dfa_quantized_describe", "dfa_cache_attention_describe"]
 
 
 class Branch(ctypes.Structure):
@@ -47,6 +48,17 @@ class Quantized(ctypes.Structure):
 
 class Cache(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "scales")] + [(n, ctypes.c_int32) for n in ("pages", "heads", "page", "D")]
+
+
+CALL_PRODUCT, CALL_LINEAR, CALL_DX, CALL_DW = 0, 1, 2, 3
+
+
+class QuantizedForm(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("few_rows", "tile", "splits", "paired")]
+
+
+class CacheAttentionForm(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("tile_rows", "row_tiles", "splits", "split_tokens")]
 
 
 class Launch(ctypes.Structure):
@@ -135,6 +147,8 @@ def lib():
         L.dfa_cache_append.argtypes = [vp, vp, Strides, Strides, ctypes.c_int, i32, i32, Cache, vp, i32, i64, vp, vp, vp]
         L.dfa_cache_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, ctypes.c_int, i64]
         L.dfa_cache_attention.argtypes = [vp, Strides, ctypes.c_int, i32, i32, i32, Cache, vp, i32, i64, vp, vp, i32, f32, i64, vp, vp, vp, st, vp]
+        L.dfa_quantized_describe.argtypes = [i32, ctypes.c_int, i64, i64, i64, ctypes.POINTER(QuantizedForm)]
+        L.dfa_cache_attention_describe.argtypes = [i32, i32, i32, i32, i32, ctypes.c_int, i64, ctypes.POINTER(CacheAttentionForm)]
         for name in EXPORTS + BENCH_EXPORTS:
             if name != "dfa_error_string":
                 getattr(L, name).restype = ctypes.c_size_t if name.endswith("_workspace_bytes") else ctypes.c_int
@@ -913,3 +927,17 @@ def cache_attention(q, cache, table, lengths, scale, causal=True, counts=None, m
                                      lse.data_ptr() if want_lse else None, ptr, size, _stream()), "dfa_cache_attention")
     _keep(keep)
     return out, lse
+
+
+def describe_quantized(call, dtype_code, M, N, K):
+    """QuantizedForm that a call (CALL_*) of this size takes (no GPU needed)."""
+    form = QuantizedForm()
+    _check(lib().dfa_quantized_describe(call, dtype_code, M, N, K, ctypes.byref(form)), "dfa_quantized_describe")
+    return form
+
+
+def describe_cache_attention(B, M, H, heads, D, dtype_code, max_length):
+    """CacheAttentionForm that a call of this size takes (no GPU needed)."""
+    form = CacheAttentionForm()
+    _check(lib().dfa_cache_attention_describe(B, M, H, heads, D, dtype_code, max_length, ctypes.byref(form)), "dfa_cache_attention_describe")
+    return form

@@ -5,7 +5,7 @@
 #include <cmath>
 #include <new>
 
-#include "../../include/dfa.h"
+#include "../../include/dfa_bench.h"
 #include "dfa_cache.h"
 
 namespace {
@@ -314,6 +314,44 @@ int dfa_cache_attention(const void* q, dfa_strides_t sq, dfa_dtype_t dt, int32_t
     p.pieces = B * cache.heads * s.row_tiles * s.splits;
     p.per_die = (p.pieces + p.dies - 1) / p.dies;
     return status(launch_cache_attention(p, s, dt == DFA_F32, cache.D, static_cast<hipStream_t>(stream)));
+}
+
+// ---- which form a call takes (dfa_bench.h) ----
+
+int dfa_quantized_describe(int32_t call, dfa_dtype_t dt, int64_t M, int64_t N, int64_t K, dfa_quantized_form_t* form) {
+    if (!form) return DFA_ERR_NULL;
+    if (!known(dt)) return DFA_ERR_DTYPE;
+    if (call < DFA_CALL_PRODUCT || call > DFA_CALL_DW) return DFA_ERR_SHAPE;
+    const bool f32 = dt == DFA_F32, gradient = call == DFA_CALL_DX || call == DFA_CALL_DW;
+    int rc = gradient ? check_product_sizes(M, K, N) : check_product_sizes(M, N, K);
+    if (rc == DFA_OK && gradient) rc = check_product_sizes(N, K, M);
+    if (rc != DFA_OK) return rc;
+    const ChipShape chip = chip_or_default();
+    *form = dfa_quantized_form_t{};
+    if (call == DFA_CALL_LINEAR) form->few_rows = few_rows_blocks(M, N, K, f32, chip);
+    if (form->few_rows) return DFA_OK;
+    ProductShape s = product_shape(M, N, k_steps(K), f32, chip);
+    if (gradient) {
+        const ProductShape s1 = product_shape(M, K, k_steps(N), f32, chip), s2 = product_shape(N, K, k_steps(M), true, chip);
+        ProductParams p1{}, p2{};
+        p1.M = M, p1.N = K, p1.splits = s1.splits;
+        p2.M = N, p2.N = K, p2.splits = s2.splits;
+        form->paired = pair_fits(p1, p2, s1, s2, chip);
+        s = call == DFA_CALL_DX ? s1 : s2;
+    }
+    form->tile = s.tile, form->splits = s.splits;
+    return DFA_OK;
+}
+
+int dfa_cache_attention_describe(int32_t B, int32_t M, int32_t H, int32_t heads, int32_t D, dfa_dtype_t dt, int64_t max_length,
+                                 dfa_cache_attention_form_t* form) {
+    if (!form) return DFA_ERR_NULL;
+    if (!known(dt)) return DFA_ERR_DTYPE;
+    const int rc = check_attention_sizes(B, M, H, heads, D, max_length);
+    if (rc != DFA_OK) return rc;
+    const CacheAttentionShape s = cache_attention_shape(B, M, H, heads, D, dt == DFA_F32, max_length, chip_or_default());
+    *form = dfa_cache_attention_form_t{16 * s.blocks, s.row_tiles, s.splits, s.split_chunks * 64};
+    return DFA_OK;
 }
 
 }  // extern "C"
