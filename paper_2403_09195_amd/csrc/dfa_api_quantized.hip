@@ -131,7 +131,7 @@ int64_t attention_bytes(const CacheAttentionShape& s, int32_t B, int32_t heads) 
 
 int check_attention_sizes(int32_t B, int32_t M, int32_t H, int32_t heads, int32_t D, int64_t max_length) {
     if (B < 1 || M < 1 || heads < 1 || H < heads || H % heads || (D != 64 && D != 128) || max_length < 0) return DFA_ERR_SHAPE;
-    if ((int64_t)M * (H / heads) > kMaxSize - 256 || max_length > kMaxSize - 256) return DFA_ERR_TOO_LARGE;
+    if ((int64_t)M * (H / heads) > kMaxSize - 256 || max_length > kMaxSize - 256 || (int64_t)B * heads > kMaxSize) return DFA_ERR_TOO_LARGE;
     return DFA_OK;
 }
 
