@@ -13,7 +13,11 @@ namespace {
 using namespace dfa;
 
 constexpr int64_t kMaxSize = 0x7fffffff;            // rows, columns
+constexpr int64_t kMaxThreads = (int64_t)1 << 32;   // a grid holds fewer
 constexpr int64_t kMaxPitch = (int64_t)1 << 23;     // bytes of a quantised row: tiles address up to 256 rows with 32-bit offsets
+
+// Whether workgroups of this size, and the few more that even the dies' runs out, make a grid: it holds fewer than 2^32 threads.
+bool grid_fits(int64_t workgroups, int64_t threads) { return workgroups < kMaxThreads / threads - 64; }
 
 int64_t up(int64_t x, int64_t of) { return (x + of - 1) / of * of; }
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
@@ -34,7 +38,7 @@ int check_quantized(const dfa_quantized_t& q, int64_t rows, int64_t cols) {
 
 int check_product_sizes(int64_t M, int64_t N, int64_t K) {
     if (M <= 0 || N <= 0 || K <= 0) return DFA_ERR_SHAPE;
-    if (M > kMaxSize || N > kMaxSize || K > kMaxPitch || up(M, 128) / 128 * (up(N, 128) / 128) >= ((int64_t)1 << 30)) return DFA_ERR_TOO_LARGE;
+    if (M > kMaxSize || N > kMaxSize || K > kMaxPitch || !grid_fits(up(M, 128) / 128 * (up(N, 128) / 128), 256)) return DFA_ERR_TOO_LARGE;
     return DFA_OK;
 }
 
@@ -102,9 +106,10 @@ int run_product(const dfa_quantized_t& a, const dfa_quantized_t& b, void* y, dfa
     return status(launch_product(product_params(a, b, y, M, N, K, ldy, s, parts), s, chip, dt == DFA_F32, static_cast<hipStream_t>(stream)));
 }
 
-// Sizes of a quantisation whose grid is counted in 32 bits.
+// Sizes of a quantisation that a grid holds, in tiles of 32 rows or of 128.
 bool quantize_fits(int64_t rows, int64_t cols) {
-    return rows <= kMaxSize && cols <= kMaxSize && up(rows, 32) / 32 * (up(cols, 128) / 128) <= kMaxSize;
+    if (rows > kMaxSize || cols > kMaxSize) return false;
+    return grid_fits(up(rows, 32) / 32 * (up(cols, 128) / 128), 256) && grid_fits(up(rows, 128) / 128 * (up(cols, 128) / 128), 512);
 }
 
 // Sizes of a cache and of what addresses it; lengths and pages themselves are device memory, which the kernels bound.
@@ -230,7 +235,7 @@ int dfa_quantized_linear_backward(const void* dy, int64_t lddy, const void* x, i
     if (lddy < N || (dw && (ldx < K || lddw < K)) || (dx && lddx < K)) return DFA_ERR_SHAPE;
     const int64_t es = size_of(dt);
     if (!matrix_aligned(dy, es) || !matrix_aligned(x, es) || !matrix_aligned(dx, es) || !matrix_aligned(dw, 4) || !aligned16(workspace)) return DFA_ERR_ALIGN;
-    if (!quantize_fits(M, N) || !quantize_fits(M, K) || up(M, 128) / 128 * (up(N, 128) / 128 + up(K, 128) / 128) > kMaxSize) return DFA_ERR_TOO_LARGE;
+    if (!quantize_fits(M, N) || !quantize_fits(M, K) || !grid_fits(up(M, 128) / 128 * (up(N, 128) / 128 + up(K, 128) / 128), 512)) return DFA_ERR_TOO_LARGE;
     ChipShape chip;
     rc = this_chip(&chip);
     if (rc != DFA_OK) return rc;
@@ -272,7 +277,8 @@ int dfa_cache_append(const void* k, const void* v, dfa_strides_t sk, dfa_strides
     if (!rows_aligned(k, sk, size_of(dt)) || !rows_aligned(v, sv, size_of(dt)) || !matrix_aligned(counts, 4)) return DFA_ERR_ALIGN;
     // tokens start anywhere in a page, and no more pages than the table names are touched
     const int64_t blocks = std::min(((int64_t)T + cache.page - 2) / cache.page + 1, (int64_t)width);
-    if (T > kMaxSize - 256 || B * blocks * 2 * cache.heads > kMaxSize) return DFA_ERR_TOO_LARGE;
+    const int32_t threads = std::max(cache.page * cache.D / 32, 64);
+    if (T > kMaxSize - 256 || !grid_fits(B * blocks, threads) || !grid_fits(B * blocks * 2 * cache.heads, threads)) return DFA_ERR_TOO_LARGE;
     p.k = k, p.skb = sk.b, p.skn = sk.n, p.skh = sk.h;
     p.v = v, p.svb = sv.b, p.svn = sv.n, p.svh = sv.h;
     p.cache = view(cache, shift, table, width, ld_table, lengths, counts);
@@ -301,7 +307,8 @@ int dfa_cache_attention(const void* q, dfa_strides_t sq, dfa_dtype_t dt, int32_t
     if (rc != DFA_OK) return rc;
     const CacheAttentionShape s = cache_attention_shape(B, M, H, cache.heads, cache.D, dt == DFA_F32, max_length, chip);
     // (the merge takes up to 64 workgroups for a tile)
-    if ((int64_t)B * cache.heads * s.row_tiles * std::max(s.splits, 64) > kMaxSize) return DFA_ERR_TOO_LARGE;
+    const int64_t tiles = (int64_t)B * cache.heads * s.row_tiles;
+    if (!grid_fits(tiles, 256) || !grid_fits(tiles * (s.splits > 1 ? std::max(s.splits, 64) : 1), 256)) return DFA_ERR_TOO_LARGE;
     if (!room(workspace, workspace_bytes, attention_bytes(s, B, cache.heads))) return DFA_ERR_WORKSPACE;
     CacheAttentionParams p{};
     p.q = q, p.sqb = sq.b, p.sqn = sq.n, p.sqh = sq.h;
