@@ -29,7 +29,6 @@ namespace {
 constexpr int kShareWaves = 4;
 constexpr int kChunk = 64;                  // tokens
 constexpr float kNothing = -3.4e38f;        // a running maximum of scores that has seen none
-constexpr float kLowest = -3e38f;           // the same as an exponent
 constexpr float kLarge = 4096.f;            // exponents beyond which a wave subtracts the maximum before it scales
 
 // The four lanes of a query row (r16, in every group of 16) combine their values.
@@ -84,6 +83,10 @@ __device__ __forceinline__ int sequence_length(const CacheView& c, int b) {
 }
 __device__ __forceinline__ int sequence_count(const CacheAttentionParams& p, int b) {
     return p.cache.counts ? min(max(p.cache.counts[b], 0), p.M) : p.M;
+}
+// lse of a row whose largest score, unscaled, is `top`.
+__device__ __forceinline__ float row_lse(const CacheAttentionParams& p, float top, float sum) {
+    return sum == 0.f ? -INFINITY : __builtin_fmaf(top, p.scale_log2 * kLn2, __builtin_amdgcn_logf(sum) * kLn2);
 }
 // Splits that hold some of a sequence's tokens; the last one takes what is behind it too.
 __device__ __forceinline__ int splits_used(const CacheAttentionParams& p, int length) {
@@ -392,11 +395,11 @@ __device__ __forceinline__ void attend(const CacheAttentionParams& p) {
         }
     }
 
-    // ---- the four waves' states into one: 2 and 3 to 0 and 1, then 1 to 0
+    // ---- the four waves' states into one: 2 and 3 to 0 and 1, then 1 to 0.  Maxima stay unscaled, here and in partial results: their differences, not the scaled
+    // maxima, are what is rounded, and a scaled maximum may pass fp32's range.
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         sum[r] = row_sum(sum[r]);
-        top[r] = top[r] > kNothing ? top[r] * p.scale_log2 : kLowest;     // exponents of 2 from here on
     }
 #pragma unroll
     for (int half = kShareWaves / 2; half >= 1; half /= 2) {
@@ -414,7 +417,7 @@ __device__ __forceinline__ void attend(const CacheAttentionParams& p) {
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const float other = merge_stat[wave][2 * r][lane], m = fmaxf(top[r], other);
-                const float mine = __builtin_amdgcn_exp2f(top[r] - m), theirs = __builtin_amdgcn_exp2f(other - m);
+                const float mine = __builtin_amdgcn_exp2f((top[r] - m) * p.scale_log2), theirs = __builtin_amdgcn_exp2f((other - m) * p.scale_log2);
                 top[r] = m;
                 sum[r] = sum[r] * mine + merge_stat[wave][2 * r + 1][lane] * theirs;
 #pragma unroll
@@ -453,7 +456,7 @@ __device__ __forceinline__ void attend(const CacheAttentionParams& p) {
             if constexpr (sizeof(T) == 4) *reinterpret_cast<floatx4*>(out + 16 * n) = o;
             else *reinterpret_cast<bf16x4*>(out + 16 * n) = bf16x4{(__bf16)o[0], (__bf16)o[1], (__bf16)o[2], (__bf16)o[3]};
         }
-        if (p.lse && g4 == 0) p.lse[((int64_t)b * p.H + at.head) * p.M + at.i] = sum[r] == 0.f ? -INFINITY : (top[r] + __builtin_amdgcn_logf(sum[r])) * kLn2;
+        if (p.lse && g4 == 0) p.lse[((int64_t)b * p.H + at.head) * p.M + at.i] = row_lse(p, top[r], sum[r]);
     }
 }
 
@@ -488,7 +491,7 @@ __global__ __launch_bounds__(256) void cache_attention_merge_kernel(CacheAttenti
     const bool live = in_tile < kRows && rho < p.M * p.group;
     const float* const part = p.parts + (int64_t)id * p.splits * kPart;
 
-    float top = kLowest, sum = 0.f;
+    float top = kNothing, sum = 0.f;
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
     const int used = splits_used(p, sequence_length(c, b));
     if (live) {
@@ -506,14 +509,14 @@ __global__ __launch_bounds__(256) void cache_attention_merge_kernel(CacheAttenti
 #pragma unroll
             for (int u = 0; u < kMergeAtOnce; ++u)
                 if (s0 + u * shares < used) m = fmaxf(m, t[u]);
-            const float shrink = __builtin_amdgcn_exp2f(top - m);
+            const float shrink = __builtin_amdgcn_exp2f((top - m) * p.scale_log2);
             sum *= shrink;
             acc *= shrink;
             top = m;
 #pragma unroll
             for (int u = 0; u < kMergeAtOnce; ++u)
                 if (s0 + u * shares < used) {
-                    const float w = __builtin_amdgcn_exp2f(t[u] - m);
+                    const float w = __builtin_amdgcn_exp2f((t[u] - m) * p.scale_log2);
                     sum += w * l[u];
                     acc += a[u] * w;
                 }
@@ -526,11 +529,11 @@ __global__ __launch_bounds__(256) void cache_attention_merge_kernel(CacheAttenti
         if (share != 0) return;
         float m = top;
         for (int x = 1; x < shares; ++x) m = fmaxf(m, tops[place + x]);
-        const float own = __builtin_amdgcn_exp2f(top - m);
+        const float own = __builtin_amdgcn_exp2f((top - m) * p.scale_log2);
         sum *= own;
         acc *= own;
         for (int x = 1; x < shares; ++x) {
-            const float w = __builtin_amdgcn_exp2f(tops[place + x] - m);
+            const float w = __builtin_amdgcn_exp2f((tops[place + x] - m) * p.scale_log2);
             sum += sums[place + x] * w;
             acc += accs[tid + x * kLanes] * w;
         }
@@ -542,7 +545,7 @@ __global__ __launch_bounds__(256) void cache_attention_merge_kernel(CacheAttenti
     T* const out = static_cast<T*>(p.out) + (((int64_t)b * p.M + q.i) * p.H + q.head) * D + d;
     if constexpr (sizeof(T) == 4) *reinterpret_cast<floatx4*>(out) = o;
     else *reinterpret_cast<bf16x4*>(out) = bf16x4{(__bf16)o[0], (__bf16)o[1], (__bf16)o[2], (__bf16)o[3]};
-    if (p.lse && d == 0) p.lse[((int64_t)b * p.H + q.head) * p.M + q.i] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    if (p.lse && d == 0) p.lse[((int64_t)b * p.H + q.head) * p.M + q.i] = row_lse(p, top, sum);
 }
 
 template <typename T, int D, int R>

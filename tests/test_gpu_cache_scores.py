@@ -35,7 +35,7 @@ def _reference(k, v, q, scale, ends, dtype):
     for i in range(M):
         z, size = scale * (k[:ends[i]] @ q[i]), scale * (np.abs(k[:ends[i]]) @ np.abs(q[i]))
         top = z.max()
-        near = z > top - 64
+        near = z >= top - 64
         p = np.exp(z - top)
         out[i], lse[i] = p @ v[:ends[i]] / p.sum(), top + np.log(p.sum())
         delta = (D + 8) * 2.0 ** -24 * size[near].max() + 2.0 ** -21 * (1 + np.abs(z - top)[near].max() * 2.0 ** -3)
@@ -72,3 +72,65 @@ def test_maxima_that_climb(B, M, D, low, dtype):
         err, lse_err = np.abs(out.double().cpu().numpy()[0, :, 0] - want), np.abs(lse.double().cpu().numpy()[0, 0] - want_lse)
         print(f"[climb {M} {D} {low} {dtype} {limit}] worst err/bar {float((err / bar).max()):.3f}, lse {float((lse_err / lse_bar).max()):.3f}", flush=True)
         assert (err <= bar).all() and (lse_err <= lse_bar).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("M,D", [(1, 64), (20, 64), (40, 64), (1, 128), (20, 128)])
+def test_differences_of_large_scores(B, M, D, dtype):
+    """Whole numbers near 2^22 as scores, exact in fp32, a quarter of which is what the exponential takes: rows are ordinary softmax rows of the differences, however
+    the walk is shared out.  Bars: exponentials and logarithms (2^-21, a part that grows with the difference), sums of the weights, the result's rounding."""
+    import torch
+    rng = np.random.default_rng(M + D)
+    page, T = 16, 800
+    cache = B.kv_cache(51, 1, page, D)
+    table = rng.permutation(51)[None].astype(np.int32)
+    k = np.zeros((T, D))
+    k[:, 0], k[:, 1:5] = 8, rng.integers(-4, 5, (T, 4))
+    v = rng.standard_normal((T, D))
+    on_gpu = lambda x: torch.from_numpy(x.astype(np.float32)).view(1, -1, 1, D).cuda()
+    B.cache_append(on_gpu(k), on_gpu(v), cache, _ints(table), _ints([T]))
+    kk, vv, _ = cache_ref.Model(cache).sequence(0, table, T)
+    np.testing.assert_array_equal(kk[:, 0], k)
+    q = np.zeros((M, D))
+    q[:, 0], q[:, 1:5] = 2.0 ** 19, rng.choice([-1.0, 1.0], (M, 4))
+    qt = on_gpu(q).to({"bf16": torch.bfloat16, "fp32": torch.float32}[dtype])
+    half = ref.HALF_STEP[dtype]
+    for limit in (1, 300, None):
+        out, lse = B.cache_attention(qt, cache, _ints(table), _ints([T]), 0.25, max_length=limit)
+        for i in range(M):
+            n = T - (M - 1 - i)
+            z = 0.25 * (k[:n] @ q[i])
+            p = np.exp(z - z.max())
+            want, want_lse = p @ vv[:n, 0] / p.sum(), z.max() + np.log(p.sum())
+            delta = 2.0 ** -21 * (1 + (z.max() - z.min()) / 8)
+            bar = (half + 2 * delta + 2 * n * 2.0 ** -24) * (p @ np.abs(vv[:n, 0]) / p.sum()) * 1.01 + half * np.abs(want)
+            assert (np.abs(out.double().cpu().numpy()[0, i, 0] - want) <= bar).all(), (limit, i)
+            assert abs(float(lse[0, 0, i]) - want_lse) <= 2.0 ** -21 * want_lse, (limit, i)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("M,D", [(1, 64), (20, 64), (40, 64), (20, 128)])
+def test_scores_that_pass_fp32_when_scaled(B, M, D, sign, dtype):
+    """Scores of up to 2^108 times a scale of 2^30, all of one sign: the row is the mean of its best tokens' values, lse is infinite."""
+    import torch
+    rng = np.random.default_rng(M + D)
+    page, T = 32, 700
+    cache = B.kv_cache(24, 1, page, D)
+    table = rng.permutation(24)[None].astype(np.int32)
+    k = rng.integers(1, 9, (T, D)).astype(np.float64)
+    on_gpu = lambda x: torch.from_numpy(x.astype(np.float32)).view(1, -1, 1, D).cuda()
+    B.cache_append(on_gpu(k), on_gpu(rng.standard_normal((T, D))), cache, _ints(table), _ints([T]))
+    kk, vv, _ = cache_ref.Model(cache).sequence(0, table, T)
+    np.testing.assert_array_equal(kk[:, 0], k)
+    q = sign * rng.integers(1, 9, (M, D)) * 2.0 ** 96
+    scores = q @ k.T                                                           # exact: whole numbers below 2^13 times 2^96
+    scores[np.arange(T)[None, :] >= T - (M - 1 - np.arange(M))[:, None]] = -np.inf
+    best = scores == scores.max(1, keepdims=True)
+    want = best @ vv[:, 0] / best.sum(1, keepdims=True)
+    bar = (2.0 ** -8 if dtype == "bf16" else 0.0) * np.abs(want) + 2.0 ** -20 * np.abs(vv).max()
+    qt = on_gpu(q).to({"bf16": torch.bfloat16, "fp32": torch.float32}[dtype])
+    for limit in (1, 300, None):
+        out, lse = B.cache_attention(qt, cache, _ints(table), _ints([T]), 2.0 ** 30, max_length=limit)
+        assert (np.abs(out.double().cpu().numpy()[0, :, 0] - want) <= bar).all()
+        assert bool((lse == sign * float("inf")).all())
