@@ -64,6 +64,21 @@ __device__ __forceinline__ void split_parts(const float (&x)[8], bf16x8 (&part)[
         }
 }
 
+// The same of a row of q, cut off instead of rounded: numbers next to the largest stay finite.
+template <int N>
+__device__ __forceinline__ void cut_parts(const float (&x)[8], bf16x8 (&part)[N]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float rest = x[i];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const uint32_t u = __builtin_bit_cast(uint32_t, rest);
+            part[n][i] = __builtin_bit_cast(__bf16, (uint16_t)(u >> 16));
+            rest -= __builtin_bit_cast(float, u & 0xffff0000u);
+        }
+    }
+}
+
 // A row of a tile: query row i and head of the tile's row rho.
 struct QueryRow {
     int i, head;
@@ -185,17 +200,43 @@ __device__ __forceinline__ void attend(const CacheAttentionParams& p) {
 
     // q: this lane's 8 channels of each product, 16*g4 + 8*(j & 1) + 64*(j / 2)
     bf16x8 qf[R][NJ][NP];
+    // fp32: the lowest parts of numbers below 2^-110 would be below bf16's least, 2^-133.  A row whose largest is below 2^-64 is taken times 2^48 (its
+    // products with any keys stay below 2^120 then), and its scores' scale by so much less.
+    constexpr float kLift = 0x1p48f;
+    float row_scale[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const QueryRow at = query_row(p, kv_head, min(row0 + 16 * r + r16, rows - 1));
         const T* const src = static_cast<const T*>(p.q) + b * p.sqb + at.i * p.sqn + at.head * p.sqh + 16 * g4;
+        if constexpr (NP == 1) {
+            // (loaded piece by piece: with all of them first, the compiler's order of the walk takes 5 % longer for 1024 rows, 15 % for 48)
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            float x[8];
-            load_row<T, 8>(src + 8 * (j & 1) + 64 * (j / 2), 8, true, x);
-            split_parts<NP>(x, qf[r][j]);
+            for (int j = 0; j < NJ; ++j) {
+                float x[8];
+                load_row<T, 8>(src + 8 * (j & 1) + 64 * (j / 2), 8, true, x);
+                split_parts<NP>(x, qf[r][j]);
+            }
+        } else {
+            float x[NJ][8], most = 0.f;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) load_row<T, 8>(src + 8 * (j & 1) + 64 * (j / 2), 8, true, x[j]);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[j][i]));
+            const bool small = row_max(most) < 0x1p-64f;
+            row_scale[r] = small ? p.scale_log2 / kLift : p.scale_log2;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                if (small) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[j][i] *= kLift;
+                }
+                cut_parts<NP>(x[j], qf[r][j]);
+            }
         }
     }
+    auto scale_log2 = [&](int r) { return NP > 1 ? row_scale[r] : p.scale_log2; };
 
     floatx4 acc[R][NB];
     float top[R], sum[R];
@@ -312,23 +353,23 @@ __device__ __forceinline__ void attend(const CacheAttentionParams& p) {
             for (int e = 2; e < 16; ++e) m = fmaxf(m, s[e]);
             m = fmaxf(row_max(m), top[r]);
             if (__any(m > top[r])) {
-                const float shrink = __builtin_amdgcn_exp2f((top[r] - m) * p.scale_log2);
+                const float shrink = __builtin_amdgcn_exp2f((top[r] - m) * scale_log2(r));
                 top[r] = m;
                 sum[r] *= shrink;
 #pragma unroll
                 for (int n = 0; n < NB; ++n) acc[r][n] *= shrink;
-                if (__any(m > kNothing && fabsf(m) * p.scale_log2 > kLarge)) large = true;
+                if (__any(m > kNothing && fabsf(m) * scale_log2(r) > kLarge)) large = true;
             }
             if (large) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[e] -= m;
                 m = 0.f;
             }
-            const float shift = m > kNothing ? -m * p.scale_log2 : 0.f;
+            const float shift = m > kNothing ? -m * scale_log2(r) : 0.f;
             float w[2][8];
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                w[e / 8][e % 8] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], p.scale_log2, shift));
+                w[e / 8][e % 8] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], scale_log2(r), shift));
                 sum[r] += w[e / 8][e % 8];
             }
             if constexpr (!kHold) {
@@ -400,6 +441,7 @@ __device__ __forceinline__ void attend(const CacheAttentionParams& p) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         sum[r] = row_sum(sum[r]);
+        if (NP > 1 && row_scale[r] < p.scale_log2 && top[r] > kNothing) top[r] /= kLift;
     }
 #pragma unroll
     for (int half = kShareWaves / 2; half >= 1; half /= 2) {

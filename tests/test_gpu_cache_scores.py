@@ -134,3 +134,54 @@ def test_scores_that_pass_fp32_when_scaled(B, M, D, sign, dtype):
         out, lse = B.cache_attention(qt, cache, _ints(table), _ints([T]), 2.0 ** 30, max_length=limit)
         assert (np.abs(out.double().cpu().numpy()[0, :, 0] - want) <= bar).all()
         assert bool((lse == sign * float("inf")).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("power", [-70, -112, -120, -135])
+@pytest.mark.parametrize("M,D", [(1, 64), (20, 64), (40, 64), (1, 128), (20, 128)])
+def test_small_queries_against_large_keys(B, M, D, power, dtype):
+    """Queries down to fp32's least numbers against keys of up to 2^120, ordinary scores; every third row of ordinary size, whose scores are huge."""
+    import torch
+    rng = np.random.default_rng(M + D - power)
+    page, T = 32, 500
+    cache = B.kv_cache(17, 1, page, D)
+    table = rng.permutation(17)[None].astype(np.int32)
+    up = min(-power - 2, 118)
+    on_gpu = lambda x: torch.from_numpy(x.astype(np.float32)).view(1, -1, 1, D).cuda()
+    B.cache_append(on_gpu(rng.standard_normal((T, D)) * 2.0 ** up), on_gpu(rng.standard_normal((T, D))), cache, _ints(table), _ints([T]))
+    kk, vv, there = cache_ref.Model(cache).sequence(0, table, T)
+    assert there.all()
+    q = rng.standard_normal((M, D)) * 2.0 ** np.where(np.arange(M) % 3 == 1, 0, power)[:, None]
+    qt = on_gpu(q).to({"bf16": torch.bfloat16, "fp32": torch.float32}[dtype])
+    qe = qt.double().cpu().numpy()[0, :, 0]
+    scale = 2.0 ** (-power - up - 2)
+    want, want_lse, bar, lse_bar = _reference(kk[:, 0], vv[:, 0], qe, scale, T - (M - 1 - np.arange(M)), dtype)
+    assert (bar[0] <= 0.02 * np.abs(vv).max()).all()
+    for limit in (1, None):
+        out, lse = B.cache_attention(qt, cache, _ints(table), _ints([T]), scale, max_length=limit)
+        got_lse = lse.double().cpu().numpy()[0, 0]
+        over = np.abs(want_lse) > 3.4028235e38               # rounds to an infinity of its sign
+        assert (got_lse[over] == np.copysign(np.inf, want_lse[over])).all() and np.isfinite(got_lse[~over]).all()
+        err, lse_err = np.abs(out.double().cpu().numpy()[0, :, 0] - want), np.where(over, 0.0, np.abs(got_lse - want_lse))
+        print(f"[small {M} {D} {power} {dtype} {limit}] worst err/bar {float((err / bar).max()):.3f}, lse {float((lse_err / lse_bar).max()):.3f}", flush=True)
+        assert (err <= bar).all() and (lse_err <= lse_bar).all()
+
+
+@pytest.mark.parametrize("M,D", [(1, 64), (20, 64), (20, 128)])
+def test_queries_next_to_the_largest_number(B, M, D):
+    """fp32 queries that would round to infinity in bf16."""
+    import torch
+    rng = np.random.default_rng(M + D)
+    page, T = 16, 200
+    cache = B.kv_cache(14, 1, page, D)
+    table = rng.permutation(14)[None].astype(np.int32)
+    on_gpu = lambda x: torch.from_numpy(x.astype(np.float32)).view(1, -1, 1, D).cuda()
+    B.cache_append(on_gpu(rng.standard_normal((T, D)) * 2.0 ** -110), on_gpu(rng.standard_normal((T, D))), cache, _ints(table), _ints([T]))
+    kk, vv, _ = cache_ref.Model(cache).sequence(0, table, T)
+    q = rng.choice([-1.0, 1.0], (M, D)) * float(np.float32(3.4028234e38)) * (1 - rng.integers(0, 100, (M, D)) * 2.0 ** -24)
+    qt = on_gpu(q)
+    assert torch.isfinite(qt).all() and torch.isinf(qt.to(torch.bfloat16)).all()
+    scale = 2.0 ** -19
+    want, want_lse, bar, lse_bar = _reference(kk[:, 0], vv[:, 0], qt.double().cpu().numpy()[0, :, 0], scale, T - (M - 1 - np.arange(M)), "fp32")
+    out, lse = B.cache_attention(qt, cache, _ints(table), _ints([T]), scale)
+    assert (np.abs(out.double().cpu().numpy()[0, :, 0] - want) <= bar).all() and (np.abs(lse.double().cpu().numpy()[0, 0] - want_lse) <= lse_bar).all()
