@@ -321,8 +321,9 @@ int dfa_encoder_stack(const void *x, const void *w_qkv, const void *w_o, int32_t
  * ---- Products of 8-bit operands --------------------------------------------------------------------------------------------
  * A quantised matrix of `rows` rows of `cols` elements: OCP e4m3 values in blocks that share a power of two, 2^e with the smallest
  * e >= -126 for which the block's largest finite |x| is at most 448 * 2^e.  A value is the e4m3 number nearest to x / 2^e (ties to even); x that is
- * not finite is NaN.  A block is 128 elements of a row (block_rows = 1), or 128 rows by 128 columns (block_rows = 128: the same
- * values for the matrix and its transpose, the form for weights that a backward pass reads too).
+ * not finite is NaN.  (x of 1.9375 * 2^127 or more is held as 2^128, which fp32 takes as infinite.)  A block is 128 elements of a row
+ * (block_rows = 1), or 128 rows by 128 columns (block_rows = 128: the same values for the matrix and its transpose, the form for weights that a
+ * backward pass reads too).
  *   values  device, bytes [rows][ld], ld (a multiple of 128) at least cols; columns from cols to the next multiple of 128 hold 0
  *   scales  device, bytes [ld / 128][ld_scales], e + 127 of the block that holds row r and columns 128 c .. 128 c + 127 at
  *           [c][r] (128 equal ones for a 128 x 128 block); ld_scales (a multiple of 16) at least rows
@@ -341,12 +342,17 @@ int dfa_quantize(const void *x, dfa_dtype_t dt, int64_t rows, int64_t cols, int6
                  const dfa_quantized_t *q, const dfa_quantized_t *q_t, void *stream);
 
 /*
- * y[m][n] = sum_k a[m][k] * b[n][k] of the values that a [M][K] and b [N][K] hold: exact products, fp32 sums, rounded once to dt.
+ * y[m][n] = sum_k a[m][k] * b[n][k] of the values that a [M][K] and b [N][K] hold.
+ *   dt = DFA_F32   exact products, fp32 sums.  Values below 2^-126, scale included, may count as 0, and one of 2^128 as infinite
+ *   dt = DFA_BF16  the matrix instruction adds up the products of 16 neighbouring k (16 j to 16 j + 15) at a time and cuts each of them off at 2^-13 of the
+ *                  power of two of the largest: up to 16 * 2^-13 of that product's magnitude for each 16 k (2.3e-5 of the sum of magnitudes, rms, on random
+ *                  values; where large terms cancel, what is smaller than that may be lost altogether).  These sums are added up in fp32 and rounded
+ *                  once to bf16.  Where that does not do: DFA_F32.
+ * This holds for the projection and its gradients below too (dw is always fp32).
  *   y          device, dtype dt, [M][N] with row pitch ldy (elements); must not overlap a or b
  *   workspace  device, 16-byte aligned, dfa_quantized_product_workspace_bytes(dt, M, N, K) (0 = none, NULL allowed): partial sums of
  *              products whose k-steps are shared out over workgroups.  Written and read by this call only: calls that may
  *              overlap need one each.
- * (fp32: values that lie below fp32's normal range, 2^-126, scale included, may count as 0; this holds for the operators below too.)
  * The sums are in a fixed order: equal calls give equal results.  Asynchronous on `stream`; allocates nothing.
  */
 size_t dfa_quantized_product_workspace_bytes(dfa_dtype_t dt, int64_t M, int64_t N, int64_t K);
@@ -413,7 +419,9 @@ int dfa_cache_append(const void *k, const void *v, dfa_strides_t sk, dfa_strides
  *   workspace   device, 16-byte aligned, dfa_cache_attention_workspace_bytes() of the same arguments (0 = none, NULL allowed); written and
  *           read by this call only: calls that may overlap, captured ones among them, need one each.
  * dt = DFA_BF16: bf16 operands, probabilities rounded to bf16 before the second product, fp32 sums and statistics; dt = DFA_F32: 24-bit
- * operands throughout.  Cached values below 2^-126, scale included, may count as 0.  Keys, values and rows that are not finite reach only the
+ * operands throughout (of elements of q below 2^-110 in a row whose largest is 2^-64 or more, bits below 2^-133 count as 0).  Cached values below 2^-126,
+ * scale included, may count as 0.  Scores are right at any size as long as q . k, before the scale, and the sums of weighted values are fp32 numbers; what passes
+ * fp32's range there counts as infinite, a cached value of 2^128 too.  Keys, values and rows that are not finite reach only the
  * rows that attend to them.  One launch, two where the walk is shared out over workgroups; equal calls give equal results.
  * Asynchronous on `stream`; allocates nothing.
  */

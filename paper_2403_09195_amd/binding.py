@@ -757,7 +757,8 @@ def _result(out, shape, dtype, like, name):
 
 
 def quantized_product(a, b, dtype, out=None, workspace="auto"):
-    """y [M, N] of `dtype` (bf16 or fp32): y[m][n] = sum_k a[m][k] b[n][k] of QuantizedMatrix a [M, K] and b [N, K]."""
+    """y [M, N] of `dtype` (bf16 or fp32): y[m][n] = sum_k a[m][k] b[n][k] of QuantizedMatrix a [M, K] and b [N, K].  fp32: exact products, fp32 sums; bf16: of 16
+    neighbouring k, what lies below 2^-13 of the largest product is cut off (include/dfa.h)."""
     import torch
     dev = _device(("a", a.values), ("a.scales", a.scales), ("b", b.values), ("b.scales", b.scales))
     if _elsewhere(dev):
@@ -775,7 +776,7 @@ def quantized_product(a, b, dtype, out=None, workspace="auto"):
 
 
 def quantized_linear(x, w, out=None, workspace="auto"):
-    """y = x . w^T of x's dtype (bf16 or fp32): x [..., K], quantised by the call in 1 x 128 blocks, w a QuantizedMatrix [N, K]."""
+    """y = x . w^T of x's dtype (bf16 or fp32): x [..., K], quantised by the call in 1 x 128 blocks, w a QuantizedMatrix [N, K].  Sums as in quantized_product."""
     if out is None and isinstance(workspace, str) and workspace == "auto":
         res = _native_call("quantized_linear", x, w)
         if res is not None:
