@@ -14,8 +14,9 @@
 // average, of each, which the sum over keys averages out; the row sum is taken before that rounding).  fp32 calls carry q and the probabilities as the
 // sum of three bf16 numbers, 24 bits, through both products.
 // Bound: the cache's bytes while there are few query rows (a chunk's conversions and products take a quarter of the time that its 8 or 16 KB take at
-// the rate of memory), the vector ALU (exponentials, conversions) beyond some 64 rows.  64 rows of 32 heads against up to 8192 tokens of 8 heads of 128:
-// 120 us, 5.0 TB/s (5.9 with equal lengths); 2 x 1024 rows of 12 heads of 64 against 5000 tokens: 59 us, 478 TFLOP/s, vector instructions in 59 % of the slots.
+// the rate of memory), what a wave does one after the other (conversions, scores, exponentials, products) beyond some 64 rows.  64 rows of 32 heads against up to
+// 8192 tokens of 8 heads of 128: 120 us, 5.0 TB/s (5.9 with equal lengths); 2 x 1024 rows of 12 heads of 64 against 5000 tokens: 60 us, 470 TFLOP/s, vector
+// instructions in 58 % of the slots, matrix cores 17 %.
 #include <algorithm>
 #include <cmath>
 
@@ -515,7 +516,7 @@ __global__ __launch_bounds__(64 * kShareWaves) void cache_attention_wide_kernel(
 
 // Merges the splits of a tile's rows: D / 4 lanes to a row and share of its splits, `shares` (a power of two) to a row, each of which
 // takes every `shares`-th split, four at a time.  Their loads do not wait to hear which splits were used: every trip to memory is a microsecond or two,
-// and one after the other (one share, the length first) they were 9.8 us of one image's row, now 3.2.
+// and one after the other (one share, the length first) they were 9.8 us of one image's row, now 3.2 to 3.7.
 constexpr int kMergeAtOnce = 4;
 template <typename T, int D, int R>
 __global__ __launch_bounds__(256) void cache_attention_merge_kernel(CacheAttentionParams p, int shares, int groups) {

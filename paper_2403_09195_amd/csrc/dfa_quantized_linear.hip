@@ -90,7 +90,7 @@ __device__ __forceinline__ void store16(Y* row, int64_t n, int64_t N, const floa
 // alternating stages.  LDS row 16*m + r of 64 holds row 4*r + m of the tile, so that a fragment reads 16 consecutive LDS rows;
 // chunk c of LDS row rho sits at c ^ (rho & 7), which spreads a chunk column over all banks.
 // Bound: a step of a 256-row tile takes 2048 cycles of the matrix cores and 2048 of LDS (192 KB of fragments, 64 KB of copies), and with operands drawn
-// at random the chip's power; 16384 x 4096 x 4096 in bf16: 220 to 241 us, 2.3 to 2.5 PFLOP/s, matrix cores busy 53 % of the cycles.
+// at random the chip's power; 16384 x 4096 x 4096 in bf16: 229 to 238 us, 2.3 to 2.4 PFLOP/s, matrix cores busy 53 % of the cycles (the two add up: 3870 a step).
 template <int T> constexpr uint32_t kTileBytes = T * kScaleBlock;
 template <int T> constexpr uint32_t kTileStage = 2 * (kTileBytes<T> + T);          // both tiles, both sets of scales
 
@@ -414,6 +414,7 @@ hipError_t launch_pair_typed(const ProductParams& p1, const ProductParams& p2, c
 // a compute unit: what LDS hands out, 96 KB a step at 128 bytes a clock), 1.48 with a 256-row one; 1.05, 1.75 and 2.8 for fp32 results; results and partial
 // sums go at 4 TB/s, and summing takes a launch of 3 us.  Estimated / measured on M x N x K, the two best forms, bf16 results (tile / splits):
 // 512 x 2304 x 768 128/1 8 / 7.1, 256/1 14 / 14.9; 4096 x 2304 x 768 128/1 14 / 16.1, 256/1 18 / 17.3; 4096 x 4096 x 4096 256/1 60 / 58.2, 128/1 67 / 65.5;
+// 32768 x 768 x 2304 128/1 58 / 72.3, 256/1 66 / 69.2 (many rounds of 128-row tiles are estimated too short; 8192 x 768 x 2304 128/1 21.9, 256/1 32.9 measured);
 // 64 x 4096 x 4096 128/4 13 / 13.0, 128/1 20 / 20.3; 512 x 4096 x 4096 128/1 21 / 22.7, 128/2 24 / 25.3; 2304 x 768 x 32768 128/4 76 / 75.7, 128/3 74 / 79.8.
 ProductShape product_shape(int64_t M, int64_t N, int32_t n_k, bool f32, const ChipShape& chip) {
     const double cus = chip.cus > 0 ? chip.cus : 1, dies = chip.dies > 0 ? chip.dies : 1, rate = 4e6, out = (double)M * N * (f32 ? 4 : 2) / rate, partial = (double)M * N * 8 / rate;
