@@ -434,6 +434,46 @@ int dfa_cache_attention(const void *q, dfa_strides_t sq, dfa_dtype_t dt, int32_t
  * call is using it any more. */
 int dfa_release_plans(void);
 
+/*
+ * ---- Packed prompts ----------------------------------------------------------------------------------------------------------
+ * Sequences that lie one behind the other: rows starts[b] .. starts[b + 1] - 1 of the T rows of a packed tensor are sequence b's, in order.
+ *   starts  device, int32 [B + 1], ascending from 0; starts[B] <= T.  Equal neighbours: an empty sequence.  (Other values are read as the nearest that
+ *           lie within 0 .. T; starts that do not ascend leave results undefined, but no access leaves the tensors.)
+ * Nothing about the lengths is needed on the host: a captured launch serves whatever `starts` holds when it is replayed.
+ */
+
+/*
+ * out[i, h] = softmax(scale * q[i, h] . k) v over the keys of head h / (H / Hkv) in row i's sequence, and its lse.
+ *   q       device, dtype dt, [T, H, D] through strides (b is not used; every row 16-byte aligned; rows less than 2^25 bytes apart); k, v: [T, Hkv, D];
+ *           H a multiple of Hkv, D 64 or 128
+ *   causal  0: a row attends to its whole sequence; otherwise to the rows before it and itself
+ *   out     device, dtype dt, contiguous [T, H, D], apart from q, k and v;  lse device, fp32 [H, T], or NULL
+ *           rows of no sequence (from starts[B] on) are 0 and -inf
+ * bf16: probabilities are rounded to bf16 before they meet v; sums are fp32.  fp32: products of three bf16 parts a number (24 bits; bits
+ * below 2^-133 are lost, and what rounds to 2^128 in bf16 counts as infinite).  scale * q . k must be an fp32 number.
+ * Sums are in a fixed order: equal calls give equal results.  Asynchronous on `stream`; allocates nothing.
+ */
+int dfa_prompt_attention(const void *q, const void *k, const void *v, dfa_strides_t sq, dfa_strides_t sk, dfa_strides_t sv, dfa_dtype_t dt, int32_t T,
+                         int32_t H, int32_t Hkv, int32_t D, const int32_t *starts, int32_t B, int32_t causal, float scale, void *out, float *lse,
+                         void *stream);
+
+/*
+ * Gradients of the above for a gradient dout [T, H, D] of out:
+ *   dv_j = sum_i P_ij dout_i,  dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  P_ij = exp(scale q_i . k_j - lse_i),
+ *   dS_ij = P_ij (dout_i . v_j - dout_i . out_i), the sums of dk and dv over the query heads of a key head too.
+ *   out, lse    device, what the forward call returned;  out, dout, dq contiguous [T, H, D], dk and dv contiguous [T, Hkv, D], dtype dt, 16-byte aligned;
+ *               H * D elements take less than 2^25 bytes.  dq, dk, dv overlap nothing else.  Rows of no sequence are 0.
+ *   workspace   device, 16-byte aligned, ..._workspace_bytes() of the same sizes; written and read by this call only: calls that may overlap, captured
+ *               ones among them, need one each.
+ * bf16: P and dS are rounded to bf16 before they meet q, k and dout.  A value that is not finite in q, k, v or dout makes all gradients of its
+ * sequence and heads undefined, those of others not.  Sums are in a fixed order.  Asynchronous on `stream`; allocates nothing.
+ */
+size_t dfa_prompt_attention_backward_workspace_bytes(int32_t T, int32_t H, int32_t Hkv, int32_t D, int32_t B);
+int dfa_prompt_attention_backward(const void *q, const void *k, const void *v, dfa_strides_t sq, dfa_strides_t sk, dfa_strides_t sv, const void *out,
+                                  const float *lse, const void *dout, dfa_dtype_t dt, int32_t T, int32_t H, int32_t Hkv, int32_t D, const int32_t *starts,
+                                  int32_t B, int32_t causal, float scale, void *dq, void *dk, void *dv, void *workspace, size_t workspace_bytes,
+                                  void *stream);
+
 #ifdef __cplusplus
 }
 #endif

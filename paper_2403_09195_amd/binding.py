@@ -26,6 +26,7 @@ EXPORTS = [
     "dfa_quantize", "dfa_quantized_product", "dfa_quantized_product_workspace_bytes", "dfa_quantized_linear",
     "dfa_quantized_linear_workspace_bytes", "dfa_quantized_linear_backward", "dfa_quantized_linear_backward_workspace_bytes",
     "dfa_cache_append", "dfa_cache_attention", "dfa_cache_attention_workspace_bytes",
+    "dfa_prompt_attention", "dfa_prompt_attention_backward", "dfa_prompt_attention_backward_workspace_bytes",
 ]
 BENCH_EXPORTS = ["dfa_launch_describe", "dfa_launch_image", "dfa_forward_timed", "dfa_mfma_peak", "dfa_dense_unfused", "dfa_dense_unfused_workspace_bytes",
                  "dfa_quantized_describe", "dfa_cache_attention_describe"]
@@ -149,6 +150,10 @@ def lib():
         L.dfa_cache_attention.argtypes = [vp, Strides, ctypes.c_int, i32, i32, i32, Cache, vp, i32, i64, vp, vp, i32, f32, i64, vp, vp, vp, st, vp]
         L.dfa_quantized_describe.argtypes = [i32, ctypes.c_int, i64, i64, i64, ctypes.POINTER(QuantizedForm)]
         L.dfa_cache_attention_describe.argtypes = [i32, i32, i32, i32, i32, ctypes.c_int, i64, ctypes.POINTER(CacheAttentionForm)]
+        L.dfa_prompt_attention.argtypes = [vp, vp, vp, Strides, Strides, Strides, ctypes.c_int, i32, i32, i32, i32, vp, i32, i32, f32, vp, vp, vp]
+        L.dfa_prompt_attention_backward_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+        L.dfa_prompt_attention_backward.argtypes = [vp, vp, vp, Strides, Strides, Strides, vp, vp, vp, ctypes.c_int, i32, i32, i32, i32, vp, i32, i32, f32,
+                                                    vp, vp, vp, vp, st, vp]
         for name in EXPORTS + BENCH_EXPORTS:
             if name != "dfa_error_string":
                 getattr(L, name).restype = ctypes.c_size_t if name.endswith("_workspace_bytes") else ctypes.c_int
@@ -942,3 +947,78 @@ def describe_cache_attention(B, M, H, heads, D, dtype_code, max_length):
     form = CacheAttentionForm()
     _check(lib().dfa_cache_attention_describe(B, M, H, heads, D, dtype_code, max_length, ctypes.byref(form)), "dfa_cache_attention_describe")
     return form
+
+
+# ---- packed prompts ------------------------------------------------------------------------------------------------------------
+
+def _packed_rows(t, name, heads=None):
+    """Element strides of a packed [T, heads, D] tensor with contiguous D."""
+    if t.dim() != 3 or t.stride(2) != 1:
+        raise DfaError(-5, f"{name} must be [T, heads, D] with contiguous D")
+    if heads is not None and t.shape[1] != heads:
+        raise DfaError(-2, f"{name} must have {heads} heads")
+    return Strides(0, t.stride(0), t.stride(1))
+
+
+def _packed(q, k, v, starts):
+    """Checks of a packed call's tensors: (strides of q, k, v, dtype code, T, H, Hkv, D, starts pointer, B)."""
+    import torch
+    if k.dim() != 3 or q.dim() != 3 or v.shape != k.shape or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2]:
+        raise DfaError(-2, f"q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not belong together")
+    if k.dtype != q.dtype or v.dtype != q.dtype:
+        raise DfaError(-4, "k and v must have q's dtype")
+    if starts.dtype != torch.int32:
+        raise TypeError("starts must be int32")
+    if starts.dim() != 1 or starts.shape[0] < 2 or not starts.is_contiguous():
+        raise DfaError(-2, "starts must be contiguous and hold the first row of each sequence and the end of the last")
+    return (_packed_rows(q, "q"), _packed_rows(k, "k"), _packed_rows(v, "v"), _dtype_code(q), q.shape[0], q.shape[1], k.shape[1], q.shape[2],
+            starts.data_ptr(), starts.shape[0] - 1)
+
+
+def _like(given, shape, dtype, like, name):
+    """A contiguous result: the caller's, if it is what the call writes, or a new one."""
+    import torch
+    if given is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    _device(("q", like), (name, given))
+    if given.dtype != dtype or tuple(given.shape) != tuple(shape) or not given.is_contiguous():
+        raise DfaError(-2, f"{name} must be a contiguous {dtype} {tuple(shape)}")
+    return given
+
+
+def prompt_attention(q, k, v, starts, scale, causal=True, out=None, lse=None, want_lse=True):
+    """Attention within each of many sequences that lie one behind the other -> (out [T, H, D], lse fp32 [H, T] or None).  q [T, H, D], k and v
+    [T, Hkv, D] (bf16 or fp32, may be strided views, as the heads of one projection's result are; H a multiple of Hkv); starts int32 [B + 1]: sequence b is
+    rows starts[b] .. starts[b + 1] - 1, the rows behind the last are 0 and -inf.  causal: a row attends to those before it and itself."""
+    import torch
+    dev = _device(("q", q), ("k", k), ("v", v), ("starts", starts))
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return prompt_attention(q, k, v, starts, scale, causal, out, lse, want_lse)
+    sq, sk, sv, code, T, H, Hkv, D, at, B = _packed(q, k, v, starts)
+    out = _like(out, (T, H, D), q.dtype, q, "out")
+    if want_lse:
+        lse = _like(lse, (H, T), torch.float32, q, "lse")
+    _check(lib().dfa_prompt_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), sq, sk, sv, code, T, H, Hkv, D, at, B, int(bool(causal)), scale,
+                                      out.data_ptr(), lse.data_ptr() if want_lse else None, _stream()), "dfa_prompt_attention")
+    return out, lse if want_lse else None
+
+
+def prompt_attention_backward(q, k, v, out, lse, dout, starts, scale, causal=True, workspace="auto"):
+    """(dq, dk, dv) of prompt_attention for a gradient dout [T, H, D] of its out; out and lse: what it returned.  Gradients of shared heads are sums over
+    the query heads; those of rows of no sequence are 0."""
+    import torch
+    dev = _device(("q", q), ("k", k), ("v", v), ("out", out), ("lse", lse), ("dout", dout), ("starts", starts))
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return prompt_attention_backward(q, k, v, out, lse, dout, starts, scale, causal, workspace)
+    sq, sk, sv, code, T, H, Hkv, D, at, B = _packed(q, k, v, starts)
+    out, dout, lse = (_like(x, shape, dtype, q, name) for x, shape, dtype, name in
+                      ((out, (T, H, D), q.dtype, "out"), (dout, (T, H, D), q.dtype, "dout"), (lse, (H, T), torch.float32, "lse")))
+    dq, dk, dv = (torch.empty((T, n, D), dtype=q.dtype, device=q.device) for n in (H, Hkv, Hkv))
+    ptr, size, keep = _call_workspace(workspace, lib().dfa_prompt_attention_backward_workspace_bytes(T, H, Hkv, D, B), q)
+    _check(lib().dfa_prompt_attention_backward(q.data_ptr(), k.data_ptr(), v.data_ptr(), sq, sk, sv, out.data_ptr(), lse.data_ptr(), dout.data_ptr(), code,
+                                               T, H, Hkv, D, at, B, int(bool(causal)), scale, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ptr, size,
+                                               _stream()), "dfa_prompt_attention_backward")
+    _keep(keep)
+    return dq, dk, dv

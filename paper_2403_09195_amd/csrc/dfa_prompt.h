@@ -1,0 +1,223 @@
+// Attention within packed sequences (gfx950): arguments of its kernels, and what they share.
+//
+// Rows starts[b] .. starts[b + 1] - 1 of q, k and v are sequence b's.  Nothing of this is known on the host, so a launch has a
+// slot for every tile there might be: sequence b's tiles of R rows take slots floor(starts[b] / R) + b and on, of which it has
+// floor(starts[b + 1] / R) - floor(starts[b] / R) + 1, never fewer than ceil(length / R).  The rows behind the last sequence
+// are a sequence of their own, B, whose results are zeros.
+#pragma once
+#include "dfa_device.h"
+#include "dfa_mfma.h"
+
+namespace dfa {
+
+struct PromptParams {
+    const void *q, *k, *v;                  // [T, H, D], [T, Hkv, D] through strides (elements)
+    int64_t sqn, sqh, skn, skh, svn, svh;
+    const int32_t* starts;                  // [B + 1]
+    int32_t B, T, H, Hkv, group;            // group = H / Hkv
+    int32_t causal;
+    float scale;
+    void* out;                              // [T, H, D] contiguous; backward: read
+    float* lse;                             // [H, T], forward: may be NULL; backward: read
+    // backward
+    const void* dout;                       // [T, H, D] contiguous
+    void *dq, *dk, *dv;                     // [T, H, D], [T, Hkv, D], contiguous
+    float *ndelta, *lse2;                   // [H, T] workspace: -(dout . out) and lse * log2(e) of every row
+    float* parts;                           // [shares][2][T][Hkv][D] workspace: dk and dv of a share of the group's heads
+    int32_t shares;
+};
+hipError_t launch_prompt_fwd(const PromptParams& p, bool f32, int32_t D, const ChipShape& chip, hipStream_t st);
+// Workgroups that share the query heads of a key head out in the launch of dk and dv.
+int32_t prompt_bwd_shares(int32_t T, int32_t B, int32_t H, int32_t Hkv, const ChipShape& chip);
+hipError_t launch_prompt_bwd(const PromptParams& p, bool f32, int32_t D, hipStream_t st);
+hipError_t launch_prompt_fwd_f32(const PromptParams& p, int32_t D, hipStream_t st);
+hipError_t launch_prompt_bwd_f32(const PromptParams& p, int32_t D, hipStream_t st);      // without the sum of the shares
+
+// Slots of tiles of R rows.
+inline int64_t prompt_slots(int32_t T, int32_t B, int32_t R) { return (int64_t)T / R + B + 1; }
+
+// A tile: rows t0 .. t0 + R - 1 of the n rows from `first` on.
+struct PromptTile {
+    int32_t first, n, t0;
+    bool rest;              // rows of no sequence
+    bool empty;             // a slot without a tile
+};
+
+// starts[i] within the rows there are; sequence 0 starts at row 0.
+__device__ __forceinline__ int32_t prompt_start(const PromptParams& p, int32_t i) {
+    return i == 0 ? 0 : min(max(p.starts[i], 0), p.T);
+}
+
+// The tile of a slot: the last b with floor(starts[b] / R) + b <= slot, 64 candidates to a trip to memory.  (Starts that do not ascend
+// give some tile inside the rows, or none.)
+template <int R>
+__device__ __forceinline__ PromptTile prompt_tile(const PromptParams& p, int32_t slot, int lane) {
+    int32_t lo = 0, n = p.B + 1, here, next;
+    for (;;) {
+        const int32_t step = (n + 63) / 64;
+        const int32_t at = (int32_t)min((int64_t)lo + (int64_t)lane * step, (int64_t)p.B);
+        const int32_t start = prompt_start(p, at);
+        const bool in = (int64_t)lane * step < n;
+        const int32_t count = __popcll(__ballot(in && start / R + at <= slot));
+        const int32_t idx = max(count, 1) - 1;
+        lo += idx * step;
+        n = min(step, n - idx * step);
+        if (n <= 1) {
+            here = __builtin_amdgcn_readlane(start, idx);
+            // with a step of one, the next lane holds the next start
+            next = lo == p.B ? p.T : step == 1 && idx < 63 ? __builtin_amdgcn_readlane(start, idx + 1) : prompt_start(p, lo + 1);
+            break;
+        }
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    PromptTile t;
+    t.first = here;
+    t.n = __builtin_amdgcn_readfirstlane(max(next, here)) - here;
+    t.t0 = (slot - (here / R + lo)) * R;
+    t.rest = lo == p.B;
+    t.empty = t.t0 < 0 || t.t0 >= t.n;
+    return t;
+}
+
+// Workgroup x of a launch of slots * heads -> (slot, head).  Workgroups go to the dies in turn: with a multiple of eight heads a die
+// keeps H / 8 neighbouring ones, whose keys and values then stay in its L2.  Tiles at the end of a sequence, the longest where
+// attention is causal, come first.
+__device__ __forceinline__ void prompt_place(int32_t x, int32_t slots, int32_t heads, int32_t& slot, int32_t& head) {
+    if (heads % kDies == 0) {
+        const int32_t per = heads / kDies, i = x / kDies;
+        head = x % kDies * per + i % per;
+        slot = slots - 1 - i / per;
+    } else {
+        head = x % heads;
+        slot = slots - 1 - x / heads;
+    }
+}
+
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+// ---- 32-row blocks of bf16 rows in LDS, D elements a row, no padding -------------------------------------------------------------
+// Row rho's 16-byte chunk c sits at chunk c ^ swizzle(rho).  kKeys: read as rows (16 consecutive rows spread a chunk column over all banks),
+// in the order sigma (bits 2 and 3 of the row number exchanged) that puts the result of the first product into the slots of the second;
+// kValues: read transposed (64 bytes of each of four consecutive rows spread over all banks), in order; kBoth: sigma, read either way.
+enum class PromptOrder { kKeys, kValues, kBoth };
+
+template <int D, PromptOrder kOrder>
+__device__ __forceinline__ int prompt_swizzle(int rho) {
+    if constexpr (D == 128) {
+        return kOrder == PromptOrder::kKeys ? rho & 15 : kOrder == PromptOrder::kValues ? (rho & 3) << 2 : ((rho & 3) << 2) | ((rho >> 2) & 3);
+    } else {
+        // two rows to the banks
+        return kOrder == PromptOrder::kKeys ? (rho >> 1) & 7 : kOrder == PromptOrder::kValues ? (rho & 2) << 1 : ((rho & 2) << 1) | ((rho & 4) >> 1) | ((rho & 8) >> 3);
+    }
+}
+__device__ __forceinline__ int prompt_sigma(int rho) { return (rho & 0x13) | ((rho & 4) << 1) | ((rho & 8) >> 1); }
+
+// The copies of one block by four waves: rows k0 .. k0 + 31 of `rows` rows from base on, `pitch` bytes apart; rows behind the last
+// re-read it.  lds_block: address of the block in LDS.
+template <int D>
+constexpr int kPromptCopies = D / 64;        // a wave's copies of one block
+template <int D, PromptOrder kOrder>
+__device__ __forceinline__ void prompt_copy(const char* base, uint32_t pitch, int32_t k0, int32_t rows, int wave, int lane, uint32_t lds_block) {
+    constexpr int kLanes = D / 8, kRows = 64 / kLanes;           // lanes of a row, rows of a copy
+    const int32_t from = min(k0, rows - 1), room = rows - 1 - from;
+    const void* const src = uniform_ptr(base + (int64_t)from * pitch);
+    asm volatile("" : "+v"(lane));           // worked out afresh: kept across the main loop these would be spilled
+#pragma unroll
+    for (int u = 0; u < kPromptCopies<D>; ++u) {
+        const int first = kRows * (kPromptCopies<D> * wave + u), rho = first + lane / kLanes;
+        const int row = kOrder == PromptOrder::kValues ? rho : prompt_sigma(rho);
+        const uint32_t chunk = (uint32_t)(lane % kLanes) ^ prompt_swizzle<D, kOrder>(rho);
+        copy16_to_lds(src, (uint32_t)min(row, room) * pitch + 16u * chunk, lds_block + (uint32_t)(first * D * 2));
+    }
+}
+
+// Element offsets of a lane's reads: rows (lane (j, g): row j, chunk 2 * kk + g at row_at ^ 16 * kk) and transposed (32 d from 32 * db on at
+// col_at ^ 32 * db, rows 16 * st + 8 * g .. + 7 of the block's order).
+template <int D, PromptOrder kOrder>
+__device__ __forceinline__ int prompt_row_at(int lane) {
+    const int j = lane & 31, g = lane >> 5;
+    return j * D + 8 * (g ^ prompt_swizzle<D, kOrder>(j));
+}
+template <int D>
+__device__ __forceinline__ bf16x8 prompt_row(const uint16_t* block, int row_at, int kk) {
+    return *reinterpret_cast<const bf16x8*>(block + (row_at ^ (16 * kk)));
+}
+template <int D>
+__device__ __forceinline__ int prompt_value_at(int lane) {
+    const int i16 = lane & 15, g = lane >> 5, row = (i16 >> 2) + 8 * g;
+    const int chunk = (2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1)) ^ prompt_swizzle<D, PromptOrder::kValues>(row);
+    return row * D + 8 * chunk + 4 * (i16 & 1);
+}
+// A operand (32 d x 16 rows) of kValues blocks: rows 16 * st + 8 * g + 0 .. 7
+template <int D>
+__device__ __forceinline__ bf16x8 prompt_value(const uint16_t* block, int value_at, int db, int st) {
+    const uint16_t* const at = block + (value_at ^ (32 * db)) + 16 * st * D;
+    const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(DFA_LDS_PTR(short4v, at));
+    const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(DFA_LDS_PTR(short4v, at + 4 * D));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// The same of kBoth blocks: positions 16 * st + 8 * g + 0 .. 7, which sigma puts into rows 16 * st + 4 * g + 0 .. 3 and eight further on.
+template <int D>
+__device__ __forceinline__ int prompt_turned_at(int lane) {
+    const int i16 = lane & 15, g = lane >> 5, row = (i16 >> 2) + 4 * g;
+    const int chunk = (2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1)) ^ prompt_swizzle<D, PromptOrder::kBoth>(row);
+    return row * D + 8 * chunk + 4 * (i16 & 1);
+}
+template <int D>
+__device__ __forceinline__ bf16x8 prompt_turned(const uint16_t* block, int turned_at, int db, int st) {
+    constexpr int kEight = 8 * (D == 128 ? 2 : 1);               // row bit 3 in the swizzle, in elements
+    const uint16_t* const at = block + (turned_at ^ (32 * db)) + 16 * st * D;
+    const uint16_t* const further = block + (turned_at ^ (32 * db) ^ kEight) + (16 * st + 8) * D;
+    const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(DFA_LDS_PTR(short4v, at));
+    const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(DFA_LDS_PTR(short4v, further));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+__device__ __forceinline__ floatx16 prompt_zero() {
+    floatx16 z;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) z[v] = 0.f;
+    return z;
+}
+// Register v of lane (j, g) of a first product is position 16 * (v / 8) + 8 * g + v % 8 of its block.
+__device__ __forceinline__ int prompt_position(int v, int g) { return 16 * (v >> 3) + 8 * g + (v & 7); }
+
+__device__ __forceinline__ float uniform_float(float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+}
+
+// A wave's 32 rows of a result, held transposed (lane (j, g), register v of part db: row j, d = 32 db + 8 (v / 4) + 4 g + v % 4), times `by`, leave
+// through LDS of the wave's own (32 * (D * size + 16) bytes): whole lines.  Row r of `rows` goes to to + r * pitch.
+template <int D, typename T>
+__device__ __forceinline__ void store_rows(const floatx16 (&acc)[D / 32], float by, char* mine, T* to, int64_t pitch, int rows, int lane) {
+    constexpr int kPitch = D * (int)sizeof(T) + 16, kLanes = D * (int)sizeof(T) / 16, kRows = 64 / kLanes;
+    const int j = lane & 31, g = lane >> 5;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            char* const at = mine + j * kPitch + (32 * db + 8 * v + 4 * g) * (int)sizeof(T);
+            if constexpr (sizeof(T) == 2) {
+                *reinterpret_cast<bf16x4*>(at) = bf16x4{(__bf16)(acc[db][4 * v] * by), (__bf16)(acc[db][4 * v + 1] * by), (__bf16)(acc[db][4 * v + 2] * by),
+                                                        (__bf16)(acc[db][4 * v + 3] * by)};
+            } else {
+                *reinterpret_cast<float4*>(at) = make_float4(acc[db][4 * v] * by, acc[db][4 * v + 1] * by, acc[db][4 * v + 2] * by, acc[db][4 * v + 3] * by);
+            }
+        }
+#pragma unroll
+    for (int i = 0; i < 32 / kRows; ++i) {
+        const int r = kRows * i + lane / kLanes, ch = lane % kLanes;
+        const u32x4 x = *reinterpret_cast<const u32x4*>(mine + r * kPitch + 16 * ch);
+        if (r < rows) *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(to + r * pitch) + 16 * ch) = x;
+    }
+}
+
+// Zeros of `rows` rows of D elements.
+template <int D, typename T>
+__device__ __forceinline__ void zero_rows(T* to, int64_t pitch, int rows) {
+    constexpr int kLanes = D * (int)sizeof(T) / 16;
+    for (int i = threadIdx.x; i < rows * kLanes; i += 256) *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(to + (int64_t)(i / kLanes) * pitch) + 16 * (i % kLanes)) = u32x4{0u, 0u, 0u, 0u};
+}
+
+}  // namespace dfa

@@ -1,0 +1,320 @@
+// Attention within packed sequences, forward, bf16 (gfx950): see dfa_prompt.h for the slots of tiles and the blocks in LDS.
+//
+// out_i = sum_j softmax_j(scale q_i . k_j) v_j and lse_i over the keys j of row i's sequence, j <= i where causal.  One pass
+// over the keys with a reference exponent, a running sum and an accumulator per row.
+//
+// A workgroup of four waves takes 128 * QB consecutive rows of one sequence and head, a wave 32 * QB of them, and walks the
+// sequence's keys in blocks of 32, which go global -> LDS several stages ahead (global_load_lds).  Per block S^T = K Q^T and O^T +=
+// V^T P^T on v_mfma_f32_32x32x16_bf16; the registers of S^T, rounded, are the operand P^T as they stand.  Work is in beats: the
+// products of the next block's scores and of the block before, and between them, slot by slot, the exponentials of the block in hand.
+#include "dfa_prompt.h"
+
+namespace dfa {
+
+namespace {
+
+// If a lane's partial row sum of one block exceeds this, exponents may have left the comfortable range and the reference moves up.
+constexpr float kCalm = 256.0f;
+// The reference before the first score: below any score, and finite (a masked score minus it is a clean -inf).
+constexpr float kLowest = -3.0e38f;
+
+template <int D, int QB>
+struct Wave {
+    static constexpr int kSteps = D / 16, kHalves = D / 32;          // 16-d steps of a score, 32-d parts of a row
+    bf16x8 q[QB][kSteps];
+    floatx16 acc[kHalves][QB];
+    float ref[QB], sum[QB];                  // reference exponent; this lane's part of the row sum (the other half of the keys is lane ^ 32's)
+    int row_at, value_at;
+    float c;                                 // scale * log2(e)
+
+    // S^T of one block on its own
+    __device__ __forceinline__ void scores(const uint16_t* kb, floatx16 (&s)[QB]) const {
+#pragma unroll
+        for (int kk = 0; kk < kSteps; ++kk) {
+            const bf16x8 kf = prompt_row<D>(kb, row_at, kk);
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) s[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[qb][kk], kk == 0 ? prompt_zero() : s[qb], 0, 0, 0);
+        }
+    }
+    __device__ __forceinline__ void accumulate(const uint16_t* vb, const u32x4 (&p)[QB][2]) {
+#pragma unroll
+        for (int db = 0; db < kHalves; ++db)
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                const bf16x8 vf = prompt_value<D>(vb, value_at, db, st);
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb)
+                    acc[db][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, p[qb][st]), acc[db][qb], 0, 0, 0);
+            }
+    }
+
+    // One beat: scores of the next block (K at kb -> s_next), p_prev times the previous block's values (vb), numerators of s (-> p).  The
+    // numerators are added up before they are rounded: lse is exact to fp32.
+    template <bool kScores, bool kAccumulate>
+    __device__ __forceinline__ void beat(const uint16_t* kb, const uint16_t* vb, const floatx16 (&s)[QB], floatx16 (&s_next)[QB], const u32x4 (&p_prev)[QB][2],
+                                         u32x4 (&p)[QB][2], float (&psum)[QB]) {
+        constexpr int kProducts = 2 * QB * kSteps, kSlots = 8 * QB, kPer = kProducts / kSlots;
+        constexpr int kAhead = QB == 2 ? 1 : 2, kBuffers = kAhead + 1;              // fragments are read this many groups ahead
+        bf16x8 kf[kBuffers], vf[kBuffers];
+        float t[kSlots][2], a[QB][2];
+        auto load = [&](int r) {
+            if (kScores) kf[r % kBuffers] = prompt_row<D>(kb, row_at, r);
+            if (kAccumulate) vf[r % kBuffers] = prompt_value<D>(vb, value_at, r >> 1, r & 1);
+        };
+        auto product = [&](int k) {          // group r = k / (2 QB): scores of d-step r, then the accumulation of (32 d, 16 keys) number r
+            const int r = k / (2 * QB), w = k % (2 * QB);
+            if (w == 0 && r + kAhead < kSteps) load(r + kAhead);
+            if (w < QB) {
+                if (kScores) s_next[w] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[r % kBuffers], q[w][r], r == 0 ? prompt_zero() : s_next[w], 0, 0, 0);
+            } else if (kAccumulate) {
+                const int qb = w - QB;
+                acc[r >> 1][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[r % kBuffers], __builtin_bit_cast(bf16x8, p_prev[qb][r & 1]), acc[r >> 1][qb], 0, 0, 0);
+            }
+        };
+#pragma unroll
+        for (int r = 0; r < kAhead; ++r) load(r);
+#pragma unroll
+        for (int m = 0; m < kSlots + 2; ++m) {
+            if (m >= 2)
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) product(kPer * (m - 2) + i);
+            if (m < kSlots) {
+                const int qb = m >> 3, v = 2 * (m & 7);
+                t[m][0] = fmaf(s[qb][v], c, -ref[qb]);
+                t[m][1] = fmaf(s[qb][v + 1], c, -ref[qb]);
+            }
+            if (m >= 1 && m <= kSlots) {
+                t[m - 1][0] = __builtin_amdgcn_exp2f(t[m - 1][0]);
+                t[m - 1][1] = __builtin_amdgcn_exp2f(t[m - 1][1]);
+            }
+            if (m >= 2) {
+                const int i = m - 2, qb = i >> 3, pr = i & 7;
+                const bf16x2 w = {(__bf16)t[i][0], (__bf16)t[i][1]};
+                p[qb][pr >> 2][pr & 3] = __builtin_bit_cast(uint32_t, w);
+                a[qb][0] = pr == 0 ? t[i][0] : a[qb][0] + t[i][0];
+                a[qb][1] = pr == 0 ? t[i][1] : a[qb][1] + t[i][1];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) psum[qb] = a[qb][0] + a[qb][1];
+    }
+
+    // The end of a beat: the numerators stand, or (rarely) the references move up to the block's maxima and they are taken again.
+    __device__ __forceinline__ void settle(const floatx16 (&s)[QB], u32x4 (&p)[QB][2], float (&psum)[QB]) {
+        bool calm = psum[0] <= kCalm;        // false for NaN too
+        if (QB == 2) calm = calm && psum[QB - 1] <= kCalm;
+        if (__builtin_expect(__ballot(!calm) != 0ull, 0)) {
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) {
+                float top = s[qb][0];
+#pragma unroll
+                for (int v = 1; v < 16; ++v) top = fmaxf(top, s[qb][v]);
+                top = wave_half_max(top);
+                const float now = fmaxf(ref[qb], top * c), by = __builtin_amdgcn_exp2f(ref[qb] - now);
+                ref[qb] = now;
+                sum[qb] *= by;
+#pragma unroll
+                for (int db = 0; db < kHalves; ++db)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) acc[db][qb][v] *= by;
+                float a = 0.f;
+#pragma unroll
+                for (int v = 0; v < 8; ++v) {
+                    const float e0 = __builtin_amdgcn_exp2f(fmaf(s[qb][2 * v], c, -now)), e1 = __builtin_amdgcn_exp2f(fmaf(s[qb][2 * v + 1], c, -now));
+                    const bf16x2 w = {(__bf16)e0, (__bf16)e1};
+                    p[qb][v >> 2][v & 3] = __builtin_bit_cast(uint32_t, w);
+                    a += e0 + e1;
+                }
+                psum[qb] = a;
+            }
+        }
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) sum[qb] += psum[qb];
+    }
+};
+
+// kPer: 32-key blocks of a stage; kStages stages in LDS.
+template <int D, int QB, int kPer, int kStages, int kEu>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu))) void prompt_fwd_kernel(const PromptParams p, int32_t slots) {
+    constexpr int R = 128 * QB, kBlock = 32 * D, kStage = kPer * kBlock;            // elements
+    constexpr int kCopies = 2 * kPer * kPromptCopies<D>;                             // of a wave and stage
+    // the walk is in the stages of three blocks at once (accumulation, numerators, scores); the others are on their way
+    constexpr int kAhead = kStages - (kPer == 1 ? 3 : 2);
+    static_assert(kAhead >= 1, "a stage is filled while the walk is in others");
+    __shared__ __attribute__((aligned(1024))) uint16_t lds[kStages][2][kStage];      // keys, values
+
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, g = lane >> 5;
+    int32_t slot, h;
+    prompt_place(blockIdx.x, slots, p.H, slot, h);
+    const PromptTile tile = prompt_tile<R>(p, slot, lane);
+    if (tile.empty) return;
+    const int32_t rows = min(R, tile.n - tile.t0);                                   // of the tile
+    const int64_t row0 = (int64_t)tile.first + tile.t0;                              // of the packed rows
+    uint16_t* const out = static_cast<uint16_t*>(p.out) + (row0 * p.H + h) * D;
+    float* const lse = p.lse ? p.lse + (int64_t)h * p.T + row0 : nullptr;
+    if (tile.rest) {
+        for (int i = tid; i < rows * (D / 8); i += 256) *reinterpret_cast<u32x4*>(out + (int64_t)(i / (D / 8)) * p.H * D + 8 * (i % (D / 8))) = u32x4{0u, 0u, 0u, 0u};
+        if (lse)
+            for (int i = tid; i < rows; i += 256) lse[i] = -INFINITY;
+        return;
+    }
+
+    const int32_t keys = p.causal ? tile.t0 + rows : tile.n;                         // that the tile's rows attend to
+    const int32_t n_steps = (keys + 63) / 64;                                        // pairs of blocks
+    const int32_t my0 = tile.t0 + 32 * QB * wave;                                    // the wave's first row in the sequence
+    const bool live = my0 < tile.n;
+    const int32_t my_steps = p.causal ? (min(my0 + 32 * QB, keys) + 63) / 64 : n_steps;
+
+    const char* const kbase = reinterpret_cast<const char*>(static_cast<const uint16_t*>(p.k) + tile.first * p.skn + (h / p.group) * p.skh);
+    const char* const vbase = reinterpret_cast<const char*>(static_cast<const uint16_t*>(p.v) + tile.first * p.svn + (h / p.group) * p.svh);
+    const uint32_t kpitch = (uint32_t)(p.skn * 2), vpitch = (uint32_t)(p.svn * 2);
+    const uint32_t lds_addr = (uint32_t)(uintptr_t)DFA_LDS_PTR(void, &lds[0][0][0]);
+    const int32_t n_stages = 2 * n_steps / kPer;
+    auto issue = [&](int32_t stage, int at) {
+        const uint32_t to = lds_addr + (uint32_t)(at * 2 * kStage * 2);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            prompt_copy<D, PromptOrder::kKeys>(kbase, kpitch, 32 * (stage * kPer + i), keys, wave, lane, to + (uint32_t)(i * kBlock * 2));
+            prompt_copy<D, PromptOrder::kValues>(vbase, vpitch, 32 * (stage * kPer + i), keys, wave, lane, to + (uint32_t)((kStage + i * kBlock) * 2));
+        }
+    };
+
+    Wave<D, QB> w;
+    {
+        const uint16_t* const q = static_cast<const uint16_t*>(p.q) + row0 * p.sqn + h * p.sqh;
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            const int64_t row = min(32 * QB * wave + 32 * qb + j, rows - 1);
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) w.q[qb][kk] = *reinterpret_cast<const bf16x8*>(q + row * p.sqn + 16 * kk + 8 * g);
+        }
+    }
+#pragma unroll
+    for (int s = 0; s <= kAhead; ++s)
+        if (s < n_stages) issue(s, s);
+    // (waited for here, with what was issued after it: the compiler then places no wait of its own for them in the loop)
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) asm volatile("" : "+v"(w.q[qb][kk]));
+    wait_vmcnt<0>();
+    __syncthreads();
+
+    w.c = uniform_float(p.scale * kLog2e);
+    w.row_at = prompt_row_at<D, PromptOrder::kKeys>(lane);
+    w.value_at = prompt_value_at<D>(lane);
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        w.ref[qb] = kLowest;
+        w.sum[qb] = 0.f;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) w.acc[db][qb] = prompt_zero();
+    }
+
+    // scores that a row does not see, of the block from key k0 on
+    auto mask = [&](floatx16 (&s)[QB], int32_t k0) {
+        if (k0 + 32 <= (p.causal ? min(my0 + 1, keys) : keys)) return;
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            const int32_t last = min(p.causal ? my0 + 32 * qb + j : keys - 1, keys - 1) - k0;
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                if (prompt_position(v, g) > last) s[qb][v] = -INFINITY;
+        }
+    };
+    // block n's keys and values in LDS
+    auto at = [&](int32_t n, int tensor) { return &lds[(n / kPer) % kStages][tensor][(n % kPer) * kBlock]; };
+    // Block n is scored next: its stage has landed once at most the stages behind it, up to kAhead - 1 of them, are under way.  Every wave is
+    // done with block n - 2's numerators and block n - 3's accumulation then, so the stage before those can be filled.
+    auto enter = [&](int32_t n) {
+        const int32_t s = n / kPer;
+        if (s > kAhead && s < n_stages) {
+            if (s + kAhead - 1 < n_stages) wait_vmcnt<(kAhead - 1) * kCopies>();
+            else wait_vmcnt<0>();
+        }
+        __syncthreads();
+        if (s + kAhead < n_stages) issue(s + kAhead, (s + kAhead) % kStages);
+    };
+
+    floatx16 s_a[QB], s_b[QB];
+    u32x4 p_a[QB][2], p_b[QB][2];
+    float psum[QB];
+    if (live) w.scores(at(0, 0), s_a);
+    if (kPer == 1) enter(1);
+    if (live) {
+        mask(s_a, 0);
+        w.template beat<true, false>(at(1, 0), at(0, 1), s_a, s_b, p_b, p_a, psum);
+        w.settle(s_a, p_a, psum);
+    }
+    // trip s: beat 2 s + 1 (scores of block 2 s + 2, accumulation of 2 s) and beat 2 s + 2
+    for (int32_t s = 0; s < n_steps; ++s) {
+        const bool more = live && s + 1 < my_steps, ends = live && s + 1 == my_steps;
+        enter(2 * s + 2);
+        if (more) {
+            mask(s_b, 64 * s + 32);
+            w.template beat<true, true>(at(2 * s + 2, 0), at(2 * s, 1), s_b, s_a, p_a, p_b, psum);
+            w.settle(s_b, p_b, psum);
+        }
+        if (ends) {
+            mask(s_b, 64 * s + 32);
+            w.template beat<false, true>(at(2 * s, 0), at(2 * s, 1), s_b, s_a, p_a, p_b, psum);
+            w.settle(s_b, p_b, psum);
+            w.accumulate(at(2 * s + 1, 1), p_b);
+        }
+        if (kPer == 1) enter(2 * s + 3);
+        if (more) {
+            mask(s_a, 64 * s + 64);
+            w.template beat<true, true>(at(2 * s + 3, 0), at(2 * s + 1, 1), s_a, s_b, p_b, p_a, psum);
+            w.settle(s_a, p_a, psum);
+        }
+    }
+
+    // rows leave through LDS, each wave's through a piece of its own: whole lines
+    int lane_e = lane;
+    asm volatile("" : "+v"(lane_e));
+    const int je = lane_e & 31, ge = lane_e >> 5;
+    __syncthreads();
+    constexpr int kPitch = 2 * D + 16;
+    static_assert(sizeof(lds) >= 4 * 32 * QB * kPitch, "every wave's rows fit the stages");
+    if (!live) return;
+    char* const mine = reinterpret_cast<char*>(&lds[0][0][0]) + wave * (32 * QB * kPitch);
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        const float total = wave_half_sum(w.sum[qb]);
+        const float inv = total == 0.f ? 0.f : 1.0f / total;
+        const int r = 32 * QB * wave + 32 * qb + je;
+        if (lse && ge == 0 && r < rows) lse[r] = total == 0.f ? -INFINITY : (w.ref[qb] + __builtin_amdgcn_logf(total)) * kLn2;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const bf16x4 o = {(__bf16)(w.acc[db][qb][4 * v] * inv), (__bf16)(w.acc[db][qb][4 * v + 1] * inv), (__bf16)(w.acc[db][qb][4 * v + 2] * inv),
+                                  (__bf16)(w.acc[db][qb][4 * v + 3] * inv)};
+                *reinterpret_cast<bf16x4*>(mine + (32 * qb + je) * kPitch + (32 * db + 8 * v + 4 * ge) * 2) = o;
+            }
+    }
+    constexpr int kLanes = D / 8, kRowsAtOnce = 64 / kLanes;
+#pragma unroll
+    for (int i = 0; i < 32 * QB / kRowsAtOnce; ++i) {
+        const int r = kRowsAtOnce * i + lane_e / kLanes, ch = lane_e % kLanes, row = 32 * QB * wave + r;
+        const u32x4 x = *reinterpret_cast<const u32x4*>(mine + r * kPitch + 16 * ch);
+        if (row < rows) *reinterpret_cast<u32x4*>(out + (int64_t)row * p.H * D + 8 * ch) = x;
+    }
+}
+
+template <int D, int QB, int kPer, int kStages, int kEu>
+hipError_t launch(const PromptParams& p, hipStream_t st) {
+    const int64_t slots = prompt_slots(p.T, p.B, 128 * QB);
+    hipLaunchKernelGGL((prompt_fwd_kernel<D, QB, kPer, kStages, kEu>), dim3((unsigned)(slots * p.H)), dim3(256), 0, st, p, (int32_t)slots);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_prompt_fwd(const PromptParams& p, bool f32, int32_t D, const ChipShape&, hipStream_t st) {
+    if (f32) return launch_prompt_fwd_f32(p, D, st);
+    return D == 64 ? launch<64, 2, 2, 4, 2>(p, st) : launch<128, 1, 1, 5, 2>(p, st);
+}
+
+}  // namespace dfa
