@@ -474,6 +474,70 @@ int dfa_prompt_attention_backward(const void *q, const void *k, const void *v, d
                                   int32_t B, int32_t causal, float scale, void *dq, void *dk, void *dv, void *workspace, size_t workspace_bytes,
                                   void *stream);
 
+/*
+ * Root-mean-square norm of the rows of x, a residual added first:
+ *   h = x + residual (x without one),  r = (mean of h^2 over the row + eps)^(-1/2),  y = h r weight
+ * in fp32 from the operands to the one rounding of h and of y (y comes of the unrounded h).
+ *   x, residual  device, dtype dt, [M][C] with row pitches (elements; rows may start at any element); residual may be NULL
+ *   weight       device, [C], of weight_dt (fp32 rows take fp32 weights, bf16 rows either), or NULL for ones;  eps >= 0
+ *   h            device, dtype dt, [M][C] with row pitch ldh, or NULL; may be x or residual itself (same pointer and pitch)
+ *   y            device, dtype dt, [M][C] with row pitch ldy, or NULL
+ *   q            host struct or NULL: receives y in e4m3, blocks of 128 along the rows, as dfa_quantize does (from the fp32 values, not from
+ *                y's rounded ones); one of y and q at least.  Values up to the next multiple of 128 columns (zeros) and scale bytes up to the next multiple of 16
+ *                rows are written.
+ * h, y and q apart from the operands and each other (but for h as said).  Rows are exact at any size that fp32 holds: sums of squares that overflow, or fall below
+ * 1e-30 beside an eps that does, are taken again, scaled.  C is 32768 at most.  Asynchronous on `stream`; allocates nothing.
+ */
+int dfa_rms_norm(const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, dfa_dtype_t weight_dt, dfa_dtype_t dt, float eps,
+                 void *h, int64_t ldh, void *y, int64_t ldy, const dfa_quantized_t *q, int64_t M, int64_t C, void *stream);
+
+/*
+ * Gradients of the above for gradients dy of y and dh of h (NULL: none), with g = dy weight and u = h r:
+ *   dx = r (g - u mean(g u)) + dh   of x and of the residual alike;  dw = sum over the rows of dy u, fp32 [C], or NULL (not wanted)
+ *   h           device, dtype dt, what the forward call stored (x where there was no residual); dy, dh, dx likewise [M][C] with row pitches;
+ *               dx may be dy or dh itself (same pointer and pitch), else apart from the operands
+ *   workspace   device, 16-byte aligned, ..._workspace_bytes(M, C) (0 = none, NULL allowed; not used without dw): partial sums of dw.  Written and read by this
+ *               call only: calls that may overlap, captured ones among them, need one each.
+ * Sums are in a fixed order: equal calls give equal results.  Asynchronous on `stream`; allocates nothing.
+ */
+size_t dfa_rms_norm_backward_workspace_bytes(int64_t M, int64_t C);
+int dfa_rms_norm_backward(const void *dy, int64_t lddy, const void *h, int64_t ldh, const void *weight, dfa_dtype_t weight_dt, dfa_dtype_t dt, float eps,
+                          const void *dh, int64_t lddh, void *dx, int64_t lddx, float *dw, int64_t M, int64_t C, void *workspace, size_t workspace_bytes,
+                          void *stream);
+
+/*
+ * Pages for a step's new tokens.  `free_pages` (device, int32 [capacity]) is a stack: its first n_free[0] entries are pages that no sequence
+ * holds.  Sequence b holds lengths[b] tokens and gets counts[b] more (0 allowed): it takes ceil(new length / page) - ceil(length / page) pages from the top
+ * of the stack, sequence after sequence, page after page, which go into its row of the table behind those it has.
+ *   table        device, int32 [B][width] with pitch ld_table; other entries are left as they were
+ *   new_lengths  device, int32 [B], lengths + counts; new_n_free device, int32 [1]; may be lengths and n_free themselves (else apart from everything)
+ *   starts       device, int32 [B + 1]: where each sequence's new tokens start among the step's packed rows
+ *   slots        device, int64 [rows], positions device, int32 [rows]: of every packed row its place in the cache, page number * page + place in the
+ *                page, and its place in the sequence; -1 behind the last
+ *   refused      device, int32 [1]: 0, or why the step does not fit: 1 too few free pages, 2 a sequence longer than width * page tokens, 4 more than `rows` new
+ *                tokens (added up where several hold); 8 a count or length below 0.  A step that does not fit changes nothing: lengths, n_free and
+ *                table stay, starts are 0, slots and positions -1.
+ * page: 16, 32, 64 or 128.  n_free outside 0 .. capacity counts as the nearest.  One launch for up to 4096 rows, two for more.  Asynchronous on `stream`; allocates
+ * nothing.
+ */
+int dfa_cache_reserve(const int32_t *counts, const int32_t *lengths, int32_t B, int32_t page, int32_t *table, int32_t width, int64_t ld_table,
+                      const int32_t *free_pages, int32_t capacity, const int32_t *n_free, int32_t *new_lengths, int32_t *new_n_free, int32_t *starts,
+                      int64_t *slots, int32_t *positions, int32_t rows, int32_t *refused, void *stream);
+
+/*
+ * Gives the pages of every sequence with done[b] != 0 (device, int32 [B]) back: the first ceil(lengths[b] / page) entries of its row of the table go
+ * onto the stack, sequence after sequence, and lengths[b] becomes 0.  refused: 0, or 1 if the stack has no room for them: nothing is changed then.
+ */
+int dfa_cache_release(const int32_t *done, int32_t *lengths, int32_t B, int32_t page, const int32_t *table, int32_t width, int64_t ld_table,
+                      int32_t *free_pages, int32_t capacity, int32_t *n_free, int32_t *refused, void *stream);
+
+/*
+ * dfa_cache_append of packed rows: rows starts[b] .. starts[b + 1] - 1 of k and v (device, dtype dt, [T, heads, D] through strides, b not used) are
+ * the last tokens of sequence b.  Rows of no sequence are not read.
+ */
+int dfa_cache_append_packed(const void *k, const void *v, dfa_strides_t sk, dfa_strides_t sv, dfa_dtype_t dt, int32_t T, const int32_t *starts, int32_t B,
+                            dfa_cache_t cache, const int32_t *table, int32_t width, int64_t ld_table, const int32_t *lengths, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,6 +27,7 @@ EXPORTS = [
     "dfa_quantized_linear_workspace_bytes", "dfa_quantized_linear_backward", "dfa_quantized_linear_backward_workspace_bytes",
     "dfa_cache_append", "dfa_cache_attention", "dfa_cache_attention_workspace_bytes",
     "dfa_prompt_attention", "dfa_prompt_attention_backward", "dfa_prompt_attention_backward_workspace_bytes",
+    "dfa_rms_norm", "dfa_rms_norm_backward", "dfa_rms_norm_backward_workspace_bytes", "dfa_cache_reserve", "dfa_cache_release", "dfa_cache_append_packed",
 ]
 BENCH_EXPORTS = ["dfa_launch_describe", "dfa_launch_image", "dfa_forward_timed", "dfa_mfma_peak", "dfa_dense_unfused", "dfa_dense_unfused_workspace_bytes",
                  "dfa_quantized_describe", "dfa_cache_attention_describe"]
@@ -154,6 +155,12 @@ def lib():
         L.dfa_prompt_attention_backward_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
         L.dfa_prompt_attention_backward.argtypes = [vp, vp, vp, Strides, Strides, Strides, vp, vp, vp, ctypes.c_int, i32, i32, i32, i32, vp, i32, i32, f32,
                                                     vp, vp, vp, vp, st, vp]
+        L.dfa_rms_norm.argtypes = [vp, i64, vp, i64, vp, ctypes.c_int, ctypes.c_int, f32, vp, i64, vp, i64, ctypes.POINTER(qm), i64, i64, vp]
+        L.dfa_rms_norm_backward_workspace_bytes.argtypes = [i64, i64]
+        L.dfa_rms_norm_backward.argtypes = [vp, i64, vp, i64, vp, ctypes.c_int, ctypes.c_int, f32, vp, i64, vp, i64, vp, i64, i64, vp, st, vp]
+        L.dfa_cache_reserve.argtypes = [vp, vp, i32, i32, vp, i32, i64, vp, i32, vp, vp, vp, vp, vp, vp, i32, vp, vp]
+        L.dfa_cache_release.argtypes = [vp, vp, i32, i32, vp, i32, i64, vp, i32, vp, vp, vp]
+        L.dfa_cache_append_packed.argtypes = [vp, vp, Strides, Strides, ctypes.c_int, i32, vp, i32, Cache, vp, i32, i64, vp, vp]
         for name in EXPORTS + BENCH_EXPORTS:
             if name != "dfa_error_string":
                 getattr(L, name).restype = ctypes.c_size_t if name.endswith("_workspace_bytes") else ctypes.c_int
@@ -877,10 +884,12 @@ def _sequences(table, lengths, counts, B):
     return table.data_ptr(), width, table.stride(0) if B > 1 else width, lengths.data_ptr(), None if counts is None else counts.data_ptr()
 
 
-def cache_append(k, v, cache, table, lengths, counts=None):
+def cache_append(k, v, cache, table, lengths, counts=None, starts=None):
     """Writes k, v [B, T, heads, D] (bf16 or fp32, may be strided views) into the pages of a KvCache as the last tokens of every sequence.
     table int32 [B, width]: pages of the sequences; lengths int32 [B]: tokens held, the new ones included; counts int32 [B]: how many of the T
-    rows there are (None: all)."""
+    rows there are (None: all).  With starts (int32 [B + 1]) k and v are packed, [T, heads, D]: rows starts[b] .. starts[b + 1] - 1 are sequence b's."""
+    if starts is not None:
+        return _cache_append_packed(k, v, cache, table, lengths, counts, starts)
     if _native_call("cache_append", k, v, cache, table, lengths, counts):
         return
     import torch
@@ -1022,3 +1031,145 @@ def prompt_attention_backward(q, k, v, out, lse, dout, starts, scale, causal=Tru
                                                _stream()), "dfa_prompt_attention_backward")
     _keep(keep)
     return dq, dk, dv
+
+
+def _cache_append_packed(k, v, cache, table, lengths, counts, starts):
+    import torch
+    dev = _device(("k", k), ("v", v), ("cache.k", cache.k), ("cache.v", cache.v), ("cache.scales", cache.scales), ("table", table), ("lengths", lengths),
+                  ("starts", starts))
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return _cache_append_packed(k, v, cache, table, lengths, counts, starts)
+    if counts is not None:
+        raise ValueError("counts and starts do not go together")
+    c = _cache(cache)
+    sk, sv, _, code, T, heads, _, D, at, B = _packed(k, v, v, starts)
+    if v.shape != k.shape or heads != c.heads or D != c.D:
+        raise DfaError(-2, f"k {tuple(k.shape)} and v {tuple(v.shape)} are not rows of a cache of {c.heads} heads of {c.D}")
+    where, width, ld, held, _ = _sequences(table, lengths, None, B)
+    _check(lib().dfa_cache_append_packed(k.data_ptr(), v.data_ptr(), sk, sv, code, T, at, B, c, where, width, ld, held, _stream()), "dfa_cache_append_packed")
+
+
+class Reserved(NamedTuple):
+    """What cache_reserve leaves of a step: int32 lengths [B] and n_free [1] after it; starts [B + 1] of its packed rows; slots int64 [rows] (page * page size +
+    place in the page) and positions int32 [rows] of every row, -1 behind the last; refused int32 [1], 0 where the step fits (include/dfa.h)."""
+    lengths: "torch.Tensor"
+    n_free: "torch.Tensor"
+    starts: "torch.Tensor"
+    slots: "torch.Tensor"
+    positions: "torch.Tensor"
+    refused: "torch.Tensor"
+
+
+def _int_vectors(*tensors):
+    """Refuses (name, tensor, length) that is not a contiguous int32 vector of this length (None: of any)."""
+    import torch
+    for name, t, n in tensors:
+        if t.dtype != torch.int32:
+            raise TypeError(f"{name} must be int32")
+        if t.dim() != 1 or not t.is_contiguous() or (n is not None and t.shape[0] != n) or t.shape[0] < 1:
+            raise DfaError(-2, f"{name} must be contiguous and have {n if n is not None else 'at least one'} entries")
+
+
+def cache_reserve(counts, lengths, table, free, n_free, page, rows, in_place=False):
+    """Pages for counts int32 [B] new tokens of sequences that hold lengths int32 [B], written into table int32 [B, width] -> Reserved.  free int32
+    [capacity]: a stack of pages, of which the first n_free int32 [1] are free; page: tokens of a page; rows: room for the step's packed rows.
+    in_place: lengths and n_free are updated themselves (a captured step finds them so at its next replay).  A step that does not fit changes nothing."""
+    import torch
+    dev = _device(("counts", counts), ("lengths", lengths), ("table", table), ("free", free), ("n_free", n_free))
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return cache_reserve(counts, lengths, table, free, n_free, page, rows, in_place)
+    B = counts.shape[0] if counts.dim() else 0
+    _int_vectors(("counts", counts, None), ("free", free, None), ("n_free", n_free, 1))
+    at, width, ld, held, asked = _sequences(table, lengths, counts, B)
+    rows = int(rows)
+    whole = torch.empty((2 * max(rows, 0) + max(rows, 0) + 2 * B + 3,), dtype=torch.int32, device=counts.device)     # one allocation: slots first, for their alignment
+    cut = 2 * max(rows, 0)
+    slots = whole[:cut].view(torch.int64)
+    positions, starts, refused = whole[cut:cut + rows], whole[cut + rows:cut + rows + B + 1], whole[cut + rows + B + 1:cut + rows + B + 2]
+    after, left = (lengths, n_free) if in_place else (whole[cut + rows + B + 2:cut + rows + 2 * B + 2], whole[cut + rows + 2 * B + 2:])
+    _check(lib().dfa_cache_reserve(asked, held, B, page, at, width, ld, free.data_ptr(), free.shape[0], n_free.data_ptr(), after.data_ptr(), left.data_ptr(),
+                                   starts.data_ptr(), slots.data_ptr(), positions.data_ptr(), rows, refused.data_ptr(), _stream()), "dfa_cache_reserve")
+    return Reserved(after, left, starts, slots, positions, refused)
+
+
+def cache_release(done, lengths, table, free, n_free, page):
+    """Gives the pages of the sequences with done int32 [B] != 0 back to the stack (see cache_reserve); their lengths become 0.  Returns refused int32 [1]: 1 if
+    the stack has no room for them (nothing is changed then)."""
+    import torch
+    dev = _device(("done", done), ("lengths", lengths), ("table", table), ("free", free), ("n_free", n_free))
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return cache_release(done, lengths, table, free, n_free, page)
+    B = done.shape[0] if done.dim() else 0
+    _int_vectors(("done", done, None), ("free", free, None), ("n_free", n_free, 1))
+    at, width, ld, held, _ = _sequences(table, lengths, None, B)
+    refused = torch.empty((1,), dtype=torch.int32, device=done.device)
+    _check(lib().dfa_cache_release(done.data_ptr(), held, B, page, at, width, ld, free.data_ptr(), free.shape[0], n_free.data_ptr(), refused.data_ptr(),
+                                   _stream()), "dfa_cache_release")
+    return refused
+
+
+# ---- root-mean-square norm -----------------------------------------------------------------------------------------------------
+
+def _norm_weight(weight, C, code):
+    """(pointer, dtype code) of a norm's weight."""
+    if weight is None:
+        return None, code
+    if weight.dim() != 1 or weight.shape[0] != C or not weight.is_contiguous():
+        raise DfaError(-2, f"weight must be contiguous and have {C} elements")
+    return weight.data_ptr(), _dtype_code(weight)
+
+
+def _same_shape(like, *tensors):
+    for name, t in tensors:
+        if t is not None and t.dtype != like.dtype:
+            raise DfaError(-4, f"{name} must have x's dtype")
+        if t is not None and t.shape != like.shape:
+            raise DfaError(-2, f"{name} must have x's shape {tuple(like.shape)}")
+
+
+def rms_norm(x, weight, eps, residual=None, quantized=False, h=None):
+    """(y, h) with h = x + residual (None without a residual) and y = h * rsqrt(mean(h^2) + eps) * weight over the last dimension, in fp32 up to one rounding each.
+    x [..., C] bf16 or fp32; weight [C] (fp32 for fp32 rows, either for bf16; None: ones).  quantized: y is a QuantizedMatrix of its rows in blocks of 1 x 128,
+    what quantized_product takes; "both": y is (y, QuantizedMatrix).  h: a tensor for the sum, which may be x or residual itself."""
+    import torch
+    given = [(n, t) for n, t in (("x", x), ("weight", weight), ("residual", residual), ("h", h)) if t is not None]
+    dev = _device(*given)
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return rms_norm(x, weight, eps, residual, quantized, h)
+    _same_shape(x, ("residual", residual), ("h", h))
+    code, (M, ldx), C = _dtype_code(x), _rows_of(x, "x"), x.shape[-1]
+    w, w_code = _norm_weight(weight, C, code)
+    ldr = _rows_of(residual, "residual")[1] if residual is not None else 0
+    if h is None and residual is not None:
+        h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y = None if quantized is True else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    q = _empty_quantized(M, C, x) if quantized else None
+    _check(lib().dfa_rms_norm(x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr, w, w_code, code, eps, None if h is None else h.data_ptr(),
+                              0 if h is None else _rows_of(h, "h")[1], None if y is None else y.data_ptr(), C, ctypes.byref(_quantized(q, "q")) if q else None,
+                              M, C, _stream()), "dfa_rms_norm")
+    return ((y, q) if y is not None and q else y if q is None else q), h
+
+
+def rms_norm_backward(dy, h, weight, eps, dh=None, want_dw=True, workspace="auto"):
+    """(dx, dw) of rms_norm for gradients dy of y and dh of h (None: none): dx of x and of the residual alike, dw fp32 [C] (None if not wanted).  h: the sum that
+    rms_norm returned (x where there was no residual)."""
+    import torch
+    dev = _device(*((n, t) for n, t in (("dy", dy), ("h", h), ("weight", weight), ("dh", dh)) if t is not None))
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return rms_norm_backward(dy, h, weight, eps, dh, want_dw, workspace)
+    _same_shape(dy, ("h", h), ("dh", dh))
+    code, (M, lddy), C = _dtype_code(dy), _rows_of(dy, "dy"), dy.shape[-1]
+    w, w_code = _norm_weight(weight, C, code)
+    dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
+    dw = torch.empty((C,), dtype=torch.float32, device=dy.device) if want_dw else None
+    ptr, size, keep = _call_workspace(workspace, lib().dfa_rms_norm_backward_workspace_bytes(M, C) if want_dw else 0, dy)
+    _check(lib().dfa_rms_norm_backward(dy.data_ptr(), lddy, h.data_ptr(), _rows_of(h, "h")[1], w, w_code, code, eps, None if dh is None else dh.data_ptr(),
+                                       0 if dh is None else _rows_of(dh, "dh")[1], dx.data_ptr(), C, None if dw is None else dw.data_ptr(), M, C, ptr, size,
+                                       _stream()), "dfa_rms_norm_backward")
+    _keep(keep)
+    return dx, dw

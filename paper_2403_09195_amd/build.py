@@ -12,7 +12,7 @@ LIB_PATH = os.path.join(_PKG, "libdfa.so")
 # named for the interpreter it is built with: another one does not find it, and says so, instead of failing inside it
 TORCH_MODULE_PATH = os.path.join(_PKG, "_dfa_torch" + sysconfig.get_config_var("EXT_SUFFIX"))
 
-SOURCES = ["dfa_api.hip", "dfa_fwd_bf16.hip", "dfa_fwd_short.hip", "dfa_fwd_f32.hip", "dfa_bwd.hip", "dfa_bwd_bf16.hip", "dfa_bwd_short.hip", "dfa_linear_bf16.hip", "dfa_dense.hip", "dfa_api_quantized.hip", "dfa_quantize.hip", "dfa_quantized_linear.hip", "dfa_cache_append.hip", "dfa_cache_attention.hip", "dfa_api_packed.hip", "dfa_prompt_fwd.hip", "dfa_prompt_bwd.hip", "dfa_prompt_f32.hip", "dfa_aux.hip", "dfa_probe.hip", "dfa_plan.cpp"]
+SOURCES = ["dfa_api.hip", "dfa_fwd_bf16.hip", "dfa_fwd_short.hip", "dfa_fwd_f32.hip", "dfa_bwd.hip", "dfa_bwd_bf16.hip", "dfa_bwd_short.hip", "dfa_linear_bf16.hip", "dfa_dense.hip", "dfa_api_quantized.hip", "dfa_quantize.hip", "dfa_quantized_linear.hip", "dfa_cache_append.hip", "dfa_cache_attention.hip", "dfa_api_packed.hip", "dfa_prompt_fwd.hip", "dfa_prompt_bwd.hip", "dfa_prompt_f32.hip", "dfa_norm.hip", "dfa_reserve.hip", "dfa_aux.hip", "dfa_probe.hip", "dfa_plan.cpp"]
 
 
 def hipcc_command(out: str = LIB_PATH, extra=()):

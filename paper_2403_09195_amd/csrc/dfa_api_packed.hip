@@ -6,6 +6,8 @@
 #include <new>
 
 #include "../../include/dfa.h"
+#include "dfa_cache.h"
+#include "dfa_norm.h"
 #include "dfa_prompt.h"
 
 namespace {
@@ -74,6 +76,30 @@ int64_t backward_bytes(int32_t T, int32_t H, int32_t Hkv, int32_t D, int32_t sha
     return up((int64_t)2 * H * T * 4, 256) + (shares > 1 ? (int64_t)shares * 2 * T * Hkv * D * 4 : 0);
 }
 
+int check_norm_sizes(int64_t M, int64_t C) {
+    if (M < 1 || C < 1) return DFA_ERR_SHAPE;
+    return C > kNormMaxCols || !grid_fits(M, 1024) ? DFA_ERR_TOO_LARGE : DFA_OK;
+}
+int check_eps(float eps) { return std::isfinite(eps) && eps >= 0.f ? DFA_OK : DFA_ERR_SHAPE; }
+// fp32 rows take fp32 weights, bf16 rows either
+int check_norm_types(dfa_dtype_t dt, dfa_dtype_t weight_dt, const void* weight) {
+    return known(dt) && (!weight || (known(weight_dt) && (dt == DFA_BF16 || weight_dt == DFA_F32))) ? DFA_OK : DFA_ERR_DTYPE;
+}
+
+int64_t norm_backward_bytes(int64_t M, int64_t C, const ChipShape& chip) {
+    const int64_t n = norm_backward_workgroups(M, C, chip);
+    return n > 1 ? up(n * C * 4, 256) : 0;
+}
+
+int32_t page_shift_of(int32_t page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : page == 128 ? 7 : 0; }
+
+int check_table(int32_t B, int32_t page, const int32_t* table, int32_t width, int64_t ld_table, const int32_t* free_pages, int32_t capacity) {
+    if (!table || !free_pages) return DFA_ERR_NULL;
+    if (!page_shift_of(page) || B < 1 || width < 1 || ld_table < width || capacity < 1) return DFA_ERR_SHAPE;
+    if (!aligned(table, 4) || !aligned(free_pages, 4)) return DFA_ERR_ALIGN;
+    return (int64_t)width * page > 0x7fffffff - 256 || B > (1 << 30) ? DFA_ERR_TOO_LARGE : DFA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -118,6 +144,110 @@ int dfa_prompt_attention_backward(const void* q, const void* k, const void* v, d
     p.ndelta = static_cast<float*>(workspace), p.lse2 = p.ndelta + (int64_t)H * T;
     p.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + up((int64_t)2 * H * T * 4, 256));
     return status(launch_prompt_bwd(p, dt == DFA_F32, D, static_cast<hipStream_t>(stream)));
+}
+
+int dfa_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* weight, dfa_dtype_t weight_dt, dfa_dtype_t dt, float eps, void* h,
+                 int64_t ldh, void* y, int64_t ldy, const dfa_quantized_t* q, int64_t M, int64_t C, void* stream) {
+    if (!x || (!y && !q)) return DFA_ERR_NULL;
+    int rc = check_norm_types(dt, weight_dt, weight);
+    if (rc == DFA_OK) rc = check_norm_sizes(M, C);
+    if (rc == DFA_OK) rc = check_eps(eps);
+    if (rc != DFA_OK) return rc;
+    if (ldx < C || (residual && ldr < C) || (h && ldh < C) || (y && ldy < C)) return DFA_ERR_SHAPE;
+    const int64_t es = size_of(dt);
+    if (!aligned(x, es) || !aligned(residual, es) || !aligned(h, es) || !aligned(y, es) || !aligned(weight, size_of(weight_dt))) return DFA_ERR_ALIGN;
+    NormParams p{};
+    if (q) {
+        if (!q->values || !q->scales) return DFA_ERR_NULL;
+        if (q->ld < up(C, kScaleBlock) || q->ld_scales < up(M, 16)) return DFA_ERR_SHAPE;
+        if (q->ld % kScaleBlock || q->ld_scales % 16 || !aligned(q->values, 16) || !aligned(q->scales, 16)) return DFA_ERR_ALIGN;
+        p.values = static_cast<uint8_t*>(q->values), p.scales = static_cast<uint8_t*>(q->scales), p.ldv = q->ld, p.lds = q->ld_scales;
+    }
+    p.x = x, p.residual = residual, p.weight = weight, p.ldx = ldx, p.ldr = ldr, p.M = M, p.C = C, p.eps = eps;
+    p.h = h, p.y = y, p.ldh = ldh, p.ldy = ldy;
+    ChipShape chip;
+    rc = this_chip(&chip);
+    if (rc != DFA_OK) return rc;
+    return status(launch_norm(p, dt == DFA_F32, weight && weight_dt == DFA_F32, chip, static_cast<hipStream_t>(stream)));
+}
+
+size_t dfa_rms_norm_backward_workspace_bytes(int64_t M, int64_t C) {
+    return check_norm_sizes(M, C) == DFA_OK ? (size_t)norm_backward_bytes(M, C, chip_or_default()) : 0;
+}
+
+int dfa_rms_norm_backward(const void* dy, int64_t lddy, const void* h, int64_t ldh, const void* weight, dfa_dtype_t weight_dt, dfa_dtype_t dt, float eps,
+                          const void* dh, int64_t lddh, void* dx, int64_t lddx, float* dw, int64_t M, int64_t C, void* workspace, size_t workspace_bytes,
+                          void* stream) {
+    if (!dy || !h || !dx) return DFA_ERR_NULL;
+    int rc = check_norm_types(dt, weight_dt, weight);
+    if (rc == DFA_OK) rc = check_norm_sizes(M, C);
+    if (rc == DFA_OK) rc = check_eps(eps);
+    if (rc != DFA_OK) return rc;
+    if (lddy < C || ldh < C || (dh && lddh < C) || lddx < C) return DFA_ERR_SHAPE;
+    const int64_t es = size_of(dt);
+    if (!aligned(dy, es) || !aligned(h, es) || !aligned(dh, es) || !aligned(dx, es) || !aligned(weight, size_of(weight_dt)) || !aligned(dw, 4) ||
+        !aligned(workspace, 16))
+        return DFA_ERR_ALIGN;
+    ChipShape chip;
+    rc = this_chip(&chip);
+    if (rc != DFA_OK) return rc;
+    const int64_t need = dw ? norm_backward_bytes(M, C, chip) : 0;
+    if (need && (!workspace || workspace_bytes < (size_t)need)) return DFA_ERR_WORKSPACE;
+    NormBackwardParams p{};
+    p.dy = dy, p.h = h, p.weight = weight, p.dh = dh, p.lddy = lddy, p.ldh = ldh, p.lddh = lddh, p.M = M, p.C = C, p.eps = eps;
+    p.dx = dx, p.lddx = lddx, p.dw = dw, p.parts = static_cast<float*>(workspace), p.workgroups = norm_backward_workgroups(M, C, chip);
+    return status(launch_norm_backward(p, dt == DFA_F32, weight && weight_dt == DFA_F32, static_cast<hipStream_t>(stream)));
+}
+
+int dfa_cache_reserve(const int32_t* counts, const int32_t* lengths, int32_t B, int32_t page, int32_t* table, int32_t width, int64_t ld_table,
+                      const int32_t* free_pages, int32_t capacity, const int32_t* n_free, int32_t* new_lengths, int32_t* new_n_free, int32_t* starts,
+                      int64_t* slots, int32_t* positions, int32_t rows, int32_t* refused, void* stream) {
+    for (const void* p : {(const void*)counts, (const void*)lengths, (const void*)n_free, (const void*)new_lengths, (const void*)new_n_free,
+                          (const void*)starts, (const void*)slots, (const void*)positions, (const void*)refused})
+        if (!p) return DFA_ERR_NULL;
+    const int rc = check_table(B, page, table, width, ld_table, free_pages, capacity);
+    if (rc != DFA_OK) return rc;
+    if (rows < 1) return DFA_ERR_SHAPE;
+    if (rows > 0x7fffffff - 4096) return DFA_ERR_TOO_LARGE;
+    for (const void* p : {(const void*)counts, (const void*)lengths, (const void*)n_free, (const void*)new_lengths, (const void*)new_n_free,
+                          (const void*)starts, (const void*)positions, (const void*)refused})
+        if (!aligned(p, 4)) return DFA_ERR_ALIGN;
+    if (!aligned(slots, 8)) return DFA_ERR_ALIGN;
+    const ReserveParams p{counts, lengths, B, page_shift_of(page), rows, table, ld_table, width, free_pages, capacity, n_free, new_lengths, new_n_free,
+                          starts, slots, positions, refused};
+    return status(launch_reserve(p, static_cast<hipStream_t>(stream)));
+}
+
+int dfa_cache_release(const int32_t* done, int32_t* lengths, int32_t B, int32_t page, const int32_t* table, int32_t width, int64_t ld_table,
+                      int32_t* free_pages, int32_t capacity, int32_t* n_free, int32_t* refused, void* stream) {
+    if (!done || !lengths || !n_free || !refused) return DFA_ERR_NULL;
+    const int rc = check_table(B, page, table, width, ld_table, free_pages, capacity);
+    if (rc != DFA_OK) return rc;
+    if (!aligned(done, 4) || !aligned(lengths, 4) || !aligned(n_free, 4) || !aligned(refused, 4)) return DFA_ERR_ALIGN;
+    return status(launch_release(ReleaseParams{done, lengths, B, page_shift_of(page), table, ld_table, width, free_pages, capacity, n_free, refused},
+                                 static_cast<hipStream_t>(stream)));
+}
+
+int dfa_cache_append_packed(const void* k, const void* v, dfa_strides_t sk, dfa_strides_t sv, dfa_dtype_t dt, int32_t T, const int32_t* starts, int32_t B,
+                            dfa_cache_t cache, const int32_t* table, int32_t width, int64_t ld_table, const int32_t* lengths, void* stream) {
+    if (!k || !v || !starts || !lengths || !table || !cache.k || !cache.v || !cache.scales) return DFA_ERR_NULL;
+    if (!known(dt)) return DFA_ERR_DTYPE;
+    const int32_t shift = page_shift_of(cache.page);
+    if (!shift || (cache.D != 64 && cache.D != 128) || cache.pages < 1 || cache.heads < 1 || B < 1 || T < 1 || width < 1 || ld_table < width) return DFA_ERR_SHAPE;
+    const int64_t es = size_of(dt);
+    if (!rows_aligned(k, sk, es) || !rows_aligned(v, sv, es) || !aligned(starts, 4) || !aligned(lengths, 4) || !aligned(table, 4) || !aligned(cache.k, 16) ||
+        !aligned(cache.v, 16))
+        return DFA_ERR_ALIGN;
+    const int64_t blocks = (int64_t)T / cache.page + 2 * (int64_t)B;
+    if ((int64_t)width * cache.page > 0x7fffffff - 256 || T > 0x7fffffff - 256 || blocks > 0x3fffffff ||
+        !grid_fits(blocks * 2 * cache.heads, std::max(cache.page * cache.D / 32, 64)))
+        return DFA_ERR_TOO_LARGE;
+    AppendParams p{};
+    p.k = k, p.skn = sk.n, p.skh = sk.h, p.v = v, p.svn = sv.n, p.svh = sv.h;
+    p.cache = CacheView{static_cast<uint8_t*>(cache.k), static_cast<uint8_t*>(cache.v), static_cast<uint8_t*>(cache.scales), cache.pages, cache.heads, shift,
+                        table, ld_table, width, lengths, nullptr};
+    p.B = B, p.T = T, p.page_blocks = (int32_t)blocks, p.starts = starts;
+    return status(launch_cache_append(p, dt == DFA_F32, cache.D, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -23,6 +23,7 @@ struct AppendParams {
     int64_t skb, skn, skh, svb, svn, svh;
     CacheView cache;
     int32_t B, T, page_blocks;              // pages that T tokens can touch
+    const int32_t* starts;                  // [B + 1] where k and v are [T, heads, D] of packed sequences (dfa_packed.h): page_blocks is the slots then
 };
 hipError_t launch_cache_append(const AppendParams& p, bool f32, int32_t D, hipStream_t st);
 

@@ -7,6 +7,7 @@
 // 8 channels of R neighbouring tokens, so that loads run along tokens' rows and the R tokens of a channel are one piece of a row of values.  The
 // tokens are loaded while the page is still being looked up (eight 1024^2 images, 12 heads: 37.4 us behind it, 32.4 this way, 4.7 TB/s).
 #include "dfa_cache.h"
+#include "dfa_packed.h"
 
 namespace dfa {
 
@@ -19,7 +20,8 @@ __device__ __forceinline__ uint32_t moved(uint32_t v, float factor) {
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(__builtin_amdgcn_cvt_f32_fp8(bytes, 2) * factor, __builtin_amdgcn_cvt_f32_fp8(bytes, 3) * factor, two, true);
 }
 
-template <typename T, int D, int P>
+// kPacked: the tokens of all sequences lie one behind the other; a workgroup finds its sequence and page from their starts.
+template <typename T, int D, int P, bool kPacked>
 __global__ __launch_bounds__((P * D / 32 < 64 ? 64 : P * D / 32)) void cache_append_kernel(AppendParams p) {
     constexpr int kThreads = P * D / 32 < 64 ? 64 : P * D / 32, kWaves = kThreads / 64;
     constexpr int kChunks = D / 8, R = P / (kThreads / kChunks);             // 4 tokens a thread, 2 in the smallest page
@@ -29,14 +31,20 @@ __global__ __launch_bounds__((P * D / 32 < 64 ? 64 : P * D / 32)) void cache_app
 
     const CacheView& c = p.cache;
     int id = blockIdx.x;
-    const int j = id % p.page_blocks;
+    int j = id % p.page_blocks;
     id /= p.page_blocks;
     const bool of_v = id & 1;
     id >>= 1;
-    const int h = id % c.heads, b = id / c.heads;
+    const int h = id % c.heads;
+    int b = id / c.heads, packed_first = 0, packed_rows = 0;
+    if constexpr (kPacked) {
+        const PackedSequence s = packed_sequence<P, 2>(p.starts, p.B, p.T, j, threadIdx.x & 63);
+        if (s.b == p.B || s.tile < 0) return;
+        b = s.b, j = s.tile, packed_first = s.first, packed_rows = s.end - s.first;
+    }
 
     // the sequence's new tokens take places start .. start + n - 1; slots first .. last - 1 of this page are among them
-    const int n = c.counts ? min(max(c.counts[b], 0), p.T) : p.T;
+    const int n = kPacked ? packed_rows : c.counts ? min(max(c.counts[b], 0), p.T) : p.T;
     const int64_t start = (int64_t)c.lengths[b] - n;
     const int64_t at = (start > 0 ? start >> c.page_shift : 0) + j;
     if (at >= c.width) return;
@@ -48,7 +56,8 @@ __global__ __launch_bounds__((P * D / 32 < 64 ? 64 : P * D / 32)) void cache_app
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int ch = tid % kChunks, slot = tid / kChunks * R;
     const int64_t sn = of_v ? p.svn : p.skn;
-    const T* const src = of_v ? static_cast<const T*>(p.v) + b * p.svb + h * p.svh : static_cast<const T*>(p.k) + b * p.skb + h * p.skh;
+    const T* const src = of_v ? static_cast<const T*>(p.v) + (kPacked ? packed_first * p.svn : b * p.svb) + h * p.svh
+                              : static_cast<const T*>(p.k) + (kPacked ? packed_first * p.skn : b * p.skb) + h * p.skh;
     Chunk<T> x[R];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -123,17 +132,19 @@ __global__ __launch_bounds__((P * D / 32 < 64 ? 64 : P * D / 32)) void cache_app
     if (tid == 0 && byte != before) *scale = (uint8_t)byte;
 }
 
-template <typename T, int D>
+template <typename T, int D, bool kPacked>
 hipError_t launch(const AppendParams& p, hipStream_t st) {
-    const dim3 grid((unsigned)((int64_t)p.B * p.cache.heads * 2 * p.page_blocks));
+    const dim3 grid((unsigned)((int64_t)(kPacked ? 1 : p.B) * p.cache.heads * 2 * p.page_blocks));
     switch (p.cache.page_shift) {
-        case 4: hipLaunchKernelGGL((cache_append_kernel<T, D, 16>), grid, dim3(D / 2 < 64 ? 64 : D / 2), 0, st, p); break;
-        case 5: hipLaunchKernelGGL((cache_append_kernel<T, D, 32>), grid, dim3(D), 0, st, p); break;
-        case 6: hipLaunchKernelGGL((cache_append_kernel<T, D, 64>), grid, dim3(2 * D), 0, st, p); break;
-        default: hipLaunchKernelGGL((cache_append_kernel<T, D, 128>), grid, dim3(4 * D), 0, st, p); break;
+        case 4: hipLaunchKernelGGL((cache_append_kernel<T, D, 16, kPacked>), grid, dim3(D / 2 < 64 ? 64 : D / 2), 0, st, p); break;
+        case 5: hipLaunchKernelGGL((cache_append_kernel<T, D, 32, kPacked>), grid, dim3(D), 0, st, p); break;
+        case 6: hipLaunchKernelGGL((cache_append_kernel<T, D, 64, kPacked>), grid, dim3(2 * D), 0, st, p); break;
+        default: hipLaunchKernelGGL((cache_append_kernel<T, D, 128, kPacked>), grid, dim3(4 * D), 0, st, p); break;
     }
     return hipGetLastError();
 }
+template <typename T, int D>
+hipError_t launch(const AppendParams& p, hipStream_t st) { return p.starts ? launch<T, D, true>(p, st) : launch<T, D, false>(p, st); }
 
 }  // namespace
 

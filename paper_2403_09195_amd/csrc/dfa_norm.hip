@@ -1,0 +1,348 @@
+// Root-mean-square norm with the residual's addition and a result in 8 bits, and its gradients (gfx950).
+//
+//   h = x + residual,  r = (mean of h^2 over the row + eps)^(-1/2),  y = h r w
+//   g = dy w,  u = h r,  dx = r (g - u mean(g u)) + dh,  dw = sum over the rows of dy u
+// In fp32 from the operands to the one rounding of each result: y comes of h before it is rounded.
+//
+// Bound: memory; every operand is read once and every result written once.  A row is held in registers by kThreads threads, pieces of
+// eight elements kThreads pieces apart, so that every wave-wide load is of whole lines and a block of 128 elements is 16 neighbouring lanes'.
+#include <algorithm>
+
+#include "dfa_norm.h"
+
+namespace dfa {
+
+namespace {
+
+// A row of up to 8 * kThreads * N elements in workgroups of at least 256 threads.
+template <int kThreads> constexpr int kNormGroup = kThreads < 256 ? 256 : kThreads;
+
+template <typename T>
+__device__ __forceinline__ void to_floats(const Chunk<T>& c, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (sizeof(T) == 4) x[i] = __builtin_bit_cast(float, c.w[i]);
+        else x[i] = __builtin_bit_cast(float, i & 1 ? c.w[i / 2] & 0xffff0000u : c.w[i / 2] << 16);
+    }
+}
+// Elements at .. at + 7 of a row of `cols`, 0 behind the last.
+template <typename T>
+__device__ __forceinline__ Chunk<T> load_chunk(const T* row, int64_t at, int64_t cols) {
+    if (at + 8 <= cols) return load_whole_chunk(row + at);
+    if (at < cols) return load_part_chunk(row, at, cols);
+    Chunk<T> c;
+    clear(c);
+    return c;
+}
+template <typename T>
+__device__ __forceinline__ void store_chunk(T* row, int64_t at, int64_t cols, const float (&x)[8]) {
+    if (at + 8 <= cols) {
+        Chunk<T> c;
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) c.w[i] = __builtin_bit_cast(uint32_t, x[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
+                const bf16x2v v = {(__bf16)x[2 * i], (__bf16)x[2 * i + 1]};
+                c.w[i] = __builtin_bit_cast(uint32_t, v);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+            reinterpret_cast<words_anywhere*>(row + at)[i] = words_anywhere{c.w[4 * i], c.w[4 * i + 1], c.w[4 * i + 2], c.w[4 * i + 3]};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (at + i < cols) row[at + i] = (T)x[i];
+    }
+}
+
+// Sum over a row's threads, the same in all of them.  `lds`: 16 numbers.
+template <int kThreads>
+__device__ __forceinline__ float row_sum(float x, float* lds) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
+    if constexpr (kThreads > 64) {
+        __syncthreads();                     // the last sum has been read
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+        __syncthreads();
+        x = lds[0];
+#pragma unroll
+        for (int w = 1; w < kThreads / 64; ++w) x += lds[w];
+    }
+    return x;
+}
+
+// Whether a sum of squares is one to go on with.  Rows beyond 2^60 or so overflow it, and rows below 2^-60 or so lose bits in it that count where
+// eps is no larger: they are summed up again, scaled.
+__device__ __forceinline__ bool ordinary(float sum, float eps) { return !(sum > 1e37f) && !(sum < 1e-30f && eps < 1e-30f); }
+
+// The scale of the second sum.
+__device__ __forceinline__ float unusual_by(float sum) { return sum > 1.f ? 0x1p-80f : 0x1p80f; }
+
+// r of a row whose sum of squares is `sum`.  All threads of the row call it.
+template <int kThreads, int N>
+__device__ __forceinline__ float row_scale(const float (&h)[N][8], float sum, float eps, float cols, float* lds) {
+    if (ordinary(sum, eps)) return rsqrtf(sum / cols + eps);
+    const float by = unusual_by(sum);
+    float s = 0.f;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s = fmaf(h[n][i] * by, h[n][i] * by, s);
+    s = row_sum<kThreads>(s, lds);
+    return rsqrtf(s / cols + eps * by * by) * by;
+}
+
+template <typename T, typename W, int kThreads, int N>
+__global__ __launch_bounds__(kNormGroup<kThreads>) void norm_kernel(const NormParams p) {
+    constexpr int kRows = kNormGroup<kThreads> / kThreads;
+    __shared__ float lds[16];
+    const int i = threadIdx.x % kThreads;
+    const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kThreads;
+    if (row >= p.M) return;                  // (whole rows' threads: with a barrier in the sum, a workgroup has one row)
+    Chunk<T> x[N], res[N];
+    Chunk<W> wt[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) x[n] = load_chunk(static_cast<const T*>(p.x) + row * p.ldx, 8 * (i + n * kThreads), p.C);
+    if (p.residual)
+#pragma unroll
+        for (int n = 0; n < N; ++n) res[n] = load_chunk(static_cast<const T*>(p.residual) + row * p.ldr, 8 * (i + n * kThreads), p.C);
+    if (p.weight)
+#pragma unroll
+        for (int n = 0; n < N; ++n) wt[n] = load_chunk(static_cast<const W*>(p.weight), 8 * (i + n * kThreads), p.C);
+    float h[N][8], sum = 0.f;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        to_floats(x[n], h[n]);
+        if (p.residual) {
+            float r[8];
+            to_floats(res[n], r);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[n][e] += r[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum = fmaf(h[n][e], h[n][e], sum);
+    }
+    sum = row_sum<kThreads>(sum, lds);
+    const float r = row_scale<kThreads>(h, sum, p.eps, (float)p.C, lds);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const int64_t at = 8 * (i + n * kThreads);
+        if (p.h && at < p.C) store_chunk(static_cast<T*>(p.h) + row * p.ldh, at, p.C, h[n]);
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = h[n][e] * r;
+        if (p.weight) {
+            float w[8];
+            to_floats(wt[n], w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] *= w[e];
+        }
+        if (p.y && at < p.C) store_chunk(static_cast<T*>(p.y) + row * p.ldy, at, p.C, y);
+        if (p.values) {
+            // elements behind the last are zeros and take part as such (an infinite r makes them NaN otherwise)
+            Chunk<float> c;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) c.w[e] = at + e < p.C ? __builtin_bit_cast(uint32_t, y[e]) : 0u;
+            const uint32_t byte = scale_byte(row16_max(chunk_max<float, 1>(&c)));
+            if (at < (p.C + 127) / 128 * 128) {
+                *reinterpret_cast<u32x2*>(p.values + row * p.ldv + at) = chunk_to_e4m3(c, scale_of(byte));
+                if ((i & 15) == 0) p.scales[at / 128 * p.lds + row] = (uint8_t)byte;
+            }
+        }
+    }
+    // scale bytes behind the last row, up to a multiple of 16
+    if (p.values && row == p.M - 1)
+        for (int64_t b = i; b < (p.C + 127) / 128; b += kThreads)
+            for (int64_t m = p.M; m < (p.M + 15) / 16 * 16; ++m) p.scales[b * p.lds + m] = (uint8_t)kLeastScaleByte;
+}
+
+// A workgroup takes every `workgroups`-th row (group of rows): its part of dw stays in registers.
+template <typename T, typename W, int kThreads, int N>
+__global__ __launch_bounds__(kNormGroup<kThreads>) void norm_backward_kernel(const NormBackwardParams p) {
+    constexpr int kGroup = kNormGroup<kThreads>, kRows = kGroup / kThreads;
+    __shared__ float lds[16];
+    __shared__ float merged[kRows > 1 ? kRows * kThreads * 8 : 1];
+    const int i = threadIdx.x % kThreads, sub = threadIdx.x / kThreads;
+    Chunk<W> wx[N];
+    float dw[N][8];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dw[n][e] = 0.f;
+        if (p.weight) wx[n] = load_chunk(static_cast<const W*>(p.weight), 8 * (i + n * kThreads), p.C);
+    }
+    // (operands stay as they lie in memory and are taken apart twice: half the registers in bf16)
+    for (int64_t row = (int64_t)blockIdx.x * kRows + sub; row < p.M; row += (int64_t)p.workgroups * kRows) {
+        Chunk<T> hx[N], dyx[N], dhx[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) hx[n] = load_chunk(static_cast<const T*>(p.h) + row * p.ldh, 8 * (i + n * kThreads), p.C);
+#pragma unroll
+        for (int n = 0; n < N; ++n) dyx[n] = load_chunk(static_cast<const T*>(p.dy) + row * p.lddy, 8 * (i + n * kThreads), p.C);
+        if (p.dh)
+#pragma unroll
+            for (int n = 0; n < N; ++n) dhx[n] = load_chunk(static_cast<const T*>(p.dh) + row * p.lddh, 8 * (i + n * kThreads), p.C);
+        // g and h of piece n
+        auto operands = [&](int n, float (&g)[8], float (&h)[8]) {
+            to_floats(hx[n], h);
+            to_floats(dyx[n], g);
+            if (p.weight) {
+                float w[8];
+                to_floats(wx[n], w);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) g[e] *= w[e];
+            }
+        };
+        float squares = 0.f, both = 0.f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            float g[8], h[8];
+            operands(n, g, h);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                squares = fmaf(h[e], h[e], squares);
+                both = fmaf(g[e], h[e], both);
+            }
+        }
+        squares = row_sum<kThreads>(squares, lds);
+        both = row_sum<kThreads>(both, lds);
+        float r, mean;
+        if (ordinary(squares, p.eps)) {
+            r = rsqrtf(squares / (float)p.C + p.eps);
+            mean = both * r / (float)p.C;
+        } else {
+            const float by = unusual_by(squares);
+            squares = both = 0.f;
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                float g[8], h[8];
+                operands(n, g, h);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) squares = fmaf(h[e] * by, h[e] * by, squares);
+            }
+            r = rsqrtf(row_sum<kThreads>(squares, lds) / (float)p.C + p.eps * by * by) * by;
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                float g[8], h[8];
+                operands(n, g, h);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) both = fmaf(g[e], h[e] * r, both);
+            }
+            mean = row_sum<kThreads>(both, lds) / (float)p.C;
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int64_t at = 8 * (i + n * kThreads);
+            float g[8], h[8], dy[8], dh[8], dx[8];
+            operands(n, g, h);
+            to_floats(dyx[n], dy);
+            if (p.dh) to_floats(dhx[n], dh);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float u = h[e] * r;
+                dw[n][e] = fmaf(dy[e], u, dw[n][e]);
+                dx[e] = r * fmaf(-u, mean, g[e]);
+                if (p.dh) dx[e] += dh[e];
+            }
+            if (at < p.C) store_chunk(static_cast<T*>(p.dx) + row * p.lddx, at, p.C, dx);
+        }
+    }
+    if (!p.dw) return;
+    float* const to = p.workgroups > 1 ? p.parts + (int64_t)blockIdx.x * p.C : p.dw;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        if constexpr (kRows > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) merged[(sub * 8 + e) * kThreads + i] = dw[n][e];
+            __syncthreads();
+            if (sub != 0) continue;
+#pragma unroll
+            for (int s = 1; s < kRows; ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) dw[n][e] += merged[(s * 8 + e) * kThreads + i];
+        }
+        const int64_t at = 8 * (i + n * kThreads);
+        if (at < p.C) store_chunk(to, at, p.C, dw[n]);
+    }
+}
+
+// dw of the workgroups' parts: 64 columns a workgroup, 16 waves that take every sixteenth part.
+__global__ __launch_bounds__(1024) void norm_sum_kernel(const float* parts, float* dw, int64_t C, int32_t count) {
+    __shared__ float lds[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    float s = 0.f;
+    if (c < C)
+        for (int32_t i = wave; i < count; i += 16) s += parts[i * C + c];
+    lds[wave][lane] = s;
+    __syncthreads();
+    if (wave || c >= C) return;
+#pragma unroll
+    for (int w = 1; w < 16; ++w) s += lds[w][lane];
+    dw[c] = s;
+}
+
+// Threads of a row and pieces of a thread.
+struct NormForm {
+    int threads, pieces;
+};
+NormForm norm_form(int64_t M, int64_t cols) {
+    const int64_t pieces = (cols + 7) / 8;
+    const int threads = pieces <= 128 && M >= 1024 ? 64 : pieces <= 512 ? 256 : pieces <= 2048 ? 512 : 1024;
+    const int64_t n = (pieces + threads - 1) / threads;
+    return NormForm{threads, n <= 1 ? 1 : n <= 2 ? 2 : 4};
+}
+
+template <typename T, typename W, int kThreads, int N>
+hipError_t launch_form(const NormParams& p, hipStream_t st) {
+    constexpr int kRows = kNormGroup<kThreads> / kThreads;
+    hipLaunchKernelGGL((norm_kernel<T, W, kThreads, N>), dim3((unsigned)((p.M + kRows - 1) / kRows)), dim3(kNormGroup<kThreads>), 0, st, p);
+    return hipGetLastError();
+}
+template <typename T, typename W, int kThreads, int N>
+hipError_t launch_form(const NormBackwardParams& p, hipStream_t st) {
+    hipLaunchKernelGGL((norm_backward_kernel<T, W, kThreads, N>), dim3((unsigned)p.workgroups), dim3(kNormGroup<kThreads>), 0, st, p);
+    return hipGetLastError();
+}
+template <typename T, typename W, typename Params>
+hipError_t launch_typed(const Params& p, NormForm f, hipStream_t st) {
+    switch (f.threads * 8 + f.pieces) {
+        case 64 * 8 + 1: return launch_form<T, W, 64, 1>(p, st);
+        case 64 * 8 + 2: return launch_form<T, W, 64, 2>(p, st);
+        case 256 * 8 + 1: return launch_form<T, W, 256, 1>(p, st);
+        case 256 * 8 + 2: return launch_form<T, W, 256, 2>(p, st);
+        case 512 * 8 + 2: return launch_form<T, W, 512, 2>(p, st);
+        case 512 * 8 + 4: return launch_form<T, W, 512, 4>(p, st);
+        default: return launch_form<T, W, 1024, 4>(p, st);
+    }
+}
+template <typename Params>
+hipError_t launch_any(const Params& p, NormForm f, bool f32, bool weight_f32, hipStream_t st) {
+    if (f32) return launch_typed<float, float>(p, f, st);
+    return weight_f32 ? launch_typed<__bf16, float>(p, f, st) : launch_typed<__bf16, __bf16>(p, f, st);
+}
+
+}  // namespace
+
+hipError_t launch_norm(const NormParams& p, bool f32, bool weight_f32, const ChipShape&, hipStream_t st) {
+    return launch_any(p, norm_form(p.M, p.values ? (p.C + 127) / 128 * 128 : p.C), f32, weight_f32, st);
+}
+
+int32_t norm_backward_workgroups(int64_t M, int64_t C, const ChipShape& chip) {
+    const NormForm f = norm_form(M, C);
+    const int64_t rows = f.threads == 64 ? 4 : 1, most = (M + rows - 1) / rows;
+    return (int32_t)std::min<int64_t>(most, (f.threads == 1024 ? 1 : f.threads == 512 ? 2 : 4) * chip.cus);
+}
+
+hipError_t launch_norm_backward(const NormBackwardParams& p, bool f32, bool weight_f32, hipStream_t st) {
+    const hipError_t e = launch_any(p, norm_form(p.M, p.C), f32, weight_f32, st);
+    if (e != hipSuccess || !p.dw || p.workgroups == 1) return e;
+    hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)((p.C + 63) / 64)), dim3(1024), 0, st, p.parts, p.dw, p.C, p.workgroups);
+    return hipGetLastError();
+}
+
+}  // namespace dfa

@@ -1,12 +1,11 @@
 // Attention within packed sequences (gfx950): arguments of its kernels, and what they share.
 //
-// Rows starts[b] .. starts[b + 1] - 1 of q, k and v are sequence b's.  Nothing of this is known on the host, so a launch has a
-// slot for every tile there might be: sequence b's tiles of R rows take slots floor(starts[b] / R) + b and on, of which it has
-// floor(starts[b + 1] / R) - floor(starts[b] / R) + 1, never fewer than ceil(length / R).  The rows behind the last sequence
-// are a sequence of their own, B, whose results are zeros.
+// Sequences are packed (dfa_packed.h); a tile is R rows of one sequence and head.  Sequence b has floor(starts[b + 1] / R) - floor(starts[b] / R) + 1
+// slots, never fewer than ceil(length / R).  The rows behind the last sequence are a sequence of their own, B, whose results are zeros.
 #pragma once
 #include "dfa_device.h"
 #include "dfa_mfma.h"
+#include "dfa_packed.h"
 
 namespace dfa {
 
@@ -43,39 +42,15 @@ struct PromptTile {
     bool empty;             // a slot without a tile
 };
 
-// starts[i] within the rows there are; sequence 0 starts at row 0.
-__device__ __forceinline__ int32_t prompt_start(const PromptParams& p, int32_t i) {
-    return i == 0 ? 0 : min(max(p.starts[i], 0), p.T);
-}
-
-// The tile of a slot: the last b with floor(starts[b] / R) + b <= slot, 64 candidates to a trip to memory.  (Starts that do not ascend
-// give some tile inside the rows, or none.)
 template <int R>
 __device__ __forceinline__ PromptTile prompt_tile(const PromptParams& p, int32_t slot, int lane) {
-    int32_t lo = 0, n = p.B + 1, here, next;
-    for (;;) {
-        const int32_t step = (n + 63) / 64;
-        const int32_t at = (int32_t)min((int64_t)lo + (int64_t)lane * step, (int64_t)p.B);
-        const int32_t start = prompt_start(p, at);
-        const bool in = (int64_t)lane * step < n;
-        const int32_t count = __popcll(__ballot(in && start / R + at <= slot));
-        const int32_t idx = max(count, 1) - 1;
-        lo += idx * step;
-        n = min(step, n - idx * step);
-        if (n <= 1) {
-            here = __builtin_amdgcn_readlane(start, idx);
-            // with a step of one, the next lane holds the next start
-            next = lo == p.B ? p.T : step == 1 && idx < 63 ? __builtin_amdgcn_readlane(start, idx + 1) : prompt_start(p, lo + 1);
-            break;
-        }
-    }
-    lo = __builtin_amdgcn_readfirstlane(lo);
+    const PackedSequence s = packed_sequence<R, 1>(p.starts, p.B, p.T, slot, lane);
     PromptTile t;
-    t.first = here;
-    t.n = __builtin_amdgcn_readfirstlane(max(next, here)) - here;
-    t.t0 = (slot - (here / R + lo)) * R;
-    t.rest = lo == p.B;
-    t.empty = t.t0 < 0 || t.t0 >= t.n;
+    t.first = s.first;
+    t.n = s.end - s.first;
+    t.t0 = s.tile * R;
+    t.rest = s.b == p.B;
+    t.empty = s.tile < 0 || t.t0 >= t.n;
     return t;
 }
 
