@@ -149,6 +149,46 @@ __device__ __forceinline__ bf16x8 prompt_turned(const uint16_t* block, int turne
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+// ---- values that are not finite, behind a mask ------------------------------------------------------------------------------------
+// A weight of zero makes NaN of a value that is not finite.  In blocks that some row sees in part such values are taken out of the product and
+// added to the rows that see them.  (Rare, and only the last blocks of a walk are looked at: two pieces of 32 D bytes a lane.)
+__device__ __forceinline__ uint32_t odd_halves(uint32_t w) { return ((w & 0x7fff7fffu) + 0x00800080u) & 0x80008000u; }
+template <int D>
+__device__ __forceinline__ bool prompt_odd_values(const uint16_t* block) {
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(block + 8 * ((threadIdx.x & 63) + 64 * i));
+        any |= odd_halves(w[0]) | odd_halves(w[1]) | odd_halves(w[2]) | odd_halves(w[3]);
+    }
+    return __ballot(any != 0u) != 0ull;
+}
+// Zeros in the places of such values.
+__device__ __forceinline__ bf16x8 without_odd(const bf16x8& x) {
+    u32x4 w = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t odd = odd_halves(w[i]) >> 15;                   // bits 0 and 16
+        w[i] &= ~(odd * 0xffffu);
+    }
+    return __builtin_bit_cast(bf16x8, w);
+}
+// Adds them (kValues block) to the accumulators of the rows that see them: row (lane & 31) sees positions up to `last`.
+template <int D>
+__device__ __forceinline__ void add_odd(const uint16_t* block, int32_t last, int lane, floatx16& acc, int db) {
+    const int g = lane >> 5;
+#pragma unroll 1
+    for (int pos = 0; pos < 32; ++pos) {
+        const int swizzle = prompt_swizzle<D, PromptOrder::kValues>(pos);
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int d = 32 * db + 8 * (v >> 2) + 4 * g + (v & 3);
+            const uint32_t bits = block[pos * D + 8 * ((d >> 3) ^ swizzle) + (d & 7)];
+            if (pos <= last && (bits & 0x7f80u) == 0x7f80u) acc[v] += __builtin_bit_cast(float, bits << 16);
+        }
+    }
+}
+
 __device__ __forceinline__ floatx16 prompt_zero() {
     floatx16 z;
 #pragma unroll

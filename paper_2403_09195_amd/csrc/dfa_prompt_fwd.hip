@@ -27,6 +27,15 @@ struct Wave {
     int row_at, value_at;
     float c;                                 // scale * log2(e)
 
+    __device__ __forceinline__ void begin() {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            ref[qb] = kLowest;
+            sum[qb] = 0.f;
+#pragma unroll
+            for (int db = 0; db < kHalves; ++db) acc[db][qb] = prompt_zero();
+        }
+    }
     // S^T of one block on its own
     __device__ __forceinline__ void scores(const uint16_t* kb, floatx16 (&s)[QB]) const {
 #pragma unroll
@@ -46,6 +55,22 @@ struct Wave {
                 for (int qb = 0; qb < QB; ++qb)
                     acc[db][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, p[qb][st]), acc[db][qb], 0, 0, 0);
             }
+    }
+
+    // The same of a block that rows see up to position `last` of it, with values that are not finite in it.
+    __device__ __forceinline__ void accumulate_odd(const uint16_t* vb, const u32x4 (&p)[QB][2], const int32_t (&last)[QB], int lane) {
+#pragma unroll
+        for (int db = 0; db < kHalves; ++db) {
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                const bf16x8 vf = without_odd(prompt_value<D>(vb, value_at, db, st));
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb)
+                    acc[db][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, p[qb][st]), acc[db][qb], 0, 0, 0);
+            }
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) add_odd<D>(vb, last[qb], lane, acc[db][qb], db);
+        }
     }
 
     // One beat: scores of the next block (K at kb -> s_next), p_prev times the previous block's values (vb), numerators of s (-> p).  The
@@ -204,13 +229,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
     w.c = uniform_float(p.scale * kLog2e);
     w.row_at = prompt_row_at<D, PromptOrder::kKeys>(lane);
     w.value_at = prompt_value_at<D>(lane);
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-        w.ref[qb] = kLowest;
-        w.sum[qb] = 0.f;
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db) w.acc[db][qb] = prompt_zero();
-    }
+    w.begin();
 
     // scores that a row does not see, of the block from key k0 on
     auto mask = [&](floatx16 (&s)[QB], int32_t k0) {
@@ -240,6 +259,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
     floatx16 s_a[QB], s_b[QB];
     u32x4 p_a[QB][2], p_b[QB][2];
     float psum[QB];
+    bool odd = false;                        // values that are not finite in the wave's last two blocks
     if (live) w.scores(at(0, 0), s_a);
     if (kPer == 1) enter(1);
     if (live) {
@@ -257,7 +277,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
             w.settle(s_b, p_b, psum);
         }
         if (ends) {
+            // (a mask reaches no further back than these two blocks)
             mask(s_b, 64 * s + 32);
+            odd = prompt_odd_values<D>(at(2 * s, 1)) || prompt_odd_values<D>(at(2 * s + 1, 1));
             w.template beat<false, true>(at(2 * s, 0), at(2 * s, 1), s_b, s_a, p_a, p_b, psum);
             w.settle(s_b, p_b, psum);
             w.accumulate(at(2 * s + 1, 1), p_b);
@@ -276,7 +298,32 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
     const int je = lane_e & 31, ge = lane_e >> 5;
     __syncthreads();
     constexpr int kPitch = 2 * D + 16;
-    static_assert(sizeof(lds) >= 4 * 32 * QB * kPitch, "every wave's rows fit the stages");
+    static_assert(sizeof(lds) >= 4 * 32 * QB * kPitch + 16, "every wave's rows fit the stages, and four flags");
+    // Some row of the tile may not see such a value: the walk is done again, block after block, with them taken out of the products.  (In place, in
+    // the wave's last two beats, this would cost the loop its registers: 111 to 142 of D = 64 are spilled then.)
+    int32_t* const flags = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(lds) + sizeof(lds)) - 4;
+    if (lane == 0) flags[wave] = odd;
+    __syncthreads();
+    if (__builtin_expect(__builtin_amdgcn_readfirstlane(flags[0] | flags[1] | flags[2] | flags[3]) != 0, 0)) {
+        w.begin();
+        for (int32_t n = 0; n < 2 * n_steps; ++n) {
+            __syncthreads();                 // the flags, and block n - 1, have been read
+            prompt_copy<D, PromptOrder::kKeys>(kbase, kpitch, 32 * n, keys, wave, lane_e, lds_addr);
+            prompt_copy<D, PromptOrder::kValues>(vbase, vpitch, 32 * n, keys, wave, lane_e, lds_addr + kStage * 2);
+            wait_vmcnt<0>();
+            __syncthreads();
+            if (!live || n >= 2 * my_steps) continue;
+            w.scores(lds[0][0], s_a);
+            mask(s_a, 32 * n);
+            w.template beat<false, false>(lds[0][0], lds[0][1], s_a, s_b, p_b, p_a, psum);
+            w.settle(s_a, p_a, psum);
+            int32_t last[QB];
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) last[qb] = min(p.causal ? my0 + 32 * qb + je : keys - 1, keys - 1) - 32 * n;
+            w.accumulate_odd(lds[0][1], p_a, last, lane_e);
+        }
+        __syncthreads();
+    }
     if (!live) return;
     char* const mine = reinterpret_cast<char*>(&lds[0][0][0]) + wave * (32 * QB * kPitch);
 #pragma unroll
