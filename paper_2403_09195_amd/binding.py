@@ -167,7 +167,9 @@ def lib():
         from . import _dfa_torch
         _dfa_torch.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
             L.dfa_forward_alloc, L.dfa_backward, L.dfa_quantized_linear, L.dfa_quantized_linear_workspace_bytes, L.dfa_quantized_linear_backward,
-            L.dfa_quantized_linear_backward_workspace_bytes, L.dfa_cache_append, L.dfa_cache_attention, L.dfa_cache_attention_workspace_bytes)))
+            L.dfa_quantized_linear_backward_workspace_bytes, L.dfa_cache_append, L.dfa_cache_attention, L.dfa_cache_attention_workspace_bytes,
+            L.dfa_prompt_attention, L.dfa_prompt_attention_backward, L.dfa_prompt_attention_backward_workspace_bytes, L.dfa_rms_norm, L.dfa_rms_norm_backward,
+            L.dfa_rms_norm_backward_workspace_bytes, L.dfa_cache_reserve, L.dfa_cache_append_packed)))
         global _native_forward, _native_backward, _native
         _native_forward, _native_backward, _native = _dfa_torch.forward, _dfa_torch.backward, _dfa_torch
         _lib = L
@@ -999,6 +1001,10 @@ def prompt_attention(q, k, v, starts, scale, causal=True, out=None, lse=None, wa
     """Attention within each of many sequences that lie one behind the other -> (out [T, H, D], lse fp32 [H, T] or None).  q [T, H, D], k and v
     [T, Hkv, D] (bf16 or fp32, may be strided views, as the heads of one projection's result are; H a multiple of Hkv); starts int32 [B + 1]: sequence b is
     rows starts[b] .. starts[b + 1] - 1, the rows behind the last are 0 and -inf.  causal: a row attends to those before it and itself."""
+    if out is None and lse is None and want_lse:
+        res = _native_call("prompt_attention", q, k, v, starts, scale, causal)
+        if res is not None:
+            return res
     import torch
     dev = _device(("q", q), ("k", k), ("v", v), ("starts", starts))
     if _elsewhere(dev):
@@ -1016,6 +1022,10 @@ def prompt_attention(q, k, v, starts, scale, causal=True, out=None, lse=None, wa
 def prompt_attention_backward(q, k, v, out, lse, dout, starts, scale, causal=True, workspace="auto"):
     """(dq, dk, dv) of prompt_attention for a gradient dout [T, H, D] of its out; out and lse: what it returned.  Gradients of shared heads are sums over
     the query heads; those of rows of no sequence are 0."""
+    if isinstance(workspace, str) and workspace == "auto":
+        res = _native_call("prompt_attention_backward", q, k, v, out, lse, dout, starts, scale, causal)
+        if res is not None:
+            return res
     import torch
     dev = _device(("q", q), ("k", k), ("v", v), ("out", out), ("lse", lse), ("dout", dout), ("starts", starts))
     if _elsewhere(dev):
@@ -1034,6 +1044,8 @@ def prompt_attention_backward(q, k, v, out, lse, dout, starts, scale, causal=Tru
 
 
 def _cache_append_packed(k, v, cache, table, lengths, counts, starts):
+    if counts is None and _native_call("cache_append_packed", k, v, cache, table, lengths, starts):
+        return
     import torch
     dev = _device(("k", k), ("v", v), ("cache.k", cache.k), ("cache.v", cache.v), ("cache.scales", cache.scales), ("table", table), ("lengths", lengths),
                   ("starts", starts))
@@ -1075,6 +1087,10 @@ def cache_reserve(counts, lengths, table, free, n_free, page, rows, in_place=Fal
     """Pages for counts int32 [B] new tokens of sequences that hold lengths int32 [B], written into table int32 [B, width] -> Reserved.  free int32
     [capacity]: a stack of pages, of which the first n_free int32 [1] are free; page: tokens of a page; rows: room for the step's packed rows.
     in_place: lengths and n_free are updated themselves (a captured step finds them so at its next replay).  A step that does not fit changes nothing."""
+    if not in_place:
+        res = _native_call("cache_reserve", counts, lengths, table, free, n_free, page, rows)
+        if res is not None:
+            return Reserved(*res)
     import torch
     dev = _device(("counts", counts), ("lengths", lengths), ("table", table), ("free", free), ("n_free", n_free))
     if _elsewhere(dev):
@@ -1134,6 +1150,14 @@ def rms_norm(x, weight, eps, residual=None, quantized=False, h=None):
     """(y, h) with h = x + residual (None without a residual) and y = h * rsqrt(mean(h^2) + eps) * weight over the last dimension, in fp32 up to one rounding each.
     x [..., C] bf16 or fp32; weight [C] (fp32 for fp32 rows, either for bf16; None: ones).  quantized: y is a QuantizedMatrix of its rows in blocks of 1 x 128,
     what quantized_product takes; "both": y is (y, QuantizedMatrix).  h: a tensor for the sum, which may be x or residual itself."""
+    if h is None:
+        res = _native_call("rms_norm", x, weight, eps, residual, quantized is not True, bool(quantized))
+        if res is not None:
+            y, h, values, scales = res
+            if values is not None:
+                q = QuantizedMatrix(values, scales, x.shape[-1])
+                y = q if y is None else (y, q)
+            return y, h
     import torch
     given = [(n, t) for n, t in (("x", x), ("weight", weight), ("residual", residual), ("h", h)) if t is not None]
     dev = _device(*given)
@@ -1157,6 +1181,10 @@ def rms_norm(x, weight, eps, residual=None, quantized=False, h=None):
 def rms_norm_backward(dy, h, weight, eps, dh=None, want_dw=True, workspace="auto"):
     """(dx, dw) of rms_norm for gradients dy of y and dh of h (None: none): dx of x and of the residual alike, dw fp32 [C] (None if not wanted).  h: the sum that
     rms_norm returned (x where there was no residual)."""
+    if want_dw and isinstance(workspace, str) and workspace == "auto":
+        res = _native_call("rms_norm_backward", dy, h, weight, eps, dh)
+        if res is not None:
+            return res
     import torch
     dev = _device(*((n, t) for n, t in (("dy", dy), ("h", h), ("weight", weight), ("dh", dh)) if t is not None))
     if _elsewhere(dev):

@@ -34,6 +34,18 @@ struct Library {                               // of the operators on 8-bit oper
 };
 Library g_lib = {};
 
+struct PackedLibrary {                         // of the operators on packed prompts
+    decltype(&dfa_prompt_attention) attention;
+    decltype(&dfa_prompt_attention_backward) attention_backward;
+    decltype(&dfa_prompt_attention_backward_workspace_bytes) attention_backward_bytes;
+    decltype(&dfa_rms_norm) norm;
+    decltype(&dfa_rms_norm_backward) norm_backward;
+    decltype(&dfa_rms_norm_backward_workspace_bytes) norm_backward_bytes;
+    decltype(&dfa_cache_reserve) reserve;
+    decltype(&dfa_cache_append_packed) append;
+};
+PackedLibrary g_packed = {};
+
 constexpr int kMaxOffsets = 1024;
 
 // A Python list or tuple; the items are borrowed.
@@ -151,7 +163,7 @@ PyObject* as_tuple(at::Tensor (&t)[n]) {
     PyObject* const tuple = PyTuple_New((Py_ssize_t)n);
     if (!tuple) return nullptr;
     for (size_t i = 0; i < n; ++i) {
-        PyObject* const o = THPVariable_Wrap(std::move(t[i]));
+        PyObject* const o = THPVariable_Wrap(std::move(t[i]));        // (None for one that was never made)
         if (!o) {
             Py_DECREF(tuple);
             return nullptr;
@@ -407,14 +419,203 @@ PyObject* cache_attention(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     END_HANDLE_TH_ERRORS
 }
 
-// bind(addresses in the loaded libdfa.so of dfa_forward_alloc, dfa_backward and Library's functions in order)
+// ---- the operators on packed prompts ----------------------------------------------------------------------------------------
+
+// A contiguous int32 vector (of n entries, or of any number).
+const at::Tensor* int_vector(PyObject* o, int64_t n = -1) {
+    const at::Tensor* const t = device_tensor(o);
+    if (!t || t->scalar_type() != at::kInt || t->dim() != 1 || t->size(0) < 1 || t->size(0) > INT32_MAX || !t->is_contiguous()) return nullptr;
+    return n < 0 || t->size(0) == n ? t : nullptr;
+}
+
+// q [T, H, D], k and v [T, Hkv, D] with contiguous last dimension, and starts.
+struct Packed {
+    const at::Tensor* t[3];
+    dfa_strides_t s[3];
+    dfa_dtype_t dt;
+    int64_t T, H, Hkv, D;
+    const at::Tensor* starts;
+    int32_t B;
+};
+bool read_packed(PyObject* const* qkv, PyObject* starts, Packed* p) {
+    for (int i = 0; i < 3; ++i) {
+        p->t[i] = device_tensor(qkv[i]);
+        dfa_dtype_t dt;
+        if (!p->t[i] || !float_type(*p->t[i], &dt) || p->t[i]->dim() != 3 || p->t[i]->stride(2) != 1 || p->t[i]->numel() == 0) return false;
+        if (i && dt != p->dt) return false;
+        p->dt = dt;
+        p->s[i] = dfa_strides_t{0, p->t[i]->stride(0), p->t[i]->stride(1)};
+    }
+    const at::Tensor &q = *p->t[0], &k = *p->t[1];
+    p->T = q.size(0), p->H = q.size(1), p->D = q.size(2), p->Hkv = k.size(1);
+    if (p->t[2]->sizes() != k.sizes() || k.size(0) != p->T || k.size(2) != p->D || p->T > INT32_MAX || p->H > INT32_MAX || p->D > INT32_MAX) return false;
+    p->starts = int_vector(starts);
+    if (!p->starts || p->starts->size(0) < 2) return false;
+    p->B = (int32_t)p->starts->size(0) - 1;
+    return true;
+}
+
+// A contiguous tensor of this type and these sizes.
+const at::Tensor* exactly(PyObject* o, at::ScalarType type, at::IntArrayRef sizes) {
+    const at::Tensor* const t = device_tensor(o);
+    return t && t->scalar_type() == type && t->sizes() == sizes && t->is_contiguous() ? t : nullptr;
+}
+
+// prompt_attention(q, k, v, starts, scale, causal) -> (out, lse), a negative status, or None
+PyObject* prompt_attention(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    Packed p;
+    if (nargs != 6 || !g_packed.attention || !PyFloat_CheckExact(args[4]) || !PyBool_Check(args[5]) || !read_packed(args, args[3], &p)) Py_RETURN_NONE;
+    const at::Tensor& q = *p.t[0];
+    at::Tensor res[2] = {at::empty({p.T, p.H, p.D}, q.options()), at::empty({p.H, p.T}, q.options().dtype(at::kFloat))};
+    int rc;
+    {
+        pybind11::gil_scoped_release release;
+        rc = g_packed.attention(q.data_ptr(), p.t[1]->data_ptr(), p.t[2]->data_ptr(), p.s[0], p.s[1], p.s[2], p.dt, (int32_t)p.T, (int32_t)p.H, (int32_t)p.Hkv,
+                                (int32_t)p.D, p.starts->data_ptr<int32_t>(), p.B, args[5] == Py_True, (float)PyFloat_AS_DOUBLE(args[4]), res[0].data_ptr(),
+                                res[1].data_ptr<float>(), c10::hip::getCurrentHIPStream().stream());
+    }
+    return rc != DFA_OK ? PyLong_FromLong(rc) : as_tuple(res);
+    END_HANDLE_TH_ERRORS
+}
+
+// prompt_attention_backward(q, k, v, out, lse, dout, starts, scale, causal) -> (dq, dk, dv), a negative status, or None
+PyObject* prompt_attention_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    Packed p;
+    if (nargs != 9 || !g_packed.attention_backward || !PyFloat_CheckExact(args[7]) || !PyBool_Check(args[8]) || !read_packed(args, args[6], &p)) Py_RETURN_NONE;
+    const at::Tensor& q = *p.t[0];
+    const at::Tensor *const out = exactly(args[3], q.scalar_type(), {p.T, p.H, p.D}), *const lse = exactly(args[4], at::kFloat, {p.H, p.T}),
+                     *const dout = exactly(args[5], q.scalar_type(), {p.T, p.H, p.D});
+    if (!out || !lse || !dout) Py_RETURN_NONE;
+    at::Tensor res[3] = {at::empty({p.T, p.H, p.D}, q.options()), at::empty({p.T, p.Hkv, p.D}, q.options()), at::empty({p.T, p.Hkv, p.D}, q.options())};
+    const size_t bytes = g_packed.attention_backward_bytes((int32_t)p.T, (int32_t)p.H, (int32_t)p.Hkv, (int32_t)p.D, p.B);
+    const Room room(bytes, q);
+    int rc;
+    {
+        pybind11::gil_scoped_release release;
+        rc = g_packed.attention_backward(q.data_ptr(), p.t[1]->data_ptr(), p.t[2]->data_ptr(), p.s[0], p.s[1], p.s[2], out->data_ptr(), lse->data_ptr<float>(),
+                                         dout->data_ptr(), p.dt, (int32_t)p.T, (int32_t)p.H, (int32_t)p.Hkv, (int32_t)p.D, p.starts->data_ptr<int32_t>(), p.B,
+                                         args[8] == Py_True, (float)PyFloat_AS_DOUBLE(args[7]), res[0].data_ptr(), res[1].data_ptr(), res[2].data_ptr(), room.ptr,
+                                         bytes, c10::hip::getCurrentHIPStream().stream());
+    }
+    return rc != DFA_OK ? PyLong_FromLong(rc) : as_tuple(res);
+    END_HANDLE_TH_ERRORS
+}
+
+// A norm's rows (contiguous) and weight (None: none).
+struct NormCall {
+    const at::Tensor *x, *weight;
+    dfa_dtype_t dt, weight_dt;
+    int64_t M, C;
+    float eps;
+};
+bool read_norm(PyObject* x, PyObject* weight, PyObject* eps, NormCall* n) {
+    n->x = device_tensor(x);
+    if (!n->x || !float_type(*n->x, &n->dt) || !read_rows(*n->x, &n->M, &n->C) || !PyFloat_CheckExact(eps)) return false;
+    n->eps = (float)PyFloat_AS_DOUBLE(eps);
+    n->weight = nullptr, n->weight_dt = n->dt;
+    if (weight == Py_None) return true;
+    n->weight = device_tensor(weight);
+    return n->weight && float_type(*n->weight, &n->weight_dt) && n->weight->dim() == 1 && n->weight->size(0) == n->C && n->weight->is_contiguous();
+}
+const void* pointer(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
+
+// rms_norm(x, weight, eps, residual, whether y, whether in 8 bits) -> (y, h, values, scales) with None for what there is not, a negative status, or None
+PyObject* rms_norm(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    NormCall n;
+    if (nargs != 6 || !g_packed.norm || !read_norm(args[0], args[1], args[2], &n)) Py_RETURN_NONE;
+    const at::Tensor* const res = args[3] == Py_None ? nullptr : exactly(args[3], n.x->scalar_type(), n.x->sizes());
+    if (args[3] != Py_None && !res) Py_RETURN_NONE;
+    const bool plain = args[4] == Py_True, eight = args[5] == Py_True;
+    const int64_t ld = up(n.C, 128), lds = up(n.M, 16);
+    at::Tensor r[4];
+    if (plain) r[0] = at::empty(n.x->sizes(), n.x->options());
+    if (res) r[1] = at::empty(n.x->sizes(), n.x->options());
+    if (eight) r[2] = at::empty({n.M, ld}, n.x->options().dtype(at::kFloat8_e4m3fn)), r[3] = at::empty({ld / 128, lds}, n.x->options().dtype(at::kByte));
+    const dfa_quantized_t q{eight ? r[2].data_ptr() : nullptr, eight ? r[3].data_ptr() : nullptr, ld, lds};
+    int rc;
+    {
+        pybind11::gil_scoped_release release;
+        rc = g_packed.norm(n.x->data_ptr(), n.C, pointer(res), n.C, pointer(n.weight), n.weight_dt, n.dt, n.eps, res ? r[1].data_ptr() : nullptr, n.C,
+                           plain ? r[0].data_ptr() : nullptr, n.C, eight ? &q : nullptr, n.M, n.C, c10::hip::getCurrentHIPStream().stream());
+    }
+    return rc != DFA_OK ? PyLong_FromLong(rc) : as_tuple(r);
+    END_HANDLE_TH_ERRORS
+}
+
+// rms_norm_backward(dy, h, weight, eps, dh) -> (dx, dw), a negative status, or None
+PyObject* rms_norm_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    NormCall n;
+    if (nargs != 5 || !g_packed.norm_backward || !read_norm(args[0], args[2], args[3], &n)) Py_RETURN_NONE;
+    const at::Tensor *const h = exactly(args[1], n.x->scalar_type(), n.x->sizes()), *const dh = args[4] == Py_None ? nullptr : exactly(args[4], n.x->scalar_type(), n.x->sizes());
+    if (!h || (args[4] != Py_None && !dh)) Py_RETURN_NONE;
+    at::Tensor r[2] = {at::empty(n.x->sizes(), n.x->options()), at::empty({n.C}, n.x->options().dtype(at::kFloat))};
+    const size_t bytes = g_packed.norm_backward_bytes(n.M, n.C);
+    const Room room(bytes, *n.x);
+    int rc;
+    {
+        pybind11::gil_scoped_release release;
+        rc = g_packed.norm_backward(n.x->data_ptr(), n.C, h->data_ptr(), n.C, pointer(n.weight), n.weight_dt, n.dt, n.eps, pointer(dh), n.C, r[0].data_ptr(), n.C,
+                                    r[1].data_ptr<float>(), n.M, n.C, room.ptr, bytes, c10::hip::getCurrentHIPStream().stream());
+    }
+    return rc != DFA_OK ? PyLong_FromLong(rc) : as_tuple(r);
+    END_HANDLE_TH_ERRORS
+}
+
+// cache_reserve(counts, lengths, table, free, n_free, page, rows) -> (lengths, n_free, starts, slots, positions, refused), a negative status, or None
+PyObject* cache_reserve(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    const at::Tensor* const counts = nargs == 7 ? int_vector(args[0]) : nullptr;
+    if (!counts || !g_packed.reserve) Py_RETURN_NONE;
+    const int64_t B = counts->size(0);
+    const at::Tensor *const lengths = int_vector(args[1], B), *const table = device_tensor(args[2]), *const free = int_vector(args[3]), *const n_free = int_vector(args[4], 1);
+    int32_t page, rows;
+    if (!lengths || !table || !free || !n_free || !as_int32(args[5], &page) || !as_int32(args[6], &rows) || rows < 1) Py_RETURN_NONE;
+    if (table->scalar_type() != at::kInt || table->dim() != 2 || table->size(0) != B || table->size(1) < 1 || table->size(1) > INT32_MAX || !table->is_contiguous()) Py_RETURN_NONE;
+    const at::TensorOptions o = counts->options();
+    at::Tensor r[6] = {at::empty({B}, o), at::empty({1}, o), at::empty({B + 1}, o), at::empty({rows}, o.dtype(at::kLong)), at::empty({rows}, o), at::empty({1}, o)};
+    int rc;
+    {
+        pybind11::gil_scoped_release release;
+        rc = g_packed.reserve(counts->data_ptr<int32_t>(), lengths->data_ptr<int32_t>(), (int32_t)B, page, table->data_ptr<int32_t>(), (int32_t)table->size(1), table->size(1),
+                              free->data_ptr<int32_t>(), (int32_t)free->size(0), n_free->data_ptr<int32_t>(), r[0].data_ptr<int32_t>(), r[1].data_ptr<int32_t>(),
+                              r[2].data_ptr<int32_t>(), r[3].data_ptr<int64_t>(), r[4].data_ptr<int32_t>(), rows, r[5].data_ptr<int32_t>(),
+                              c10::hip::getCurrentHIPStream().stream());
+    }
+    return rc != DFA_OK ? PyLong_FromLong(rc) : as_tuple(r);
+    END_HANDLE_TH_ERRORS
+}
+
+// cache_append_packed(k, v, cache, table, lengths, starts) -> True, a negative status, or None
+PyObject* cache_append_packed(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    Packed p;
+    Sequences s;
+    if (nargs != 6 || !g_packed.append) Py_RETURN_NONE;
+    PyObject* const kkv[3] = {args[0], args[0], args[1]};
+    if (!read_packed(kkv, args[5], &p) || !read_sequences(args[2], args[3], args[4], Py_None, p.B, &s) || p.Hkv != s.cache.heads || p.D != s.cache.D) Py_RETURN_NONE;
+    int rc;
+    {
+        pybind11::gil_scoped_release release;
+        rc = g_packed.append(p.t[1]->data_ptr(), p.t[2]->data_ptr(), p.s[1], p.s[2], p.dt, (int32_t)p.T, p.starts->data_ptr<int32_t>(), p.B, s.cache, s.table, s.width,
+                             s.ld_table, s.lengths, c10::hip::getCurrentHIPStream().stream());
+    }
+    if (rc != DFA_OK) return PyLong_FromLong(rc);
+    Py_RETURN_TRUE;
+    END_HANDLE_TH_ERRORS
+}
+
+// bind(addresses in the loaded libdfa.so of dfa_forward_alloc, dfa_backward, Library's functions and PackedLibrary's, in order)
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-    if (nargs != 9) {
-        PyErr_SetString(PyExc_TypeError, "bind takes nine addresses");
+    if (nargs != 17) {
+        PyErr_SetString(PyExc_TypeError, "bind takes seventeen addresses");
         return nullptr;
     }
-    void* at[9];
-    for (int i = 0; i < 9; ++i) at[i] = PyLong_AsVoidPtr(args[i]);
+    void* at[17];
+    for (int i = 0; i < 17; ++i) at[i] = PyLong_AsVoidPtr(args[i]);
     if (PyErr_Occurred()) return nullptr;
     g_forward = reinterpret_cast<ForwardAlloc>(at[0]);
     g_backward = reinterpret_cast<Backward>(at[1]);
@@ -422,6 +623,10 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
                     reinterpret_cast<decltype(Library::linear_backward)>(at[4]), reinterpret_cast<decltype(Library::linear_backward_bytes)>(at[5]),
                     reinterpret_cast<decltype(Library::append)>(at[6]), reinterpret_cast<decltype(Library::attention)>(at[7]),
                     reinterpret_cast<decltype(Library::attention_bytes)>(at[8])};
+    g_packed = PackedLibrary{reinterpret_cast<decltype(PackedLibrary::attention)>(at[9]), reinterpret_cast<decltype(PackedLibrary::attention_backward)>(at[10]),
+                             reinterpret_cast<decltype(PackedLibrary::attention_backward_bytes)>(at[11]), reinterpret_cast<decltype(PackedLibrary::norm)>(at[12]),
+                             reinterpret_cast<decltype(PackedLibrary::norm_backward)>(at[13]), reinterpret_cast<decltype(PackedLibrary::norm_backward_bytes)>(at[14]),
+                             reinterpret_cast<decltype(PackedLibrary::reserve)>(at[15]), reinterpret_cast<decltype(PackedLibrary::append)>(at[16])};
     Py_RETURN_NONE;
 }
 
@@ -435,6 +640,12 @@ PyMethodDef g_methods[] = {
     {"quantized_linear_backward", method(quantized_linear_backward), METH_FASTCALL, nullptr},
     {"cache_append", method(cache_append), METH_FASTCALL, nullptr},
     {"cache_attention", method(cache_attention), METH_FASTCALL, nullptr},
+    {"prompt_attention", method(prompt_attention), METH_FASTCALL, nullptr},
+    {"prompt_attention_backward", method(prompt_attention_backward), METH_FASTCALL, nullptr},
+    {"rms_norm", method(rms_norm), METH_FASTCALL, nullptr},
+    {"rms_norm_backward", method(rms_norm_backward), METH_FASTCALL, nullptr},
+    {"cache_reserve", method(cache_reserve), METH_FASTCALL, nullptr},
+    {"cache_append_packed", method(cache_append_packed), METH_FASTCALL, nullptr},
     {"bind", method(bind), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
