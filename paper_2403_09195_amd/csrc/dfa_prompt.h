@@ -149,6 +149,58 @@ __device__ __forceinline__ bf16x8 prompt_turned(const uint16_t* block, int turne
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+// ---- the same reads and copies from addresses that are worked out once --------------------------------------------------------------
+// Bytes from the start of a block; a block's own offset is the wave's, in a scalar register.
+typedef __attribute__((address_space(3))) char lds_char;
+template <int D, PromptOrder kOrder>
+struct RowReads {
+    uint32_t at[D / 16];
+    __device__ __forceinline__ void begin(uint32_t ring, int lane) {
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) at[kk] = ring + 2u * (uint32_t)(prompt_row_at<D, kOrder>(lane) ^ (16 * kk));
+    }
+    __device__ __forceinline__ bf16x8 operator()(uint32_t block, int kk) const {
+        return *reinterpret_cast<__attribute__((address_space(3))) bf16x8*>(at[kk] + block);
+    }
+};
+template <int D>
+struct ValueReads {
+    uint32_t at[D / 32];
+    __device__ __forceinline__ void begin(uint32_t ring, int lane) {
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) at[db] = ring + 2u * (uint32_t)(prompt_value_at<D>(lane) ^ (32 * db));
+    }
+    __device__ __forceinline__ bf16x8 operator()(uint32_t block, int db, int st) const {
+        lds_char* const from = reinterpret_cast<lds_char*>(at[db] + block);
+        const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) short4v*>(from + 32 * st * D));
+        const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) short4v*>(from + 32 * st * D + 8 * D));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
+// What a lane fetches of whole blocks; others go the way of prompt_copy.
+template <int D, PromptOrder kOrder>
+struct BlockCopies {
+    uint32_t from[kPromptCopies<D>];
+    __device__ __forceinline__ void begin(uint32_t pitch, int wave, int lane) {
+        constexpr int kLanes = D / 8, kRows = 64 / kLanes;
+#pragma unroll
+        for (int u = 0; u < kPromptCopies<D>; ++u) {
+            const int rho = kRows * (kPromptCopies<D> * wave + u) + lane / kLanes;
+            from[u] = (uint32_t)(kOrder == PromptOrder::kValues ? rho : prompt_sigma(rho)) * pitch + 16u * ((uint32_t)(lane % kLanes) ^ prompt_swizzle<D, kOrder>(rho));
+        }
+    }
+    __device__ __forceinline__ void operator()(const char* base, uint32_t pitch, int32_t k0, int32_t rows, int wave, int lane, uint32_t lds_block) const {
+        if (k0 + 32 <= rows) {
+            constexpr int kRows = 512 / D;
+            const void* const src = uniform_ptr(base + (int64_t)k0 * pitch);
+#pragma unroll
+            for (int u = 0; u < kPromptCopies<D>; ++u) copy16_to_lds(src, from[u], lds_block + (uint32_t)(kRows * (kPromptCopies<D> * wave + u) * D * 2));
+        } else {
+            prompt_copy<D, kOrder>(base, pitch, k0, rows, wave, lane, lds_block);
+        }
+    }
+};
+
 // ---- values that are not finite, behind a mask ------------------------------------------------------------------------------------
 // A weight of zero makes NaN of a value that is not finite.  In blocks that some row sees in part such values are taken out of the product and
 // added to the rows that see them.  (Rare, and only the last blocks of a walk are looked at: two pieces of 32 D bytes a lane.)

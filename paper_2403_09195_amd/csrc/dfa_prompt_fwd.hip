@@ -24,7 +24,8 @@ struct Wave {
     bf16x8 q[QB][kSteps];
     floatx16 acc[kHalves][QB];
     float ref[QB], sum[QB];                  // reference exponent; this lane's part of the row sum (the other half of the keys is lane ^ 32's)
-    int row_at, value_at;
+    RowReads<D, PromptOrder::kKeys> key;
+    ValueReads<D> value;
     float c;                                 // scale * log2(e)
 
     __device__ __forceinline__ void begin() {
@@ -37,20 +38,20 @@ struct Wave {
         }
     }
     // S^T of one block on its own
-    __device__ __forceinline__ void scores(const uint16_t* kb, floatx16 (&s)[QB]) const {
+    __device__ __forceinline__ void scores(uint32_t kb, floatx16 (&s)[QB]) const {
 #pragma unroll
         for (int kk = 0; kk < kSteps; ++kk) {
-            const bf16x8 kf = prompt_row<D>(kb, row_at, kk);
+            const bf16x8 kf = key(kb, kk);
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) s[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[qb][kk], kk == 0 ? prompt_zero() : s[qb], 0, 0, 0);
         }
     }
-    __device__ __forceinline__ void accumulate(const uint16_t* vb, const u32x4 (&p)[QB][2]) {
+    __device__ __forceinline__ void accumulate(uint32_t vb, const u32x4 (&p)[QB][2]) {
 #pragma unroll
         for (int db = 0; db < kHalves; ++db)
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
-                const bf16x8 vf = prompt_value<D>(vb, value_at, db, st);
+                const bf16x8 vf = value(vb, db, st);
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb)
                     acc[db][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, p[qb][st]), acc[db][qb], 0, 0, 0);
@@ -58,33 +59,33 @@ struct Wave {
     }
 
     // The same of a block that rows see up to position `last` of it, with values that are not finite in it.
-    __device__ __forceinline__ void accumulate_odd(const uint16_t* vb, const u32x4 (&p)[QB][2], const int32_t (&last)[QB], int lane) {
+    __device__ __forceinline__ void accumulate_odd(uint32_t vb, const uint16_t* block, const u32x4 (&p)[QB][2], const int32_t (&last)[QB], int lane) {
 #pragma unroll
         for (int db = 0; db < kHalves; ++db) {
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
-                const bf16x8 vf = without_odd(prompt_value<D>(vb, value_at, db, st));
+                const bf16x8 vf = without_odd(value(vb, db, st));
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb)
                     acc[db][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, p[qb][st]), acc[db][qb], 0, 0, 0);
             }
 #pragma unroll
-            for (int qb = 0; qb < QB; ++qb) add_odd<D>(vb, last[qb], lane, acc[db][qb], db);
+            for (int qb = 0; qb < QB; ++qb) add_odd<D>(block, last[qb], lane, acc[db][qb], db);
         }
     }
 
     // One beat: scores of the next block (K at kb -> s_next), p_prev times the previous block's values (vb), numerators of s (-> p).  The
     // numerators are added up before they are rounded: lse is exact to fp32.
     template <bool kScores, bool kAccumulate>
-    __device__ __forceinline__ void beat(const uint16_t* kb, const uint16_t* vb, const floatx16 (&s)[QB], floatx16 (&s_next)[QB], const u32x4 (&p_prev)[QB][2],
+    __device__ __forceinline__ void beat(uint32_t kb, uint32_t vb, const floatx16 (&s)[QB], floatx16 (&s_next)[QB], const u32x4 (&p_prev)[QB][2],
                                          u32x4 (&p)[QB][2], float (&psum)[QB]) {
         constexpr int kProducts = 2 * QB * kSteps, kSlots = 8 * QB, kPer = kProducts / kSlots;
         constexpr int kAhead = QB == 2 ? 1 : 2, kBuffers = kAhead + 1;              // fragments are read this many groups ahead
         bf16x8 kf[kBuffers], vf[kBuffers];
         float t[kSlots][2], a[QB][2];
         auto load = [&](int r) {
-            if (kScores) kf[r % kBuffers] = prompt_row<D>(kb, row_at, r);
-            if (kAccumulate) vf[r % kBuffers] = prompt_value<D>(vb, value_at, r >> 1, r & 1);
+            if (kScores) kf[r % kBuffers] = key(kb, r);
+            if (kAccumulate) vf[r % kBuffers] = value(vb, r >> 1, r & 1);
         };
         auto product = [&](int k) {          // group r = k / (2 QB): scores of d-step r, then the accumulation of (32 d, 16 keys) number r
             const int r = k / (2 * QB), w = k % (2 * QB);
@@ -159,15 +160,15 @@ struct Wave {
     }
 };
 
-// kPer: 32-key blocks of a stage; kStages stages in LDS.
-template <int D, int QB, int kPer, int kStages, int kEu>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu))) void prompt_fwd_kernel(const PromptParams p, int32_t slots) {
-    constexpr int R = 128 * QB, kBlock = 32 * D, kStage = kPer * kBlock;            // elements
-    constexpr int kCopies = 2 * kPer * kPromptCopies<D>;                             // of a wave and stage
-    // the walk is in the stages of three blocks at once (accumulation, numerators, scores); the others are on their way
-    constexpr int kAhead = kStages - (kPer == 1 ? 3 : 2);
-    static_assert(kAhead >= 1, "a stage is filled while the walk is in others");
-    __shared__ __attribute__((aligned(1024))) uint16_t lds[kStages][2][kStage];      // keys, values
+// Blocks in LDS: keys of four; values of as many as lie between where the tile's first wave ends and where its last one does, two pairs at least.
+constexpr int kRing = 4;
+template <int QB> constexpr int kValueRing = 4 * QB;
+
+template <int D, int QB>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_fwd_kernel(const PromptParams p, int32_t slots) {
+    constexpr int R = 128 * QB, kBlock = 32 * D;                                     // rows; elements of a block
+    constexpr int kCopies = 2 * kPromptCopies<D>;                                    // a wave's, of a block's keys and values
+    __shared__ __attribute__((aligned(1024))) uint16_t lds[kRing + kValueRing<QB>][kBlock];
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, g = lane >> 5;
     int32_t slot, h;
@@ -194,15 +195,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
     const char* const kbase = reinterpret_cast<const char*>(static_cast<const uint16_t*>(p.k) + tile.first * p.skn + (h / p.group) * p.skh);
     const char* const vbase = reinterpret_cast<const char*>(static_cast<const uint16_t*>(p.v) + tile.first * p.svn + (h / p.group) * p.svh);
     const uint32_t kpitch = (uint32_t)(p.skn * 2), vpitch = (uint32_t)(p.svn * 2);
-    const uint32_t lds_addr = (uint32_t)(uintptr_t)DFA_LDS_PTR(void, &lds[0][0][0]);
-    const int32_t n_stages = 2 * n_steps / kPer;
-    auto issue = [&](int32_t stage, int at) {
-        const uint32_t to = lds_addr + (uint32_t)(at * 2 * kStage * 2);
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            prompt_copy<D, PromptOrder::kKeys>(kbase, kpitch, 32 * (stage * kPer + i), keys, wave, lane, to + (uint32_t)(i * kBlock * 2));
-            prompt_copy<D, PromptOrder::kValues>(vbase, vpitch, 32 * (stage * kPer + i), keys, wave, lane, to + (uint32_t)((kStage + i * kBlock) * 2));
-        }
+    const uint32_t lds_addr = (uint32_t)(uintptr_t)DFA_LDS_PTR(void, &lds[0][0]);
+    constexpr uint32_t kBytes = kBlock * 2, kValuesAt = kRing * kBytes;
+    auto key_slot = [](int32_t n) { return (uint32_t)(n & (kRing - 1)) * kBytes; };
+    auto value_slot = [](int32_t n) { return (uint32_t)(n & (kValueRing<QB> - 1)) * kBytes; };
+    BlockCopies<D, PromptOrder::kKeys> key_copies;
+    BlockCopies<D, PromptOrder::kValues> value_copies;
+    key_copies.begin(kpitch, wave, lane);
+    value_copies.begin(vpitch, wave, lane);
+    const int32_t n_blocks = 2 * n_steps;
+    auto issue_keys = [&](int32_t n) {
+        if (n < n_blocks) key_copies(kbase, kpitch, 32 * n, keys, wave, lane, lds_addr + key_slot(n));
+    };
+    auto issue_values = [&](int32_t n) {
+        if (n < n_blocks) value_copies(vbase, vpitch, 32 * n, keys, wave, lane, lds_addr + kValuesAt + value_slot(n));
     };
 
     Wave<D, QB> w;
@@ -215,20 +221,23 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
             for (int kk = 0; kk < D / 16; ++kk) w.q[qb][kk] = *reinterpret_cast<const bf16x8*>(q + row * p.sqn + 16 * kk + 8 * g);
         }
     }
-#pragma unroll
-    for (int s = 0; s <= kAhead; ++s)
-        if (s < n_stages) issue(s, s);
+    issue_keys(0);
+    issue_keys(1);
+    issue_values(0);
     // (waited for here, with what was issued after it: the compiler then places no wait of its own for them in the loop)
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) asm volatile("" : "+v"(w.q[qb][kk]));
     wait_vmcnt<0>();
+    issue_keys(2);
+    issue_values(1);
+    issue_keys(3);
     __syncthreads();
 
     w.c = uniform_float(p.scale * kLog2e);
-    w.row_at = prompt_row_at<D, PromptOrder::kKeys>(lane);
-    w.value_at = prompt_value_at<D>(lane);
+    w.key.begin(lds_addr, lane);
+    w.value.begin(lds_addr + kValuesAt, lane);
     w.begin();
 
     // scores that a row does not see, of the block from key k0 on
@@ -242,54 +251,53 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
                 if (prompt_position(v, g) > last) s[qb][v] = -INFINITY;
         }
     };
-    // block n's keys and values in LDS
-    auto at = [&](int32_t n, int tensor) { return &lds[(n / kPer) % kStages][tensor][(n % kPer) * kBlock]; };
-    // Block n is scored next: its stage has landed once at most the stages behind it, up to kAhead - 1 of them, are under way.  Every wave is
-    // done with block n - 2's numerators and block n - 3's accumulation then, so the stage before those can be filled.
+    // Before beat n - 1, which scores block n and accumulates block n - 2: they have landed once at most what the two calls before this one
+    // issued is under way, and everyone is done with the keys of block n - 1 and the values of block n - 3, whose places are filled.
     auto enter = [&](int32_t n) {
-        const int32_t s = n / kPer;
-        if (s > kAhead && s < n_stages) {
-            if (s + kAhead - 1 < n_stages) wait_vmcnt<(kAhead - 1) * kCopies>();
+        if (n > 1) {
+            if (n + 2 < n_blocks) wait_vmcnt<2 * kCopies>();
             else wait_vmcnt<0>();
         }
         __syncthreads();
-        if (s + kAhead < n_stages) issue(s + kAhead, (s + kAhead) % kStages);
+        issue_keys(n + 3);
+        issue_values(n + 1);
     };
 
     floatx16 s_a[QB], s_b[QB];
     u32x4 p_a[QB][2], p_b[QB][2];
     float psum[QB];
-    bool odd = false;                        // values that are not finite in the wave's last two blocks
-    if (live) w.scores(at(0, 0), s_a);
-    if (kPer == 1) enter(1);
+    bool odd = false;                        // values that are not finite in the wave's last two blocks: a mask reaches no further back
+    if (live) w.scores(0, s_a);
+    enter(1);
     if (live) {
         mask(s_a, 0);
-        w.template beat<true, false>(at(1, 0), at(0, 1), s_a, s_b, p_b, p_a, psum);
+        w.template beat<true, false>(key_slot(1), 0, s_a, s_b, p_b, p_a, psum);
         w.settle(s_a, p_a, psum);
     }
-    // trip s: beat 2 s + 1 (scores of block 2 s + 2, accumulation of 2 s) and beat 2 s + 2
-    for (int32_t s = 0; s < n_steps; ++s) {
-        const bool more = live && s + 1 < my_steps, ends = live && s + 1 == my_steps;
+    // trip s: beat 2 s + 1 (scores of block 2 s + 2, accumulation of 2 s) and beat 2 s + 2.  A wave whose rows see no more goes along with the copies; its
+    // last two blocks' values are still there at the end.
+    for (int32_t s = 0; s + 1 < n_steps; ++s) {
+        const bool more = live && s + 1 < my_steps;
         enter(2 * s + 2);
         if (more) {
-            mask(s_b, 64 * s + 32);
-            w.template beat<true, true>(at(2 * s + 2, 0), at(2 * s, 1), s_b, s_a, p_a, p_b, psum);
+            w.template beat<true, true>(key_slot(2 * s + 2), value_slot(2 * s), s_b, s_a, p_a, p_b, psum);
             w.settle(s_b, p_b, psum);
         }
-        if (ends) {
-            // (a mask reaches no further back than these two blocks)
-            mask(s_b, 64 * s + 32);
-            odd = prompt_odd_values<D>(at(2 * s, 1)) || prompt_odd_values<D>(at(2 * s + 1, 1));
-            w.template beat<false, true>(at(2 * s, 0), at(2 * s, 1), s_b, s_a, p_a, p_b, psum);
-            w.settle(s_b, p_b, psum);
-            w.accumulate(at(2 * s + 1, 1), p_b);
-        }
-        if (kPer == 1) enter(2 * s + 3);
+        enter(2 * s + 3);
         if (more) {
             mask(s_a, 64 * s + 64);
-            w.template beat<true, true>(at(2 * s + 3, 0), at(2 * s + 1, 1), s_a, s_b, p_b, p_a, psum);
+            w.template beat<true, true>(key_slot(2 * s + 3), value_slot(2 * s + 1), s_a, s_b, p_b, p_a, psum);
             w.settle(s_a, p_a, psum);
         }
+    }
+    enter(n_blocks);
+    if (live) {
+        const int32_t last = 2 * my_steps - 1;
+        mask(s_b, 32 * last);
+        odd = prompt_odd_values<D>(lds[kRing + ((last - 1) & (kValueRing<QB> - 1))]) || prompt_odd_values<D>(lds[kRing + (last & (kValueRing<QB> - 1))]);
+        w.template beat<false, true>(0, value_slot(last - 1), s_b, s_a, p_a, p_b, psum);
+        w.settle(s_b, p_b, psum);
+        w.accumulate(value_slot(last), p_b);
     }
 
     // rows leave through LDS, each wave's through a piece of its own: whole lines
@@ -298,7 +306,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
     const int je = lane_e & 31, ge = lane_e >> 5;
     __syncthreads();
     constexpr int kPitch = 2 * D + 16;
-    static_assert(sizeof(lds) >= 4 * 32 * QB * kPitch + 16, "every wave's rows fit the stages, and four flags");
+    static_assert(sizeof(lds) >= 4 * 32 * kPitch + 16, "32 rows of every wave fit, and four flags");
     // Some row of the tile may not see such a value: the walk is done again, block after block, with them taken out of the products.  (In place, in
     // the wave's last two beats, this would cost the loop its registers: 111 to 142 of D = 64 are spilled then.)
     int32_t* const flags = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(lds) + sizeof(lds)) - 4;
@@ -309,51 +317,41 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
         for (int32_t n = 0; n < 2 * n_steps; ++n) {
             __syncthreads();                 // the flags, and block n - 1, have been read
             prompt_copy<D, PromptOrder::kKeys>(kbase, kpitch, 32 * n, keys, wave, lane_e, lds_addr);
-            prompt_copy<D, PromptOrder::kValues>(vbase, vpitch, 32 * n, keys, wave, lane_e, lds_addr + kStage * 2);
+            prompt_copy<D, PromptOrder::kValues>(vbase, vpitch, 32 * n, keys, wave, lane_e, lds_addr + kValuesAt);
             wait_vmcnt<0>();
             __syncthreads();
             if (!live || n >= 2 * my_steps) continue;
-            w.scores(lds[0][0], s_a);
+            w.scores(0, s_a);
             mask(s_a, 32 * n);
-            w.template beat<false, false>(lds[0][0], lds[0][1], s_a, s_b, p_b, p_a, psum);
+            w.template beat<false, false>(0, 0, s_a, s_b, p_b, p_a, psum);
             w.settle(s_a, p_a, psum);
             int32_t last[QB];
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) last[qb] = min(p.causal ? my0 + 32 * qb + je : keys - 1, keys - 1) - 32 * n;
-            w.accumulate_odd(lds[0][1], p_a, last, lane_e);
+            w.accumulate_odd(0, lds[kRing], p_a, last, lane_e);
         }
         __syncthreads();
     }
     if (!live) return;
-    char* const mine = reinterpret_cast<char*>(&lds[0][0][0]) + wave * (32 * QB * kPitch);
+    char* const mine = reinterpret_cast<char*>(lds) + wave * (32 * kPitch);
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
         const float total = wave_half_sum(w.sum[qb]);
         const float inv = total == 0.f ? 0.f : 1.0f / total;
-        const int r = 32 * QB * wave + 32 * qb + je;
-        if (lse && ge == 0 && r < rows) lse[r] = total == 0.f ? -INFINITY : (w.ref[qb] + __builtin_amdgcn_logf(total)) * kLn2;
+        const int r0 = 32 * QB * wave + 32 * qb;
+        if (lse && ge == 0 && r0 + je < rows) lse[r0 + je] = total == 0.f ? -INFINITY : (w.ref[qb] + __builtin_amdgcn_logf(total)) * kLn2;
+        floatx16 acc[D / 32];
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const bf16x4 o = {(__bf16)(w.acc[db][qb][4 * v] * inv), (__bf16)(w.acc[db][qb][4 * v + 1] * inv), (__bf16)(w.acc[db][qb][4 * v + 2] * inv),
-                                  (__bf16)(w.acc[db][qb][4 * v + 3] * inv)};
-                *reinterpret_cast<bf16x4*>(mine + (32 * qb + je) * kPitch + (32 * db + 8 * v + 4 * ge) * 2) = o;
-            }
-    }
-    constexpr int kLanes = D / 8, kRowsAtOnce = 64 / kLanes;
-#pragma unroll
-    for (int i = 0; i < 32 * QB / kRowsAtOnce; ++i) {
-        const int r = kRowsAtOnce * i + lane_e / kLanes, ch = lane_e % kLanes, row = 32 * QB * wave + r;
-        const u32x4 x = *reinterpret_cast<const u32x4*>(mine + r * kPitch + 16 * ch);
-        if (row < rows) *reinterpret_cast<u32x4*>(out + (int64_t)row * p.H * D + 8 * ch) = x;
+        for (int db = 0; db < D / 32; ++db) acc[db] = w.acc[db][qb];
+        // (the wave's LDS accesses are in order: the next rows are written when these have been read)
+        store_rows<D>(acc, inv, mine, out + (int64_t)r0 * p.H * D, (int64_t)p.H * D, rows - r0, lane_e);
     }
 }
 
-template <int D, int QB, int kPer, int kStages, int kEu>
+template <int D, int QB>
 hipError_t launch(const PromptParams& p, hipStream_t st) {
     const int64_t slots = prompt_slots(p.T, p.B, 128 * QB);
-    hipLaunchKernelGGL((prompt_fwd_kernel<D, QB, kPer, kStages, kEu>), dim3((unsigned)(slots * p.H)), dim3(256), 0, st, p, (int32_t)slots);
+    hipLaunchKernelGGL((prompt_fwd_kernel<D, QB>), dim3((unsigned)(slots * p.H)), dim3(256), 0, st, p, (int32_t)slots);
     return hipGetLastError();
 }
 
@@ -361,7 +359,7 @@ hipError_t launch(const PromptParams& p, hipStream_t st) {
 
 hipError_t launch_prompt_fwd(const PromptParams& p, bool f32, int32_t D, const ChipShape&, hipStream_t st) {
     if (f32) return launch_prompt_fwd_f32(p, D, st);
-    return D == 64 ? launch<64, 2, 2, 4, 2>(p, st) : launch<128, 1, 1, 5, 2>(p, st);
+    return D == 64 ? launch<64, 2>(p, st) : launch<128, 1>(p, st);
 }
 
 }  // namespace dfa
