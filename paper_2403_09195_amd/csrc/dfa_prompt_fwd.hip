@@ -80,6 +80,7 @@ struct Wave {
     __device__ __forceinline__ void beat(uint32_t kb, uint32_t vb, const floatx16 (&s)[QB], floatx16 (&s_next)[QB], const u32x4 (&p_prev)[QB][2],
                                          u32x4 (&p)[QB][2], float (&psum)[QB]) {
         constexpr int kProducts = 2 * QB * kSteps, kSlots = 8 * QB, kPer = kProducts / kSlots;
+        static_assert(kPer == 1 || kPer == 2, "a product for every half of a slot, or for every slot");
         constexpr int kAhead = QB == 2 ? 1 : 2, kBuffers = kAhead + 1;              // fragments are read this many groups ahead
         bf16x8 kf[kBuffers], vf[kBuffers];
         float t[kSlots][2], a[QB][2];
@@ -99,28 +100,36 @@ struct Wave {
         };
 #pragma unroll
         for (int r = 0; r < kAhead; ++r) load(r);
-#pragma unroll
-        for (int m = 0; m < kSlots + 2; ++m) {
-            if (m >= 2)
-#pragma unroll
-                for (int i = 0; i < kPer; ++i) product(kPer * (m - 2) + i);
+        // Pair m's exponents in slot m, its exponentials in slot m + 1, its sum and its rounding in slot m + 2, a half of each behind a product.  (The
+        // empty asm statements hold results in their slots: the compiler would move them behind the last product.)
+        auto first_half = [&](int m) {
             if (m < kSlots) {
                 const int qb = m >> 3, v = 2 * (m & 7);
                 t[m][0] = fmaf(s[qb][v], c, -ref[qb]);
                 t[m][1] = fmaf(s[qb][v + 1], c, -ref[qb]);
             }
-            if (m >= 1 && m <= kSlots) {
-                t[m - 1][0] = __builtin_amdgcn_exp2f(t[m - 1][0]);
-                t[m - 1][1] = __builtin_amdgcn_exp2f(t[m - 1][1]);
-            }
+            if (m >= 1 && m <= kSlots) t[m - 1][0] = __builtin_amdgcn_exp2f(t[m - 1][0]);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto second_half = [&](int m) {
+            if (m >= 1 && m <= kSlots) t[m - 1][1] = __builtin_amdgcn_exp2f(t[m - 1][1]);
             if (m >= 2) {
                 const int i = m - 2, qb = i >> 3, pr = i & 7;
                 const bf16x2 w = {(__bf16)t[i][0], (__bf16)t[i][1]};
-                p[qb][pr >> 2][pr & 3] = __builtin_bit_cast(uint32_t, w);
+                uint32_t bits = __builtin_bit_cast(uint32_t, w);
                 a[qb][0] = pr == 0 ? t[i][0] : a[qb][0] + t[i][0];
                 a[qb][1] = pr == 0 ? t[i][1] : a[qb][1] + t[i][1];
+                asm volatile("" : "+v"(bits), "+v"(a[qb][0]), "+v"(a[qb][1]));
+                p[qb][pr >> 2][pr & 3] = bits;
             }
             __builtin_amdgcn_sched_barrier(0);
+        };
+#pragma unroll
+        for (int m = 0; m < kSlots + 2; ++m) {
+            if (m >= 2) product(kPer * (m - 2));
+            first_half(m);
+            if (m >= 2 && kPer == 2) product(kPer * (m - 2) + 1);
+            second_half(m);
         }
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) psum[qb] = a[qb][0] + a[qb][1];
