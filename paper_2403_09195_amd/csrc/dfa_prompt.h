@@ -21,7 +21,7 @@ struct PromptParams {
     // backward
     const void* dout;                       // [T, H, D] contiguous
     void *dq, *dk, *dv;                     // [T, H, D], [T, Hkv, D], contiguous
-    float *ndelta, *lse2;                   // [H, T] workspace: -(dout . out) and lse * log2(e) of every row
+    float *ndelta, *lse2;                   // [H, T] workspace: -(dout . out) of every row, and lse * log2(e) (bf16: -lse / scale)
     float* parts;                           // [shares][2][T][Hkv][D] workspace: dk and dv of a share of the group's heads
     int32_t shares;
 };
@@ -174,6 +174,24 @@ struct ValueReads {
         lds_char* const from = reinterpret_cast<lds_char*>(at[db] + block);
         const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) short4v*>(from + 32 * st * D));
         const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) short4v*>(from + 32 * st * D + 8 * D));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
+template <int D>
+struct TurnedReads {
+    uint32_t at[D / 32], further[D / 32];
+    __device__ __forceinline__ void begin(uint32_t ring, int lane) {
+        constexpr int kEight = 8 * (D == 128 ? 2 : 1);
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) {
+            const int lo = prompt_turned_at<D>(lane) ^ (32 * db);
+            at[db] = ring + 2u * (uint32_t)lo;
+            further[db] = ring + 2u * (uint32_t)((lo ^ kEight) + 8 * D);
+        }
+    }
+    __device__ __forceinline__ bf16x8 operator()(uint32_t block, int db, int st) const {
+        const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) short4v*>(reinterpret_cast<lds_char*>(at[db] + block) + 32 * st * D));
+        const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) short4v*>(reinterpret_cast<lds_char*>(further[db] + block) + 32 * st * D));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };

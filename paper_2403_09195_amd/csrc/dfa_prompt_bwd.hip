@@ -84,7 +84,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         lse2[qb] = l == -INFINITY ? INFINITY : l * kLog2e;       // a row without weights has none here either
         if (g == 0 && r < rows) {
             p.ndelta[(int64_t)h * p.T + row0 + r] = nd[qb];
-            p.lse2[(int64_t)h * p.T + row0 + r] = lse2[qb];
+            p.lse2[(int64_t)h * p.T + row0 + r] = l == -INFINITY ? -INFINITY : -l / p.scale;         // what the other launch's scores start from
         }
     }
 #pragma unroll
@@ -159,14 +159,91 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     }
 }
 
-// dk and dv: 128 keys of one key head, 32 to a wave, walked along the rows of its query heads (of a share of them).  Per block S = Q K^T,
-// dP - delta = dO V^T started from -delta, dV^T += dO^T P, dK^T += Q^T dS.
+// A wave of the launch of dk and dv: 32 keys, their dk and dv, and one beat of its walk along the rows.
+template <int D>
+struct KeyWave {
+    static constexpr int kSteps = D / 16, kHalves = D / 32;
+    bf16x8 k[kSteps], v[kSteps];
+    floatx16 dk[kHalves], dv[kHalves];
+    RowReads<D, PromptOrder::kBoth> row;     // of a block's q; its dout lies kTensor behind
+    TurnedReads<D> turned;
+    float c;                                 // scale * log2(e)
+    static constexpr uint32_t kTensor = 64 * D;                      // bytes of a block
+    bf16x8 f[2][4];                          // fragments of a group of products: q, dout (rows), dout, q (transposed)
+
+    // Register e of a lane's first product, for 16 numbers of a block's rows in LDS
+    __device__ __forceinline__ static void start(const float* numbers, int g, floatx16& x) {
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            const float4 a = *reinterpret_cast<const float4*>(numbers + 16 * (e >> 3) + 8 * g + (e & 7));
+            x[e] = a.x, x[e + 1] = a.y, x[e + 2] = a.z, x[e + 3] = a.w;
+        }
+    }
+    // Group r: first products with the rows at `next`, second ones with the rows at `prev`.
+    template <bool kFirst, bool kSecond>
+    __device__ __forceinline__ void load(int r, uint32_t next, uint32_t prev) {
+        if (kFirst) f[r & 1][0] = row(next, r), f[r & 1][1] = row(next + kTensor, r);
+        if (kSecond) f[r & 1][2] = turned(prev + kTensor, r >> 1, r & 1), f[r & 1][3] = turned(prev, r >> 1, r & 1);
+    }
+
+    // kFirst products: S and dP of the next block (rows at `next`, starting from s_next and dp_next); P and dS of s and dp -> pp and dd; kSecond products: dV and dK
+    // of the block before (at `prev`), with pp_prev and dd_prev.  Vector instructions stand between the products, one number of a lane after the other: its
+    // exponent, its exponential and its product with dP, each pair's rounding.  A wave has its SIMD to itself, so whatever it waited for would stand still: the first
+    // fragments are read before a beat begins, and those of the beat behind this one (next2, prev2) and what its scores start from (`begin`) within this one.
+    template <bool kFirst, bool kSecond>
+    __device__ __forceinline__ void beat(uint32_t next, uint32_t prev, uint32_t next2, uint32_t prev2, const float* begin, int g, floatx16& s, floatx16& dp, floatx16& s_next,
+                                         floatx16& dp_next, const u32x4 (&pp_prev)[2], const u32x4 (&dd_prev)[2], u32x4 (&pp)[2], u32x4 (&dd)[2]) {
+        constexpr int kGroups = kSteps, kProducts = 4 * kGroups;
+        float t[16], ds[16];
+        auto product = [&](int i) {
+            const int r = i >> 2;
+            if ((i & 3) == 0) {
+                if (r + 1 < kGroups) load<kFirst, kSecond>(r + 1, next, prev);
+                else load<true, true>(0, next2, prev2);
+            }
+            switch (i & 3) {
+                case 0: if (kFirst) s_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[r & 1][0], k[r], s_next, 0, 0, 0); break;
+                case 1: if (kSecond) dv[r >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[r & 1][2], __builtin_bit_cast(bf16x8, pp_prev[r & 1]), dv[r >> 1], 0, 0, 0); break;
+                case 2: if (kSecond) dk[r >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[r & 1][3], __builtin_bit_cast(bf16x8, dd_prev[r & 1]), dk[r >> 1], 0, 0, 0); break;
+                default: if (kFirst) dp_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[r & 1][1], v[r], dp_next, 0, 0, 0);
+            }
+        };
+#pragma unroll
+        for (int m = 0; m < 18; ++m) {
+#pragma unroll
+            for (int i = kProducts * m / 18; i < kProducts * (m + 1) / 18; ++i) {
+                product(i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (m < 8) t[2 * m] = s[2 * m] * c, t[2 * m + 1] = s[2 * m + 1] * c;
+            if (m >= 1 && m <= 16) t[m - 1] = __builtin_amdgcn_exp2f(t[m - 1]);
+            if (m >= 2) {
+                const int i = m - 2;
+                ds[i] = t[i] * dp[i];
+                if (i & 1) {
+                    const bf16x2 a = {(__bf16)t[i - 1], (__bf16)t[i]}, b = {(__bf16)ds[i - 1], (__bf16)ds[i]};
+                    uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
+                    asm volatile("" : "+v"(x), "+v"(y));             // (rounded here, not behind the last product)
+                    pp[i >> 3][(i >> 1) & 3] = x;
+                    dd[i >> 3][(i >> 1) & 3] = y;
+                }
+            }
+            if (m == 10) start(begin, g, s);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        start(begin + 32, g, dp);
+    }
+};
+
+// dk and dv: 128 keys of one key head, 32 to a wave, walked along the rows of its query heads (of a share of them).  Per block S = Q K^T and
+// dP = dO V^T, started from -lse / scale and -delta, dV^T += dO^T P, dK^T += Q^T dS.
 template <int D, int kEu>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu))) void prompt_dkdv_kernel(const PromptParams p, int32_t slots) {
-    constexpr int R = 128, kBlock = 32 * D, kSteps = D / 16, kHalves = D / 32;
-    constexpr int kStages = 4, kAhead = kStages - 1, kCopies = 2 * kPromptCopies<D> + 1;
+    constexpr int R = 128, kBlock = 32 * D, kHalves = D / 32;
+    // the walk is in five blocks between two barriers: second products, numbers, first products, and what is read ahead
+    constexpr int kStages = 8, kCopies = 2 * kPromptCopies<D> + 1;
     __shared__ __attribute__((aligned(1024))) uint16_t lds[kStages][2][kBlock];      // q, dout
-    __shared__ __attribute__((aligned(256))) float scalars[kStages][2][32];          // lse2, -delta
+    __shared__ __attribute__((aligned(256))) float scalars[kStages][2][32];          // -lse / scale, -delta
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, g = lane >> 5;
     int32_t slot, unit;
@@ -197,93 +274,114 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
 
     const uint32_t lds_addr = (uint32_t)(uintptr_t)DFA_LDS_PTR(void, &lds[0][0][0]), sc_addr = (uint32_t)(uintptr_t)DFA_LDS_PTR(void, &scalars[0][0][0]);
     const uint32_t qpitch = (uint32_t)(p.sqn * 2), gpitch = (uint32_t)((int64_t)p.H * D * 2);
+    constexpr uint32_t kStageBytes = 2 * kBlock * 2;
+    auto stage_of = [](int32_t n) { return (uint32_t)(n & (kStages - 1)) * kStageBytes; };
+    BlockCopies<D, PromptOrder::kBoth> q_copies, g_copies;
+    q_copies.begin(qpitch, wave, lane);
+    g_copies.begin(gpitch, wave, lane);
     int32_t ih = h0, ib = first_block;                                                // the next block to be issued
     auto issue = [&](int32_t n) {
-        const uint32_t at = (uint32_t)(n % kStages);
+        if (n >= n_blocks) return;
         const char* const qb = reinterpret_cast<const char*>(static_cast<const uint16_t*>(p.q) + tile.first * p.sqn + ih * p.sqh);
         const char* const gb = reinterpret_cast<const char*>(static_cast<const uint16_t*>(p.dout) + ((int64_t)tile.first * p.H + ih) * D);
-        prompt_copy<D, PromptOrder::kBoth>(qb, qpitch, 32 * ib, tile.n, wave, lane, lds_addr + at * (2 * kBlock * 2));
-        prompt_copy<D, PromptOrder::kBoth>(gb, gpitch, 32 * ib, tile.n, wave, lane, lds_addr + at * (2 * kBlock * 2) + kBlock * 2);
+        q_copies(qb, qpitch, 32 * ib, tile.n, wave, lane, lds_addr + stage_of(n));
+        g_copies(gb, gpitch, 32 * ib, tile.n, wave, lane, lds_addr + stage_of(n) + kBlock * 2);
         // (every wave fetches the same 64 numbers)
         const int64_t r = (int64_t)ih * p.T + tile.first + min(32 * ib + (lane & 31), tile.n - 1);
-        copy4_to_lds((lane < 32 ? p.lse2 : p.ndelta) + r, sc_addr + at * 256u);
+        copy4_to_lds((lane < 32 ? p.lse2 : p.ndelta) + r, sc_addr + (uint32_t)(n & (kStages - 1)) * 256u);
         if (++ib == first_block + per_head) ib = first_block, ++ih;
     };
 
-    bf16x8 kf[kSteps], vf[kSteps];
+    KeyWave<D> w;
     {
         const int64_t row = row0 + min(32 * wave + j, rows - 1);
         const uint16_t* const kp = static_cast<const uint16_t*>(p.k) + row * p.skn + hk * p.skh;
         const uint16_t* const vp = static_cast<const uint16_t*>(p.v) + row * p.svn + hk * p.svh;
 #pragma unroll
-        for (int kk = 0; kk < kSteps; ++kk) {
-            kf[kk] = *reinterpret_cast<const bf16x8*>(kp + 16 * kk + 8 * g);
-            vf[kk] = *reinterpret_cast<const bf16x8*>(vp + 16 * kk + 8 * g);
+        for (int kk = 0; kk < D / 16; ++kk) {
+            w.k[kk] = *reinterpret_cast<const bf16x8*>(kp + 16 * kk + 8 * g);
+            w.v[kk] = *reinterpret_cast<const bf16x8*>(vp + 16 * kk + 8 * g);
         }
     }
 #pragma unroll
-    for (int s = 0; s < kAhead; ++s)
-        if (s < n_blocks) issue(s);
+    for (int n = 0; n < 5; ++n) issue(n);
 #pragma unroll
-    for (int kk = 0; kk < kSteps; ++kk) asm volatile("" : "+v"(kf[kk]), "+v"(vf[kk]));
-    const float c = uniform_float(p.scale * kLog2e);
-    const int row_at = prompt_row_at<D, PromptOrder::kBoth>(lane), turned = prompt_turned_at<D>(lane);
-    floatx16 dka[kHalves], dva[kHalves];
+    for (int kk = 0; kk < D / 16; ++kk) asm volatile("" : "+v"(w.k[kk]), "+v"(w.v[kk]));
+    wait_vmcnt<0>();
+    issue(5);
+    __syncthreads();
+    w.c = uniform_float(p.scale * kLog2e);
+    w.row.begin(lds_addr, lane);
+    w.turned.begin(lds_addr, lane);
 #pragma unroll
-    for (int db = 0; db < kHalves; ++db) dka[db] = dva[db] = prompt_zero();
+    for (int db = 0; db < kHalves; ++db) w.dk[db] = w.dv[db] = prompt_zero();
 
-    int32_t b = first_block;
-    for (int32_t n = 0; n < n_blocks; ++n) {
-        if (n == 0 || n + kAhead > n_blocks) wait_vmcnt<0>();
-        else wait_vmcnt<(kAhead - 1) * kCopies>();
+    // Before beats n and n + 1, whose products are of blocks n - 1 to n + 2 and which read ahead of block n + 3: it has landed once at most the copies of
+    // the block behind it are under way, and everyone is done with block n - 2, so that n + 6 can take its place.
+    auto enter = [&](int32_t n) {
+        if (n > 1) {
+            if (n + 4 < n_blocks) wait_vmcnt<kCopies>();
+            else wait_vmcnt<0>();
+        }
         __syncthreads();
-        if (n + kAhead < n_blocks) issue(n + kAhead);
-        const int32_t i0 = 32 * b;                                                    // the block's first row
+        issue(n + 5);
+        issue(n + 6);
+    };
+    // rows of block n (number b of its head) that do not see the lane's key
+    int32_t b = first_block;
+    auto mask = [&](floatx16& s) {
+        const int32_t i0 = 32 * b;
         if (++b == first_block + per_head) b = first_block;
-        if (!live || (p.causal && i0 + 31 < my0)) continue;
-        const uint16_t *const qb = lds[n % kStages][0], *const gb = lds[n % kStages][1];
-        const float *const l2 = scalars[n % kStages][0] + 8 * g, *const nd = scalars[n % kStages][1] + 8 * g;
-        floatx16 s, dp;
+        if (i0 + 32 <= tile.n && (!p.causal || i0 >= my0 + 31)) return;
+        const int32_t from = p.causal ? my0 + j - i0 : 0, to = tile.n - i0;
 #pragma unroll
-        for (int v = 0; v < 16; v += 4) {
-            const float4 x = *reinterpret_cast<const float4*>(nd + 16 * (v >> 3) + (v & 7));
-            dp[v] = x.x, dp[v + 1] = x.y, dp[v + 2] = x.z, dp[v + 3] = x.w;
+        for (int e = 0; e < 16; ++e)
+            if (prompt_position(e, g) < from || prompt_position(e, g) >= to) s[e] = -INFINITY;
+    };
+
+    floatx16 s_a, s_b, dp_a, dp_b;
+    u32x4 pp_a[2], pp_b[2], dd_a[2], dd_b[2];
+    auto begin = [&](int32_t n) { return &scalars[n & (kStages - 1)][0][0]; };
+    if (live) {
+        w.start(begin(0), g, s_a);
+        w.start(begin(0) + 32, g, dp_a);
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+            s_a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w.row(0, kk), w.k[kk], s_a, 0, 0, 0);
+            dp_a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w.row(w.kTensor, kk), w.v[kk], dp_a, 0, 0, 0);
         }
-#pragma unroll
-        for (int kk = 0; kk < kSteps; ++kk) {
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(prompt_row<D>(qb, row_at, kk), kf[kk], kk == 0 ? prompt_zero() : s, 0, 0, 0);
-            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(prompt_row<D>(gb, row_at, kk), vf[kk], dp, 0, 0, 0);
+        w.start(begin(1), g, s_b);
+        w.start(begin(1) + 32, g, dp_b);
+        w.template load<true, false>(0, stage_of(1), 0);
+        mask(s_a);
+        w.template beat<true, false>(stage_of(1), 0, stage_of(2), stage_of(0), begin(2), g, s_a, dp_a, s_b, dp_b, pp_b, dd_b, pp_a, dd_a);
+    }
+    // Pairs of beats: block n is in s_b and dp_b, block n - 1's P and dS are in pp_a and dd_a, what block n + 1 starts from is in s_a and dp_a.  (What is
+    // read of blocks behind the last is not used.)
+    int32_t n = 1;
+    for (; n + 1 < n_blocks; n += 2) {
+        enter(n);
+        if (live) {
+            mask(s_b);
+            w.template beat<true, true>(stage_of(n + 1), stage_of(n - 1), stage_of(n + 2), stage_of(n), begin(n + 2), g, s_b, dp_b, s_a, dp_a, pp_a, dd_a, pp_b, dd_b);
+            mask(s_a);
+            w.template beat<true, true>(stage_of(n + 2), stage_of(n), stage_of(n + 3), stage_of(n + 1), begin(n + 3), g, s_a, dp_a, s_b, dp_b, pp_b, dd_b, pp_a, dd_a);
         }
-        float pr[16], ds[16];
+    }
+    // blocks n - 1 and, if there is one, n
+    if (live) {
+        if (n < n_blocks) {
+            mask(s_b);
+        } else {
 #pragma unroll
-        for (int v = 0; v < 16; v += 4) {
-            const float4 x = *reinterpret_cast<const float4*>(l2 + 16 * (v >> 3) + (v & 7));
-            const float l[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                pr[v + e] = __builtin_amdgcn_exp2f(fmaf(s[v + e], c, -l[e]));
-                ds[v + e] = pr[v + e] * dp[v + e];
-            }
+            for (int e = 0; e < 16; ++e) s_b[e] = -INFINITY, dp_b[e] = 0.f;
         }
-        if (i0 + 32 > tile.n || (p.causal && i0 < my0 + 31)) {
-            const int32_t from = p.causal ? my0 + j - i0 : 0, to = tile.n - i0;        // positions of rows that see key j, and that there are
+        w.template beat<false, true>(0, stage_of(n - 1), 0, stage_of(n), begin(0), g, s_b, dp_b, s_a, dp_a, pp_a, dd_a, pp_b, dd_b);
+        if (n < n_blocks)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int pos = prompt_position(v, g);
-                const bool seen = pos >= from && pos < to;
-                pr[v] = seen ? pr[v] : 0.f;
-                ds[v] = seen ? ds[v] : 0.f;
-            }
-        }
-        u32x4 pp[2], dd[2];
-        pack(pr, pp);
-        pack(ds, dd);
-#pragma unroll
-        for (int db = 0; db < kHalves; ++db)
-#pragma unroll
-            for (int st = 0; st < 2; ++st) {
-                dva[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(prompt_turned<D>(gb, turned, db, st), __builtin_bit_cast(bf16x8, pp[st]), dva[db], 0, 0, 0);
-                dka[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(prompt_turned<D>(qb, turned, db, st), __builtin_bit_cast(bf16x8, dd[st]), dka[db], 0, 0, 0);
+            for (int r = 0; r < D / 16; ++r) {
+                w.dv[r >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w.turned(stage_of(n) + w.kTensor, r >> 1, r & 1), __builtin_bit_cast(bf16x8, pp_b[r & 1]), w.dv[r >> 1], 0, 0, 0);
+                w.dk[r >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w.turned(stage_of(n), r >> 1, r & 1), __builtin_bit_cast(bf16x8, dd_b[r & 1]), w.dk[r >> 1], 0, 0, 0);
             }
     }
 
@@ -300,16 +398,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
                     *reinterpret_cast<float4*>(to + 32 * db + 8 * v) =
-                        make_float4(dka[db][4 * v] * p.scale, dka[db][4 * v + 1] * p.scale, dka[db][4 * v + 2] * p.scale, dka[db][4 * v + 3] * p.scale);
-                    *reinterpret_cast<float4*>(to + tensor + 32 * db + 8 * v) = make_float4(dva[db][4 * v], dva[db][4 * v + 1], dva[db][4 * v + 2], dva[db][4 * v + 3]);
+                        make_float4(w.dk[db][4 * v] * p.scale, w.dk[db][4 * v + 1] * p.scale, w.dk[db][4 * v + 2] * p.scale, w.dk[db][4 * v + 3] * p.scale);
+                    *reinterpret_cast<float4*>(to + tensor + 32 * db + 8 * v) = make_float4(w.dv[db][4 * v], w.dv[db][4 * v + 1], w.dv[db][4 * v + 2], w.dv[db][4 * v + 3]);
                 }
         }
     } else {
         constexpr int kMine = 32 * (2 * D + 16);
         static_assert(sizeof(lds) >= 4 * kMine, "every wave's rows fit the stages");
         char* const mine = reinterpret_cast<char*>(&lds[0][0][0]) + wave * kMine;
-        store_rows<D>(dka, p.scale, mine, dk + r0 * pitch, pitch, rows - r0, lane_e);
-        store_rows<D>(dva, 1.f, mine, dv + r0 * pitch, pitch, rows - r0, lane_e);
+        store_rows<D>(w.dk, p.scale, mine, dk + r0 * pitch, pitch, rows - r0, lane_e);
+        store_rows<D>(w.dv, 1.f, mine, dv + r0 * pitch, pitch, rows - r0, lane_e);
     }
 }
 
