@@ -45,6 +45,77 @@ __device__ __forceinline__ PackedSequence packed_sequence(const int32_t* starts,
     return s;
 }
 
+// Sum over a wave, the same in all lanes.
+__device__ __forceinline__ int32_t wave_total(int32_t x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);      // row_shr 1, 2, 4, 8: a row's total in its last lane
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);     // row_bcast 15 into rows 1 and 3, row_bcast 31 into rows 2 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+    return __builtin_amdgcn_readlane(x, 63);
+}
+
+// The tile of a rank, where tiles are ranked by `level`: a sequence of n tiles has one of every level 1 .. n, highest levels come first and equal
+// ones in the sequences' order.  For launches whose tiles take as long as their level says: the longest then start first, whatever the lengths are.  (Bisection for the
+// level with the sequences' numbers of tiles in registers: up to 64 * kRankedPerLane sequences.)  b == B: rows behind the last sequence, `level` counts their tiles from 0; they
+// and slots without a tile come last.
+constexpr int kRankedPerLane = 4;
+struct RankedTile {
+    int32_t b, first, end, level;
+};
+template <int R>
+__device__ __forceinline__ RankedTile packed_ranked(const int32_t* starts, int32_t B, int32_t T, int32_t rank, int lane) {
+    int32_t tiles[kRankedPerLane], most = 0;
+#pragma unroll
+    for (int i = 0; i < kRankedPerLane; ++i) {
+        const int32_t b = 64 * i + lane;
+        const int32_t here = packed_start(starts, min(b, B), T), next = packed_start(starts, min(b + 1, B), T);
+        tiles[i] = b < B ? (max(next - here, 0) + R - 1) / R : 0;
+    }
+    int32_t all = 0;
+#pragma unroll
+    for (int i = 0; i < kRankedPerLane; ++i) all += tiles[i];
+    all = wave_total(all);
+    most = all;
+    RankedTile t;
+    const int32_t last = packed_start(starts, B, T);
+    if (rank >= all) {
+        t.b = B, t.first = __builtin_amdgcn_readfirstlane(last), t.end = T, t.level = rank - all;
+        return t;
+    }
+    // tiles of level m and above
+    auto above = [&](int32_t m) {
+        int32_t n = 0;
+#pragma unroll
+        for (int i = 0; i < kRankedPerLane; ++i) n += max(tiles[i] - m + 1, 0);
+        return wave_total(n);
+    };
+    int32_t lo = 1, hi = min(most, (T + R - 1) / R);              // the highest level with above(level) > rank is in lo .. hi
+    while (lo < hi) {
+        const int32_t mid = lo + (hi - lo + 1) / 2;
+        if (above(mid) > rank) lo = mid;
+        else hi = mid - 1;
+    }
+    int32_t k = rank - above(lo + 1);                             // among the tiles of this level
+    t.b = 0;
+#pragma unroll
+    for (int i = 0; i < kRankedPerLane; ++i) {
+        const uint64_t has = __ballot(tiles[i] >= lo);
+        const int32_t n = __popcll(has);
+        if (k >= 0 && k < n) {
+            // the lane with k such lanes before it
+            const bool mine = tiles[i] >= lo && __popcll(has & ((1ull << lane) - 1)) == k;
+            t.b = 64 * i + (int32_t)__builtin_ctzll(__ballot(mine));
+        }
+        k -= n;
+    }
+    t.first = __builtin_amdgcn_readfirstlane(packed_start(starts, t.b, T));
+    t.end = __builtin_amdgcn_readfirstlane(max(packed_start(starts, t.b + 1, T), t.first));
+    t.level = lo;
+    return t;
+}
+
 struct ReserveParams {
     const int32_t *counts, *lengths;        // [B]
     int32_t B, page_shift, rows;

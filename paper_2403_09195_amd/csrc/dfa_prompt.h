@@ -54,6 +54,20 @@ __device__ __forceinline__ PromptTile prompt_tile(const PromptParams& p, int32_t
     return t;
 }
 
+// The same, the tiles ranked by how many rows see their keys: for launches along the rows.
+template <int R>
+__device__ __forceinline__ PromptTile prompt_key_tile(const PromptParams& p, int32_t rank, int lane) {
+    if (p.B > 64 * kRankedPerLane) return prompt_tile<R>(p, rank, lane);
+    const RankedTile s = packed_ranked<R>(p.starts, p.B, p.T, rank, lane);
+    PromptTile t;
+    t.first = s.first;
+    t.n = s.end - s.first;
+    t.rest = s.b == p.B;
+    t.t0 = (t.rest ? s.level : (t.n + R - 1) / R - s.level) * R;
+    t.empty = t.t0 < 0 || t.t0 >= t.n;
+    return t;
+}
+
 // Workgroup x of a launch of slots * heads -> (slot, head).  Workgroups go to the dies in turn: with a multiple of eight heads a die
 // keeps H / 8 neighbouring ones, whose keys and values then stay in its L2.  Tiles at the end of a sequence, the longest where
 // attention is causal, come first.

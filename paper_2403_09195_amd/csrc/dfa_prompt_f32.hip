@@ -328,7 +328,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
     prompt_place(blockIdx.x, slots, p.Hkv * p.shares, slot, unit);
     slot = slots - 1 - slot;
     const int32_t hk = unit / p.shares, share = unit % p.shares;
-    const PromptTile tile = prompt_tile<R>(p, slot, lane);
+    const PromptTile tile = prompt_key_tile<R>(p, slot, lane);
     if (tile.empty) return;
     const int32_t rows = min(R, tile.n - tile.t0);
     const int64_t row0 = (int64_t)tile.first + tile.t0, pitch = (int64_t)p.Hkv * D, result = (row0 * p.Hkv + hk) * D;
