@@ -87,7 +87,7 @@ int check_norm_types(dfa_dtype_t dt, dfa_dtype_t weight_dt, const void* weight) 
 }
 
 int64_t norm_backward_bytes(int64_t M, int64_t C, const ChipShape& chip) {
-    const int64_t n = norm_backward_workgroups(M, C, chip);
+    const int64_t n = std::max(norm_backward_workgroups(M, C, false, chip), norm_backward_workgroups(M, C, true, chip));
     return n > 1 ? up(n * C * 4, 256) : 0;
 }
 
@@ -195,7 +195,7 @@ int dfa_rms_norm_backward(const void* dy, int64_t lddy, const void* h, int64_t l
     if (need && (!workspace || workspace_bytes < (size_t)need)) return DFA_ERR_WORKSPACE;
     NormBackwardParams p{};
     p.dy = dy, p.h = h, p.weight = weight, p.dh = dh, p.lddy = lddy, p.ldh = ldh, p.lddh = lddh, p.M = M, p.C = C, p.eps = eps;
-    p.dx = dx, p.lddx = lddx, p.dw = dw, p.parts = static_cast<float*>(workspace), p.workgroups = norm_backward_workgroups(M, C, chip);
+    p.dx = dx, p.lddx = lddx, p.dw = dw, p.parts = static_cast<float*>(workspace), p.workgroups = norm_backward_workgroups(M, C, dt == DFA_F32, chip);
     return status(launch_norm_backward(p, dt == DFA_F32, weight && weight_dt == DFA_F32, static_cast<hipStream_t>(stream)));
 }
 

@@ -29,7 +29,7 @@ struct NormBackwardParams {
     float* parts;                           // [workgroups][C] workspace where there is more than one
     int32_t workgroups;
 };
-int32_t norm_backward_workgroups(int64_t M, int64_t C, const ChipShape& chip);
+int32_t norm_backward_workgroups(int64_t M, int64_t C, bool f32, const ChipShape& chip);
 hipError_t launch_norm_backward(const NormBackwardParams& p, bool f32, bool weight_f32, hipStream_t st);
 
 }  // namespace dfa

@@ -270,20 +270,29 @@ __global__ __launch_bounds__(kNormGroup<kThreads>) void norm_backward_kernel(con
     }
 }
 
-// dw of the workgroups' parts: 64 columns a workgroup, 16 waves that take every sixteenth part.
+// dw of the workgroups' parts: 16 columns a workgroup, 64 threads that take every 64th part of each.  (64 columns and 16 threads: 20 us instead of 3.5 for 1024
+// parts of 768 columns, where twelve workgroups then read 64 parts one after the other.)
 __global__ __launch_bounds__(1024) void norm_sum_kernel(const float* parts, float* dw, int64_t C, int32_t count) {
-    __shared__ float lds[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    __shared__ float lds[64][17];
+    const int col = threadIdx.x & 15, group = threadIdx.x >> 4;
+    const int64_t c = min((int64_t)blockIdx.x * 16 + col, C - 1);
     float s = 0.f;
-    if (c < C)
-        for (int32_t i = wave; i < count; i += 16) s += parts[i * C + c];
-    lds[wave][lane] = s;
+#pragma unroll 8
+    for (int32_t i = group; i < count; i += 64) s += parts[i * C + c];
+    lds[group][col] = s;
     __syncthreads();
-    if (wave || c >= C) return;
+    if (group >= 16) return;
+    // thread (col, group): 16 sums of four, then lanes 16 apart and waves
+    float q = 0.f;
 #pragma unroll
-    for (int w = 1; w < 16; ++w) s += lds[w][lane];
-    dw[c] = s;
+    for (int i = 0; i < 4; ++i) q += lds[4 * group + i][col];
+    q += __shfl_xor(q, 16);
+    q += __shfl_xor(q, 32);
+    __shared__ float waves[4][16];
+    if ((threadIdx.x & 63) < 16) waves[threadIdx.x >> 6][col] = q;
+    // (four waves are left: the others have ended)
+    __syncthreads();
+    if (group == 0 && (int64_t)blockIdx.x * 16 + col < C) dw[c] = waves[0][col] + waves[1][col] + waves[2][col] + waves[3][col];
 }
 
 // Threads of a row and pieces of a thread.
@@ -332,16 +341,19 @@ hipError_t launch_norm(const NormParams& p, bool f32, bool weight_f32, const Chi
     return launch_any(p, norm_form(p.M, p.values ? (p.C + 127) / 128 * 128 : p.C), f32, weight_f32, st);
 }
 
-int32_t norm_backward_workgroups(int64_t M, int64_t C, const ChipShape& chip) {
+// As many as are resident at once by their registers: each takes the same number of rows, give or take one, and none waits for a place.  (32768 rows of 768 in bf16:
+// 44.5 us with three to a compute unit, 55.3 with two, 58.4 with four, of which one waits.)
+int32_t norm_backward_workgroups(int64_t M, int64_t C, bool f32, const ChipShape& chip) {
     const NormForm f = norm_form(M, C);
     const int64_t rows = f.threads == 64 ? 4 : 1, most = (M + rows - 1) / rows;
-    return (int32_t)std::min<int64_t>(most, (f.threads == 1024 ? 1 : f.threads == 512 ? 2 : 4) * chip.cus);
+    const int32_t resident = f.threads > 256 ? 1 : f.pieces == 1 ? 4 : f32 ? 2 : 3;
+    return (int32_t)std::min<int64_t>(most, resident * chip.cus);
 }
 
 hipError_t launch_norm_backward(const NormBackwardParams& p, bool f32, bool weight_f32, hipStream_t st) {
     const hipError_t e = launch_any(p, norm_form(p.M, p.C), f32, weight_f32, st);
     if (e != hipSuccess || !p.dw || p.workgroups == 1) return e;
-    hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)((p.C + 63) / 64)), dim3(1024), 0, st, p.parts, p.dw, p.C, p.workgroups);
+    hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)((p.C + 15) / 16)), dim3(1024), 0, st, p.parts, p.dw, p.C, p.workgroups);
     return hipGetLastError();
 }
 
