@@ -143,7 +143,7 @@ int dfa_prompt_attention_backward(const void* q, const void* k, const void* v, d
     p.out = const_cast<void*>(out), p.lse = const_cast<float*>(lse), p.dout = dout, p.dq = dq, p.dk = dk, p.dv = dv;
     p.ndelta = static_cast<float*>(workspace), p.lse2 = p.ndelta + (int64_t)H * T;
     p.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + up((int64_t)2 * H * T * 4, 256));
-    return status(launch_prompt_bwd(p, dt == DFA_F32, D, static_cast<hipStream_t>(stream)));
+    return status(launch_prompt_bwd(p, dt == DFA_F32, D, chip, static_cast<hipStream_t>(stream)));
 }
 
 int dfa_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* weight, dfa_dtype_t weight_dt, dfa_dtype_t dt, float eps, void* h,

@@ -28,9 +28,14 @@ struct PromptParams {
 hipError_t launch_prompt_fwd(const PromptParams& p, bool f32, int32_t D, const ChipShape& chip, hipStream_t st);
 // Workgroups that share the query heads of a key head out in the launch of dk and dv.
 int32_t prompt_bwd_shares(int32_t T, int32_t B, int32_t H, int32_t Hkv, const ChipShape& chip);
-hipError_t launch_prompt_bwd(const PromptParams& p, bool f32, int32_t D, hipStream_t st);
-hipError_t launch_prompt_fwd_f32(const PromptParams& p, int32_t D, hipStream_t st);
-hipError_t launch_prompt_bwd_f32(const PromptParams& p, int32_t D, hipStream_t st);      // without the sum of the shares
+hipError_t launch_prompt_bwd(const PromptParams& p, bool f32, int32_t D, const ChipShape& chip, hipStream_t st);
+// small: tiles of half the rows, whose walk the waves of a workgroup share out
+hipError_t launch_prompt_fwd_f32(const PromptParams& p, int32_t D, bool small, hipStream_t st);
+hipError_t launch_prompt_bwd_f32(const PromptParams& p, int32_t D, bool small, hipStream_t st);      // without the sum of the shares
+// Whether a launch of 128-row tiles is so few workgroups that its longest walk decides.
+inline bool prompt_small(int32_t T, int32_t B, int32_t heads, const ChipShape& chip) {
+    return ((int64_t)T / 128 + (B < T ? B : T)) * heads < 4 * (int64_t)chip.cus;
+}
 
 // Slots of tiles of R rows.
 inline int64_t prompt_slots(int32_t T, int32_t B, int32_t R) { return (int64_t)T / R + B + 1; }
@@ -64,6 +69,20 @@ __device__ __forceinline__ PromptTile prompt_key_tile(const PromptParams& p, int
     t.n = s.end - s.first;
     t.rest = s.b == p.B;
     t.t0 = (t.rest ? s.level : (t.n + R - 1) / R - s.level) * R;
+    t.empty = t.t0 < 0 || t.t0 >= t.n;
+    return t;
+}
+
+// The same, ranked by how many keys the rows see where attention is causal: for launches of a few rounds of workgroups.
+template <int R>
+__device__ __forceinline__ PromptTile prompt_row_tile(const PromptParams& p, int32_t slot, int32_t slots, int lane) {
+    if (p.B > 64 * kRankedPerLane) return prompt_tile<R>(p, slot, lane);
+    const RankedTile s = packed_ranked<R>(p.starts, p.B, p.T, slots - 1 - slot, lane);
+    PromptTile t;
+    t.first = s.first;
+    t.n = s.end - s.first;
+    t.rest = s.b == p.B;
+    t.t0 = (t.rest ? s.level : s.level - 1) * R;
     t.empty = t.t0 < 0 || t.t0 >= t.n;
     return t;
 }

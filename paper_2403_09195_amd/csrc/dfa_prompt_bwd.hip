@@ -441,8 +441,8 @@ int32_t prompt_bwd_shares(int32_t T, int32_t B, int32_t H, int32_t Hkv, const Ch
     return (int32_t)std::min(group, std::max<int64_t>(1, (2 * chip.cus + workgroups - 1) / workgroups));
 }
 
-hipError_t launch_prompt_bwd(const PromptParams& p, bool f32, int32_t D, hipStream_t st) {
-    const hipError_t e = f32 ? launch_prompt_bwd_f32(p, D, st) : D == 64 ? launch<64, 2, 2>(p, st) : launch<128, 1, 1>(p, st);
+hipError_t launch_prompt_bwd(const PromptParams& p, bool f32, int32_t D, const ChipShape& chip, hipStream_t st) {
+    const hipError_t e = f32 ? launch_prompt_bwd_f32(p, D, prompt_small(p.T, p.B, p.H, chip), st) : D == 64 ? launch<64, 2, 2>(p, st) : launch<128, 1, 1>(p, st);
     if (e != hipSuccess || p.shares == 1) return e;
     const int64_t tensor = (int64_t)p.T * p.Hkv * D;
     const dim3 grid((unsigned)((2 * tensor / 4 + 255) / 256));

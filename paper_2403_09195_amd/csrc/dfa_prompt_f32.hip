@@ -39,28 +39,30 @@ __device__ __forceinline__ Split8 split_apart(const float4& a, const float4& b) 
 // Parts of a block in LDS, each [32][D].
 template <int D> constexpr int kPart = 32 * D;
 
-// What a thread carries of a block: pieces of eight elements, one of D = 64, two of D = 128.
-template <int D>
+// What a thread of kThreads carries of kBlocks blocks, one behind the other: pieces of eight elements.
+template <int D, int kThreads, int kBlocks>
 struct Piece {
-    float4 x[D / 64][2];
-    // rows k0 .. k0 + 31 of `rows`, `pitch` elements apart; rows behind the last re-read it
+    static constexpr int kPerBlock = 32 * D / 8, kPieces = kBlocks * kPerBlock / kThreads;
+    static_assert(kPieces >= 1, "a piece for every thread");
+    float4 x[kPieces][2];
+    // rows k0 .. k0 + 32 * kBlocks - 1 of `rows`, `pitch` elements apart; rows behind the last re-read it
     __device__ __forceinline__ void load(const float* base, int64_t pitch, int32_t k0, int32_t rows) {
 #pragma unroll
-        for (int u = 0; u < D / 64; ++u) {
-            const int i = u * 256 + threadIdx.x, row = i / (D / 8), ch = i % (D / 8);
+        for (int u = 0; u < kPieces; ++u) {
+            const int i = u * kThreads + threadIdx.x, row = i / (D / 8), ch = i % (D / 8);
             const float* const from = base + (int64_t)min(k0 + row, rows - 1) * pitch + 8 * ch;
             x[u][0] = *reinterpret_cast<const float4*>(from);
             x[u][1] = *reinterpret_cast<const float4*>(from + 4);
         }
     }
-    // (kValues: the forward's values, see split_apart)
+    // parts of block 0; a block's parts lie `stride` elements behind those of the one before.  (kValues: the forward's values, see split_apart)
     template <PromptOrder kOrder>
-    __device__ __forceinline__ void store(uint16_t* parts) const {
+    __device__ __forceinline__ void store(uint16_t* parts, int stride) const {
 #pragma unroll
-        for (int u = 0; u < D / 64; ++u) {
-            const int i = u * 256 + threadIdx.x, row = i / (D / 8), ch = i % (D / 8);
+        for (int u = 0; u < kPieces; ++u) {
+            const int i = u * kThreads + threadIdx.x, row = i / (D / 8) % 32, ch = i % (D / 8);
             const int rho = kOrder == PromptOrder::kValues ? row : prompt_sigma(row);
-            uint16_t* const to = parts + rho * D + 8 * (ch ^ prompt_swizzle<D, kOrder>(rho));
+            uint16_t* const to = parts + i / kPerBlock * stride + rho * D + 8 * (ch ^ prompt_swizzle<D, kOrder>(rho));
             const Split8 s = kOrder == PromptOrder::kValues ? split_apart(x[u][0], x[u][1]) : split_plain(x[u][0], x[u][1]);
             *reinterpret_cast<bf16x8*>(to) = s.h;
             *reinterpret_cast<bf16x8*>(to + kPart<D>) = s.m;
@@ -68,6 +70,32 @@ struct Piece {
         }
     }
 };
+
+// Sums the waves' results of the same rows: wave w of kGroups * kOthers keeps those of waves w + kOthers, w + 2 kOthers, ...  `lds`: room for half of the waves'
+// results.  All threads call it; the first kOthers waves have the sums.
+template <int kHalves, int kGroups, int kOthers>
+__device__ __forceinline__ void sum_groups(floatx16 (&acc)[kHalves], float4* lds, int wave, int lane) {
+#pragma unroll
+    for (int half = kGroups / 2; half >= 1; half /= 2) {
+        __syncthreads();
+        float4* const mine = lds + (wave % (half * kOthers)) * (kHalves * 4 * 64) + lane;
+        const bool gives = wave >= half * kOthers && wave < 2 * half * kOthers, takes = wave < half * kOthers;
+        if (gives)
+#pragma unroll
+            for (int i = 0; i < 4 * kHalves; ++i) {
+                const floatx16& x = acc[i >> 2];
+                mine[64 * i] = make_float4(x[4 * (i & 3)], x[4 * (i & 3) + 1], x[4 * (i & 3) + 2], x[4 * (i & 3) + 3]);
+            }
+        __syncthreads();
+        if (takes)
+#pragma unroll
+            for (int i = 0; i < 4 * kHalves; ++i) {
+                const float4 y = mine[64 * i];
+                floatx16& x = acc[i >> 2];
+                x[4 * (i & 3)] += y.x, x[4 * (i & 3) + 1] += y.y, x[4 * (i & 3) + 2] += y.z, x[4 * (i & 3) + 3] += y.w;
+            }
+    }
+}
 
 // A wave's own 32 rows as operands of first products.
 template <int D>
@@ -157,14 +185,18 @@ __device__ __forceinline__ void store_direct(const floatx16 (&acc)[D / 32], floa
             *reinterpret_cast<float4*>(row + 32 * db + 8 * v + 4 * g) = make_float4(acc[db][4 * v] * by, acc[db][4 * v + 1] * by, acc[db][4 * v + 2] * by, acc[db][4 * v + 3] * by);
 }
 
-template <int D, int kEu>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu))) void prompt_fwd_f32_kernel(const PromptParams p, int32_t slots) {
-    constexpr int R = 128, kHalves = D / 32;
-    __shared__ __attribute__((aligned(16))) uint16_t lds[2][2][3 * kPart<D>];        // keys, values
+// Forward.  RG groups of 32 rows, KG groups of waves that take every KG-th block of the walk: a step is KG blocks.  Their results are merged at
+// the end.
+template <int D, int RG, int KG, bool kDouble, int kEu>
+__global__ __launch_bounds__(64 * RG * KG) __attribute__((amdgpu_waves_per_eu(kEu, kEu))) void prompt_fwd_f32_kernel(const PromptParams p, int32_t slots) {
+    constexpr int R = 32 * RG, kHalves = D / 32, kThreads = 64 * RG * KG, kTensor = KG * 3 * kPart<D>, kBuffers = kDouble ? 2 : 1;
+    __shared__ __attribute__((aligned(16))) uint16_t lds[kBuffers][2][kTensor];      // keys, values
+    __shared__ float stats[2][KG][R];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, g = lane >> 5;
+    const int rg = wave % RG, kg = wave / RG;
     int32_t slot, h;
     prompt_place(blockIdx.x, slots, p.H, slot, h);
-    const PromptTile tile = prompt_tile<R>(p, slot, lane);
+    const PromptTile tile = prompt_row_tile<R>(p, slot, slots, lane);
     if (tile.empty) return;
     const int32_t rows = min(R, tile.n - tile.t0);
     const int64_t row0 = (int64_t)tile.first + tile.t0, pitch = (int64_t)p.H * D;
@@ -175,18 +207,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
         if (lse && tid < rows) lse[tid] = -INFINITY;
         return;
     }
-    const int32_t keys = p.causal ? tile.t0 + rows : tile.n, n_blocks = (keys + 31) / 32, my0 = tile.t0 + 32 * wave;
-    const int32_t my_blocks = my0 >= tile.n ? 0 : p.causal ? (min(my0 + 32, keys) + 31) / 32 : n_blocks;
+    const int32_t keys = p.causal ? tile.t0 + rows : tile.n, my0 = tile.t0 + 32 * rg, n_steps = (keys + 32 * KG - 1) / (32 * KG);
+    const int32_t my_blocks = my0 >= tile.n ? 0 : ((p.causal ? min(my0 + 32, keys) : keys) + 31) / 32;
     const float* const kp = static_cast<const float*>(p.k) + tile.first * p.skn + (h / p.group) * p.skh;
     const float* const vp = static_cast<const float*>(p.v) + tile.first * p.svn + (h / p.group) * p.svh;
 
-    Piece<D> kx, vx;
+    Piece<D, kThreads, KG> kx, vx;
     kx.load(kp, p.skn, 0, keys);
     vx.load(vp, p.svn, 0, keys);
     OwnRows<D> q;
-    q.load(static_cast<const float*>(p.q) + (row0 + min(32 * wave + j, rows - 1)) * p.sqn + h * p.sqh, g);
-    kx.template store<PromptOrder::kKeys>(lds[0][0]);
-    vx.template store<PromptOrder::kValues>(lds[0][1]);
+    q.load(static_cast<const float*>(p.q) + (row0 + min(32 * rg + j, rows - 1)) * p.sqn + h * p.sqh, g);
+    kx.template store<PromptOrder::kKeys>(lds[0][0], 3 * kPart<D>);
+    vx.template store<PromptOrder::kValues>(lds[0][1], 3 * kPart<D>);
     const float c = uniform_float(p.scale * kLog2e);
     const int row_at = prompt_row_at<D, PromptOrder::kKeys>(lane), value_at = prompt_value_at<D>(lane);
     floatx16 acc[kHalves];
@@ -194,17 +226,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
     for (int db = 0; db < kHalves; ++db) acc[db] = prompt_zero();
     float ref = kLowest, sum = 0.f;
 
-    for (int32_t n = 0; n < n_blocks; ++n) {
-        __syncthreads();                     // block n is in LDS, and everyone is done with block n - 1
-        const bool more = n + 1 < n_blocks;
+    for (int32_t n = 0; n < n_steps; ++n) {
+        __syncthreads();                     // the step's blocks are in LDS, and everyone is done with those of the step before
+        const bool more = n + 1 < n_steps;
         if (more) {
-            kx.load(kp, p.skn, 32 * n + 32, keys);
-            vx.load(vp, p.svn, 32 * n + 32, keys);
+            kx.load(kp, p.skn, 32 * KG * (n + 1), keys);
+            vx.load(vp, p.svn, 32 * KG * (n + 1), keys);
         }
-        if (n < my_blocks) {
-            floatx16 s = rows_times<D>(lds[n & 1][0], row_at, q, prompt_zero());
-            const int32_t last = min(p.causal ? my0 + j : keys - 1, keys - 1) - 32 * n;
-            const bool masked = 32 * n + 32 > (p.causal ? min(my0 + 1, keys) : keys);
+        const int32_t block = KG * n + kg;
+        if (block < my_blocks) {
+            const uint16_t *const kb = lds[kDouble ? n & 1 : 0][0] + kg * 3 * kPart<D>, *const vb = lds[kDouble ? n & 1 : 0][1] + kg * 3 * kPart<D>;
+            floatx16 s = rows_times<D>(kb, row_at, q, prompt_zero());
+            const int32_t last = min(p.causal ? my0 + j : keys - 1, keys - 1) - 32 * block;
+            const bool masked = 32 * block + 32 > (p.causal ? min(my0 + 1, keys) : keys);
             if (masked)
 #pragma unroll
                 for (int v = 0; v < 16; ++v)
@@ -228,28 +262,54 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
                 w[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c, -ref));
                 sum += w[v];
             }
-            if (__builtin_expect(masked && prompt_odd_values<D>(lds[n & 1][1]), 0)) columns_times_odd<D>(lds[n & 1][1], value_at, w, last, lane, acc);
-            else columns_times<D, false>(lds[n & 1][1], value_at, w, acc);
+            if (__builtin_expect(masked && prompt_odd_values<D>(vb), 0)) columns_times_odd<D>(vb, value_at, w, last, lane, acc);
+            else columns_times<D, false>(vb, value_at, w, acc);
         }
+        if (!kDouble) __syncthreads();
         if (more) {
-            kx.template store<PromptOrder::kKeys>(lds[(n + 1) & 1][0]);
-            vx.template store<PromptOrder::kValues>(lds[(n + 1) & 1][1]);
+            kx.template store<PromptOrder::kKeys>(lds[kDouble ? (n + 1) & 1 : 0][0], 3 * kPart<D>);
+            vx.template store<PromptOrder::kValues>(lds[kDouble ? (n + 1) & 1 : 0][1], 3 * kPart<D>);
         }
     }
-    const float total = wave_half_sum(sum), inv = total == 0.f ? 0.f : 1.0f / total;
-    if (32 * wave + j >= rows) return;
-    if (lse && g == 0) lse[32 * wave + j] = total == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(total)) * kLn2;
-    store_direct<D>(acc, inv, out + (32 * wave + j) * pitch, g);
+    float total = wave_half_sum(sum);
+    if constexpr (KG > 1) {
+        if (g == 0) {
+            stats[0][kg][32 * rg + j] = ref;
+            stats[1][kg][32 * rg + j] = total;
+        }
+        __syncthreads();
+        float top = kLowest;
+#pragma unroll
+        for (int k = 0; k < KG; ++k) top = fmaxf(top, stats[0][k][32 * rg + j]);
+        total = 0.f;
+#pragma unroll
+        for (int k = 0; k < KG; ++k) total += stats[1][k][32 * rg + j] * __builtin_amdgcn_exp2f(stats[0][k][32 * rg + j] - top);
+        const float by = __builtin_amdgcn_exp2f(ref - top);
+        ref = top;
+#pragma unroll
+        for (int db = 0; db < kHalves; ++db)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[db][v] *= by;
+        static_assert(sizeof(lds) >= (size_t)RG * KG / 2 * kHalves * 4 * 64 * 16, "half of the waves' results fit");
+        sum_groups<kHalves, KG, RG>(acc, reinterpret_cast<float4*>(lds), wave, lane);
+        if (kg) return;
+    }
+    const float inv = total == 0.f ? 0.f : 1.0f / total;
+    if (32 * rg + j >= rows) return;
+    if (lse && g == 0) lse[32 * rg + j] = total == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(total)) * kLn2;
+    store_direct<D>(acc, inv, out + (32 * rg + j) * pitch, g);
 }
 
-template <int D, int kEu>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu))) void prompt_dq_f32_kernel(const PromptParams p, int32_t slots) {
-    constexpr int R = 128, kHalves = D / 32;
-    __shared__ __attribute__((aligned(16))) uint16_t lds[2][2][3 * kPart<D>];        // keys, values
+// dq, groups of rows and of blocks as in the forward.
+template <int D, int RG, int KG, bool kDouble, int kEu>
+__global__ __launch_bounds__(64 * RG * KG) __attribute__((amdgpu_waves_per_eu(kEu, kEu))) void prompt_dq_f32_kernel(const PromptParams p, int32_t slots) {
+    constexpr int R = 32 * RG, kHalves = D / 32, kThreads = 64 * RG * KG, kTensor = KG * 3 * kPart<D>, kBuffers = kDouble ? 2 : 1;
+    __shared__ __attribute__((aligned(16))) uint16_t lds[kBuffers][2][kTensor];      // keys, values
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, g = lane >> 5;
+    const int rg = wave % RG, kg = wave / RG;
     int32_t slot, h;
     prompt_place(blockIdx.x, slots, p.H, slot, h);
-    const PromptTile tile = prompt_tile<R>(p, slot, lane);
+    const PromptTile tile = prompt_row_tile<R>(p, slot, slots, lane);
     if (tile.empty) return;
     const int32_t rows = min(R, tile.n - tile.t0);
     const int64_t row0 = (int64_t)tile.first + tile.t0, pitch = (int64_t)p.H * D;
@@ -258,15 +318,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
         zero_rows<D>(dq, pitch, rows);
         return;
     }
-    const int32_t keys = p.causal ? tile.t0 + rows : tile.n, n_blocks = (keys + 31) / 32, my0 = tile.t0 + 32 * wave;
-    const int32_t my_blocks = my0 >= tile.n ? 0 : p.causal ? (min(my0 + 32, keys) + 31) / 32 : n_blocks;
+    const int32_t keys = p.causal ? tile.t0 + rows : tile.n, my0 = tile.t0 + 32 * rg, n_steps = (keys + 32 * KG - 1) / (32 * KG);
+    const int32_t my_blocks = my0 >= tile.n ? 0 : ((p.causal ? min(my0 + 32, keys) : keys) + 31) / 32;
     const float* const kp = static_cast<const float*>(p.k) + tile.first * p.skn + (h / p.group) * p.skh;
     const float* const vp = static_cast<const float*>(p.v) + tile.first * p.svn + (h / p.group) * p.svh;
 
-    Piece<D> kx, vx;
+    Piece<D, kThreads, KG> kx, vx;
     kx.load(kp, p.skn, 0, keys);
     vx.load(vp, p.svn, 0, keys);
-    const int64_t row = min(32 * wave + j, rows - 1);
+    const int64_t row = min(32 * rg + j, rows - 1);
     const float* const gr = static_cast<const float*>(p.dout) + (row0 * p.H + h) * D + row * pitch;
     const float* const orow = static_cast<const float*>(p.out) + (row0 * p.H + h) * D + row * pitch;
     OwnRows<D> q, go;
@@ -279,51 +339,61 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
         part = fmaf(a.x, b.x, fmaf(a.y, b.y, fmaf(a.z, b.z, fmaf(a.w, b.w, part))));
     }
     const float nd = -wave_half_sum(part), l = p.lse[(int64_t)h * p.T + row0 + row], lse2 = l == -INFINITY ? INFINITY : l * kLog2e;
-    if (g == 0 && 32 * wave + j < rows) {
-        p.ndelta[(int64_t)h * p.T + row0 + 32 * wave + j] = nd;
-        p.lse2[(int64_t)h * p.T + row0 + 32 * wave + j] = lse2;
+    if (g == 0 && kg == 0 && 32 * rg + j < rows) {
+        p.ndelta[(int64_t)h * p.T + row0 + 32 * rg + j] = nd;
+        p.lse2[(int64_t)h * p.T + row0 + 32 * rg + j] = lse2;
     }
-    kx.template store<PromptOrder::kBoth>(lds[0][0]);
-    vx.template store<PromptOrder::kKeys>(lds[0][1]);
+    kx.template store<PromptOrder::kBoth>(lds[0][0], 3 * kPart<D>);
+    vx.template store<PromptOrder::kKeys>(lds[0][1], 3 * kPart<D>);
     const float c = uniform_float(p.scale * kLog2e);
     const int row_k = prompt_row_at<D, PromptOrder::kBoth>(lane), row_v = prompt_row_at<D, PromptOrder::kKeys>(lane), turned = prompt_turned_at<D>(lane);
     floatx16 acc[kHalves];
 #pragma unroll
     for (int db = 0; db < kHalves; ++db) acc[db] = prompt_zero();
 
-    for (int32_t n = 0; n < n_blocks; ++n) {
+    for (int32_t n = 0; n < n_steps; ++n) {
         __syncthreads();
-        const bool more = n + 1 < n_blocks;
+        const bool more = n + 1 < n_steps;
         if (more) {
-            kx.load(kp, p.skn, 32 * n + 32, keys);
-            vx.load(vp, p.svn, 32 * n + 32, keys);
+            kx.load(kp, p.skn, 32 * KG * (n + 1), keys);
+            vx.load(vp, p.svn, 32 * KG * (n + 1), keys);
         }
-        if (n < my_blocks) {
-            const floatx16 s = rows_times<D>(lds[n & 1][0], row_k, q, prompt_zero()), dp = rows_times<D>(lds[n & 1][1], row_v, go, prompt_zero());
+        const int32_t block = KG * n + kg;
+        if (block < my_blocks) {
+            const uint16_t *const kb = lds[kDouble ? n & 1 : 0][0] + kg * 3 * kPart<D>, *const vb = lds[kDouble ? n & 1 : 0][1] + kg * 3 * kPart<D>;
+            const floatx16 s = rows_times<D>(kb, row_k, q, prompt_zero()), dp = rows_times<D>(vb, row_v, go, prompt_zero());
             float ds[16];
 #pragma unroll
             for (int v = 0; v < 16; ++v) ds[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c, -lse2)) * (dp[v] + nd);
-            if (32 * n + 32 > (p.causal ? min(my0 + 1, keys) : keys)) {
-                const int32_t last = min(p.causal ? my0 + j : keys - 1, keys - 1) - 32 * n;
+            if (32 * block + 32 > (p.causal ? min(my0 + 1, keys) : keys)) {
+                const int32_t last = min(p.causal ? my0 + j : keys - 1, keys - 1) - 32 * block;
 #pragma unroll
                 for (int v = 0; v < 16; ++v) ds[v] = prompt_position(v, g) > last ? 0.f : ds[v];
             }
-            columns_times<D, true>(lds[n & 1][0], turned, ds, acc);
+            columns_times<D, true>(kb, turned, ds, acc);
         }
+        if (!kDouble) __syncthreads();
         if (more) {
-            kx.template store<PromptOrder::kBoth>(lds[(n + 1) & 1][0]);
-            vx.template store<PromptOrder::kKeys>(lds[(n + 1) & 1][1]);
+            kx.template store<PromptOrder::kBoth>(lds[kDouble ? (n + 1) & 1 : 0][0], 3 * kPart<D>);
+            vx.template store<PromptOrder::kKeys>(lds[kDouble ? (n + 1) & 1 : 0][1], 3 * kPart<D>);
         }
     }
-    if (32 * wave + j < rows) store_direct<D>(acc, p.scale, dq + (32 * wave + j) * pitch, g);
+    if constexpr (KG > 1) {
+        static_assert(sizeof(lds) >= (size_t)RG * KG / 2 * kHalves * 4 * 64 * 16, "half of the waves' results fit");
+        sum_groups<kHalves, KG, RG>(acc, reinterpret_cast<float4*>(lds), wave, lane);
+        if (kg) return;
+    }
+    if (32 * rg + j < rows) store_direct<D>(acc, p.scale, dq + (32 * rg + j) * pitch, g);
 }
 
-template <int D, int kEu>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu))) void prompt_dkdv_f32_kernel(const PromptParams p, int32_t slots) {
-    constexpr int R = 128, kHalves = D / 32;
-    __shared__ __attribute__((aligned(16))) uint16_t lds[2][2][3 * kPart<D>];        // q, dout
-    __shared__ __attribute__((aligned(16))) float scalars[2][2][32];                 // lse2, -delta
+// dk and dv: RG groups of 32 keys, KG groups of waves that take every KG-th block of the rows.
+template <int D, int RG, int KG, bool kDouble, int kEu>
+__global__ __launch_bounds__(64 * RG * KG) __attribute__((amdgpu_waves_per_eu(kEu, kEu))) void prompt_dkdv_f32_kernel(const PromptParams p, int32_t slots) {
+    constexpr int R = 32 * RG, kHalves = D / 32, kThreads = 64 * RG * KG, kTensor = KG * 3 * kPart<D>, kBuffers = kDouble ? 2 : 1;
+    __shared__ __attribute__((aligned(16))) uint16_t lds[kBuffers][2][kTensor];      // q, dout
+    __shared__ __attribute__((aligned(16))) float scalars[kBuffers][2][32 * KG];     // lse2, -delta
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, g = lane >> 5;
+    const int rg = wave % RG, kg = wave / RG;
     int32_t slot, unit;
     prompt_place(blockIdx.x, slots, p.Hkv * p.shares, slot, unit);
     slot = slots - 1 - slot;
@@ -341,27 +411,28 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
         return;
     }
     const int32_t h0 = hk * p.group + share * p.group / p.shares, h1 = hk * p.group + (share + 1) * p.group / p.shares;
-    const int32_t first_block = p.causal ? tile.t0 / 32 : 0, per_head = (tile.n + 31) / 32 - first_block, n_blocks = (h1 - h0) * per_head;
-    const int32_t my0 = tile.t0 + 32 * wave;
+    // a step is KG blocks of one head
+    const int32_t first_row = p.causal ? tile.t0 / 32 * 32 : 0, per_head = (tile.n - first_row + 32 * KG - 1) / (32 * KG), n_steps = (h1 - h0) * per_head;
+    const int32_t my0 = tile.t0 + 32 * rg;
     const bool live = my0 < tile.n;
 
-    Piece<D> qx, gx;
+    Piece<D, kThreads, KG> qx, gx;
     float sx = 0.f;
     auto load = [&](int32_t n) {
-        const int32_t hq = h0 + n / per_head, b = first_block + n % per_head;
-        qx.load(static_cast<const float*>(p.q) + tile.first * p.sqn + hq * p.sqh, p.sqn, 32 * b, tile.n);
-        gx.load(static_cast<const float*>(p.dout) + ((int64_t)tile.first * p.H + hq) * D, (int64_t)p.H * D, 32 * b, tile.n);
-        if (tid < 64) sx = (tid < 32 ? p.lse2 : p.ndelta)[(int64_t)hq * p.T + tile.first + min(32 * b + (tid & 31), tile.n - 1)];
+        const int32_t hq = h0 + n / per_head, i0 = first_row + 32 * KG * (n % per_head);
+        qx.load(static_cast<const float*>(p.q) + tile.first * p.sqn + hq * p.sqh, p.sqn, i0, tile.n);
+        gx.load(static_cast<const float*>(p.dout) + ((int64_t)tile.first * p.H + hq) * D, (int64_t)p.H * D, i0, tile.n);
+        if (tid < 64 * KG) sx = (tid < 32 * KG ? p.lse2 : p.ndelta)[(int64_t)hq * p.T + tile.first + min(i0 + tid % (32 * KG), tile.n - 1)];
     };
     auto store = [&](int at) {
-        qx.template store<PromptOrder::kBoth>(lds[at][0]);
-        gx.template store<PromptOrder::kBoth>(lds[at][1]);
-        if (tid < 64) scalars[at][tid >> 5][tid & 31] = sx;
+        qx.template store<PromptOrder::kBoth>(lds[at][0], 3 * kPart<D>);
+        gx.template store<PromptOrder::kBoth>(lds[at][1], 3 * kPart<D>);
+        if (tid < 64 * KG) scalars[at][tid / (32 * KG)][tid % (32 * KG)] = sx;
     };
     load(0);
     OwnRows<D> k, v;
     {
-        const int64_t row = row0 + min(32 * wave + j, rows - 1);
+        const int64_t row = row0 + min(32 * rg + j, rows - 1);
         k.load(static_cast<const float*>(p.k) + row * p.skn + hk * p.skh, g);
         v.load(static_cast<const float*>(p.v) + row * p.svn + hk * p.svh, g);
     }
@@ -372,14 +443,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
 #pragma unroll
     for (int db = 0; db < kHalves; ++db) dka[db] = dva[db] = prompt_zero();
 
-    for (int32_t n = 0; n < n_blocks; ++n) {
+    for (int32_t n = 0; n < n_steps; ++n) {
         __syncthreads();
-        const bool more = n + 1 < n_blocks;
+        const bool more = n + 1 < n_steps;
         if (more) load(n + 1);
-        const int32_t i0 = 32 * (first_block + n % per_head);
-        if (live && !(p.causal && i0 + 31 < my0)) {
-            const uint16_t *const qb = lds[n & 1][0], *const gb = lds[n & 1][1];
-            const float *const l2 = scalars[n & 1][0] + 8 * g, *const nd = scalars[n & 1][1] + 8 * g;
+        const int32_t i0 = first_row + 32 * (KG * (n % per_head) + kg);
+        if (live && i0 < tile.n && !(p.causal && i0 + 31 < my0)) {
+            const int at = kDouble ? n & 1 : 0;
+            const uint16_t *const qb = lds[at][0] + kg * 3 * kPart<D>, *const gb = lds[at][1] + kg * 3 * kPart<D>;
+            const float *const l2 = scalars[at][0] + 32 * kg + 8 * g, *const nd = scalars[at][1] + 32 * kg + 8 * g;
             const floatx16 s = rows_times<D>(qb, row_at, k, prompt_zero());
             float pr[16], ds[16];
 #pragma unroll
@@ -398,33 +470,62 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
                 for (int e = 0; e < 16; ++e) ds[e] = prompt_position(e, g) >= from && prompt_position(e, g) < to ? ds[e] : 0.f;
             columns_times<D, true>(qb, turned, ds, dka);
         }
-        if (more) store((n + 1) & 1);
+        if (!kDouble) __syncthreads();
+        if (more) store(kDouble ? (n + 1) & 1 : 0);
     }
-    if (32 * wave + j < rows) {
-        store_direct<D>(dka, p.scale, dk + (32 * wave + j) * pitch, g);
-        store_direct<D>(dva, 1.f, dv + (32 * wave + j) * pitch, g);
+    if constexpr (KG > 1) {
+        static_assert(sizeof(lds) >= (size_t)RG * KG / 2 * kHalves * 4 * 64 * 16, "half of the waves' results fit");
+        sum_groups<kHalves, KG, RG>(dka, reinterpret_cast<float4*>(lds), wave, lane);
+        sum_groups<kHalves, KG, RG>(dva, reinterpret_cast<float4*>(lds), wave, lane);
+        if (kg) return;
+    }
+    if (32 * rg + j < rows) {
+        store_direct<D>(dka, p.scale, dk + (32 * rg + j) * pitch, g);
+        store_direct<D>(dva, 1.f, dv + (32 * rg + j) * pitch, g);
     }
 }
 
 }  // namespace
 
-hipError_t launch_prompt_fwd_f32(const PromptParams& p, int32_t D, hipStream_t st) {
-    const int64_t slots = prompt_slots(p.T, p.B, 128);
-    const dim3 grid((unsigned)(slots * p.H));
-    if (D == 64) hipLaunchKernelGGL((prompt_fwd_f32_kernel<64, 2>), grid, dim3(256), 0, st, p, (int32_t)slots);
-    else hipLaunchKernelGGL((prompt_fwd_f32_kernel<128, 1>), grid, dim3(256), 0, st, p, (int32_t)slots);
+namespace {
+template <int D, int RG, int KG, bool kDouble, int kEu>
+hipError_t launch_fwd(const PromptParams& p, hipStream_t st) {
+    const int64_t slots = prompt_slots(p.T, p.B, 32 * RG);
+    hipLaunchKernelGGL((prompt_fwd_f32_kernel<D, RG, KG, kDouble, kEu>), dim3((unsigned)(slots * p.H)), dim3(64 * RG * KG), 0, st, p, (int32_t)slots);
     return hipGetLastError();
 }
+template <int D, int RG, int KG, bool kDouble, int kEu>
+void launch_dq(const PromptParams& p, hipStream_t st) {
+    const int64_t slots = prompt_slots(p.T, p.B, 32 * RG);
+    hipLaunchKernelGGL((prompt_dq_f32_kernel<D, RG, KG, kDouble, kEu>), dim3((unsigned)(slots * p.H)), dim3(64 * RG * KG), 0, st, p, (int32_t)slots);
+}
+template <int D, int RG, int KG, bool kDouble, int kEu>
+void launch_dkdv(const PromptParams& p, hipStream_t st) {
+    const int64_t slots = prompt_slots(p.T, p.B, 32 * RG);
+    hipLaunchKernelGGL((prompt_dkdv_f32_kernel<D, RG, KG, kDouble, kEu>), dim3((unsigned)(slots * p.Hkv * p.shares)), dim3(64 * RG * KG), 0, st, p, (int32_t)slots);
+}
+}  // namespace
 
-hipError_t launch_prompt_bwd_f32(const PromptParams& p, int32_t D, hipStream_t st) {
-    const int64_t slots = prompt_slots(p.T, p.B, 128);
-    const dim3 grid((unsigned)(slots * p.H)), kv_grid((unsigned)(slots * p.Hkv * p.shares));
+hipError_t launch_prompt_fwd_f32(const PromptParams& p, int32_t D, bool small, hipStream_t st) {
+    if (D == 64) return small ? launch_fwd<64, 2, 4, false, 2>(p, st) : launch_fwd<64, 4, 1, true, 2>(p, st);
+    return small ? launch_fwd<128, 2, 2, false, 1>(p, st) : launch_fwd<128, 4, 1, true, 1>(p, st);
+}
+
+hipError_t launch_prompt_bwd_f32(const PromptParams& p, int32_t D, bool small, hipStream_t st) {
     if (D == 64) {
-        hipLaunchKernelGGL((prompt_dq_f32_kernel<64, 2>), grid, dim3(256), 0, st, p, (int32_t)slots);
-        hipLaunchKernelGGL((prompt_dkdv_f32_kernel<64, 1>), kv_grid, dim3(256), 0, st, p, (int32_t)slots);
+        if (small) {
+            launch_dq<64, 2, 4, false, 2>(p, st);
+            launch_dkdv<64, 2, 4, false, 2>(p, st);
+        } else {
+            launch_dq<64, 4, 1, true, 2>(p, st);
+            launch_dkdv<64, 4, 1, true, 1>(p, st);
+        }
+    } else if (small) {
+        launch_dq<128, 2, 2, false, 1>(p, st);
+        launch_dkdv<128, 2, 2, false, 1>(p, st);
     } else {
-        hipLaunchKernelGGL((prompt_dq_f32_kernel<128, 1>), grid, dim3(256), 0, st, p, (int32_t)slots);
-        hipLaunchKernelGGL((prompt_dkdv_f32_kernel<128, 1>), kv_grid, dim3(256), 0, st, p, (int32_t)slots);
+        launch_dq<128, 4, 1, true, 1>(p, st);
+        launch_dkdv<128, 4, 1, true, 1>(p, st);
     }
     return hipGetLastError();
 }

@@ -366,8 +366,8 @@ hipError_t launch(const PromptParams& p, hipStream_t st) {
 
 }  // namespace
 
-hipError_t launch_prompt_fwd(const PromptParams& p, bool f32, int32_t D, const ChipShape&, hipStream_t st) {
-    if (f32) return launch_prompt_fwd_f32(p, D, st);
+hipError_t launch_prompt_fwd(const PromptParams& p, bool f32, int32_t D, const ChipShape& chip, hipStream_t st) {
+    if (f32) return launch_prompt_fwd_f32(p, D, prompt_small(p.T, p.B, p.H, chip), st);
     return D == 64 ? launch<64, 2>(p, st) : launch<128, 1>(p, st);
 }
 
