@@ -7,6 +7,8 @@
 // sequence's keys in blocks of 32, which go global -> LDS several stages ahead (global_load_lds).  Per block S^T = K Q^T and O^T +=
 // V^T P^T on v_mfma_f32_32x32x16_bf16; the registers of S^T, rounded, are the operand P^T as they stand.  Work is in beats: the
 // products of the next block's scores and of the block before, and between them, slot by slot, the exponentials of the block in hand.
+#include <algorithm>
+
 #include "dfa_prompt.h"
 
 namespace dfa {
@@ -173,13 +175,16 @@ struct Wave {
 constexpr int kRing = 4;
 template <int QB> constexpr int kValueRing = 4 * QB;
 
-template <int D, int QB>
+// KG: groups of waves that take every KG-th block of 32 keys (a "block" of the walk is KG of them then) and merge their results at the end.  For launches of
+// fewer workgroups than fit the chip, where the longest walk decides: half the rows, half the walk (1000 tokens, 16 heads of 128: 19.2 us, 24.0 with KG = 1).
+template <int D, int QB, int KG>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_fwd_kernel(const PromptParams p, int32_t slots) {
-    constexpr int R = 128 * QB, kBlock = 32 * D;                                     // rows; elements of a block
-    constexpr int kCopies = 2 * kPromptCopies<D>;                                    // a wave's, of a block's keys and values
-    __shared__ __attribute__((aligned(1024))) uint16_t lds[kRing + kValueRing<QB>][kBlock];
+    constexpr int kRowGroups = 4 / KG, R = 32 * QB * kRowGroups, kBlock = 32 * D;    // rows; elements of 32 keys or values
+    constexpr int kCopies = 2 * KG * kPromptCopies<D>;                               // a wave's, of a block's keys and values
+    __shared__ __attribute__((aligned(1024))) uint16_t lds[kRing + kValueRing<QB>][KG][kBlock];
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, g = lane >> 5;
+    const int rg = wave % kRowGroups, kg = wave / kRowGroups;
     int32_t slot, h;
     prompt_place(blockIdx.x, slots, p.H, slot, h);
     const PromptTile tile = prompt_tile<R>(p, slot, lane);
@@ -189,35 +194,39 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     uint16_t* const out = static_cast<uint16_t*>(p.out) + (row0 * p.H + h) * D;
     float* const lse = p.lse ? p.lse + (int64_t)h * p.T + row0 : nullptr;
     if (tile.rest) {
-        for (int i = tid; i < rows * (D / 8); i += 256) *reinterpret_cast<u32x4*>(out + (int64_t)(i / (D / 8)) * p.H * D + 8 * (i % (D / 8))) = u32x4{0u, 0u, 0u, 0u};
+        zero_rows<D>(out, (int64_t)p.H * D, rows);
         if (lse)
             for (int i = tid; i < rows; i += 256) lse[i] = -INFINITY;
         return;
     }
 
     const int32_t keys = p.causal ? tile.t0 + rows : tile.n;                         // that the tile's rows attend to
-    const int32_t n_steps = (keys + 63) / 64;                                        // pairs of blocks
-    const int32_t my0 = tile.t0 + 32 * QB * wave;                                    // the wave's first row in the sequence
+    const int32_t n_steps = (keys + 64 * KG - 1) / (64 * KG);                        // pairs of blocks
+    const int32_t my0 = tile.t0 + 32 * QB * rg;                                      // the wave's first row in the sequence
     const bool live = my0 < tile.n;
-    const int32_t my_steps = p.causal ? (min(my0 + 32 * QB, keys) + 63) / 64 : n_steps;
+    const int32_t my_steps = p.causal ? (min(my0 + 32 * QB, keys) + 64 * KG - 1) / (64 * KG) : n_steps;
 
     const char* const kbase = reinterpret_cast<const char*>(static_cast<const uint16_t*>(p.k) + tile.first * p.skn + (h / p.group) * p.skh);
     const char* const vbase = reinterpret_cast<const char*>(static_cast<const uint16_t*>(p.v) + tile.first * p.svn + (h / p.group) * p.svh);
     const uint32_t kpitch = (uint32_t)(p.skn * 2), vpitch = (uint32_t)(p.svn * 2);
-    const uint32_t lds_addr = (uint32_t)(uintptr_t)DFA_LDS_PTR(void, &lds[0][0]);
-    constexpr uint32_t kBytes = kBlock * 2, kValuesAt = kRing * kBytes;
-    auto key_slot = [](int32_t n) { return (uint32_t)(n & (kRing - 1)) * kBytes; };
-    auto value_slot = [](int32_t n) { return (uint32_t)(n & (kValueRing<QB> - 1)) * kBytes; };
+    const uint32_t lds_addr = (uint32_t)(uintptr_t)DFA_LDS_PTR(void, &lds[0][0][0]);
+    constexpr uint32_t kBytes = kBlock * 2, kValuesAt = kRing * KG * kBytes;
+    auto key_slot = [](int32_t n) { return (uint32_t)(n & (kRing - 1)) * (KG * kBytes); };
+    auto value_slot = [](int32_t n) { return (uint32_t)(n & (kValueRing<QB> - 1)) * (KG * kBytes); };
     BlockCopies<D, PromptOrder::kKeys> key_copies;
     BlockCopies<D, PromptOrder::kValues> value_copies;
     key_copies.begin(kpitch, wave, lane);
     value_copies.begin(vpitch, wave, lane);
     const int32_t n_blocks = 2 * n_steps;
     auto issue_keys = [&](int32_t n) {
-        if (n < n_blocks) key_copies(kbase, kpitch, 32 * n, keys, wave, lane, lds_addr + key_slot(n));
+        if (n < n_blocks)
+#pragma unroll
+            for (int i = 0; i < KG; ++i) key_copies(kbase, kpitch, 32 * (KG * n + i), keys, wave, lane, lds_addr + key_slot(n) + i * kBytes);
     };
     auto issue_values = [&](int32_t n) {
-        if (n < n_blocks) value_copies(vbase, vpitch, 32 * n, keys, wave, lane, lds_addr + kValuesAt + value_slot(n));
+        if (n < n_blocks)
+#pragma unroll
+            for (int i = 0; i < KG; ++i) value_copies(vbase, vpitch, 32 * (KG * n + i), keys, wave, lane, lds_addr + kValuesAt + value_slot(n) + i * kBytes);
     };
 
     Wave<D, QB> w;
@@ -225,7 +234,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         const uint16_t* const q = static_cast<const uint16_t*>(p.q) + row0 * p.sqn + h * p.sqh;
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
-            const int64_t row = min(32 * QB * wave + 32 * qb + j, rows - 1);
+            const int64_t row = min(32 * QB * rg + 32 * qb + j, rows - 1);
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) w.q[qb][kk] = *reinterpret_cast<const bf16x8*>(q + row * p.sqn + 16 * kk + 8 * g);
         }
@@ -245,12 +254,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     __syncthreads();
 
     w.c = uniform_float(p.scale * kLog2e);
-    w.key.begin(lds_addr, lane);
-    w.value.begin(lds_addr + kValuesAt, lane);
+    w.key.begin(lds_addr + kg * kBytes, lane);
+    w.value.begin(lds_addr + kValuesAt + kg * kBytes, lane);
     w.begin();
 
-    // scores that a row does not see, of the block from key k0 on
-    auto mask = [&](floatx16 (&s)[QB], int32_t k0) {
+    // scores that a row does not see, of the wave's part of block n
+    auto mask = [&](floatx16 (&s)[QB], int32_t n) {
+        const int32_t k0 = 32 * (KG * n + kg);
         if (k0 + 32 <= (p.causal ? min(my0 + 1, keys) : keys)) return;
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
@@ -294,7 +304,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         }
         enter(2 * s + 3);
         if (more) {
-            mask(s_a, 64 * s + 64);
+            mask(s_a, 2 * s + 2);
             w.template beat<true, true>(key_slot(2 * s + 3), value_slot(2 * s + 1), s_a, s_b, p_b, p_a, psum);
             w.settle(s_a, p_a, psum);
         }
@@ -302,8 +312,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     enter(n_blocks);
     if (live) {
         const int32_t last = 2 * my_steps - 1;
-        mask(s_b, 32 * last);
-        odd = prompt_odd_values<D>(lds[kRing + ((last - 1) & (kValueRing<QB> - 1))]) || prompt_odd_values<D>(lds[kRing + (last & (kValueRing<QB> - 1))]);
+        mask(s_b, last);
+        odd = prompt_odd_values<D>(lds[kRing + ((last - 1) & (kValueRing<QB> - 1))][kg]) || prompt_odd_values<D>(lds[kRing + (last & (kValueRing<QB> - 1))][kg]);
         w.template beat<false, true>(0, value_slot(last - 1), s_b, s_a, p_a, p_b, psum);
         w.settle(s_b, p_b, psum);
         w.accumulate(value_slot(last), p_b);
@@ -325,30 +335,64 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         w.begin();
         for (int32_t n = 0; n < 2 * n_steps; ++n) {
             __syncthreads();                 // the flags, and block n - 1, have been read
-            prompt_copy<D, PromptOrder::kKeys>(kbase, kpitch, 32 * n, keys, wave, lane_e, lds_addr);
-            prompt_copy<D, PromptOrder::kValues>(vbase, vpitch, 32 * n, keys, wave, lane_e, lds_addr + kValuesAt);
+#pragma unroll
+            for (int i = 0; i < KG; ++i) {
+                prompt_copy<D, PromptOrder::kKeys>(kbase, kpitch, 32 * (KG * n + i), keys, wave, lane_e, lds_addr + i * kBytes);
+                prompt_copy<D, PromptOrder::kValues>(vbase, vpitch, 32 * (KG * n + i), keys, wave, lane_e, lds_addr + kValuesAt + i * kBytes);
+            }
             wait_vmcnt<0>();
             __syncthreads();
             if (!live || n >= 2 * my_steps) continue;
             w.scores(0, s_a);
-            mask(s_a, 32 * n);
+            mask(s_a, n);
             w.template beat<false, false>(0, 0, s_a, s_b, p_b, p_a, psum);
             w.settle(s_a, p_a, psum);
             int32_t last[QB];
 #pragma unroll
-            for (int qb = 0; qb < QB; ++qb) last[qb] = min(p.causal ? my0 + 32 * qb + je : keys - 1, keys - 1) - 32 * n;
-            w.accumulate_odd(0, lds[kRing], p_a, last, lane_e);
+            for (int qb = 0; qb < QB; ++qb) last[qb] = min(p.causal ? my0 + 32 * qb + je : keys - 1, keys - 1) - 32 * (KG * n + kg);
+            w.accumulate_odd(0, lds[kRing][kg], p_a, last, lane_e);
         }
         __syncthreads();
+    }
+    float total[QB];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) total[qb] = wave_half_sum(w.sum[qb]);
+    if constexpr (KG > 1) {
+        // the groups' references, sums and accumulators
+        static_assert(KG == 2 && QB == 1, "two groups, of one block of rows a wave");
+        float* const stats = reinterpret_cast<float*>(lds);                          // [KG][2][R]
+        float4* const accs = reinterpret_cast<float4*>(reinterpret_cast<char*>(lds) + 4096) + rg * (D / 8 * 64) + lane_e;
+        static_assert(sizeof(lds) >= 4096 + kRowGroups * D / 8 * 64 * 16 + 16 && KG * 2 * R * 4 <= 4096, "they fit");
+        if (ge == 0) stats[(2 * kg) * R + 32 * rg + je] = w.ref[0], stats[(2 * kg + 1) * R + 32 * rg + je] = total[0];
+        __syncthreads();
+        const float other_ref = stats[(2 * (1 - kg)) * R + 32 * rg + je], other = stats[(2 * (1 - kg) + 1) * R + 32 * rg + je];
+        const float top = fmaxf(w.ref[0], other_ref), by = __builtin_amdgcn_exp2f(w.ref[0] - top);
+        total[0] = total[0] * by + other * __builtin_amdgcn_exp2f(other_ref - top);
+        w.ref[0] = top;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+            floatx16& x = w.acc[i >> 2][0];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[4 * (i & 3) + e] *= by;
+            if (kg == 1) accs[64 * i] = make_float4(x[4 * (i & 3)], x[4 * (i & 3) + 1], x[4 * (i & 3) + 2], x[4 * (i & 3) + 3]);
+        }
+        __syncthreads();
+        if (kg == 1) return;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+            floatx16& x = w.acc[i >> 2][0];
+            const float4 y = accs[64 * i];
+            x[4 * (i & 3)] += y.x, x[4 * (i & 3) + 1] += y.y, x[4 * (i & 3) + 2] += y.z, x[4 * (i & 3) + 3] += y.w;
+        }
+        __syncthreads();                     // (of the waves that are left)
     }
     if (!live) return;
     char* const mine = reinterpret_cast<char*>(lds) + wave * (32 * kPitch);
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-        const float total = wave_half_sum(w.sum[qb]);
-        const float inv = total == 0.f ? 0.f : 1.0f / total;
-        const int r0 = 32 * QB * wave + 32 * qb;
-        if (lse && ge == 0 && r0 + je < rows) lse[r0 + je] = total == 0.f ? -INFINITY : (w.ref[qb] + __builtin_amdgcn_logf(total)) * kLn2;
+        const float inv = total[qb] == 0.f ? 0.f : 1.0f / total[qb];
+        const int r0 = 32 * QB * rg + 32 * qb;
+        if (lse && ge == 0 && r0 + je < rows) lse[r0 + je] = total[qb] == 0.f ? -INFINITY : (w.ref[qb] + __builtin_amdgcn_logf(total[qb])) * kLn2;
         floatx16 acc[D / 32];
 #pragma unroll
         for (int db = 0; db < D / 32; ++db) acc[db] = w.acc[db][qb];
@@ -357,10 +401,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     }
 }
 
-template <int D, int QB>
+template <int D, int QB, int KG>
 hipError_t launch(const PromptParams& p, hipStream_t st) {
-    const int64_t slots = prompt_slots(p.T, p.B, 128 * QB);
-    hipLaunchKernelGGL((prompt_fwd_kernel<D, QB>), dim3((unsigned)(slots * p.H)), dim3(256), 0, st, p, (int32_t)slots);
+    const int64_t slots = prompt_slots(p.T, p.B, 128 * QB / KG);
+    hipLaunchKernelGGL((prompt_fwd_kernel<D, QB, KG>), dim3((unsigned)(slots * p.H)), dim3(256), 0, st, p, (int32_t)slots);
     return hipGetLastError();
 }
 
@@ -368,7 +412,15 @@ hipError_t launch(const PromptParams& p, hipStream_t st) {
 
 hipError_t launch_prompt_fwd(const PromptParams& p, bool f32, int32_t D, const ChipShape& chip, hipStream_t st) {
     if (f32) return launch_prompt_fwd_f32(p, D, prompt_small(p.T, p.B, p.H, chip), st);
-    return D == 64 ? launch<64, 2>(p, st) : launch<128, 1>(p, st);
+    // What is known of the lengths is their mean.  Two groups of waves to a walk where the workgroups of half the rows are resident at once (two to a compute unit, one of
+    // D = 128), or where walks are so long that twice as many do (us with one group / two: 12 heads of 64, 1000 tokens 19.0 / 14.1, 4000 60.5 / 44.3, 4 x 512 12.3 / 11.6,
+    // 8 x 512 14.6 / 19.2; 16 heads of 128, 300 tokens 10.9 / 11.3, 1000 24.0 / 19.2, 2000 42.2 / 39.2, 4000 88 / 123).
+    const int64_t mean = p.T / p.B, halves = std::max<int64_t>((p.T + 63) / 64, std::min(p.T, p.B)) * p.H, resident = (D == 64 ? 2 : 1) * (int64_t)chip.cus;
+    if (mean >= 384 && (halves <= resident || (mean >= 1536 && halves <= 2 * resident))) return D == 64 ? launch<64, 1, 2>(p, st) : launch<128, 1, 2>(p, st);
+    if (D == 128) return launch<128, 1, 1>(p, st);
+    // 64 rows to a wave (a fragment read feeds two products) where that leaves enough workgroups (12 heads, us with 32 rows / 64: 8 x 512 tokens 14.4 / 23.1, 16 x 512 24.1 /
+    // 24.3, 27000 tokens of 32 heads 291 / 259)
+    return ((int64_t)p.T / 128 + std::min(p.T, p.B)) * p.H < 4 * chip.cus ? launch<64, 1, 1>(p, st) : launch<64, 2, 1>(p, st);
 }
 
 }  // namespace dfa
