@@ -228,3 +228,64 @@ def test_a_captured_layer(B):
             assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
         for name in ("lengths", "table", "n_free"):
             assert torch.equal(steps[0][name], steps[1][name])
+
+
+def test_native_calls(B, monkeypatch):
+    """The ordinary calls in native code against the ones that Python marshals: the same bits."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    rand = lambda *shape, dtype=torch.bfloat16: torch.randn(shape, generator=gen, device="cuda").to(dtype)
+    for dtype in (torch.bfloat16, torch.float32):
+        x, q, starts = rand(90, 200, dtype=dtype), rand(90, 8, 64, dtype=dtype), _ints([0, 30, 30, 85])
+        w, r, dout = rand(200, dtype=dtype), rand(90, 200, dtype=dtype), rand(90, 4, 64, dtype=dtype)
+
+        def calls():
+            out, lse = B.prompt_attention(q[:, :4], q[:, 4:6], q[:, 6:], starts, 0.125)
+            got = [out, lse, *B.prompt_attention_backward(q[:, :4], q[:, 4:6], q[:, 6:], out, lse, dout, starts, 0.125, False)]
+            for residual in (None, r):
+                for quantized in (False, True, "both"):
+                    y, h = B.rms_norm(x, w, 1e-6, residual=residual, quantized=quantized)
+                    y = y if quantized == "both" else (y,)
+                    for part in y:
+                        got += [part.values.view(torch.uint8), part.scales[:, :90]] if isinstance(part, B.QuantizedMatrix) else [part]
+                    got += [h] if h is not None else []
+            got += B.rms_norm_backward(x, r, w, 1e-6) + B.rms_norm_backward(x, r, None, 1e-6, dh=x)
+            table = _ints([[0] * 4, [0] * 4])
+            got += [*B.cache_reserve(_ints([20, 1]), _ints([0, 0]), table, _ints([5, 6, 7, 8]), _ints([4]), 16, 30), table]
+            cache = B.kv_cache(9, 2, 16, 64)
+            B.cache_append(q[:, 4:6], q[:, 6:], cache, table, _ints([20, 1]), starts=_ints([0, 20, 21]))
+            return got + [t.view(torch.uint8) for t in cache]
+
+        native = calls()
+        with monkeypatch.context() as m:
+            m.setattr(B, "_native_call", lambda *a: None)
+            python = calls()
+        assert len(native) == len(python)
+        for a, b in zip(native, python):
+            assert a.dtype == b.dtype and a.shape == b.shape and torch.equal(a, b)
+
+
+def test_refusals(B):
+    import torch
+    q, starts = torch.zeros((10, 4, 64), dtype=torch.bfloat16, device="cuda"), _ints([0, 10])
+    k = q[:, :2]
+    out, lse = B.prompt_attention(q, k, k, starts, 0.125)
+    for error, call in (
+            (B.DfaError, lambda: B.prompt_attention(q, q[:, :3], q[:, :3], starts, 0.125)), (B.DfaError, lambda: B.prompt_attention(q, k, k[:5], starts, 0.125)),
+            (B.DfaError, lambda: B.prompt_attention(q, k[:5], k[:5], starts, 0.125)), (B.DfaError, lambda: B.prompt_attention(q, k.float(), k, starts, 0.125)),
+            (B.DfaError, lambda: B.prompt_attention(q.half(), k.half(), k.half(), starts, 0.125)), (B.DfaError, lambda: B.prompt_attention(q, k, k, starts, -1.0)),
+            (B.DfaError, lambda: B.prompt_attention(q, k, k, starts[:1], 0.125)), (TypeError, lambda: B.prompt_attention(q, k, k, starts.long(), 0.125)),
+            (RuntimeError, lambda: B.prompt_attention(q, k, k, starts.cpu(), 0.125)), (B.DfaError, lambda: B.prompt_attention(q[..., :32], k[..., :32], k[..., :32], starts, 0.125)),
+            (B.DfaError, lambda: B.prompt_attention(q.transpose(1, 2), k, k, starts, 0.125)), (B.DfaError, lambda: B.prompt_attention(q, k, k, starts, 0.125, out=out[:5])),
+            (B.DfaError, lambda: B.prompt_attention(q, k, k, starts, 0.125, lse=lse.double())),
+            (B.DfaError, lambda: B.prompt_attention_backward(q, k, k, out, lse[:, :5], q, starts, 0.125)),
+            (B.DfaError, lambda: B.prompt_attention_backward(q, k, k, out, lse, q, starts, 0.125, workspace=None)),
+            (B.DfaError, lambda: B.prompt_attention_backward(q, k, k, out, lse, q, starts, 0.125, workspace=torch.zeros((16,), dtype=torch.uint8, device="cuda"))),
+            (B.DfaError, lambda: B.cache_reserve(_ints([1]), _ints([0, 0]), _ints([[0]]), _ints([0]), _ints([1]), 16, 5)),
+            (B.DfaError, lambda: B.cache_reserve(_ints([1]), _ints([0]), _ints([[0]]), _ints([0]), _ints([1]), 20, 5)),
+            (B.DfaError, lambda: B.cache_reserve(_ints([1]), _ints([0]), _ints([[0]]), _ints([0]), _ints([1]), 16, 0)),
+            (TypeError, lambda: B.cache_reserve(_ints([1]).long(), _ints([0]), _ints([[0]]), _ints([0]), _ints([1]), 16, 5)),
+            (B.DfaError, lambda: B.cache_append(k, k, B.kv_cache(2, 3), _ints([[0, 1]]), _ints([10]), starts=starts)),
+            (ValueError, lambda: B.cache_append(k, k, B.kv_cache(2, 2), _ints([[0, 1]]), _ints([10]), counts=_ints([1]), starts=starts))):
+        with pytest.raises(error):
+            call()

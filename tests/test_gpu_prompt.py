@@ -87,10 +87,29 @@ def test_long(B, D, dtype):
     _check(B, [1500, 37], 2, 1, D, dtype, True, behind=200)
 
 
-def test_many_sequences(B):
-    """More sequences than a wave has lanes, and than 64 times that."""
-    _check(B, [3] * 300, 1, 1, 64, "bf16", True)
-    _check(B, [1, 0] * 2500 + [90], 1, 1, 64, "bf16", True, backward=False)
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_tiles(B, D, causal, dtype):
+    """Launches of many workgroups: larger tiles, dk and dv of a whole group in one workgroup."""
+    _check(B, [40] * 60 + [200] + [7] * 10, 16, 8, D, dtype, causal, behind=70)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [384, 449, 640])
+def test_one_prompt(B, n, D, causal, dtype):
+    """Few tiles of a long walk: waves share it out."""
+    _check(B, [n], 2, 1, D, dtype, causal, backward=n == 449)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_many_sequences(B, dtype):
+    """More sequences than a wave has lanes, than are ranked, and than 64 times 64."""
+    _check(B, [3] * 100 + [130] + [2] * 100, 1, 1, 64, dtype, True)
+    _check(B, [3] * 300, 1, 1, 64, dtype, True, behind=40)
+    _check(B, [1, 0] * 2500 + [90], 1, 1, 64, dtype, True, backward=False)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
@@ -115,31 +134,35 @@ def test_climbing_scores(B, D, dtype):
     _within(lse, l, l_tol, "lse")
 
 
+# two sequences of a few tiles; one whose walk waves share; many tiles (the value lies in the second sequence, row 50 of it, or row 500 of the only one)
+@pytest.mark.parametrize("lengths,H,at", [([150, 140], 4, 200), ([600], 4, 500), ([150] + [90] * 69, 16, 200)], ids=["few", "shared", "many"])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
-def test_values_behind_the_mask(B, value, D, dtype):
+def test_values_behind_the_mask(B, value, D, dtype, lengths, H, at):
     """A value or key that is not finite reaches the rows that see it, in that head group, and no other."""
     import torch
-    starts, at = [0, 150, 290], 200
-    q, k, v, _ = _make(5, 290, 4, 2, D, dtype)
+    starts = ref.starts_of(lengths)
+    T, end = starts[-1], next(s for s in starts if s > at)
+    q, k, v, _ = _make(5, T, H, H // 2, D, dtype)
     clean = B.prompt_attention(q, k, v, _ints(starts), D ** -0.5, True)
+    sees = torch.zeros((T,), dtype=torch.bool, device="cuda")
+    sees[at:end] = True
     for tensor in ("v", "k"):
         k2, v2 = k.clone(), v.clone()
         (v2 if tensor == "v" else k2)[at, 1, 7] = value
         out, lse = B.prompt_attention(q, k2, v2, _ints(starts), D ** -0.5, True)
-        for h in range(4):
-            before, other = torch.arange(290) < at, h < 2
-            keep = before if not other else torch.ones_like(before)
-            # rows of another head or before it: the same weights over the same values, each side within the bounds of 140 keys with |v| < 5
-            off = 2 * 5 * (2 * (140 + 66) * ref.E + ref.U[out.dtype])
-            torch.testing.assert_close(out[keep.cuda(), h].float(), clean[0][keep.cuda(), h].float(), rtol=2 * ref.U[out.dtype], atol=off)
-            torch.testing.assert_close(lse[h][keep.cuda()], clean[1][h][keep.cuda()], rtol=1e-6, atol=1e-5)
-            if not other and tensor == "v":
-                hit = out[at:, h, 7].float()
-                assert (~hit.isfinite()).all() and out[at:, h, :7].float().isfinite().all()
-                if value == value and dtype == "bf16":        # (in parts an infinite number may come out as NaN)
-                    assert (hit == value).all()
+        hit = torch.zeros((T, H), dtype=torch.bool, device="cuda")
+        hit[:, 2:4] = sees[:, None]
+        # rows of another head, sequence, or before it: the same weights over the same values, each side within the bounds of n keys with |v| < 6
+        off = 2 * 6 * ((7 * max(lengths) + 80) * ref.E + (ref.U[out.dtype] if dtype == "bf16" else 0.0))
+        torch.testing.assert_close(out[~hit].float(), clean[0][~hit].float(), rtol=2 * ref.U[out.dtype], atol=off)
+        torch.testing.assert_close(lse.t()[~hit], clean[1].t()[~hit], rtol=1e-6, atol=2 * (max(lengths) + 66) * ref.E)
+        if tensor == "v":
+            got = out[hit].float()
+            assert (~got[:, 7].isfinite()).all() and got[:, :7].isfinite().all() and got[:, 8:].isfinite().all()
+            if value == value and dtype == "bf16":        # (in parts an infinite number may come out as NaN)
+                assert (got[:, 7] == value).all()
 
 
 def test_rows_see_only_their_own(B):
