@@ -450,7 +450,8 @@ int dfa_release_plans(void);
  *   out     device, dtype dt, contiguous [T, H, D], apart from q, k and v;  lse device, fp32 [H, T], or NULL
  *           rows of no sequence (from starts[B] on) are 0 and -inf
  * bf16: probabilities are rounded to bf16 before they meet v; sums are fp32.  fp32: products of three bf16 parts a number (24 bits; bits
- * below 2^-133 are lost, and what rounds to 2^128 in bf16 counts as infinite).  scale * q . k must be an fp32 number.
+ * below 2^-133 are lost, and what rounds to 2^128 in bf16 counts as infinite).  scale lies within 2^-100 .. 2^100, and every scale * q . k
+ * within 2^127 ln 2 either way.
  * Sums are in a fixed order: equal calls give equal results.  Asynchronous on `stream`; allocates nothing.
  */
 int dfa_prompt_attention(const void *q, const void *k, const void *v, dfa_strides_t sq, dfa_strides_t sk, dfa_strides_t sv, dfa_dtype_t dt, int32_t T,

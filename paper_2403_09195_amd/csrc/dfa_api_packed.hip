@@ -17,6 +17,8 @@ using namespace dfa;
 constexpr int64_t kMaxThreads = (int64_t)1 << 32;   // a grid holds fewer
 constexpr int64_t kMaxRowBytes = (int64_t)1 << 25;  // between rows of k and v: 64 rows are addressed with 32-bit offsets
 
+constexpr float kLeastScale = 0x1p-100f;            // lse / scale, which the backward's scores start from, is an fp32 number
+
 bool grid_fits(int64_t workgroups, int64_t threads) { return workgroups < kMaxThreads / threads; }
 bool known(dfa_dtype_t dt) { return dt == DFA_BF16 || dt == DFA_F32; }
 int64_t size_of(dfa_dtype_t dt) { return dt == DFA_BF16 ? 2 : 4; }
@@ -58,7 +60,7 @@ int prompt_params(const void* q, const void* k, const void* v, dfa_strides_t sq,
     if (!known(dt)) return DFA_ERR_DTYPE;
     const int rc = check_prompt_sizes(T, H, Hkv, D, B);
     if (rc != DFA_OK) return rc;
-    if (!std::isfinite(scale) || scale <= 0.f) return DFA_ERR_SHAPE;
+    if (!(scale >= kLeastScale && scale <= 1.f / kLeastScale)) return DFA_ERR_SHAPE;
     const int64_t es = size_of(dt);
     if (!rows_aligned(q, sq, es) || !rows_aligned(k, sk, es) || !rows_aligned(v, sv, es) || !aligned(starts, 4)) return DFA_ERR_ALIGN;
     for (const dfa_strides_t& s : {sq, sk, sv})
@@ -165,10 +167,7 @@ int dfa_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, 
     }
     p.x = x, p.residual = residual, p.weight = weight, p.ldx = ldx, p.ldr = ldr, p.M = M, p.C = C, p.eps = eps;
     p.h = h, p.y = y, p.ldh = ldh, p.ldy = ldy;
-    ChipShape chip;
-    rc = this_chip(&chip);
-    if (rc != DFA_OK) return rc;
-    return status(launch_norm(p, dt == DFA_F32, weight && weight_dt == DFA_F32, chip, static_cast<hipStream_t>(stream)));
+    return status(launch_norm(p, dt == DFA_F32, weight && weight_dt == DFA_F32, static_cast<hipStream_t>(stream)));
 }
 
 size_t dfa_rms_norm_backward_workspace_bytes(int64_t M, int64_t C) {

@@ -16,7 +16,7 @@ struct NormParams {
     uint8_t *values, *scales;               // may be NULL: y in blocks of 128 (dfa_scaled.h)
     int64_t ldv, lds;
 };
-hipError_t launch_norm(const NormParams& p, bool f32, bool weight_f32, const ChipShape& chip, hipStream_t st);
+hipError_t launch_norm(const NormParams& p, bool f32, bool weight_f32, hipStream_t st);
 
 struct NormBackwardParams {
     const void *dy, *h, *weight, *dh;       // dh and weight may be NULL

@@ -281,16 +281,16 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(const float* parts, floa
     for (int32_t i = group; i < count; i += 64) s += parts[i * C + c];
     lds[group][col] = s;
     __syncthreads();
-    if (group >= 16) return;
-    // thread (col, group): 16 sums of four, then lanes 16 apart and waves
-    float q = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) q += lds[4 * group + i][col];
-    q += __shfl_xor(q, 16);
-    q += __shfl_xor(q, 32);
+    // thread (col, group) of the first four waves: 16 sums of four, then lanes 16 apart and waves
     __shared__ float waves[4][16];
-    if ((threadIdx.x & 63) < 16) waves[threadIdx.x >> 6][col] = q;
-    // (four waves are left: the others have ended)
+    if (group < 16) {
+        float q = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q += lds[4 * group + i][col];
+        q += __shfl_xor(q, 16);
+        q += __shfl_xor(q, 32);
+        if ((threadIdx.x & 63) < 16) waves[threadIdx.x >> 6][col] = q;
+    }
     __syncthreads();
     if (group == 0 && (int64_t)blockIdx.x * 16 + col < C) dw[c] = waves[0][col] + waves[1][col] + waves[2][col] + waves[3][col];
 }
@@ -337,7 +337,7 @@ hipError_t launch_any(const Params& p, NormForm f, bool f32, bool weight_f32, hi
 
 }  // namespace
 
-hipError_t launch_norm(const NormParams& p, bool f32, bool weight_f32, const ChipShape&, hipStream_t st) {
+hipError_t launch_norm(const NormParams& p, bool f32, bool weight_f32, hipStream_t st) {
     return launch_any(p, norm_form(p.M, p.values ? (p.C + 127) / 128 * 128 : p.C), f32, weight_f32, st);
 }
 

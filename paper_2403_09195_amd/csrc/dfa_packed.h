@@ -66,7 +66,7 @@ struct RankedTile {
 };
 template <int R>
 __device__ __forceinline__ RankedTile packed_ranked(const int32_t* starts, int32_t B, int32_t T, int32_t rank, int lane) {
-    int32_t tiles[kRankedPerLane], most = 0;
+    int32_t tiles[kRankedPerLane];
 #pragma unroll
     for (int i = 0; i < kRankedPerLane; ++i) {
         const int32_t b = 64 * i + lane;
@@ -77,7 +77,6 @@ __device__ __forceinline__ RankedTile packed_ranked(const int32_t* starts, int32
 #pragma unroll
     for (int i = 0; i < kRankedPerLane; ++i) all += tiles[i];
     all = wave_total(all);
-    most = all;
     RankedTile t;
     const int32_t last = packed_start(starts, B, T);
     if (rank >= all) {
@@ -91,7 +90,7 @@ __device__ __forceinline__ RankedTile packed_ranked(const int32_t* starts, int32
         for (int i = 0; i < kRankedPerLane; ++i) n += max(tiles[i] - m + 1, 0);
         return wave_total(n);
     };
-    int32_t lo = 1, hi = min(most, (T + R - 1) / R);              // the highest level with above(level) > rank is in lo .. hi
+    int32_t lo = 1, hi = min(all, (T + R - 1) / R);              // the highest level with above(level) > rank is in lo .. hi
     while (lo < hi) {
         const int32_t mid = lo + (hi - lo + 1) / 2;
         if (above(mid) > rank) lo = mid;

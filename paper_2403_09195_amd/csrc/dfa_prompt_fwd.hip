@@ -377,16 +377,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             if (kg == 1) accs[64 * i] = make_float4(x[4 * (i & 3)], x[4 * (i & 3) + 1], x[4 * (i & 3) + 2], x[4 * (i & 3) + 3]);
         }
         __syncthreads();
-        if (kg == 1) return;
+        if (kg == 0)
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-            floatx16& x = w.acc[i >> 2][0];
-            const float4 y = accs[64 * i];
-            x[4 * (i & 3)] += y.x, x[4 * (i & 3) + 1] += y.y, x[4 * (i & 3) + 2] += y.z, x[4 * (i & 3) + 3] += y.w;
-        }
-        __syncthreads();                     // (of the waves that are left)
+            for (int i = 0; i < D / 8; ++i) {
+                floatx16& x = w.acc[i >> 2][0];
+                const float4 y = accs[64 * i];
+                x[4 * (i & 3)] += y.x, x[4 * (i & 3) + 1] += y.y, x[4 * (i & 3) + 2] += y.z, x[4 * (i & 3) + 3] += y.w;
+            }
+        __syncthreads();                     // the sums have been read: the rows take their place
     }
-    if (!live) return;
+    if (!live || kg != 0) return;
     char* const mine = reinterpret_cast<char*>(lds) + wave * (32 * kPitch);
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {

@@ -158,20 +158,20 @@ template <int kBlock>
 __global__ __launch_bounds__(kBlock) void reserve_small_kernel(const ReserveParams p, bool with_rows) {
     __shared__ int32_t rows_lds[kBlock], pages_lds[kBlock], had_lds[kBlock], held_lds[kBlock];
     __shared__ int32_t wave_rows[kBlock / 64], wave_pages[kBlock / 64], wave_wrong[kBlock / 64];
+    __shared__ unsigned long long asked;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int32_t mask = (1 << p.page_shift) - 1;
     const bool there = tid < p.B;
     const int32_t held = there ? p.lengths[tid] : 0, fresh = there ? p.counts[tid] : 0, in_hand = *p.n_free;
     const int32_t n_free = min(max(in_hand, 0), p.capacity);
     const int64_t had = ((int64_t)held + mask) >> p.page_shift, has = ((int64_t)held + fresh + mask) >> p.page_shift;
-    const int32_t my_rows = min(fresh, p.rows + 1), my_pages = (int32_t)min(has - had, (int64_t)p.rows + 2);
+    const int32_t my_rows = min(fresh, p.rows + 1), my_pages = (int32_t)min(has - had, (int64_t)p.rows + 2);     // (cut only where there are too many rows)
     const uint64_t wide = __ballot(has > p.width), below = __ballot(held < 0 || fresh < 0);
-    const uint64_t more_pages = __ballot(has - had > n_free);           // (also where my_pages is not all of them)
     const int32_t rows_to = wave_sums(my_rows), pages_to = wave_sums(my_pages);
     if (lane == 63) {
         wave_rows[wave] = rows_to;
         wave_pages[wave] = pages_to;
-        wave_wrong[wave] = (more_pages ? 1 : 0) | (wide ? 2 : 0) | (below ? 8 : 0);
+        wave_wrong[wave] = (wide ? 2 : 0) | (below ? 8 : 0);
     }
     __syncthreads();
     int32_t rows = 0, pages = 0, wrong = 0, rows_before = 0, pages_before = 0;
@@ -184,6 +184,13 @@ __global__ __launch_bounds__(kBlock) void reserve_small_kernel(const ReservePara
         wrong |= wave_wrong[w];
     }
     wrong |= (pages > n_free ? 1 : 0) | (rows > p.rows ? 4 : 0);
+    if ((wrong & 12) == 4) {                 // (the same for all threads) the pages may be more than were added up
+        if (tid == 0) asked = 0;
+        __syncthreads();
+        if (there) atomicAdd(&asked, (unsigned long long)(has - had));
+        __syncthreads();
+        wrong |= asked > (unsigned long long)n_free ? 1 : 0;
+    }
     if (wrong & 8) wrong = 8;                // the sums mean nothing
     const int32_t first = wrong ? 0 : rows_before + rows_to - my_rows, first_page = pages_before + pages_to - my_pages;
     if (there) {

@@ -95,6 +95,18 @@ def test_a_step_that_does_not_fit(B, rows):
     assert s.reserve(B, [0, 0, 0, 0], rows).refused.item() == 0
 
 
+@pytest.mark.parametrize("rows", [64, 5000, 2 ** 20 + 1])
+def test_reasons_add_up(B, rows):
+    """A step of far more rows than there is room for: whether its pages are too many, too, is still told."""
+    import torch
+    table, free = torch.zeros((2, 500001), dtype=torch.int32, device="cuda"), torch.arange(10 ** 6, dtype=torch.int32, device="cuda")
+    for counts, reasons in (([8 * 10 ** 6] * 2, 4), ([8 * 10 ** 6, 8 * 10 ** 6 + 1], 5), ([0, 16 * 10 ** 6], 6), ([0, 16 * 10 ** 6 + 1], 7)):
+        r = B.cache_reserve(_ints(counts), _ints([0, 0]), table, free, _ints([10 ** 6]), 16, rows)
+        assert r.refused.item() == reasons and r.lengths.tolist() == [0, 0] and r.n_free.item() == 10 ** 6 and r.starts.tolist() == [0, 0, 0]
+        assert (r.slots == -1).all() and (r.positions == -1).all()
+    assert not table.any()
+
+
 def test_a_stack_without_room(B):
     lengths, table, free, n = _ints([30, 40]), _ints([[1, 2, 0], [3, 4, 5]]), _ints([9, 9, 9, 9]), _ints([0])
     before = free.clone()
@@ -289,3 +301,35 @@ def test_refusals(B):
             (ValueError, lambda: B.cache_append(k, k, B.kv_cache(2, 2), _ints([[0, 1]]), _ints([10]), counts=_ints([1]), starts=starts))):
         with pytest.raises(error):
             call()
+
+
+def test_two_streams(B):
+    """Calls that overlap on two streams, each with tensors of its own, against the same calls one after the other."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    sets = []
+    for dtype in (torch.bfloat16, torch.float32):
+        qkv = torch.randn((2500, 16, 64), generator=gen, device="cuda").to(dtype)
+        x, w = torch.randn((2500, 512), generator=gen, device="cuda").to(dtype), torch.randn((512,), generator=gen, device="cuda").to(dtype)
+        sets.append((qkv, x, w, _ints([0, 1200, 1300, 2500]), [_ints([300] * 40), _ints([5] * 40), torch.zeros((40, 10), dtype=torch.int32, device="cuda"),
+                                                              torch.arange(800, dtype=torch.int32, device="cuda"), _ints([800])]))
+
+    def run(qkv, x, w, starts, pages):
+        q, k, v = qkv[:, :8], qkv[:, 8:12], qkv[:, 12:]
+        out, lse = B.prompt_attention(q, k, v, starts, 0.125)
+        y, h = B.rms_norm(x, w, 1e-6, residual=x)
+        return [out, lse, y, h, *B.prompt_attention_backward(q, k, v, out, lse, out, starts, 0.125), *B.rms_norm_backward(y, h, w, 1e-6),
+                *B.cache_reserve(*pages, 64, 12000)]
+
+    want = [run(*s) for s in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    got = [[], []]
+    for _ in range(5):
+        for i, s in enumerate(sets):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(run(*s))
+    torch.cuda.synchronize()
+    for mine, theirs in zip(got, want):
+        for results in mine:
+            assert all(torch.equal(a, b) for a, b in zip(results, theirs))

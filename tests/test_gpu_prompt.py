@@ -182,6 +182,26 @@ def test_rows_see_only_their_own(B):
     assert all(torch.equal(m[50:130], n[50:130]) for m, n in zip(ga, gb))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_least_and_largest_scale(B, dtype):
+    """Powers of two that leave every product as it was leave every result so, but for their own factor."""
+    import torch
+    starts = _ints([0, 70, 200])
+    q, k, v, dout = _make(9, 200, 4, 2, 64, dtype)
+    q = q * 0.25
+
+    def run(by):
+        a, b = q * by, k * by
+        out, lse = B.prompt_attention(a, b, v, starts, 1.0 / (by * by))
+        dq, dk, dv = B.prompt_attention_backward(a, b, v, out, lse, dout, starts, 1.0 / (by * by))
+        return out, lse, dq * by, dk * by, dv
+
+    plain = run(1.0)
+    for by in (2.0 ** 50, 2.0 ** -50):
+        for a, b in zip(run(by), plain):
+            assert a.isfinite().all() and torch.equal(a, b)
+
+
 def test_starts_out_of_range(B):
     """Starts outside the rows count as the nearest; the first is 0."""
     import torch

@@ -19,7 +19,7 @@ def B():
 
 BAD_PROMPTS = [(dict(q=None), -1), (dict(k=None), -1), (dict(v=None), -1), (dict(starts=None), -1), (dict(out=None), -1), (dict(dt=2), -4), (dict(dt=-1), -4),
                (dict(T=0), -2), (dict(Bsz=0), -2), (dict(H=3), -2), (dict(H=1), -2), (dict(Hkv=0), -2), (dict(D=32), -2), (dict(D=96), -2), (dict(scale=0.0), -2),
-               (dict(scale=-1.0), -2), (dict(scale=math.inf), -2), (dict(scale=math.nan), -2), (dict(q=OK + 2), -5), (dict(s=(0, 1024, 60)), -5),
+               (dict(scale=-1.0), -2), (dict(scale=math.inf), -2), (dict(scale=math.nan), -2), (dict(scale=2.0 ** -101), -2), (dict(scale=1.5e30), -2), (dict(q=OK + 2), -5), (dict(s=(0, 1024, 60)), -5),
                (dict(s=(0, 1020, 64)), -5), (dict(starts=OK + 2), -5), (dict(out=OK + 8), -5), (dict(lse=OK + 2), -5), (dict(s=(0, 1 << 24, 64)), -7),
                (dict(s=(0, -1024, 64)), -7), (dict(T=2 ** 31 - 1), -7), (dict(Bsz=2 ** 31 - 1), -7), (dict(T=1 << 30, H=1 << 12, Hkv=1 << 12), -7)]
 
