@@ -16,21 +16,103 @@ namespace dfa {
 
 namespace {
 
-// 16 numbers of a lane -> operands of the second product
-__device__ __forceinline__ void pack(const float (&x)[16], u32x4 (&p)[2]) {
-#pragma unroll
-    for (int v = 0; v < 8; ++v) {
-        const bf16x2 w = {(__bf16)x[2 * v], (__bf16)x[2 * v + 1]};
-        p[v >> 2][v & 3] = __builtin_bit_cast(uint32_t, w);
-    }
-}
+// A wave of the launch of dq: 32 rows, their dq, and one beat of its walk along the keys.
+template <int D>
+struct RowWave {
+    static constexpr int kSteps = D / 16, kHalves = D / 32;
+    bf16x8 q[kSteps], go[kSteps];
+    floatx16 acc[kHalves];
+    float lse2, nd;                  // of the lane's row: lse * log2(e), -delta
+    uint32_t row, turned;                    // where a lane's reads of rows and of columns begin
+    float c;                                 // scale * log2(e)
+    static constexpr int kGroups = 3 * kSteps, kAhead = 3, kBuffers = kAhead + 1;    // products, each of a fragment
+    static_assert(kGroups % kBuffers == 0, "a beat ends where it began");
+    bf16x8 f[kBuffers];
 
-// dq: 128 * QB rows of one head, walked along the keys.  Per block S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.
-template <int D, int QB>
+    __device__ __forceinline__ bf16x8 row_of(uint32_t block, int kk) const {
+        return *reinterpret_cast<__attribute__((address_space(3))) bf16x8*>((row ^ (32u * kk)) + block);
+    }
+    __device__ __forceinline__ bf16x8 column_of(uint32_t block, int i) const {
+        constexpr uint32_t kEight = 16 * (D == 128 ? 2 : 1);
+        const int db = i >> 1, st = i & 1;
+        const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) short4v*>((turned ^ (64u * db)) + block + 32 * st * D));
+        const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) short4v*>((turned ^ (64u * db) ^ kEight) + block + (16 * (2 * st + 1)) * D));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    // Product i of a beat: 0: dP of step r, 1: S of step r, 2: accumulation r.  The first half of them is dP's and half of the accumulation's,
+    // in threes, the second half is S's and the rest.
+    static constexpr int kind(int i) { return i % 3 == 1 ? 2 : i < kGroups / 2 ? 0 : 1; }
+    static constexpr int step(int i) {
+        const int k = i % (kGroups / 2);
+        return i % 3 == 1 ? i / 3 : 2 * (k / 3) + (k % 3) / 2;
+    }
+
+    // dP of the block whose values lie at `values` and dS of it (from its scores s) -> ds; S of the next block (keys at `next`) -> s_next; dQ of the block before
+    // (keys at `prev`, ds_prev).  Exponentials stand between the products of the first half, products with dP and roundings between those of the second.  The
+    // fragments of the beat behind this one's first groups (values2, prev2) are read in this one.
+    template <bool kScores, bool kAccumulate>
+    __device__ __forceinline__ void beat(uint32_t values, uint32_t next, uint32_t prev, uint32_t values2, uint32_t prev2, floatx16& s, floatx16& s_next,
+                                         const u32x4 (&ds_prev)[2], u32x4 (&ds)[2]) {
+        floatx16 dp;
+        auto load = [&](int i) {
+            if (i >= kGroups) f[i % kBuffers] = kind(i - kGroups) == 2 ? column_of(prev2, step(i - kGroups)) : row_of(values2, step(i - kGroups));
+            else if (kind(i) == 0) f[i % kBuffers] = row_of(values, step(i));
+            else if (kind(i) == 1) { if (kScores) f[i % kBuffers] = row_of(next, step(i)); }
+            else if (kAccumulate) f[i % kBuffers] = column_of(prev, step(i));
+        };
+        auto product = [&](int i) {
+            const int r = step(i);
+            if (kind(i) == 0) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % kBuffers], go[r], r == 0 ? prompt_zero() : dp, 0, 0, 0);
+            else if (kind(i) == 1) { if (kScores) s_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % kBuffers], q[r], r == 0 ? prompt_zero() : s_next, 0, 0, 0); }
+            else if (kAccumulate) acc[r >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % kBuffers], __builtin_bit_cast(bf16x8, ds_prev[r & 1]), acc[r >> 1], 0, 0, 0);
+        };
+        constexpr int kHalf = kGroups / 2;
+        // behind product i of the first half: exponents of some numbers, exponentials of those before; of the second half: pairs' products and roundings
+        auto exponents = [&](int from, int to) {
+#pragma unroll
+            for (int x = from; x < to; ++x) s[x] = fmaf(s[x], c, -lse2);
+        };
+        auto exponentials = [&](int from, int to) {
+#pragma unroll
+            for (int x = from; x < to; ++x) s[x] = __builtin_amdgcn_exp2f(s[x]);
+        };
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) {
+            if (kScores || i + kAhead < kGroups) load(i + kAhead);
+            product(i);
+            __builtin_amdgcn_sched_barrier(0);
+            if (i < kHalf) {
+                exponents(16 * i / kHalf, 16 * (i + 1) / kHalf);
+                if (i > 0) exponentials(16 * (i - 1) / kHalf, 16 * i / kHalf);
+            } else {
+                if (i == kHalf) exponentials(16 * (kHalf - 1) / kHalf, 16);
+                const int k = i - kHalf - 2, n = kHalf - 2;
+                if (k >= 0)
+#pragma unroll
+                    for (int y = 8 * k / n; y < 8 * (k + 1) / n; ++y) {
+                        const bf16x2 w = {(__bf16)(s[2 * y] * (dp[2 * y] + nd)), (__bf16)(s[2 * y + 1] * (dp[2 * y + 1] + nd))};
+                        uint32_t bits = __builtin_bit_cast(uint32_t, w);
+                        asm volatile("" : "+v"(bits));               // (rounded here, not behind the last product)
+                        ds[y >> 2][y & 3] = bits;
+                    }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+};
+
+// dq: 128 rows of one head, walked along the keys.  Per block S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.
+//
+// Bound: matrix products at the power limit where walks are long (8 x 2048 tokens, 16 heads of 128, not causal: 402 us, 1.03 PFLOP/s; 420 without the beats),
+// the start and the end of a workgroup where they are short (causal: 243 us, 0.85).  32 rows a wave of D = 64, too: 64 need 336 registers for the beat (139 us for 16 causal
+// sequences of up to 2048 tokens, 16 heads; 164 with 64 rows and no beats).
+template <int D>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_dq_kernel(const PromptParams p, int32_t slots) {
-    constexpr int R = 128 * QB, kBlock = 32 * D, kSteps = D / 16, kHalves = D / 32;
-    constexpr int kStages = 4, kAhead = kStages - 1, kCopies = 2 * kPromptCopies<D>;
-    __shared__ __attribute__((aligned(1024))) uint16_t lds[kStages][2][kBlock];      // keys, values
+    constexpr int R = 128, kBlock = 32 * D, kSteps = D / 16, kHalves = D / 32, kCopies = 2 * kPromptCopies<D>;
+    // Blocks in LDS: of keys and of values those that a beat reads, two that are under way, and what is left to the waves that end first, two blocks before the
+    // last one.
+    constexpr int kKeyRing = 6, kValueRing = 4;
+    __shared__ __attribute__((aligned(1024))) uint16_t lds[kKeyRing + kValueRing][kBlock];
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, g = lane >> 5;
     int32_t slot, h;
@@ -45,118 +127,122 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         return;
     }
     const int32_t keys = p.causal ? tile.t0 + rows : tile.n;
-    const int32_t n_blocks = (keys + 31) / 32;
-    const int32_t my0 = tile.t0 + 32 * QB * wave;
+    const int32_t n_steps = (keys + 63) / 64, n_blocks = 2 * n_steps;                // pairs of blocks
+    const int32_t my0 = tile.t0 + 32 * wave;
     const bool live = my0 < tile.n;
-    const int32_t my_blocks = !live ? 0 : p.causal ? (min(my0 + 32 * QB, keys) + 31) / 32 : n_blocks;
+    const int32_t my_steps = p.causal ? (min(my0 + 32, keys) + 63) / 64 : n_steps;
 
     const char* const kbase = reinterpret_cast<const char*>(static_cast<const uint16_t*>(p.k) + tile.first * p.skn + (h / p.group) * p.skh);
     const char* const vbase = reinterpret_cast<const char*>(static_cast<const uint16_t*>(p.v) + tile.first * p.svn + (h / p.group) * p.svh);
     const uint32_t kpitch = (uint32_t)(p.skn * 2), vpitch = (uint32_t)(p.svn * 2);
-    const uint32_t lds_addr = (uint32_t)(uintptr_t)DFA_LDS_PTR(void, &lds[0][0][0]);
+    const uint32_t lds_addr = (uint32_t)(uintptr_t)DFA_LDS_PTR(void, &lds[0][0]);
+    constexpr uint32_t kBytes = kBlock * 2;
+    auto key_slot = [](int32_t n) { return (uint32_t)(n % kKeyRing) * kBytes; };
+    auto value_slot = [](int32_t n) { return (uint32_t)(kKeyRing + n % kValueRing) * kBytes; };
+    BlockCopies<D, PromptOrder::kBoth> key_copies, value_copies;
+    key_copies.begin(kpitch, wave, lane);
+    value_copies.begin(vpitch, wave, lane);
     auto issue = [&](int32_t n) {
-        const uint32_t to = lds_addr + (uint32_t)((n % kStages) * 2 * kBlock * 2);
-        prompt_copy<D, PromptOrder::kBoth>(kbase, kpitch, 32 * n, keys, wave, lane, to);
-        prompt_copy<D, PromptOrder::kKeys>(vbase, vpitch, 32 * n, keys, wave, lane, to + kBlock * 2);
+        if (n >= n_blocks) return;
+        key_copies(kbase, kpitch, 32 * n, keys, wave, lane, lds_addr + key_slot(n));
+        value_copies(vbase, vpitch, 32 * n, keys, wave, lane, lds_addr + value_slot(n));
     };
 
     // -delta and lse of the wave's rows (a lane and lane ^ 32 hold halves of a row), left for the other launch
     const uint16_t* const qp = static_cast<const uint16_t*>(p.q) + row0 * p.sqn + h * p.sqh;
     const uint16_t* const gp = static_cast<const uint16_t*>(p.dout) + (row0 * p.H + h) * D;
     const uint16_t* const op = static_cast<const uint16_t*>(p.out) + (row0 * p.H + h) * D;
-    bf16x8 q[QB][kSteps], go[QB][kSteps];
-    float lse2[QB], nd[QB];
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-        const int r = 32 * QB * wave + 32 * qb + j;
+    RowWave<D> w;
+    {
+        const int r = 32 * wave + j;
         const int64_t row = min(r, rows - 1);
         float part = 0.f;
 #pragma unroll
         for (int kk = 0; kk < kSteps; ++kk) {
-            q[qb][kk] = *reinterpret_cast<const bf16x8*>(qp + row * p.sqn + 16 * kk + 8 * g);
-            go[qb][kk] = *reinterpret_cast<const bf16x8*>(gp + row * pitch + 16 * kk + 8 * g);
+            w.q[kk] = *reinterpret_cast<const bf16x8*>(qp + row * p.sqn + 16 * kk + 8 * g);
+            w.go[kk] = *reinterpret_cast<const bf16x8*>(gp + row * pitch + 16 * kk + 8 * g);
             const bf16x8 o = *reinterpret_cast<const bf16x8*>(op + row * pitch + 16 * kk + 8 * g);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) part = fmaf((float)go[qb][kk][e], (float)o[e], part);
+            for (int e = 0; e < 8; ++e) part = fmaf((float)w.go[kk][e], (float)o[e], part);
         }
-        nd[qb] = -wave_half_sum(part);
+        w.nd = -wave_half_sum(part);
         const float l = p.lse[(int64_t)h * p.T + row0 + row];
-        lse2[qb] = l == -INFINITY ? INFINITY : l * kLog2e;       // a row without weights has none here either
+        w.lse2 = l == -INFINITY ? INFINITY : l * kLog2e;     // a row without weights has none here either
         if (g == 0 && r < rows) {
-            p.ndelta[(int64_t)h * p.T + row0 + r] = nd[qb];
+            p.ndelta[(int64_t)h * p.T + row0 + r] = w.nd;
             p.lse2[(int64_t)h * p.T + row0 + r] = l == -INFINITY ? -INFINITY : -l / p.scale;         // what the other launch's scores start from
         }
     }
+    issue(0);
+    issue(1);
 #pragma unroll
-    for (int s = 0; s < kAhead; ++s)
-        if (s < n_blocks) issue(s);
+    for (int kk = 0; kk < kSteps; ++kk) asm volatile("" : "+v"(w.q[kk]), "+v"(w.go[kk]));
+    asm volatile("" : "+v"(w.lse2), "+v"(w.nd));
+    wait_vmcnt<0>();
+    issue(2);
+    __syncthreads();
+    w.c = uniform_float(p.scale * kLog2e);
+    w.row = lds_addr + 2u * (uint32_t)prompt_row_at<D, PromptOrder::kBoth>(lane);
+    w.turned = lds_addr + 2u * (uint32_t)prompt_turned_at<D>(lane);
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-#pragma unroll
-        for (int kk = 0; kk < kSteps; ++kk) asm volatile("" : "+v"(q[qb][kk]), "+v"(go[qb][kk]));
-        asm volatile("" : "+v"(lse2[qb]), "+v"(nd[qb]));
-    }
-    const float c = uniform_float(p.scale * kLog2e);
-    const int row_k = prompt_row_at<D, PromptOrder::kBoth>(lane), row_v = prompt_row_at<D, PromptOrder::kKeys>(lane), turned = prompt_turned_at<D>(lane);
-    floatx16 acc[QB][kHalves];
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-        for (int db = 0; db < kHalves; ++db) acc[qb][db] = prompt_zero();
+    for (int db = 0; db < kHalves; ++db) w.acc[db] = prompt_zero();
 
-    for (int32_t n = 0; n < n_blocks; ++n) {
-        // block n has landed once at most the copies of the kAhead - 1 blocks behind it are under way
-        if (n == 0 || n + kAhead > n_blocks) wait_vmcnt<0>();
-        else wait_vmcnt<(kAhead - 1) * kCopies>();
+    // scores of keys that a row does not see
+    auto mask = [&](floatx16& s, int32_t n) {
+        if (32 * n + 32 <= (p.causal ? min(my0 + 1, keys) : keys)) return;
+        const int32_t last = min(p.causal ? my0 + j : keys - 1, keys - 1) - 32 * n;
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+            if (prompt_position(v, g) > last) s[v] = -INFINITY;
+    };
+    // Before beat n, which reads blocks n - 1 to n + 1: the last of them has landed once at most the copies of block n + 2 are under way, and everyone is done
+    // with the keys of block n - 2 and the values of block n - 1, where block n + 3 goes at the earliest.
+    auto enter = [&](int32_t n) {
+        if (n + 2 < n_blocks) wait_vmcnt<kCopies>();
+        else wait_vmcnt<0>();
         __syncthreads();
-        if (n + kAhead < n_blocks) issue(n + kAhead);
-        if (n >= my_blocks) continue;
-        const uint16_t *const kb = lds[n % kStages][0], *const vb = lds[n % kStages][1];
-        floatx16 s[QB], dp[QB];
+        issue(n + 3);
+    };
+
+    floatx16 s_a, s_b;
+    u32x4 ds_a[2], ds_b[2];
+    issue(3);
+    if (live) {
 #pragma unroll
-        for (int kk = 0; kk < kSteps; ++kk) {
-            const bf16x8 kf = prompt_row<D>(kb, row_k, kk), vf = prompt_row<D>(vb, row_v, kk);
+        for (int kk = 0; kk < kSteps; ++kk) s_a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w.row_of(key_slot(0), kk), w.q[kk], kk == 0 ? prompt_zero() : s_a, 0, 0, 0);
 #pragma unroll
-            for (int qb = 0; qb < QB; ++qb) {
-                s[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[qb][kk], kk == 0 ? prompt_zero() : s[qb], 0, 0, 0);
-                dp[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, go[qb][kk], kk == 0 ? prompt_zero() : dp[qb], 0, 0, 0);
-            }
+        for (int i = 0; i < w.kAhead; ++i)
+            if (w.kind(i) == 0) w.f[i] = w.row_of(value_slot(0), w.step(i));
+        mask(s_a, 0);
+        w.template beat<true, false>(value_slot(0), key_slot(1), 0, value_slot(1), key_slot(0), s_a, s_b, ds_b, ds_a);
+    }
+    // trip s: beats 2 s + 1 and 2 s + 2.  A wave whose rows see no more goes along with the copies; the last two blocks that it needs are still there at the end.
+    for (int32_t s = 0; s + 1 < n_steps; ++s) {
+        const bool more = live && s + 1 < my_steps;
+        enter(2 * s + 1);
+        if (more) w.template beat<true, true>(value_slot(2 * s + 1), key_slot(2 * s + 2), key_slot(2 * s), value_slot(2 * s + 2), key_slot(2 * s + 1), s_b, s_a, ds_a, ds_b);
+        enter(2 * s + 2);
+        if (more) {
+            mask(s_a, 2 * s + 2);
+            w.template beat<true, true>(value_slot(2 * s + 2), key_slot(2 * s + 3), key_slot(2 * s + 1), value_slot(2 * s + 3), key_slot(2 * s + 2), s_a, s_b, ds_b, ds_a);
         }
-        const bool masked = 32 * n + 32 > (p.causal ? min(my0 + 1, keys) : keys);
-        u32x4 ds[QB][2];
+    }
+    if (live) {
+        const int32_t last = 2 * my_steps - 1;
+        mask(s_b, last);
+        w.template beat<false, true>(value_slot(last), 0, key_slot(last - 1), 0, 0, s_b, s_a, ds_a, ds_b);
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) {
-            float x[16];
-#pragma unroll
-            for (int v = 0; v < 16; ++v) x[v] = __builtin_amdgcn_exp2f(fmaf(s[qb][v], c, -lse2[qb])) * (dp[qb][v] + nd[qb]);
-            if (masked) {
-                const int32_t last = min(p.causal ? my0 + 32 * qb + j : keys - 1, keys - 1) - 32 * n;
-#pragma unroll
-                for (int v = 0; v < 16; ++v) x[v] = prompt_position(v, g) > last ? 0.f : x[v];
-            }
-            pack(x, ds[qb]);
-        }
-#pragma unroll
-        for (int db = 0; db < kHalves; ++db)
-#pragma unroll
-            for (int st = 0; st < 2; ++st) {
-                const bf16x8 kt = prompt_turned<D>(kb, turned, db, st);
-#pragma unroll
-                for (int qb = 0; qb < QB; ++qb) acc[qb][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kt, __builtin_bit_cast(bf16x8, ds[qb][st]), acc[qb][db], 0, 0, 0);
-            }
+        for (int i = 0; i < kSteps; ++i)
+            w.acc[i >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w.column_of(key_slot(last), i), __builtin_bit_cast(bf16x8, ds_b[i & 1]), w.acc[i >> 1], 0, 0, 0);
     }
 
     int lane_e = lane;
     asm volatile("" : "+v"(lane_e));
     __syncthreads();
     constexpr int kMine = 32 * (2 * D + 16);
-    static_assert(sizeof(lds) >= 4 * kMine, "every wave's rows fit the stages");
+    static_assert(sizeof(lds) >= 4 * kMine, "every wave's rows fit the blocks");
     if (!live) return;
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-        const int r0 = 32 * QB * wave + 32 * qb;
-        store_rows<D>(acc[qb], p.scale, reinterpret_cast<char*>(&lds[0][0][0]) + wave * kMine, dq + r0 * pitch, pitch, rows - r0, lane_e);
-    }
+    store_rows<D>(w.acc, p.scale, reinterpret_cast<char*>(&lds[0][0]) + wave * kMine, dq + 32 * wave * pitch, pitch, rows - 32 * wave, lane_e);
 }
 
 // A wave of the launch of dk and dv: 32 keys, their dk and dv, and one beat of its walk along the rows.
@@ -426,10 +512,10 @@ __global__ __launch_bounds__(256) void prompt_sum_kernel(const PromptParams p, i
     else *reinterpret_cast<float4*>(to) = sum;
 }
 
-template <int D, int QB, int kEu>
+template <int D, int kEu>
 hipError_t launch(const PromptParams& p, hipStream_t st) {
-    const int64_t dq_slots = prompt_slots(p.T, p.B, 128 * QB), slots = prompt_slots(p.T, p.B, 128);
-    hipLaunchKernelGGL((prompt_dq_kernel<D, QB>), dim3((unsigned)(dq_slots * p.H)), dim3(256), 0, st, p, (int32_t)dq_slots);
+    const int64_t slots = prompt_slots(p.T, p.B, 128);
+    hipLaunchKernelGGL((prompt_dq_kernel<D>), dim3((unsigned)(slots * p.H)), dim3(256), 0, st, p, (int32_t)slots);
     hipLaunchKernelGGL((prompt_dkdv_kernel<D, kEu>), dim3((unsigned)(slots * p.Hkv * p.shares)), dim3(256), 0, st, p, (int32_t)slots);
     return hipGetLastError();
 }
@@ -442,8 +528,7 @@ int32_t prompt_bwd_shares(int32_t T, int32_t B, int32_t H, int32_t Hkv, const Ch
 }
 
 hipError_t launch_prompt_bwd(const PromptParams& p, bool f32, int32_t D, const ChipShape& chip, hipStream_t st) {
-    const bool small = prompt_small(p.T, p.B, p.H, chip);
-    const hipError_t e = f32 ? launch_prompt_bwd_f32(p, D, small, st) : D == 128 ? launch<128, 1, 1>(p, st) : small ? launch<64, 1, 2>(p, st) : launch<64, 2, 2>(p, st);
+    const hipError_t e = f32 ? launch_prompt_bwd_f32(p, D, prompt_small(p.T, p.B, p.H, chip), st) : D == 128 ? launch<128, 1>(p, st) : launch<64, 2>(p, st);
     if (e != hipSuccess || p.shares == 1) return e;
     const int64_t tensor = (int64_t)p.T * p.Hkv * D;
     const dim3 grid((unsigned)((2 * tensor / 4 + 255) / 256));
