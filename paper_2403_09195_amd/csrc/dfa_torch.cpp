@@ -521,6 +521,15 @@ bool read_norm(PyObject* x, PyObject* weight, PyObject* eps, NormCall* n) {
 }
 const void* pointer(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
 
+// A contiguous tensor of a type from byte `at` of an allocation on, which it keeps alive.
+at::Tensor part_of(const at::Tensor& whole, int64_t at, at::IntArrayRef sizes, at::ScalarType type) {
+    at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(whole.storage()), whole.key_set(), c10::scalarTypeToTypeMeta(type));
+    c10::TensorImpl* const impl = t.unsafeGetTensorImpl();
+    impl->set_storage_offset(at / (int64_t)c10::elementSize(type));
+    impl->set_sizes_contiguous(sizes);
+    return t;
+}
+
 // rms_norm(x, weight, eps, residual, whether y, whether in 8 bits) -> (y, h, values, scales) with None for what there is not, a negative status, or None
 PyObject* rms_norm(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     HANDLE_TH_ERRORS
@@ -533,7 +542,10 @@ PyObject* rms_norm(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     at::Tensor r[4];
     if (plain) r[0] = at::empty(n.x->sizes(), n.x->options());
     if (res) r[1] = at::empty(n.x->sizes(), n.x->options());
-    if (eight) r[2] = at::empty({n.M, ld}, n.x->options().dtype(at::kFloat8_e4m3fn)), r[3] = at::empty({ld / 128, lds}, n.x->options().dtype(at::kByte));
+    if (eight) {
+        const at::Tensor whole = at::empty({n.M * ld + ld / 128 * lds}, n.x->options().dtype(at::kByte));
+        r[2] = part_of(whole, 0, {n.M, ld}, at::kFloat8_e4m3fn), r[3] = part_of(whole, n.M * ld, {ld / 128, lds}, at::kByte);
+    }
     const dfa_quantized_t q{eight ? r[2].data_ptr() : nullptr, eight ? r[3].data_ptr() : nullptr, ld, lds};
     int rc;
     {
@@ -575,8 +587,11 @@ PyObject* cache_reserve(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     int32_t page, rows;
     if (!lengths || !table || !free || !n_free || !as_int32(args[5], &page) || !as_int32(args[6], &rows) || rows < 1) Py_RETURN_NONE;
     if (table->scalar_type() != at::kInt || table->dim() != 2 || table->size(0) != B || table->size(1) < 1 || table->size(1) > INT32_MAX || !table->is_contiguous()) Py_RETURN_NONE;
-    const at::TensorOptions o = counts->options();
-    at::Tensor r[6] = {at::empty({B}, o), at::empty({1}, o), at::empty({B + 1}, o), at::empty({rows}, o.dtype(at::kLong)), at::empty({rows}, o), at::empty({1}, o)};
+    // one allocation: six of them take 2 us
+    const int64_t at_positions = 8 * (int64_t)rows, at_starts = at_positions + 4 * (int64_t)rows, at_refused = at_starts + 4 * (B + 1), at_lengths = at_refused + 4, at_left = at_lengths + 4 * B;
+    const at::Tensor whole = at::empty({(at_left + 4) / 4}, counts->options());
+    at::Tensor r[6] = {part_of(whole, at_lengths, {B}, at::kInt), part_of(whole, at_left, {1}, at::kInt), part_of(whole, at_starts, {B + 1}, at::kInt),
+                       part_of(whole, 0, {rows}, at::kLong), part_of(whole, at_positions, {rows}, at::kInt), part_of(whole, at_refused, {1}, at::kInt)};
     int rc;
     {
         pybind11::gil_scoped_release release;
