@@ -29,9 +29,8 @@ hipError_t launch_prompt_fwd(const PromptParams& p, bool f32, int32_t D, const C
 // Workgroups that share the query heads of a key head out in the launch of dk and dv.
 int32_t prompt_bwd_shares(int32_t T, int32_t B, int32_t H, int32_t Hkv, const ChipShape& chip);
 hipError_t launch_prompt_bwd(const PromptParams& p, bool f32, int32_t D, const ChipShape& chip, hipStream_t st);
-// small: tiles of half the rows, whose walk the waves of a workgroup share out
-hipError_t launch_prompt_fwd_f32(const PromptParams& p, int32_t D, bool small, hipStream_t st);
-hipError_t launch_prompt_bwd_f32(const PromptParams& p, int32_t D, bool small, hipStream_t st);      // without the sum of the shares
+hipError_t launch_prompt_fwd_f32(const PromptParams& p, int32_t D, const ChipShape& chip, hipStream_t st);
+hipError_t launch_prompt_bwd_f32(const PromptParams& p, int32_t D, const ChipShape& chip, hipStream_t st);      // without the sum of the shares
 // Whether a launch of 128-row tiles is so few workgroups that its longest walk decides.
 inline bool prompt_small(int32_t T, int32_t B, int32_t heads, const ChipShape& chip) {
     return ((int64_t)T / 128 + (B < T ? B : T)) * heads < 4 * (int64_t)chip.cus;
@@ -335,7 +334,7 @@ __device__ __forceinline__ void store_rows(const floatx16 (&acc)[D / 32], float 
 template <int D, typename T>
 __device__ __forceinline__ void zero_rows(T* to, int64_t pitch, int rows) {
     constexpr int kLanes = D * (int)sizeof(T) / 16;
-    for (int i = threadIdx.x; i < rows * kLanes; i += 256) *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(to + (int64_t)(i / kLanes) * pitch) + 16 * (i % kLanes)) = u32x4{0u, 0u, 0u, 0u};
+    for (int i = threadIdx.x; i < rows * kLanes; i += blockDim.x) *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(to + (int64_t)(i / kLanes) * pitch) + 16 * (i % kLanes)) = u32x4{0u, 0u, 0u, 0u};
 }
 
 }  // namespace dfa

@@ -528,7 +528,7 @@ int32_t prompt_bwd_shares(int32_t T, int32_t B, int32_t H, int32_t Hkv, const Ch
 }
 
 hipError_t launch_prompt_bwd(const PromptParams& p, bool f32, int32_t D, const ChipShape& chip, hipStream_t st) {
-    const hipError_t e = f32 ? launch_prompt_bwd_f32(p, D, prompt_small(p.T, p.B, p.H, chip), st) : D == 128 ? launch<128, 1>(p, st) : launch<64, 2>(p, st);
+    const hipError_t e = f32 ? launch_prompt_bwd_f32(p, D, chip, st) : D == 128 ? launch<128, 1>(p, st) : launch<64, 2>(p, st);
     if (e != hipSuccess || p.shares == 1) return e;
     const int64_t tensor = (int64_t)p.T * p.Hkv * D;
     const dim3 grid((unsigned)((2 * tensor / 4 + 255) / 256));

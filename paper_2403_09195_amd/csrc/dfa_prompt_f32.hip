@@ -4,6 +4,8 @@
 // product's time.  The walked rows are split once, by the workgroup, on their way into LDS, where the three parts of a block lie as
 // blocks of the bf16 kernels (dfa_prompt.h): 32 rows go memory -> registers a block ahead, and registers -> LDS, split, while the other of
 // two buffers is being read.  The softmax weights are split in registers.
+#include <algorithm>
+
 #include "dfa_mfma_f32.h"
 #include "dfa_prompt.h"
 
@@ -506,26 +508,44 @@ void launch_dkdv(const PromptParams& p, hipStream_t st) {
 }
 }  // namespace
 
-hipError_t launch_prompt_fwd_f32(const PromptParams& p, int32_t D, bool small, hipStream_t st) {
-    if (D == 64) return small ? launch_fwd<64, 2, 4, false, 2>(p, st) : launch_fwd<64, 4, 1, true, 2>(p, st);
-    return small ? launch_fwd<128, 2, 2, false, 1>(p, st) : launch_fwd<128, 4, 1, true, 1>(p, st);
+// Forms by what is known of the lengths, their mean, and by how many workgroups there are.
+namespace {
+// Workgroups of R-row tiles, about.
+int64_t tiles(const PromptParams& p, int32_t R, int32_t heads) { return std::max<int64_t>((p.T + R - 1) / R, std::min(p.T, p.B)) * heads; }
+}  // namespace
+
+// Large launches: 128 rows, one walk.  Others, 64 rows: four groups of waves to a walk (two of D = 128) where a workgroup has its compute unit to itself; two groups of D = 64, two workgroups
+// to a compute unit, where there are more than that holds at once, and one's products fill the time in which the other splits its operands (12 heads of 64, us with four groups / two:
+// forward 1 x 1000 34.3 / 43.8, 4 x 512 27.6 / 27.5, 8 x 512 48.2 / 39.3, 1 x 4000 232 / 214, 64 x <= 60 28.4 / 17.7).
+hipError_t launch_prompt_fwd_f32(const PromptParams& p, int32_t D, const ChipShape& chip, hipStream_t st) {
+    const bool small = prompt_small(p.T, p.B, p.H, chip);
+    if (D == 128) return small ? launch_fwd<128, 2, 2, false, 1>(p, st) : launch_fwd<128, 4, 1, true, 1>(p, st);
+    if (!small) return launch_fwd<64, 4, 1, true, 2>(p, st);
+    return tiles(p, 64, p.H) > 2 * chip.cus ? launch_fwd<64, 2, 2, false, 2>(p, st) : launch_fwd<64, 2, 4, false, 2>(p, st);
 }
 
-hipError_t launch_prompt_bwd_f32(const PromptParams& p, int32_t D, bool small, hipStream_t st) {
-    if (D == 64) {
+// As the forward's; dq takes two groups of short walks, too (3 x <= 333 tokens 23.8 / 22.3, 1 x 77 14.9 / 10.9, 4 x 512 40.9 / 34.4, 1 x 500 26.7 / 28.0, 1 x 2000 80 / 100).  dk and dv: 32 keys and four
+// groups where that is no more than a round and a half (us with 64 keys / 32: 3 x <= 333 tokens 30.5 / 25.1, 1 x 1000 59.9 / 49.2, 1 x 2000, three rounds, 121 / 154).
+hipError_t launch_prompt_bwd_f32(const PromptParams& p, int32_t D, const ChipShape& chip, hipStream_t st) {
+    const bool small = prompt_small(p.T, p.B, p.H, chip);
+    if (D == 128) {
         if (small) {
-            launch_dq<64, 2, 4, false, 2>(p, st);
-            launch_dkdv<64, 2, 4, false, 2>(p, st);
+            launch_dq<128, 2, 2, false, 1>(p, st);
+            launch_dkdv<128, 2, 2, false, 1>(p, st);
         } else {
-            launch_dq<64, 4, 1, true, 2>(p, st);
-            launch_dkdv<64, 4, 1, true, 1>(p, st);
+            launch_dq<128, 4, 1, true, 1>(p, st);
+            launch_dkdv<128, 4, 1, true, 1>(p, st);
         }
     } else if (small) {
-        launch_dq<128, 2, 2, false, 1>(p, st);
-        launch_dkdv<128, 2, 2, false, 1>(p, st);
+        const int64_t mean = p.T / p.B, rows = tiles(p, 64, p.H), units = p.Hkv * p.shares;
+        if (rows > 2 * chip.cus || mean <= 320 || (mean <= 512 && rows > chip.cus)) launch_dq<64, 2, 2, false, 2>(p, st);
+        else launch_dq<64, 2, 4, false, 2>(p, st);
+        if (2 * tiles(p, 32, units) <= 3 * chip.cus) launch_dkdv<64, 1, 4, false, 2>(p, st);
+        else if (tiles(p, 64, units) > 2 * chip.cus) launch_dkdv<64, 2, 2, false, 2>(p, st);
+        else launch_dkdv<64, 2, 4, false, 2>(p, st);
     } else {
-        launch_dq<128, 4, 1, true, 1>(p, st);
-        launch_dkdv<128, 4, 1, true, 1>(p, st);
+        launch_dq<64, 4, 1, true, 2>(p, st);
+        launch_dkdv<64, 4, 1, true, 1>(p, st);
     }
     return hipGetLastError();
 }

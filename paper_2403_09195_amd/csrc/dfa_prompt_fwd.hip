@@ -411,7 +411,7 @@ hipError_t launch(const PromptParams& p, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_prompt_fwd(const PromptParams& p, bool f32, int32_t D, const ChipShape& chip, hipStream_t st) {
-    if (f32) return launch_prompt_fwd_f32(p, D, prompt_small(p.T, p.B, p.H, chip), st);
+    if (f32) return launch_prompt_fwd_f32(p, D, chip, st);
     // What is known of the lengths is their mean.  Two groups of waves to a walk where the workgroups of half the rows are resident at once (two to a compute unit, one of
     // D = 128), or where walks are so long that twice as many do (us with one group / two: 12 heads of 64, 1000 tokens 19.0 / 14.1, 4000 60.5 / 44.3, 4 x 512 12.3 / 11.6,
     // 8 x 512 14.6 / 19.2; 16 heads of 128, 300 tokens 10.9 / 11.3, 1000 24.0 / 19.2, 2000 42.2 / 39.2, 4000 88 / 123).

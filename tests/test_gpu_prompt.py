@@ -105,6 +105,15 @@ def test_one_prompt(B, n, D, causal, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("lengths,H,Hkv", [([40] * 43 + [130, 7], 16, 8), ([500, 300, 200], 24, 24)], ids=["short", "long"])
+def test_some_tiles(B, lengths, H, Hkv, D, causal, dtype):
+    """More tiles than the chip holds at once, but not many times as many."""
+    _check(B, lengths, H, Hkv, D, dtype, causal, behind=3)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_many_sequences(B, dtype):
     """More sequences than a wave has lanes, than are ranked, and than 64 times 64."""
     _check(B, [3] * 100 + [130] + [2] * 100, 1, 1, 64, dtype, True)
