@@ -279,7 +279,7 @@ struct KeyWave {
     template <bool kFirst, bool kSecond>
     __device__ __forceinline__ void beat(uint32_t next, uint32_t prev, uint32_t next2, uint32_t prev2, const float* begin, int g, floatx16& s, floatx16& dp, floatx16& s_next,
                                          floatx16& dp_next, const u32x4 (&pp_prev)[2], const u32x4 (&dd_prev)[2], u32x4 (&pp)[2], u32x4 (&dd)[2]) {
-        constexpr int kGroups = kSteps, kProducts = 4 * kGroups;
+        constexpr int kGroups = kSteps, kProducts = 4 * kGroups, kSpan = kProducts - 4;
         float t[16], ds[16];
         auto product = [&](int i) {
             const int r = i >> 2;
@@ -295,26 +295,28 @@ struct KeyWave {
             }
         };
 #pragma unroll
-        for (int m = 0; m < 18; ++m) {
+        for (int i = 0; i < kProducts; ++i) {
+            product(i);
+            __builtin_amdgcn_sched_barrier(0);
+            if (i < kProducts / 2)
 #pragma unroll
-            for (int i = kProducts * m / 18; i < kProducts * (m + 1) / 18; ++i) {
-                product(i);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            if (m < 8) t[2 * m] = s[2 * m] * c, t[2 * m + 1] = s[2 * m + 1] * c;
-            if (m >= 1 && m <= 16) t[m - 1] = __builtin_amdgcn_exp2f(t[m - 1]);
-            if (m >= 2) {
-                const int i = m - 2;
-                ds[i] = t[i] * dp[i];
-                if (i & 1) {
-                    const bf16x2 a = {(__bf16)t[i - 1], (__bf16)t[i]}, b = {(__bf16)ds[i - 1], (__bf16)ds[i]};
-                    uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
-                    asm volatile("" : "+v"(x), "+v"(y));             // (rounded here, not behind the last product)
-                    pp[i >> 3][(i >> 1) & 3] = x;
-                    dd[i >> 3][(i >> 1) & 3] = y;
+                for (int e = 32 * i / kProducts; e < 32 * (i + 1) / kProducts; ++e) t[e] = s[e] * c;
+            if (i >= 1 && i <= kSpan)
+#pragma unroll
+                for (int e = 16 * (i - 1) / kSpan; e < 16 * i / kSpan; ++e) t[e] = __builtin_amdgcn_exp2f(t[e]);
+            if (i >= 3 && i < kSpan + 3)
+#pragma unroll
+                for (int e = 16 * (i - 3) / kSpan; e < 16 * (i - 2) / kSpan; ++e) {
+                    ds[e] = t[e] * dp[e];
+                    if (e & 1) {
+                        const bf16x2 a = {(__bf16)t[e - 1], (__bf16)t[e]}, b = {(__bf16)ds[e - 1], (__bf16)ds[e]};
+                        uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
+                        asm volatile("" : "+v"(x), "+v"(y));         // (rounded here, not behind the last product)
+                        pp[e >> 3][(e >> 1) & 3] = x;
+                        dd[e >> 3][(e >> 1) & 3] = y;
+                    }
                 }
-            }
-            if (m == 10) start(begin, g, s);
+            if (i == kProducts * 10 / 18) start(begin, g, s);
             __builtin_amdgcn_sched_barrier(0);
         }
         start(begin + 32, g, dp);
