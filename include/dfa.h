@@ -29,7 +29,7 @@
  *   - Tensors q, k, v are addressed as base + b*stride.b + n*stride.n + h*stride.h + d
  *     (strides in elements, the D elements of one row contiguous).  Every row must start
  *     on a 16-byte boundary.  Outputs are contiguous: out [B, N, H, D], lse [B, H, N].
- *   - D must be 64.  Non-causal, no mask, no bias.
+ *   - D must be 64, and attention is not causal, unless the entry point says otherwise.  No mask, no bias.
  *   - Return value: DFA_OK (0) or a negative dfa_status_t.  Argument errors are found on
  *     the host before anything is enqueued.  No C++ exception crosses this boundary.
  *   - The attention entry points keep a per-process cache of launch plans (tile lists in
@@ -71,7 +71,9 @@ typedef enum {
                             /* and placement also w > N, N % w != 0, w % r != 0; for the     */
                             /* projections sizes that the tiles do not divide; for 8-bit     */
                             /* operands also pitches below the rows they hold, and blocks    */
-                            /* and pages of other sizes than the entry point names           */
+                            /* and pages of other sizes than the entry point names; for      */
+                            /* packed sequences D other than 64 and 128, H not a multiple of */
+                            /* Hkv, a scale or an eps outside its range                      */
     DFA_ERR_BRANCHES = -3,  /* nb < 1 or nb > DFA_MAX_BRANCHES                               */
     DFA_ERR_DTYPE = -4,     /* unknown dfa_dtype_t                                           */
     DFA_ERR_ALIGN = -5,     /* a base pointer or stride breaks the 16-byte row alignment     */
@@ -451,7 +453,7 @@ int dfa_release_plans(void);
  *           rows of no sequence (from starts[B] on) are 0 and -inf
  * bf16: probabilities are rounded to bf16 before they meet v; sums are fp32.  fp32: products of three bf16 parts a number (24 bits; bits
  * below 2^-133 are lost, and what rounds to 2^128 in bf16 counts as infinite).  scale lies within 2^-100 .. 2^100, and every scale * q . k
- * within 2^127 ln 2 either way.
+ * within 2^127 ln 2 either way.  Keys and values that are not finite reach only the rows that attend to them (an infinite fp32 value may come out as NaN there).
  * Sums are in a fixed order: equal calls give equal results.  Asynchronous on `stream`; allocates nothing.
  */
 int dfa_prompt_attention(const void *q, const void *k, const void *v, dfa_strides_t sq, dfa_strides_t sk, dfa_strides_t sv, dfa_dtype_t dt, int32_t T,
