@@ -208,3 +208,17 @@ def test_captured(B):
         torch.cuda.synchronize()
         assert torch.equal(y, y2) and torch.equal(h, h2) and torch.equal(dx, dx2) and torch.equal(dw, dw2)
         assert torch.equal(q.values.view(torch.uint8), q2.values.view(torch.uint8)) and torch.equal(q.scales[:, :600], q2.scales[:, :600])
+
+
+def test_offsets_beyond_32_bits(B):
+    """More than 2^31 elements: the last rows as they come out on their own."""
+    import torch
+    M, C = 66000, 32768
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x, w = torch.randn((M, C), generator=gen, device="cuda", dtype=torch.bfloat16), torch.randn((C,), generator=gen, device="cuda", dtype=torch.bfloat16)
+    (y, q), h = B.rms_norm(x, w, 1e-6, residual=x, quantized="both")
+    (y1, q1), h1 = B.rms_norm(x[-32:], w, 1e-6, residual=x[-32:], quantized="both")
+    assert torch.equal(y[-32:], y1) and torch.equal(h[-32:], h1)
+    assert torch.equal(q.values[-32:].view(torch.uint8), q1.values.view(torch.uint8)) and torch.equal(q.scales[:, M - 32:M], q1.scales[:, :32])
+    dx, _ = B.rms_norm_backward(y, h, w, 1e-6)
+    assert torch.equal(dx[-32:], B.rms_norm_backward(y1, h1, w, 1e-6)[0])

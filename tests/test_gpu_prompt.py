@@ -295,3 +295,27 @@ def test_captured(B):
             want_grads = B.prompt_attention_backward(q, k, v, *want, dout, starts, 0.125)
         torch.cuda.synchronize()
         assert torch.equal(out, want[0]) and torch.equal(lse, want[1]) and all(torch.equal(a, b) for a, b in zip(grads, want_grads)), lengths
+
+
+@pytest.mark.parametrize("dtype,T", [("bf16", 140000), ("fp32", 70000)])
+def test_offsets_beyond_32_bits(B, dtype, T):
+    """Tensors of more than 2^31 elements (bf16) and bytes: the last sequences, and the rows behind them, against references and the same rows on their own."""
+    import torch
+    H, Hkv, D = 128, 2, 128
+    lengths = [50] * (T // 50 - 1) + [33, 7]
+    starts = ref.starts_of(lengths)
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    rand = lambda heads: torch.randn((T, heads, D), generator=gen, device="cuda", dtype=_type(dtype))
+    q, k, v, dout = rand(H), rand(Hkv), rand(Hkv), rand(H)
+    out, lse = B.prompt_attention(q, k, v, _ints(starts), 0.1)
+    grads = B.prompt_attention_backward(q, k, v, out, lse, dout, _ints(starts), 0.1)
+    first, end = starts[-4], starts[-1]
+    cut = [s - first for s in starts[-4:]]
+    own = [t[first:end] for t in (q, k, v)]
+    o, l, o_tol, l_tol = ref.attention(*own, cut, 0.1, True)
+    _within(out[first:end], o, o_tol, "out")
+    _within(lse[:, first:end], l, l_tol, "lse")
+    want, tols = ref.attention_backward(*own, out[first:end], lse[:, first:end], dout[first:end], cut, 0.1, True)
+    for got, g, t, name in zip(grads, want, tols, ("dq", "dk", "dv")):
+        _within(got[first:end], g, t, name)
+    assert end < T and not out[end:].any() and torch.isneginf(lse[:, end:]).all() and not any(g[end:].any() for g in grads)
