@@ -33,7 +33,7 @@ hipError_t launch_prompt_fwd_f32(const PromptParams& p, int32_t D, const ChipSha
 hipError_t launch_prompt_bwd_f32(const PromptParams& p, int32_t D, const ChipShape& chip, hipStream_t st);      // without the sum of the shares
 // Whether a launch of 128-row tiles is so few workgroups that its longest walk decides.
 inline bool prompt_small(int32_t T, int32_t B, int32_t heads, const ChipShape& chip) {
-    return ((int64_t)T / 128 + (B < T ? B : T)) * heads < 4 * (int64_t)chip.cus;
+    return ((int64_t)T / 128 + B) * heads < 4 * (int64_t)chip.cus;
 }
 
 // Slots of tiles of R rows.

@@ -3,7 +3,7 @@
 // Products as in dfa_mfma_f32.h: a number is the sum of three bf16 parts, six of the nine partial products are taken, at six times a bf16
 // product's time.  The walked rows are split once, by the workgroup, on their way into LDS, where the three parts of a block lie as
 // blocks of the bf16 kernels (dfa_prompt.h): 32 rows go memory -> registers a block ahead, and registers -> LDS, split, while the other of
-// two buffers is being read.  The softmax weights are split in registers.
+// two buffers is being read.  The softmax weights are split in registers.  Small launches of the backward work dq and dk and dv side by side, behind one that leaves the rows' delta.
 #include <algorithm>
 
 #include "dfa_mfma_f32.h"
@@ -302,15 +302,34 @@ __global__ __launch_bounds__(64 * RG * KG) __attribute__((amdgpu_waves_per_eu(kE
     store_direct<D>(acc, inv, out + (32 * rg + j) * pitch, g);
 }
 
-// dq, groups of rows and of blocks as in the forward.
-template <int D, int RG, int KG, bool kDouble, int kEu>
-__global__ __launch_bounds__(64 * RG * KG) __attribute__((amdgpu_waves_per_eu(kEu, kEu))) void prompt_dq_f32_kernel(const PromptParams p, int32_t slots) {
-    constexpr int R = 32 * RG, kHalves = D / 32, kThreads = 64 * RG * KG, kTensor = KG * 3 * kPart<D>, kBuffers = kDouble ? 2 : 1;
-    __shared__ __attribute__((aligned(16))) uint16_t lds[kBuffers][2][kTensor];      // keys, values
+// How a part of the backward is worked: groups as in the forward.
+template <int D_, int RG_, int KG_, bool kDouble_>
+struct Form {
+    static constexpr int D = D_, RG = RG_, KG = KG_, R = 32 * RG, kThreads = 64 * RG * KG, kTensor = KG * 3 * kPart<D>, kBuffers = kDouble_ ? 2 : 1;
+    static constexpr bool kDouble = kDouble_;
+    typedef uint16_t Blocks[2][kTensor];                 // a step's: keys and values, or q and dout
+    typedef float Scalars[2][32 * KG];                   // lse in base 2 and -delta of a step's rows
+    static constexpr size_t kBytes = kBuffers * (sizeof(Blocks) + sizeof(Scalars));
+    static_assert(kBuffers * sizeof(Blocks) >= (size_t)RG * KG / 2 * (D / 32) * 4 * 64 * 16, "half of the waves' results fit");
+};
+
+// -delta and lse in base 2 of a row, which dk and dv take from the workspace.
+__device__ __forceinline__ float base2(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }      // a row without weights has none here either
+__device__ __forceinline__ void leave_numbers(const PromptParams& p, int64_t at, float nd, float lse2) {
+    p.ndelta[at] = nd;
+    p.lse2[at] = lse2;
+}
+
+// dq, workgroup x.  kLeave: it leaves the numbers of its rows.
+template <typename F, bool kLeave>
+__device__ __forceinline__ void dq_part(const PromptParams& p, int32_t x, int32_t slots, char* raw) {
+    constexpr int D = F::D, RG = F::RG, KG = F::KG, R = F::R, kHalves = D / 32, kThreads = F::kThreads;
+    constexpr bool kDouble = F::kDouble;
+    typename F::Blocks* const lds = reinterpret_cast<typename F::Blocks*>(raw);      // keys, values
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, g = lane >> 5;
     const int rg = wave % RG, kg = wave / RG;
     int32_t slot, h;
-    prompt_place(blockIdx.x, slots, p.H, slot, h);
+    prompt_place(x, slots, p.H, slot, h);
     const PromptTile tile = prompt_row_tile<R>(p, slot, slots, lane);
     if (tile.empty) return;
     const int32_t rows = min(R, tile.n - tile.t0);
@@ -340,11 +359,8 @@ __global__ __launch_bounds__(64 * RG * KG) __attribute__((amdgpu_waves_per_eu(kE
         const float4 a = *reinterpret_cast<const float4*>(gr + 8 * i + 4 * g), b = *reinterpret_cast<const float4*>(orow + 8 * i + 4 * g);
         part = fmaf(a.x, b.x, fmaf(a.y, b.y, fmaf(a.z, b.z, fmaf(a.w, b.w, part))));
     }
-    const float nd = -wave_half_sum(part), l = p.lse[(int64_t)h * p.T + row0 + row], lse2 = l == -INFINITY ? INFINITY : l * kLog2e;
-    if (g == 0 && kg == 0 && 32 * rg + j < rows) {
-        p.ndelta[(int64_t)h * p.T + row0 + 32 * rg + j] = nd;
-        p.lse2[(int64_t)h * p.T + row0 + 32 * rg + j] = lse2;
-    }
+    const float nd = -wave_half_sum(part), lse2 = base2(p.lse[(int64_t)h * p.T + row0 + row]);
+    if (kLeave && g == 0 && kg == 0 && 32 * rg + j < rows) leave_numbers(p, (int64_t)h * p.T + row0 + 32 * rg + j, nd, lse2);
     kx.template store<PromptOrder::kBoth>(lds[0][0], 3 * kPart<D>);
     vx.template store<PromptOrder::kKeys>(lds[0][1], 3 * kPart<D>);
     const float c = uniform_float(p.scale * kLog2e);
@@ -381,23 +397,23 @@ __global__ __launch_bounds__(64 * RG * KG) __attribute__((amdgpu_waves_per_eu(kE
         }
     }
     if constexpr (KG > 1) {
-        static_assert(sizeof(lds) >= (size_t)RG * KG / 2 * kHalves * 4 * 64 * 16, "half of the waves' results fit");
-        sum_groups<kHalves, KG, RG>(acc, reinterpret_cast<float4*>(lds), wave, lane);
+        sum_groups<kHalves, KG, RG>(acc, reinterpret_cast<float4*>(raw), wave, lane);
         if (kg) return;
     }
     if (32 * rg + j < rows) store_direct<D>(acc, p.scale, dq + (32 * rg + j) * pitch, g);
 }
 
-// dk and dv: RG groups of 32 keys, KG groups of waves that take every KG-th block of the rows.
-template <int D, int RG, int KG, bool kDouble, int kEu>
-__global__ __launch_bounds__(64 * RG * KG) __attribute__((amdgpu_waves_per_eu(kEu, kEu))) void prompt_dkdv_f32_kernel(const PromptParams p, int32_t slots) {
-    constexpr int R = 32 * RG, kHalves = D / 32, kThreads = 64 * RG * KG, kTensor = KG * 3 * kPart<D>, kBuffers = kDouble ? 2 : 1;
-    __shared__ __attribute__((aligned(16))) uint16_t lds[kBuffers][2][kTensor];      // q, dout
-    __shared__ __attribute__((aligned(16))) float scalars[kBuffers][2][32 * KG];     // lse2, -delta
+// dk and dv, workgroup x: RG groups of 32 keys, KG groups of waves that take every KG-th block of the rows.
+template <typename F>
+__device__ __forceinline__ void dkdv_part(const PromptParams& p, int32_t x, int32_t slots, char* raw) {
+    constexpr int D = F::D, RG = F::RG, KG = F::KG, R = F::R, kHalves = D / 32, kThreads = F::kThreads;
+    constexpr bool kDouble = F::kDouble;
+    typename F::Blocks* const lds = reinterpret_cast<typename F::Blocks*>(raw);      // q, dout
+    typename F::Scalars* const scalars = reinterpret_cast<typename F::Scalars*>(raw + F::kBuffers * sizeof(typename F::Blocks));
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, g = lane >> 5;
     const int rg = wave % RG, kg = wave / RG;
     int32_t slot, unit;
-    prompt_place(blockIdx.x, slots, p.Hkv * p.shares, slot, unit);
+    prompt_place(x, slots, p.Hkv * p.shares, slot, unit);
     slot = slots - 1 - slot;
     const int32_t hk = unit / p.shares, share = unit % p.shares;
     const PromptTile tile = prompt_key_tile<R>(p, slot, lane);
@@ -476,15 +492,46 @@ __global__ __launch_bounds__(64 * RG * KG) __attribute__((amdgpu_waves_per_eu(kE
         if (more) store(kDouble ? (n + 1) & 1 : 0);
     }
     if constexpr (KG > 1) {
-        static_assert(sizeof(lds) >= (size_t)RG * KG / 2 * kHalves * 4 * 64 * 16, "half of the waves' results fit");
-        sum_groups<kHalves, KG, RG>(dka, reinterpret_cast<float4*>(lds), wave, lane);
-        sum_groups<kHalves, KG, RG>(dva, reinterpret_cast<float4*>(lds), wave, lane);
+        sum_groups<kHalves, KG, RG>(dka, reinterpret_cast<float4*>(raw), wave, lane);
+        sum_groups<kHalves, KG, RG>(dva, reinterpret_cast<float4*>(raw), wave, lane);
         if (kg) return;
     }
     if (32 * rg + j < rows) {
         store_direct<D>(dka, p.scale, dk + (32 * rg + j) * pitch, g);
         store_direct<D>(dva, 1.f, dv + (32 * rg + j) * pitch, g);
     }
+}
+
+// The numbers of all rows of the sequences: a row's D numbers are D / 4 lanes'.
+template <int D>
+__global__ __launch_bounds__(256) void prompt_delta_f32_kernel(const PromptParams p) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, r = i / (D / 4);
+    if (r >= (int64_t)p.T * p.H) return;                 // (whole rows' lanes)
+    const int64_t at = (r % p.H) * p.T + r / p.H;
+    const float4 a = *reinterpret_cast<const float4*>(static_cast<const float*>(p.out) + 4 * i), b = *reinterpret_cast<const float4*>(static_cast<const float*>(p.dout) + 4 * i);
+    float delta = fmaf(a.x, b.x, fmaf(a.y, b.y, fmaf(a.z, b.z, a.w * b.w)));
+#pragma unroll
+    for (int d = 1; d < D / 4; d *= 2) delta += __shfl_xor(delta, d);
+    if (threadIdx.x % (D / 4) == 0) leave_numbers(p, at, -delta, base2(p.lse[at]));
+}
+
+// Both in one launch behind that one, the longer walks first: workgroups of either fill the places that the other leaves.
+template <typename F, int kEu>
+__global__ __launch_bounds__(F::kThreads) __attribute__((amdgpu_waves_per_eu(kEu, kEu))) void prompt_bwd_f32_kernel(const PromptParams p, int32_t dkdv_count, int32_t slots) {
+    __shared__ __attribute__((aligned(16))) char lds[F::kBytes];
+    const int32_t x = blockIdx.x;
+    if (x >= dkdv_count) dq_part<F, false>(p, x - dkdv_count, slots, lds);
+    else if (x < slots * p.Hkv * p.shares) dkdv_part<F>(p, x, slots, lds);
+}
+template <typename F, int kEu>
+__global__ __launch_bounds__(F::kThreads) __attribute__((amdgpu_waves_per_eu(kEu, kEu))) void prompt_dq_f32_kernel(const PromptParams p, int32_t slots) {
+    __shared__ __attribute__((aligned(16))) char lds[F::kBytes];
+    dq_part<F, true>(p, blockIdx.x, slots, lds);
+}
+template <typename F, int kEu>
+__global__ __launch_bounds__(F::kThreads) __attribute__((amdgpu_waves_per_eu(kEu, kEu))) void prompt_dkdv_f32_kernel(const PromptParams p, int32_t slots) {
+    __shared__ __attribute__((aligned(16))) char lds[F::kBytes];
+    dkdv_part<F>(p, blockIdx.x, slots, lds);
 }
 
 }  // namespace
@@ -496,15 +543,22 @@ hipError_t launch_fwd(const PromptParams& p, hipStream_t st) {
     hipLaunchKernelGGL((prompt_fwd_f32_kernel<D, RG, KG, kDouble, kEu>), dim3((unsigned)(slots * p.H)), dim3(64 * RG * KG), 0, st, p, (int32_t)slots);
     return hipGetLastError();
 }
-template <int D, int RG, int KG, bool kDouble, int kEu>
+template <typename F, int kEu>
 void launch_dq(const PromptParams& p, hipStream_t st) {
-    const int64_t slots = prompt_slots(p.T, p.B, 32 * RG);
-    hipLaunchKernelGGL((prompt_dq_f32_kernel<D, RG, KG, kDouble, kEu>), dim3((unsigned)(slots * p.H)), dim3(64 * RG * KG), 0, st, p, (int32_t)slots);
+    const int64_t slots = prompt_slots(p.T, p.B, F::R);
+    hipLaunchKernelGGL((prompt_dq_f32_kernel<F, kEu>), dim3((unsigned)(slots * p.H)), dim3(F::kThreads), 0, st, p, (int32_t)slots);
 }
-template <int D, int RG, int KG, bool kDouble, int kEu>
+template <typename F, int kEu>
 void launch_dkdv(const PromptParams& p, hipStream_t st) {
-    const int64_t slots = prompt_slots(p.T, p.B, 32 * RG);
-    hipLaunchKernelGGL((prompt_dkdv_f32_kernel<D, RG, KG, kDouble, kEu>), dim3((unsigned)(slots * p.Hkv * p.shares)), dim3(64 * RG * KG), 0, st, p, (int32_t)slots);
+    const int64_t slots = prompt_slots(p.T, p.B, F::R);
+    hipLaunchKernelGGL((prompt_dkdv_f32_kernel<F, kEu>), dim3((unsigned)(slots * p.Hkv * p.shares)), dim3(F::kThreads), 0, st, p, (int32_t)slots);
+}
+template <typename F, int kEu>
+void launch_both(const PromptParams& p, hipStream_t st) {
+    // (the workgroups of dq start at a multiple of eight: heads keep to their dies)
+    const int64_t slots = prompt_slots(p.T, p.B, F::R), dkdv = (slots * p.Hkv * p.shares + kDies - 1) / kDies * kDies;
+    hipLaunchKernelGGL((prompt_delta_f32_kernel<F::D>), dim3((unsigned)(((int64_t)p.T * p.H * (F::D / 4) + 255) / 256)), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((prompt_bwd_f32_kernel<F, kEu>), dim3((unsigned)(dkdv + slots * p.H)), dim3(F::kThreads), 0, st, p, (int32_t)dkdv, (int32_t)slots);
 }
 }  // namespace
 
@@ -524,28 +578,34 @@ hipError_t launch_prompt_fwd_f32(const PromptParams& p, int32_t D, const ChipSha
     return tiles(p, 64, p.H) > 2 * chip.cus ? launch_fwd<64, 2, 2, false, 2>(p, st) : launch_fwd<64, 2, 4, false, 2>(p, st);
 }
 
-// As the forward's; dq takes two groups of short walks, too (3 x <= 333 tokens 23.8 / 22.3, 1 x 77 14.9 / 10.9, 4 x 512 40.9 / 34.4, 1 x 500 26.7 / 28.0, 1 x 2000 80 / 100).  dk and dv: 32 keys and four
-// groups where that is no more than a round and a half (us with 64 keys / 32: 3 x <= 333 tokens 30.5 / 25.1, 1 x 1000 59.9 / 49.2, 1 x 2000, three rounds, 121 / 154).
+// As the forward's, by the workgroups of both parts; small launches work them side by side (us of the whole call, one launch after the other / side by side: 12 heads of 64, 1 x 77 tokens 23 / 15,
+// 1 x 500 54 / 36, 3 x <= 333 50 / 41, 1 x 1000 93 / 68, 8 x 512 120 / 116; of 128, 1 x 1000 217 / 139, 1 x 2000 408 / 384, but 8 x 512 249 / 256).  Heads of 64: 32-row tiles and four groups
+// where both parts are no more than a round and a half (both parts, 1 x 500 32.3, 64 rows and two groups 43; 3 x <= 333, 600 workgroups, 42.3, four groups of 64 rows 33.9), two groups where they are more than
+// two to a compute unit (4 x 512 59, four groups 78; 3 x <= 333 40 / 34).
 hipError_t launch_prompt_bwd_f32(const PromptParams& p, int32_t D, const ChipShape& chip, hipStream_t st) {
     const bool small = prompt_small(p.T, p.B, p.H, chip);
+    const int64_t units = p.H + p.Hkv * p.shares;
+    typedef Form<64, 2, 2, false> Pairs;
+    typedef Form<64, 2, 4, false> Fours;
+    typedef Form<64, 1, 4, false> Short;
+    typedef Form<128, 2, 2, false> Wide;
     if (D == 128) {
-        if (small) {
-            launch_dq<128, 2, 2, false, 1>(p, st);
-            launch_dkdv<128, 2, 2, false, 1>(p, st);
+        if (small && tiles(p, 64, units) <= 4 * chip.cus) {
+            launch_both<Wide, 1>(p, st);
+        } else if (small) {
+            launch_dq<Wide, 1>(p, st);
+            launch_dkdv<Wide, 1>(p, st);
         } else {
-            launch_dq<128, 4, 1, true, 1>(p, st);
-            launch_dkdv<128, 4, 1, true, 1>(p, st);
+            launch_dq<Form<128, 4, 1, true>, 1>(p, st);
+            launch_dkdv<Form<128, 4, 1, true>, 1>(p, st);
         }
     } else if (small) {
-        const int64_t mean = p.T / p.B, rows = tiles(p, 64, p.H), units = p.Hkv * p.shares;
-        if (rows > 2 * chip.cus || mean <= 320 || (mean <= 512 && rows > chip.cus)) launch_dq<64, 2, 2, false, 2>(p, st);
-        else launch_dq<64, 2, 4, false, 2>(p, st);
-        if (2 * tiles(p, 32, units) <= 3 * chip.cus) launch_dkdv<64, 1, 4, false, 2>(p, st);
-        else if (tiles(p, 64, units) > 2 * chip.cus) launch_dkdv<64, 2, 2, false, 2>(p, st);
-        else launch_dkdv<64, 2, 4, false, 2>(p, st);
+        if (2 * tiles(p, 32, units) <= 3 * chip.cus) launch_both<Short, 2>(p, st);
+        else if (tiles(p, 64, units) > 2 * chip.cus) launch_both<Pairs, 2>(p, st);
+        else launch_both<Fours, 2>(p, st);
     } else {
-        launch_dq<64, 4, 1, true, 2>(p, st);
-        launch_dkdv<64, 4, 1, true, 1>(p, st);
+        launch_dq<Form<64, 4, 1, true>, 2>(p, st);
+        launch_dkdv<Form<64, 4, 1, true>, 1>(p, st);
     }
     return hipGetLastError();
 }

@@ -107,7 +107,7 @@ def test_one_prompt(B, n, D, causal, dtype):
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("lengths,H,Hkv", [([40] * 43 + [130, 7], 16, 8), ([500, 300, 200], 24, 24)], ids=["short", "long"])
+@pytest.mark.parametrize("lengths,H,Hkv", [([40] * 43 + [130, 7], 16, 8), ([500, 300, 200], 24, 24), ([500, 300, 200], 8, 4)], ids=["short", "long", "fewer"])
 def test_some_tiles(B, lengths, H, Hkv, D, causal, dtype):
     """More tiles than the chip holds at once, but not many times as many."""
     _check(B, lengths, H, Hkv, D, dtype, causal, behind=3)
