@@ -4,8 +4,8 @@
 //   dv_j = sum_i P_ij dout_i,   dS_ij = P_ij (dout_i . v_j - delta_i),   dq_i = scale sum_j dS_ij k_j,   dk_j = scale sum_i dS_ij q_i,
 // the sums of dk and dv over the query heads of a key head too.  P is taken again from lse: nothing of the forward's is kept.
 //
-// Two launches: dq, which also leaves -delta and lse in base-2 units of every row in the workspace, and dk and dv.  In either a workgroup owns
-// the rows that its results belong to, as operands in registers, and walks the others, which go global -> LDS stages ahead: no sum
+// Two launches: dq, which also leaves -delta and -lse / scale of every row in the workspace, and dk and dv; or, where those leave places free, one that leaves these numbers and
+// one of both.  In either a workgroup owns the rows that its results belong to, as operands in registers, and walks the others, which go global -> LDS stages ahead: no sum
 // is shared between workgroups, and every one has a fixed order.  (Where a launch has few workgroups, those of a key head share its query heads
 // out: partial sums in fp32, added up in order by a third launch.)
 #include <algorithm>
@@ -16,7 +16,13 @@ namespace dfa {
 
 namespace {
 
-// A wave of the launch of dq: 32 rows, their dq, and one beat of its walk along the keys.
+// -delta and lse of a row, left for dk and dv: what their first products start from.
+__device__ __forceinline__ void leave_numbers(const PromptParams& p, int64_t at, float nd, float lse) {
+    p.ndelta[at] = nd;
+    p.lse2[at] = lse == -INFINITY ? -INFINITY : -lse / p.scale;
+}
+
+// A wave of dq: 32 rows, their dq, and one beat of its walk along the keys.
 template <int D>
 struct RowWave {
     static constexpr int kSteps = D / 16, kHalves = D / 32;
@@ -106,17 +112,20 @@ struct RowWave {
 // Bound: matrix products at the power limit where walks are long (8 x 2048 tokens, 16 heads of 128, not causal: 402 us, 1.03 PFLOP/s; 420 without the beats),
 // the start and the end of a workgroup where they are short (causal: 243 us, 0.85).  32 rows a wave of D = 64, too: 64 need 336 registers for the beat (139 us for 16 causal
 // sequences of up to 2048 tokens, 16 heads; 164 with 64 rows and no beats).
-template <int D>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_dq_kernel(const PromptParams p, int32_t slots) {
+//
+// Blocks in LDS: of keys and of values those that a beat reads, two that are under way, and what is left to the waves that end first, two blocks before the
+// last one.
+constexpr int kKeyRing = 6, kValueRing = 4;
+template <int D> constexpr size_t kDqBytes = (kKeyRing + kValueRing) * 64 * D;
+
+// Workgroup x.  kLeave: it leaves the numbers of its rows.
+template <int D, bool kLeave>
+__device__ __forceinline__ void dq_part(const PromptParams& p, int32_t x, int32_t slots, char* raw) {
     constexpr int R = 128, kBlock = 32 * D, kSteps = D / 16, kHalves = D / 32, kCopies = 2 * kPromptCopies<D>;
-    // Blocks in LDS: of keys and of values those that a beat reads, two that are under way, and what is left to the waves that end first, two blocks before the
-    // last one.
-    constexpr int kKeyRing = 6, kValueRing = 4;
-    __shared__ __attribute__((aligned(1024))) uint16_t lds[kKeyRing + kValueRing][kBlock];
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, g = lane >> 5;
     int32_t slot, h;
-    prompt_place(blockIdx.x, slots, p.H, slot, h);
+    prompt_place(x, slots, p.H, slot, h);
     const PromptTile tile = prompt_tile<R>(p, slot, lane);
     if (tile.empty) return;
     const int32_t rows = min(R, tile.n - tile.t0);
@@ -135,7 +144,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const char* const kbase = reinterpret_cast<const char*>(static_cast<const uint16_t*>(p.k) + tile.first * p.skn + (h / p.group) * p.skh);
     const char* const vbase = reinterpret_cast<const char*>(static_cast<const uint16_t*>(p.v) + tile.first * p.svn + (h / p.group) * p.svh);
     const uint32_t kpitch = (uint32_t)(p.skn * 2), vpitch = (uint32_t)(p.svn * 2);
-    const uint32_t lds_addr = (uint32_t)(uintptr_t)DFA_LDS_PTR(void, &lds[0][0]);
+    const uint32_t lds_addr = (uint32_t)(uintptr_t)DFA_LDS_PTR(void, raw);
     constexpr uint32_t kBytes = kBlock * 2;
     auto key_slot = [](int32_t n) { return (uint32_t)(n % kKeyRing) * kBytes; };
     auto value_slot = [](int32_t n) { return (uint32_t)(kKeyRing + n % kValueRing) * kBytes; };
@@ -168,10 +177,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         w.nd = -wave_half_sum(part);
         const float l = p.lse[(int64_t)h * p.T + row0 + row];
         w.lse2 = l == -INFINITY ? INFINITY : l * kLog2e;     // a row without weights has none here either
-        if (g == 0 && r < rows) {
-            p.ndelta[(int64_t)h * p.T + row0 + r] = w.nd;
-            p.lse2[(int64_t)h * p.T + row0 + r] = l == -INFINITY ? -INFINITY : -l / p.scale;         // what the other launch's scores start from
-        }
+        if (kLeave && g == 0 && r < rows) leave_numbers(p, (int64_t)h * p.T + row0 + r, w.nd, l);
     }
     issue(0);
     issue(1);
@@ -240,9 +246,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     asm volatile("" : "+v"(lane_e));
     __syncthreads();
     constexpr int kMine = 32 * (2 * D + 16);
-    static_assert(sizeof(lds) >= 4 * kMine, "every wave's rows fit the blocks");
+    static_assert(kDqBytes<D> >= 4 * kMine, "every wave's rows fit the blocks");
     if (!live) return;
-    store_rows<D>(w.acc, p.scale, reinterpret_cast<char*>(&lds[0][0]) + wave * kMine, dq + 32 * wave * pitch, pitch, rows - 32 * wave, lane_e);
+    store_rows<D>(w.acc, p.scale, raw + wave * kMine, dq + 32 * wave * pitch, pitch, rows - 32 * wave, lane_e);
 }
 
 // A wave of the launch of dk and dv: 32 keys, their dk and dv, and one beat of its walk along the rows.
@@ -325,17 +331,21 @@ struct KeyWave {
 
 // dk and dv: 128 keys of one key head, 32 to a wave, walked along the rows of its query heads (of a share of them).  Per block S = Q K^T and
 // dP = dO V^T, started from -lse / scale and -delta, dV^T += dO^T P, dK^T += Q^T dS.
-template <int D, int kEu>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu))) void prompt_dkdv_kernel(const PromptParams p, int32_t slots) {
-    constexpr int R = 128, kBlock = 32 * D, kHalves = D / 32;
-    // the walk is in five blocks between two barriers: second products, numbers, first products, and what is read ahead
-    constexpr int kStages = 8, kCopies = 2 * kPromptCopies<D> + 1;
-    __shared__ __attribute__((aligned(1024))) uint16_t lds[kStages][2][kBlock];      // q, dout
-    __shared__ __attribute__((aligned(256))) float scalars[kStages][2][32];          // -lse / scale, -delta
+//
+// The walk is in five blocks between two barriers: second products, numbers, first products, and what is read ahead.
+constexpr int kStages = 8;
+template <int D> constexpr size_t kDkdvBytes = kStages * (2 * 64 * D + 256);
+
+// Workgroup x.
+template <int D>
+__device__ __forceinline__ void dkdv_part(const PromptParams& p, int32_t x, int32_t slots, char* raw) {
+    constexpr int R = 128, kBlock = 32 * D, kHalves = D / 32, kCopies = 2 * kPromptCopies<D> + 1;
+    typedef float Scalars[2][32];            // -lse / scale, -delta
+    Scalars* const scalars = reinterpret_cast<Scalars*>(raw + kStages * 2 * kBlock * 2);             // behind the stages, of q and dout
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, g = lane >> 5;
     int32_t slot, unit;
-    prompt_place(blockIdx.x, slots, p.Hkv * p.shares, slot, unit);
+    prompt_place(x, slots, p.Hkv * p.shares, slot, unit);
     slot = slots - 1 - slot;                                                          // the first keys, which most rows see, come first
     const int32_t hk = unit / p.shares, share = unit % p.shares;
     const PromptTile tile = prompt_key_tile<R>(p, slot, lane);
@@ -360,7 +370,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
     const int32_t my0 = tile.t0 + 32 * wave;
     const bool live = my0 < tile.n;
 
-    const uint32_t lds_addr = (uint32_t)(uintptr_t)DFA_LDS_PTR(void, &lds[0][0][0]), sc_addr = (uint32_t)(uintptr_t)DFA_LDS_PTR(void, &scalars[0][0][0]);
+    const uint32_t lds_addr = (uint32_t)(uintptr_t)DFA_LDS_PTR(void, raw), sc_addr = (uint32_t)(uintptr_t)DFA_LDS_PTR(void, &scalars[0][0][0]);
     const uint32_t qpitch = (uint32_t)(p.sqn * 2), gpitch = (uint32_t)((int64_t)p.H * D * 2);
     constexpr uint32_t kStageBytes = 2 * kBlock * 2;
     auto stage_of = [](int32_t n) { return (uint32_t)(n & (kStages - 1)) * kStageBytes; };
@@ -492,11 +502,46 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu)))
         }
     } else {
         constexpr int kMine = 32 * (2 * D + 16);
-        static_assert(sizeof(lds) >= 4 * kMine, "every wave's rows fit the stages");
-        char* const mine = reinterpret_cast<char*>(&lds[0][0][0]) + wave * kMine;
+        static_assert(kDkdvBytes<D> >= 4 * kMine, "every wave's rows fit the stages");
+        char* const mine = raw + wave * kMine;
         store_rows<D>(w.dk, p.scale, mine, dk + r0 * pitch, pitch, rows - r0, lane_e);
         store_rows<D>(w.dv, 1.f, mine, dv + r0 * pitch, pitch, rows - r0, lane_e);
     }
+}
+
+template <int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_dq_kernel(const PromptParams p, int32_t slots) {
+    __shared__ __attribute__((aligned(1024))) char lds[kDqBytes<D>];
+    dq_part<D, true>(p, blockIdx.x, slots, lds);
+}
+template <int D, int kEu>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu))) void prompt_dkdv_kernel(const PromptParams p, int32_t slots) {
+    __shared__ __attribute__((aligned(1024))) char lds[kDkdvBytes<D>];
+    dkdv_part<D>(p, blockIdx.x, slots, lds);
+}
+
+// The numbers of all rows: a row's D numbers are D / 8 lanes'.
+template <int D>
+__global__ __launch_bounds__(256) void prompt_delta_kernel(const PromptParams p) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, r = i / (D / 8);
+    if (r >= (int64_t)p.T * p.H) return;                 // (whole rows' lanes)
+    const int64_t at = (r % p.H) * p.T + r / p.H;
+    const bf16x8 a = *reinterpret_cast<const bf16x8*>(static_cast<const uint16_t*>(p.out) + 8 * i), b = *reinterpret_cast<const bf16x8*>(static_cast<const uint16_t*>(p.dout) + 8 * i);
+    float delta = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) delta = fmaf((float)a[e], (float)b[e], delta);
+#pragma unroll
+    for (int d = 1; d < D / 8; d *= 2) delta += __shfl_xor(delta, d);
+    if (threadIdx.x % (D / 8) == 0) leave_numbers(p, at, -delta, p.lse[at]);
+}
+
+// Both in one launch behind that one, the longer walks first: for launches that leave places free.
+template <int D, int kEu>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kEu, kEu))) void prompt_bwd_kernel(const PromptParams p, int32_t dkdv_count, int32_t slots) {
+    __shared__ __attribute__((aligned(1024))) char lds[std::max(kDqBytes<D>, kDkdvBytes<D>)];
+    const int32_t x = blockIdx.x;
+    if (x >= dkdv_count) dq_part<D, false>(p, x - dkdv_count, slots, lds);
+    else if (x < slots * p.Hkv * p.shares) dkdv_part<D>(p, x, slots, lds);
 }
 
 // Adds up the partial sums of dk and dv, four numbers a thread.
@@ -515,10 +560,17 @@ __global__ __launch_bounds__(256) void prompt_sum_kernel(const PromptParams p, i
 }
 
 template <int D, int kEu>
-hipError_t launch(const PromptParams& p, hipStream_t st) {
+hipError_t launch(const PromptParams& p, bool both, hipStream_t st) {
     const int64_t slots = prompt_slots(p.T, p.B, 128);
-    hipLaunchKernelGGL((prompt_dq_kernel<D>), dim3((unsigned)(slots * p.H)), dim3(256), 0, st, p, (int32_t)slots);
-    hipLaunchKernelGGL((prompt_dkdv_kernel<D, kEu>), dim3((unsigned)(slots * p.Hkv * p.shares)), dim3(256), 0, st, p, (int32_t)slots);
+    if (both) {
+        // (the workgroups of dq start at a multiple of eight: heads keep to their dies)
+        const int64_t dkdv = (slots * p.Hkv * p.shares + kDies - 1) / kDies * kDies;
+        hipLaunchKernelGGL((prompt_delta_kernel<D>), dim3((unsigned)(((int64_t)p.T * p.H * (D / 8) + 255) / 256)), dim3(256), 0, st, p);
+        hipLaunchKernelGGL((prompt_bwd_kernel<D, kEu>), dim3((unsigned)(dkdv + slots * p.H)), dim3(256), 0, st, p, (int32_t)dkdv, (int32_t)slots);
+    } else {
+        hipLaunchKernelGGL((prompt_dq_kernel<D>), dim3((unsigned)(slots * p.H)), dim3(256), 0, st, p, (int32_t)slots);
+        hipLaunchKernelGGL((prompt_dkdv_kernel<D, kEu>), dim3((unsigned)(slots * p.Hkv * p.shares)), dim3(256), 0, st, p, (int32_t)slots);
+    }
     return hipGetLastError();
 }
 
@@ -530,7 +582,11 @@ int32_t prompt_bwd_shares(int32_t T, int32_t B, int32_t H, int32_t Hkv, const Ch
 }
 
 hipError_t launch_prompt_bwd(const PromptParams& p, bool f32, int32_t D, const ChipShape& chip, hipStream_t st) {
-    const hipError_t e = f32 ? launch_prompt_bwd_f32(p, D, chip, st) : D == 128 ? launch<128, 1>(p, st) : launch<64, 2>(p, st);
+    // Side by side where the launches' longest walks decide (us of the whole call, one after the other / side by side: 12 heads of 64, 3 x <= 333 tokens 31 / 23, 1 x 1000 50 / 32, 1 x 4000 177 / 121,
+    // 8 x 512 40 / 41; of 128, with one workgroup to a compute unit, 3 x <= 333 46 / 34, 4 x 512 48 / 44, 1 x 4000, 768 workgroups, 263 / 256, 8 x 512 67 / 74).
+    const int64_t tiles = std::max<int64_t>((p.T + 127) / 128, p.B) * (p.H + p.Hkv * p.shares);
+    const bool both = prompt_small(p.T, p.B, p.H, chip) && (D == 64 || tiles <= 2 * chip.cus);
+    const hipError_t e = f32 ? launch_prompt_bwd_f32(p, D, chip, st) : D == 128 ? launch<128, 1>(p, both, st) : launch<64, 2>(p, both, st);
     if (e != hipSuccess || p.shares == 1) return e;
     const int64_t tensor = (int64_t)p.T * p.Hkv * D;
     const dim3 grid((unsigned)((2 * tensor / 4 + 255) / 256));
