@@ -177,8 +177,10 @@ template <int QB> constexpr int kValueRing = 4 * QB;
 
 // KG: groups of waves that take every KG-th block of 32 keys (a "block" of the walk is KG of them then) and merge their results at the end.  For launches of
 // fewer workgroups than fit the chip, where the longest walk decides: half the rows, half the walk (1000 tokens, 16 heads of 128: 19.2 us, 24.0 with KG = 1).
+// Waves of a SIMD: 32 rows of D = 64 leave room for three (16 x 512 tokens, 12 heads: 22.6 us, 26.1 with two).
+template <int D, int QB, int KG> constexpr int kWaves = D == 64 && QB == 1 && KG == 1 ? 3 : 2;
 template <int D, int QB, int KG>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_fwd_kernel(const PromptParams p, int32_t slots) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kWaves<D, QB, KG>, kWaves<D, QB, KG>))) void prompt_fwd_kernel(const PromptParams p, int32_t slots) {
     constexpr int kRowGroups = 4 / KG, R = 32 * QB * kRowGroups, kBlock = 32 * D;    // rows; elements of 32 keys or values
     constexpr int kCopies = 2 * KG * kPromptCopies<D>;                               // a wave's, of a block's keys and values
     __shared__ __attribute__((aligned(1024))) uint16_t lds[kRing + kValueRing<QB>][KG][kBlock];
@@ -418,9 +420,11 @@ hipError_t launch_prompt_fwd(const PromptParams& p, bool f32, int32_t D, const C
     const int64_t mean = p.T / p.B, halves = std::max<int64_t>((p.T + 63) / 64, std::min(p.T, p.B)) * p.H, resident = (D == 64 ? 2 : 1) * (int64_t)chip.cus;
     if (mean >= 384 && (halves <= resident || (mean >= 1536 && halves <= 2 * resident))) return D == 64 ? launch<64, 1, 2>(p, st) : launch<128, 1, 2>(p, st);
     if (D == 128) return launch<128, 1, 1>(p, st);
-    // 64 rows to a wave (a fragment read feeds two products) where that leaves enough workgroups (12 heads, us with 32 rows / 64: 8 x 512 tokens 14.4 / 23.1, 16 x 512 24.1 /
-    // 24.3, 27000 tokens of 32 heads 291 / 259)
-    return ((int64_t)p.T / 128 + std::min(p.T, p.B)) * p.H < 4 * chip.cus ? launch<64, 1, 1>(p, st) : launch<64, 2, 1>(p, st);
+    // 64 rows to a wave (a fragment read feeds two products, but two waves to a SIMD) where that leaves enough workgroups, and walks are long enough for the products to decide
+    // (us with 32 rows / 64: 8 x 512 tokens, 12 heads 14.4 / 23.1, 32 x 512 36.1 / 40.1, 24 of up to 2048, 32 heads 260 / 263, 8 x 4096, 12 heads 254 / 251, not causal 432 / 392, 16384 tokens, 32 heads
+    // 1107 / 1023).
+    const bool enough = ((int64_t)p.T / 128 + std::min(p.T, p.B)) * p.H >= 4 * chip.cus;
+    return enough && (p.causal ? mean / 2 : mean) >= 1024 ? launch<64, 2, 1>(p, st) : launch<64, 1, 1>(p, st);
 }
 
 }  // namespace dfa

@@ -113,6 +113,12 @@ def test_some_tiles(B, lengths, H, Hkv, D, causal, dtype):
     _check(B, lengths, H, Hkv, D, dtype, causal, behind=3)
 
 
+@pytest.mark.parametrize("causal,n", [(True, 2090), (False, 1500)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_tiles_of_long_walks(B, D, causal, n):
+    _check(B, [n], 96, 8, D, "bf16", causal, behind=10, backward=False)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_many_sequences(B, dtype):
     """More sequences than a wave has lanes, than are ranked, and than 64 times 64."""
@@ -143,8 +149,8 @@ def test_climbing_scores(B, D, dtype):
     _within(lse, l, l_tol, "lse")
 
 
-# two sequences of a few tiles; one whose walk waves share; many tiles (the value lies in the second sequence, row 50 of it, or row 500 of the only one)
-@pytest.mark.parametrize("lengths,H,at", [([150, 140], 4, 200), ([600], 4, 500), ([150] + [90] * 69, 16, 200)], ids=["few", "shared", "many"])
+# two sequences of a few tiles; one whose walk waves share; many tiles; many tiles of long walks (the value lies in the second sequence, row 50 of it, or in the only one)
+@pytest.mark.parametrize("lengths,H,at", [([150, 140], 4, 200), ([600], 4, 500), ([150] + [90] * 69, 16, 200), ([2090], 64, 1995)], ids=["few", "shared", "many", "long"])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
