@@ -4,7 +4,7 @@
 //   g = dy w,  u = h r,  dx = r (g - u mean(g u)) + dh,  dw = sum over the rows of dy u
 // In fp32 from the operands to the one rounding of each result: y comes of h before it is rounded.
 //
-// Bound: memory; every operand is read once and every result written once.  A row is held in registers by kThreads threads, pieces of
+// Bound: memory (16384 x 4096 with the residual to 8 bits 81.6 us, 5.8 TB/s; gradients of 32768 x 768 34.3 us, 5.9 TB/s, and 4.3 for the sum of dw); every operand is read once and every result written once.  A row is held in registers by kThreads threads, pieces of
 // eight elements kThreads pieces apart, so that every wave-wide load is of whole lines and a block of 128 elements is 16 neighbouring lanes'.
 #include <algorithm>
 
@@ -270,6 +270,79 @@ __global__ __launch_bounds__(kNormGroup<kThreads>) void norm_backward_kernel(con
     }
 }
 
+// The same of rows that registers do not hold (1024 threads have 128 each): a thread reads its pieces again where it uses them, from the caches, and its part of dw stays in LDS, every
+// number its own thread's.  2048 rows of 32768 in bf16: 134 us, 4.0 TB/s; 423 with all of it in registers and spilled.
+template <typename T, typename W>
+__global__ __launch_bounds__(1024) void norm_backward_wide_kernel(const NormBackwardParams p) {
+    constexpr int kThreads = 1024;
+    __shared__ float lds[16];
+    __shared__ float dw[kNormMaxCols / 8][8 + 1];        // of a piece (a number between pieces: lanes meet different banks)
+    const int i = threadIdx.x;
+    const int64_t pieces = (p.C + 7) / 8;
+    for (int64_t n = i; n < pieces; n += kThreads)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dw[n][e] = 0.f;
+    for (int64_t row = blockIdx.x; row < p.M; row += p.workgroups) {
+        const T *const h_row = static_cast<const T*>(p.h) + row * p.ldh, *const dy_row = static_cast<const T*>(p.dy) + row * p.lddy;
+        auto operands = [&](int64_t n, float (&dy)[8], float (&g)[8], float (&h)[8]) {
+            to_floats(load_chunk(h_row, 8 * n, p.C), h);
+            to_floats(load_chunk(dy_row, 8 * n, p.C), dy);
+            float w[8];
+            if (p.weight) to_floats(load_chunk(static_cast<const W*>(p.weight), 8 * n, p.C), w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) g[e] = p.weight ? dy[e] * w[e] : dy[e];
+        };
+        // the sums of (h by)^2 and of g h of
+        auto sums = [&](float by, float of, float& squares, float& both) {
+            squares = both = 0.f;
+            for (int64_t n = i; n < pieces; n += kThreads) {
+                float dy[8], g[8], h[8];
+                operands(n, dy, g, h);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    squares = fmaf(h[e] * by, h[e] * by, squares);
+                    both = fmaf(g[e], h[e] * of, both);
+                }
+            }
+            squares = row_sum<kThreads>(squares, lds);
+            both = row_sum<kThreads>(both, lds);
+        };
+        float squares, both, r, mean;
+        sums(1.f, 1.f, squares, both);
+        if (ordinary(squares, p.eps)) {
+            r = rsqrtf(squares / (float)p.C + p.eps);
+            mean = both * r / (float)p.C;
+        } else {
+            const float by = unusual_by(squares);
+            sums(by, 0.f, squares, both);
+            r = rsqrtf(squares / (float)p.C + p.eps * by * by) * by;
+            sums(0.f, r, squares, both);
+            mean = both / (float)p.C;
+        }
+        for (int64_t n = i; n < pieces; n += kThreads) {
+            float dy[8], g[8], h[8], dh[8], dx[8];
+            operands(n, dy, g, h);
+            if (p.dh) to_floats(load_chunk(static_cast<const T*>(p.dh) + row * p.lddh, 8 * n, p.C), dh);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float u = h[e] * r;
+                dw[n][e] = fmaf(dy[e], u, dw[n][e]);
+                dx[e] = r * fmaf(-u, mean, g[e]);
+                if (p.dh) dx[e] += dh[e];
+            }
+            store_chunk(static_cast<T*>(p.dx) + row * p.lddx, 8 * n, p.C, dx);
+        }
+    }
+    if (!p.dw) return;
+    float* const to = p.workgroups > 1 ? p.parts + (int64_t)blockIdx.x * p.C : p.dw;
+    for (int64_t n = i; n < pieces; n += kThreads) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = dw[n][e];
+        store_chunk(to, 8 * n, p.C, x);
+    }
+}
+
 // dw of the workgroups' parts: 16 columns a workgroup, 64 threads that take every 64th part of each.  (64 columns and 16 threads: 20 us instead of 3.5 for 1024
 // parts of 768 columns, where twelve workgroups then read 64 parts one after the other.)
 __global__ __launch_bounds__(1024) void norm_sum_kernel(const float* parts, float* dw, int64_t C, int32_t count) {
@@ -314,7 +387,8 @@ hipError_t launch_form(const NormParams& p, hipStream_t st) {
 }
 template <typename T, typename W, int kThreads, int N>
 hipError_t launch_form(const NormBackwardParams& p, hipStream_t st) {
-    hipLaunchKernelGGL((norm_backward_kernel<T, W, kThreads, N>), dim3((unsigned)p.workgroups), dim3(kNormGroup<kThreads>), 0, st, p);
+    if constexpr (kThreads == 1024) hipLaunchKernelGGL((norm_backward_wide_kernel<T, W>), dim3((unsigned)p.workgroups), dim3(1024), 0, st, p);
+    else hipLaunchKernelGGL((norm_backward_kernel<T, W, kThreads, N>), dim3((unsigned)p.workgroups), dim3(kNormGroup<kThreads>), 0, st, p);
     return hipGetLastError();
 }
 template <typename T, typename W, typename Params>

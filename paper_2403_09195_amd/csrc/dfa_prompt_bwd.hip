@@ -332,6 +332,9 @@ struct KeyWave {
 // dk and dv: 128 keys of one key head, 32 to a wave, walked along the rows of its query heads (of a share of them).  Per block S = Q K^T and
 // dP = dO V^T, started from -lse / scale and -delta, dV^T += dO^T P, dK^T += Q^T dS.
 //
+// Bound: a fragment from LDS for every product, with one wave to a SIMD of D = 128 (8 x 2048 tokens, 16 heads, not causal: 571 us, 0.96 PFLOP/s; causal 380-395; of 64, two waves: 160, 0.86).  Two waves of
+// 128 with the values from LDS take 374 against 379, and twice as long for a walk (prompts of a few hundred workgroups 569 / 398).
+//
 // The walk is in five blocks between two barriers: second products, numbers, first products, and what is read ahead.
 constexpr int kStages = 8;
 template <int D> constexpr size_t kDkdvBytes = kStages * (2 * 64 * D + 256);

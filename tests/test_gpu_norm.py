@@ -52,7 +52,7 @@ def _check_quantized(B, q, y):
 
 
 SIZES = [(1, 1), (1, 4096), (3, 7), (5, 129), (17, 1000), (2, 2049), (33, 768), (4, 4097), (2, 8200), (2, 16384), (1, 20001), (1, 32768), (1030, 96), (1100, 777), (1025, 1024),
-         (5000, 300), (3500, 1000), (2000, 2100), (1100, 4000), (600, 4500), (300, 9000)]
+         (5000, 300), (3500, 1000), (2000, 2100), (1100, 4000), (600, 4500), (300, 9000), (530, 20001)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
