@@ -418,10 +418,10 @@ hipError_t launch(const PromptParams& p, hipStream_t st) {
 hipError_t launch_prompt_fwd(const PromptParams& p, bool f32, int32_t D, const ChipShape& chip, hipStream_t st) {
     if (f32) return launch_prompt_fwd_f32(p, D, chip, st);
     // What is known of the lengths is their mean.  Two groups of waves to a walk where the workgroups of half the rows are resident at once (two to a compute unit, one of
-    // D = 128), or where walks are so long that twice as many do (us with one group / two: 12 heads of 64, 1000 tokens 19.0 / 14.1, 4000 60.5 / 44.3, 4 x 512 12.3 / 11.6,
-    // 8 x 512 14.6 / 19.2; 16 heads of 128, 300 tokens 10.9 / 11.3, 1000 24.0 / 19.2, 2000 42.2 / 39.2, 4000 88 / 123).
+    // D = 128), or where walks are so long that half as many more do (us with one group / two: 12 heads of 64, 1000 tokens 19.0 / 14.1, 2 x 2000 33.7 / 29.2, 3000 45 / 33, 4 x 512 12.3 / 11.6,
+    // 8 x 512 14.6 / 19.2, 32 heads, 2000 tokens 36.5 / 40.1; 16 heads of 128, 300 tokens 10.9 / 11.3, 1000 24.0 / 19.2, 2000 42.2 / 39.2, 4000 88 / 123).
     const int64_t mean = p.T / p.B, halves = std::max<int64_t>((p.T + 63) / 64, std::min(p.T, p.B)) * p.H, resident = (D == 64 ? 2 : 1) * (int64_t)chip.cus;
-    if (mean >= 384 && (halves <= resident || (mean >= 1536 && halves <= 2 * resident))) return D == 64 ? launch<64, 1, 2>(p, st) : launch<128, 1, 2>(p, st);
+    if (mean >= 384 && (halves <= resident || (mean >= 1536 && 2 * halves <= 3 * resident))) return D == 64 ? launch<64, 1, 2>(p, st) : launch<128, 1, 2>(p, st);
     if (D == 128) return launch<128, 1, 1>(p, st);
     // 64 rows to a wave (a fragment read feeds two products, but two waves to a SIMD) where that leaves enough workgroups, and walks are long enough for the products to decide
     // (us with 32 rows / 64: 8 x 512 tokens, 12 heads 14.4 / 23.1, 32 x 512 36.1 / 40.1, 24 of up to 2048, 32 heads 260 / 263, 8 x 4096, 12 heads 254 / 251, not causal 432 / 392, 16384 tokens, 32 heads
