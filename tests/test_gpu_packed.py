@@ -64,7 +64,7 @@ class Step:
 
 
 @pytest.mark.parametrize("page", [16, 32, 64, 128])
-@pytest.mark.parametrize("Bsz,most", [(1, 1), (1, 5000), (3, 40), (70, 200), (1023, 9), (1024, 3), (1025, 3), (2500, 12)])
+@pytest.mark.parametrize("Bsz,most", [(1, 1), (1, 5000), (3, 40), (70, 200), (1023, 9), (1024, 3), (1025, 3), (2500, 12), (4500, 4)])
 def test_steps(B, Bsz, most, page):
     """Prompts, single tokens, sequences that end and begin again; one launch and two."""
     width = 2 * most // page + 4
