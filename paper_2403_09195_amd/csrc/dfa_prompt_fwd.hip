@@ -9,7 +9,7 @@
 // products of the next block's scores and of the block before, and between them, slot by slot, the exponentials of the block in hand.
 //
 // Bound: the power limit and a fragment from LDS for every product where walks are long (16384 tokens, 32 heads of 128 in 8: 1.91-2.00 ms, 1.10-1.15 PFLOP/s; on zeros 1.41 ms), the ends of workgroups where they
-// are short (24 prompts of up to 2048 tokens: 445-471 us).  32 rows a wave of D = 128: 64 take 512 registers, one wave to a SIMD, and 3.0 ms instead of 2.2 (without the beats).
+// are short (24 prompts of up to 2048 tokens: 445-471 us).  32 rows a wave of D = 128: 64 take 512 registers, one wave to a SIMD, and 2.25 ms instead of 1.99.
 #include <algorithm>
 
 #include "dfa_prompt.h"
