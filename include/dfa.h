@@ -488,8 +488,8 @@ int dfa_prompt_attention_backward(const void *q, const void *k, const void *v, d
  *   q            host struct or NULL: receives y in e4m3, blocks of 128 along the rows, as dfa_quantize does (from the fp32 values, not from
  *                y's rounded ones); one of y and q at least.  Values up to the next multiple of 128 columns (zeros) and scale bytes up to the next multiple of 16
  *                rows are written.
- * h, y and q apart from the operands and each other (but for h as said).  Rows are exact at any size that fp32 holds: sums of squares that overflow, or fall below
- * 1e-30 beside an eps that does, are taken again, scaled.  C is 32768 at most.  Asynchronous on `stream`; allocates nothing.
+ * h, y and q apart from the operands and each other (but for h as said).  Rows are exact at any size that fp32 holds, subnormal numbers included: sums of squares that
+ * overflow, or fall below 1e-30 beside an eps that does, are taken again, scaled, and r, which may then be no fp32 number, is held in two factors.  C is 32768 at most.  Asynchronous on `stream`; allocates nothing.
  */
 int dfa_rms_norm(const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, dfa_dtype_t weight_dt, dfa_dtype_t dt, float eps,
                  void *h, int64_t ldh, void *y, int64_t ldy, const dfa_quantized_t *q, int64_t M, int64_t C, void *stream);
@@ -501,7 +501,8 @@ int dfa_rms_norm(const void *x, int64_t ldx, const void *residual, int64_t ldr, 
  *               dx may be dy or dh itself (same pointer and pitch), else apart from the operands
  *   workspace   device, 16-byte aligned, ..._workspace_bytes(M, C) (0 = none, NULL allowed; not used without dw): partial sums of dw.  Written and read by this
  *               call only: calls that may overlap, captured ones among them, need one each.
- * Sums are in a fixed order: equal calls give equal results.  Asynchronous on `stream`; allocates nothing.
+ * Rows of h of any size, as above; a dx that fp32 does not hold is infinite or NaN.  Sums are in a fixed order: equal calls give equal results.  Asynchronous on `stream`;
+ * allocates nothing.
  */
 size_t dfa_rms_norm_backward_workspace_bytes(int64_t M, int64_t C);
 int dfa_rms_norm_backward(const void *dy, int64_t lddy, const void *h, int64_t ldh, const void *weight, dfa_dtype_t weight_dt, dfa_dtype_t dt, float eps,

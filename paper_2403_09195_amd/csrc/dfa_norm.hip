@@ -35,20 +35,25 @@ __device__ __forceinline__ Chunk<T> load_chunk(const T* row, int64_t at, int64_t
     return c;
 }
 template <typename T>
+__device__ __forceinline__ Chunk<T> to_chunk(const float (&x)[8]) {
+    Chunk<T> c;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c.w[i] = __builtin_bit_cast(uint32_t, x[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
+            const bf16x2v v = {(__bf16)x[2 * i], (__bf16)x[2 * i + 1]};
+            c.w[i] = __builtin_bit_cast(uint32_t, v);
+        }
+    }
+    return c;
+}
+template <typename T>
 __device__ __forceinline__ void store_chunk(T* row, int64_t at, int64_t cols, const float (&x)[8]) {
     if (at + 8 <= cols) {
-        Chunk<T> c;
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) c.w[i] = __builtin_bit_cast(uint32_t, x[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
-                const bf16x2v v = {(__bf16)x[2 * i], (__bf16)x[2 * i + 1]};
-                c.w[i] = __builtin_bit_cast(uint32_t, v);
-            }
-        }
+        const Chunk<T> c = to_chunk<T>(x);
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T) / 2; ++i)
             reinterpret_cast<words_anywhere*>(row + at)[i] = words_anywhere{c.w[4 * i], c.w[4 * i + 1], c.w[4 * i + 2], c.w[4 * i + 3]};
@@ -79,21 +84,18 @@ __device__ __forceinline__ float row_sum(float x, float* lds) {
 // eps is no larger: they are summed up again, scaled.
 __device__ __forceinline__ bool ordinary(float sum, float eps) { return !(sum > 1e37f) && !(sum < 1e-30f && eps < 1e-30f); }
 
-// The scale of the second sum.
-__device__ __forceinline__ float unusual_by(float sum) { return sum > 1.f ? 0x1p-80f : 0x1p80f; }
+// The scale of the second sum: a row of 32768 numbers of 2^128 does not overflow it, and one number of 2^-149 among as many zeros has a normal mean of squares.
+__device__ __forceinline__ float unusual_by(float sum) { return sum > 1.f ? 0x1p-80f : 0x1p100f; }
 
-// r of a row whose sum of squares is `sum`.  All threads of the row call it.
-template <int kThreads, int N>
-__device__ __forceinline__ float row_scale(const float (&h)[N][8], float sum, float eps, float cols, float* lds) {
-    if (ordinary(sum, eps)) return rsqrtf(sum / cols + eps);
-    const float by = unusual_by(sum);
-    float s = 0.f;
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s = fmaf(h[n][i] * by, h[n][i] * by, s);
-    s = row_sum<kThreads>(s, lds);
-    return rsqrtf(s / cols + eps * by * by) * by;
+// r of a row in two factors.  The second is a power of two, and 1 but for rows below 2^-120, whose r may be no fp32 number, and beyond 2^126, whose r is a subnormal one.
+struct RowScale {
+    float at, by;
+};
+// `sum`: of (h unusual)^2
+__device__ __forceinline__ RowScale unusual_scale(float sum, float eps, float cols, float unusual) {
+    const float r = rsqrtf(sum / cols + eps * unusual * unusual);
+    if (unusual < 1.f) return r < 0x1p-46f ? RowScale{r * 0x1p-76f, 0x1p-4f} : RowScale{r * 0x1p-80f, 1.f};
+    return r > 0x1p20f ? RowScale{r * 0x1p60f, 0x1p40f} : RowScale{r * 0x1p100f, 1.f};
 }
 
 template <typename T, typename W, int kThreads, int N>
@@ -127,11 +129,37 @@ __global__ __launch_bounds__(kNormGroup<kThreads>) void norm_kernel(const NormPa
         for (int e = 0; e < 8; ++e) sum = fmaf(h[n][e], h[n][e], sum);
     }
     sum = row_sum<kThreads>(sum, lds);
-    const float r = row_scale<kThreads>(h, sum, p.eps, (float)p.C, lds);
+    auto store_h = [&](int n) {
+        const int64_t at = 8 * (i + n * kThreads);
+        if (at < p.C) store_chunk(static_cast<T*>(p.h) + row * p.ldh, at, p.C, h[n]);
+    };
+    bool store = p.h;
+    float r;
+    if (ordinary(sum, p.eps)) {
+        r = rsqrtf(sum / (float)p.C + p.eps);
+    } else {
+        const float unusual = unusual_by(sum);
+        float s = 0.f;
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s = fmaf(h[n][e] * unusual, h[n][e] * unusual, s);
+        const RowScale scale = unusual_scale(row_sum<kThreads>(s, lds), p.eps, (float)p.C, unusual);
+        r = scale.at;
+        if (scale.by != 1.f) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                if (store) store_h(n);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) h[n][e] *= scale.by;
+            }
+            store = false;
+        }
+    }
 #pragma unroll
     for (int n = 0; n < N; ++n) {
         const int64_t at = 8 * (i + n * kThreads);
-        if (p.h && at < p.C) store_chunk(static_cast<T*>(p.h) + row * p.ldh, at, p.C, h[n]);
+        if (store) store_h(n);
         float y[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = h[n][e] * r;
@@ -214,24 +242,37 @@ __global__ __launch_bounds__(kNormGroup<kThreads>) void norm_backward_kernel(con
             r = rsqrtf(squares / (float)p.C + p.eps);
             mean = both * r / (float)p.C;
         } else {
-            const float by = unusual_by(squares);
+            const float unusual = unusual_by(squares);
             squares = both = 0.f;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 float g[8], h[8];
                 operands(n, g, h);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) squares = fmaf(h[e] * by, h[e] * by, squares);
+                for (int e = 0; e < 8; ++e) squares = fmaf(h[e] * unusual, h[e] * unusual, squares);
             }
-            r = rsqrtf(row_sum<kThreads>(squares, lds) / (float)p.C + p.eps * by * by) * by;
+            const RowScale scale = unusual_scale(row_sum<kThreads>(squares, lds), p.eps, (float)p.C, unusual);
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 float g[8], h[8];
                 operands(n, g, h);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) both = fmaf(g[e], h[e] * r, both);
+                for (int e = 0; e < 8; ++e) both = fmaf(g[e], h[e] * scale.by * scale.at, both);
             }
             mean = row_sum<kThreads>(both, lds) / (float)p.C;
+            // r (g - u mean) = at ((g by) - (h at) (mean by^2)) and dy u = (dy by) (h at): the second factor goes into dy, and below nothing is told of it
+            r = scale.at;
+            if (scale.by != 1.f) {
+                mean *= scale.by * scale.by;
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    float dy[8];
+                    to_floats(dyx[n], dy);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) dy[e] *= scale.by;
+                    dyx[n] = to_chunk<T>(dy);
+                }
+            }
         }
 #pragma unroll
         for (int n = 0; n < N; ++n) {
@@ -292,8 +333,8 @@ __global__ __launch_bounds__(1024) void norm_backward_wide_kernel(const NormBack
 #pragma unroll
             for (int e = 0; e < 8; ++e) g[e] = p.weight ? dy[e] * w[e] : dy[e];
         };
-        // the sums of (h by)^2 and of g h of
-        auto sums = [&](float by, float of, float& squares, float& both) {
+        // the sums of (h by)^2 and of g h r
+        auto sums = [&](float by, RowScale r, float& squares, float& both) {
             squares = both = 0.f;
             for (int64_t n = i; n < pieces; n += kThreads) {
                 float dy[8], g[8], h[8];
@@ -301,21 +342,23 @@ __global__ __launch_bounds__(1024) void norm_backward_wide_kernel(const NormBack
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     squares = fmaf(h[e] * by, h[e] * by, squares);
-                    both = fmaf(g[e], h[e] * of, both);
+                    both = fmaf(g[e], h[e] * r.by * r.at, both);
                 }
             }
             squares = row_sum<kThreads>(squares, lds);
             both = row_sum<kThreads>(both, lds);
         };
-        float squares, both, r, mean;
-        sums(1.f, 1.f, squares, both);
+        RowScale r{1.f, 1.f};
+        float squares, both;
+        sums(1.f, r, squares, both);
+        float mean;
         if (ordinary(squares, p.eps)) {
-            r = rsqrtf(squares / (float)p.C + p.eps);
-            mean = both * r / (float)p.C;
+            r = RowScale{rsqrtf(squares / (float)p.C + p.eps), 1.f};
+            mean = both * r.at / (float)p.C;
         } else {
             const float by = unusual_by(squares);
-            sums(by, 0.f, squares, both);
-            r = rsqrtf(squares / (float)p.C + p.eps * by * by) * by;
+            sums(by, r, squares, both);
+            r = unusual_scale(squares, p.eps, (float)p.C, by);
             sums(0.f, r, squares, both);
             mean = both / (float)p.C;
         }
@@ -325,9 +368,9 @@ __global__ __launch_bounds__(1024) void norm_backward_wide_kernel(const NormBack
             if (p.dh) to_floats(load_chunk(static_cast<const T*>(p.dh) + row * p.lddh, 8 * n, p.C), dh);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float u = h[e] * r;
+                const float u = h[e] * r.by * r.at;
                 dw[n][e] = fmaf(dy[e], u, dw[n][e]);
-                dx[e] = r * fmaf(-u, mean, g[e]);
+                dx[e] = fmaf(-u, mean, g[e]) * r.by * r.at;
                 if (p.dh) dx[e] += dh[e];
             }
             store_chunk(static_cast<T*>(p.dx) + row * p.lddx, 8 * n, p.C, dx);

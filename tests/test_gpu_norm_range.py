@@ -1,0 +1,96 @@
+"""Root-mean-square norm and its gradients on rows at both ends of fp32's range, against the 64-bit references and bounds of packed_ref.
+
+Scaling by a power of two is exact there, so the bounds are those of ordinary rows; a result below the normal range is half a subnormal step off besides."""
+import pytest
+
+import packed_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    import torch
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    from paper_2403_09195_amd import binding
+    binding.lib()
+    return binding
+
+
+def _type(name):
+    import torch
+    return {"bf16": torch.bfloat16, "fp32": torch.float32}[name]
+
+
+def _rows(seed, M, C, dtype, size=1.0):
+    """Rows of about `size`, worked out in 64 bits (a normal number times it may be subnormal)."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    return (size * torch.randn((M, C), generator=gen, device="cuda", dtype=torch.float64)).to(_type(dtype))
+
+
+def _close(got, want, tol, what):
+    over = ((got.double() - want).abs() - tol).max().item()
+    assert over <= 0, f"{what}: {over:.3e} over its bound"
+
+
+def _check(B, h, dy, w, eps):
+    """Forward and backward of rows h."""
+    import torch
+    u = ref.U[h.dtype]
+    want, _ = ref.norm(h, w, eps)
+    y, _ = B.rms_norm(h, w, eps)
+    _close(y, want, want.abs() * (u + ref.NORM_OFF), "y")
+    (want_dx, want_dw), (off, off_dw) = ref.norm_backward(dy, h, w, eps)
+    dx, dw = B.rms_norm_backward(dy, h, w, eps)
+    _close(dx, want_dx, off + u * want_dx.abs() + 2.0 ** -148, "dx")
+    _close(dw, want_dw, off_dw, "dw")
+    alone, _ = B.rms_norm_backward(torch.zeros_like(dy), h, w, eps)
+    assert (alone == 0).all(), "no gradient, none of x"
+
+
+# every form: threads and pieces of a row, and the gradients that read it again
+SIZES = [(9, 500), (5, 2500), (1030, 96), (1100, 777), (4, 4097), (2, 9000), (2, 20001)]
+
+
+@pytest.mark.parametrize("M,C", SIZES)
+@pytest.mark.parametrize("dtype,size,dy_size,eps", [
+    ("fp32", 1e-36, 1e-3, 0.0), ("fp32", 1e-39, 1e-10, 0.0), ("fp32", 1e-41, 1e-12, 0.0), ("fp32", 2e-44, 1e-15, 0.0), ("fp32", 1e-21, 1.0, 2.0 ** -140),
+    ("fp32", 4e37, 1e10, 0.0), ("fp32", 4e37, 1e10, 1e-6), ("bf16", 1e-38, 1e-9, 0.0), ("bf16", 1e-39, 1e-10, 0.0), ("bf16", 4e37, 1e10, 0.0)])
+def test_rows_at_the_ends_of_the_range(B, M, C, dtype, size, dy_size, eps):
+    """Their root mean square, or one over it, is no normal fp32 number.  (Six times 4e37 is below 2^128.)"""
+    _check(B, _rows(1, M, C, dtype, size).clamp(-3e38, 3e38), _rows(2, M, C, dtype, dy_size), _rows(3, 1, C, dtype)[0], eps)
+
+
+@pytest.mark.parametrize("C", [64, 1000, 4097, 32768])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_one_least_number_in_a_row(B, C, dtype):
+    """The smallest mean of squares there is, and zeros beside it."""
+    import torch
+    least = 2.0 ** -149 if dtype == "fp32" else 2.0 ** -133
+    h = torch.zeros((3, C), dtype=torch.float64)
+    h[0, 0], h[1, C // 2], h[2, C - 1] = least, -least, 3 * least
+    _check(B, h.to(_type(dtype)).cuda(), _rows(2, 3, C, dtype, 1e-12), _rows(3, 1, C, dtype)[0], 0.0)
+
+
+def test_eight_bits_and_the_sum_of_such_rows(B):
+    import torch
+    x, res, w = _rows(1, 7, 300, "fp32", 1e-40), _rows(2, 7, 300, "fp32", 1e-40), _rows(3, 1, 300, "fp32")[0]
+    (y, q), h = B.rms_norm(x, w, 0.0, residual=res, quantized="both")
+    want, sums = ref.norm(x, w, 0.0, res)
+    assert torch.equal(h.double(), sums)                     # (sums of subnormal numbers are exact)
+    _close(y, want, want.abs() * (ref.E + ref.NORM_OFF), "y")
+    again = B.quantize(y)
+    assert torch.equal(q.values.view(torch.uint8), again.values.view(torch.uint8)) and torch.equal(q.scales[:, :7], again.scales[:, :7])
+
+
+def test_rows_of_zeros(B):
+    """eps alone is what they are divided by; the largest and the least there is."""
+    import torch
+    for eps in (2.0 ** -149, 2.0 ** -140, 1e-30, 1e-6, 1e30):
+        h, dy = torch.zeros((4, 600), device="cuda"), torch.full((4, 600), 2.0 ** -60, device="cuda")
+        y, _ = B.rms_norm(h, None, eps)
+        dx, dw = B.rms_norm_backward(dy, h, None, eps)
+        assert (y == 0).all() and (dw == 0).all()
+        want = dy.double() / torch.tensor(eps, dtype=torch.float32).double().sqrt().item()
+        _close(dx, want, ref.NORM_OFF * want, "dx")
