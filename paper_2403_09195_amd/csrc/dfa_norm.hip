@@ -84,6 +84,9 @@ __device__ __forceinline__ float row_sum(float x, float* lds) {
 // eps is no larger: they are summed up again, scaled.
 __device__ __forceinline__ bool ordinary(float sum, float eps) { return !(sum > 1e37f) && !(sum < 1e-30f && eps < 1e-30f); }
 
+// The same of a sum of g h, which may overflow where neither they nor the result do: it is taken again with u for h.
+__device__ __forceinline__ bool ordinary_both(float sum) { return fabsf(sum) <= 1e37f; }
+
 // The scale of the second sum: a row of 32768 numbers of 2^128 does not overflow it, and one number of 2^-149 among as many zeros has a normal mean of squares.
 __device__ __forceinline__ float unusual_by(float sum) { return sum > 1.f ? 0x1p-80f : 0x1p100f; }
 
@@ -238,20 +241,26 @@ __global__ __launch_bounds__(kNormGroup<kThreads>) void norm_backward_kernel(con
         squares = row_sum<kThreads>(squares, lds);
         both = row_sum<kThreads>(both, lds);
         float r, mean;
-        if (ordinary(squares, p.eps)) {
+        if (ordinary(squares, p.eps) && ordinary_both(both)) {
             r = rsqrtf(squares / (float)p.C + p.eps);
             mean = both * r / (float)p.C;
         } else {
-            const float unusual = unusual_by(squares);
-            squares = both = 0.f;
+            RowScale scale{0.f, 1.f};
+            if (ordinary(squares, p.eps)) {
+                scale.at = rsqrtf(squares / (float)p.C + p.eps);
+            } else {
+                const float unusual = unusual_by(squares);
+                squares = 0.f;
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                float g[8], h[8];
-                operands(n, g, h);
+                for (int n = 0; n < N; ++n) {
+                    float g[8], h[8];
+                    operands(n, g, h);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) squares = fmaf(h[e] * unusual, h[e] * unusual, squares);
+                    for (int e = 0; e < 8; ++e) squares = fmaf(h[e] * unusual, h[e] * unusual, squares);
+                }
+                scale = unusual_scale(row_sum<kThreads>(squares, lds), p.eps, (float)p.C, unusual);
             }
-            const RowScale scale = unusual_scale(row_sum<kThreads>(squares, lds), p.eps, (float)p.C, unusual);
+            both = 0.f;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 float g[8], h[8];
@@ -352,13 +361,16 @@ __global__ __launch_bounds__(1024) void norm_backward_wide_kernel(const NormBack
         float squares, both;
         sums(1.f, r, squares, both);
         float mean;
-        if (ordinary(squares, p.eps)) {
-            r = RowScale{rsqrtf(squares / (float)p.C + p.eps), 1.f};
+        const bool plain = ordinary(squares, p.eps);
+        if (plain) r.at = rsqrtf(squares / (float)p.C + p.eps);
+        if (plain && ordinary_both(both)) {
             mean = both * r.at / (float)p.C;
         } else {
-            const float by = unusual_by(squares);
-            sums(by, r, squares, both);
-            r = unusual_scale(squares, p.eps, (float)p.C, by);
+            if (!plain) {
+                const float by = unusual_by(squares);
+                sums(by, r, squares, both);
+                r = unusual_scale(squares, p.eps, (float)p.C, by);
+            }
             sums(0.f, r, squares, both);
             mean = both / (float)p.C;
         }

@@ -94,3 +94,11 @@ def test_rows_of_zeros(B):
         assert (y == 0).all() and (dw == 0).all()
         want = dy.double() / torch.tensor(eps, dtype=torch.float32).double().sqrt().item()
         _close(dx, want, ref.NORM_OFF * want, "dx")
+
+
+@pytest.mark.parametrize("M,C", SIZES)
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("size,dy_size", [(1e10, 1e30), (1e17, 1e22), (1e3, 1e34)])
+def test_gradients_whose_products_with_the_row_overflow(B, M, C, dtype, size, dy_size):
+    """Rows that are summed up as they are, with gradients that fp32 holds and products that it does not."""
+    _check(B, _rows(1, M, C, dtype, size), _rows(2, M, C, dtype, dy_size), _rows(3, 1, C, dtype)[0], 1e-6)
