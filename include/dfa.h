@@ -489,7 +489,9 @@ int dfa_prompt_attention_backward(const void *q, const void *k, const void *v, d
  *                y's rounded ones); one of y and q at least.  Values up to the next multiple of 128 columns (zeros) and scale bytes up to the next multiple of 16
  *                rows are written.
  * h, y and q apart from the operands and each other (but for h as said).  Rows are exact at any size that fp32 holds, subnormal numbers included: sums of squares that
- * overflow, or fall below 1e-30 beside an eps that does, are taken again, scaled, and r, which may then be no fp32 number, is held in two factors.  C is 32768 at most.  Asynchronous on `stream`; allocates nothing.
+ * overflow, or fall below 1e-30 beside an eps that does, are taken again, scaled, and r, which may then be no fp32 number, is held in two factors.  C is 32768 at most,
+ * and M (a grid holds fewer than 2^32 threads) 2^26 - 4 up to 1024 columns, 2^24 - 1 up to 4096, 2^23 - 1 up to 16384 and 2^22 - 1 beyond.
+ * Asynchronous on `stream`; allocates nothing.
  */
 int dfa_rms_norm(const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, dfa_dtype_t weight_dt, dfa_dtype_t dt, float eps,
                  void *h, int64_t ldh, void *y, int64_t ldy, const dfa_quantized_t *q, int64_t M, int64_t C, void *stream);
@@ -501,8 +503,8 @@ int dfa_rms_norm(const void *x, int64_t ldx, const void *residual, int64_t ldr, 
  *               dx may be dy or dh itself (same pointer and pitch), else apart from the operands
  *   workspace   device, 16-byte aligned, ..._workspace_bytes(M, C) (0 = none, NULL allowed; not used without dw): partial sums of dw.  Written and read by this
  *               call only: calls that may overlap, captured ones among them, need one each.
- * Rows of h of any size, as above; g h may overflow (where it falls below 2^-126 it loses bits); a dx that fp32 does not hold is infinite or NaN.  Sums are in a fixed order: equal calls give equal results.  Asynchronous on `stream`;
- * allocates nothing.
+ * Rows of h of any size, as above, and any number of them; g h may overflow (where it falls below 2^-126 it loses bits); a dx that fp32 does not hold is
+ * infinite or NaN.  Sums are in a fixed order: equal calls give equal results.  Asynchronous on `stream`; allocates nothing.
  */
 size_t dfa_rms_norm_backward_workspace_bytes(int64_t M, int64_t C);
 int dfa_rms_norm_backward(const void *dy, int64_t lddy, const void *h, int64_t ldh, const void *weight, dfa_dtype_t weight_dt, dfa_dtype_t dt, float eps,

@@ -78,9 +78,15 @@ int64_t backward_bytes(int32_t T, int32_t H, int32_t Hkv, int32_t D, int32_t sha
     return up((int64_t)2 * H * T * 4, 256) + (shares > 1 ? (int64_t)shares * 2 * T * Hkv * D * 4 : 0);
 }
 
+constexpr int64_t kNormMaxElements = (int64_t)1 << 48;     // more than any memory holds: byte offsets stay in 64 bits
+
 int check_norm_sizes(int64_t M, int64_t C) {
     if (M < 1 || C < 1) return DFA_ERR_SHAPE;
-    return C > kNormMaxCols || !grid_fits(M, 1024) ? DFA_ERR_TOO_LARGE : DFA_OK;
+    return C > kNormMaxCols || M > kNormMaxElements / C ? DFA_ERR_TOO_LARGE : DFA_OK;
+}
+int check_norm_grid(int64_t M, int64_t C) {
+    const NormGrid grid = norm_grid(M, C);
+    return grid_fits(grid.workgroups, grid.threads) ? DFA_OK : DFA_ERR_TOO_LARGE;
 }
 int check_eps(float eps) { return std::isfinite(eps) && eps >= 0.f ? DFA_OK : DFA_ERR_SHAPE; }
 // fp32 rows take fp32 weights, bf16 rows either
@@ -153,6 +159,7 @@ int dfa_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, 
     if (!x || (!y && !q)) return DFA_ERR_NULL;
     int rc = check_norm_types(dt, weight_dt, weight);
     if (rc == DFA_OK) rc = check_norm_sizes(M, C);
+    if (rc == DFA_OK) rc = check_norm_grid(M, C);
     if (rc == DFA_OK) rc = check_eps(eps);
     if (rc != DFA_OK) return rc;
     if (ldx < C || (residual && ldr < C) || (h && ldh < C) || (y && ldy < C)) return DFA_ERR_SHAPE;

@@ -16,6 +16,12 @@ struct NormParams {
     uint8_t *values, *scales;               // may be NULL: y in blocks of 128 (dfa_scaled.h)
     int64_t ldv, lds;
 };
+// The forward's launch.  (The gradients' workgroups walk along the rows: any number of them.)
+struct NormGrid {
+    int64_t workgroups;
+    int32_t threads;                        // of each
+};
+NormGrid norm_grid(int64_t M, int64_t C);
 hipError_t launch_norm(const NormParams& p, bool f32, bool weight_f32, hipStream_t st);
 
 struct NormBackwardParams {

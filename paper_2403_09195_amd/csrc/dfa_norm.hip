@@ -466,6 +466,13 @@ hipError_t launch_any(const Params& p, NormForm f, bool f32, bool weight_f32, hi
 
 }  // namespace
 
+// (The columns that blocks of 128 add to a row do not change its threads.)
+NormGrid norm_grid(int64_t M, int64_t C) {
+    const int32_t threads = norm_form(M, C).threads;
+    const int64_t rows = threads < 256 ? 256 / threads : 1;
+    return NormGrid{M / rows + (M % rows != 0), std::max(threads, 256)};
+}
+
 hipError_t launch_norm(const NormParams& p, bool f32, bool weight_f32, hipStream_t st) {
     return launch_any(p, norm_form(p.M, p.values ? (p.C + 127) / 128 * 128 : p.C), f32, weight_f32, st);
 }

@@ -102,3 +102,26 @@ def test_rows_of_zeros(B):
 def test_gradients_whose_products_with_the_row_overflow(B, M, C, dtype, size, dy_size):
     """Rows that are summed up as they are, with gradients that fp32 holds and products that it does not."""
     _check(B, _rows(1, M, C, dtype, size), _rows(2, M, C, dtype, dy_size), _rows(3, 1, C, dtype)[0], 1e-6)
+
+
+def test_more_rows_than_a_grid_has_places_for_one_each(B):
+    """The norm of the heads of 131072 tokens and a few: forward and dx as of parts of the rows, dw against 64 bits."""
+    import torch
+    M, C, cut = 2 ** 22 + 5, 64, 1 << 21
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x, dy = (torch.randn((M, C), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    w = torch.randn((C,), generator=gen, device="cuda").bfloat16()
+    (y, q), _ = B.rms_norm(x, w, 1e-6, quantized="both")
+    dx, dw = B.rms_norm_backward(dy, x, w, 1e-6)
+    for rows in (slice(0, cut), slice(cut, 2 * cut), slice(M - 40, M)):
+        (y1, q1), _ = B.rms_norm(x[rows], w, 1e-6, quantized="both")
+        n = y1.shape[0]
+        assert torch.equal(y[rows], y1) and torch.equal(q.values[rows].view(torch.uint8), q1.values.view(torch.uint8)) and torch.equal(q.scales[:, rows], q1.scales[:, :n])
+        assert torch.equal(dx[rows], B.rms_norm_backward(dy[rows], x[rows], w, 1e-6, want_dw=False)[0])
+    last = slice(M - 300, M)
+    want, _ = ref.norm(x[last], w, 1e-6)
+    _close(y[last], want, want.abs() * (2.0 ** -8 + ref.NORM_OFF), "y")
+    # the workgroups that are resident take 4096 rows at once at least: 1025 of a column are added up one after the other, then three, and sixteen of the parts and eight
+    u = x.double() / torch.sqrt(x.double().square().mean(1, keepdim=True) + 1e-6)
+    products = dy.double() * u
+    _close(dw, products.sum(0), (1025 + 3 + 16 + 8 + 2) * ref.E * products.abs().sum(0) + ref.NORM_OFF * products.abs().sum(0), "dw")
