@@ -454,6 +454,7 @@ int dfa_release_plans(void);
  * bf16: probabilities are rounded to bf16 before they meet v; sums are fp32.  fp32: products of three bf16 parts a number (24 bits; bits
  * below 2^-133 are lost, and what rounds to 2^128 in bf16 counts as infinite).  scale lies within 2^-100 .. 2^100, and every scale * q . k
  * within 2^127 ln 2 either way.  Keys and values that are not finite reach only the rows that attend to them (an infinite fp32 value may come out as NaN there).
+ * (T / 32 + B + 1) H lies below 2^24: a grid holds fewer than 2^32 threads.
  * Sums are in a fixed order: equal calls give equal results.  Asynchronous on `stream`; allocates nothing.
  */
 int dfa_prompt_attention(const void *q, const void *k, const void *v, dfa_strides_t sq, dfa_strides_t sk, dfa_strides_t sv, dfa_dtype_t dt, int32_t T,

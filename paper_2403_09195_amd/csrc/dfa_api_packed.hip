@@ -139,7 +139,8 @@ int dfa_prompt_attention_backward(const void* q, const void* k, const void* v, d
     PromptParams p;
     int rc = prompt_params(q, k, v, sq, sk, sv, dt, T, H, Hkv, D, starts, B, causal, scale, &p);
     if (rc != DFA_OK) return rc;
-    if ((int64_t)H * D * size_of(dt) >= kMaxRowBytes || !grid_fits((int64_t)T * Hkv * D / 512 + 1, 256)) return DFA_ERR_TOO_LARGE;
+    // (the launches along all elements are made only where the tiles are few: their grids fit)
+    if ((int64_t)H * D * size_of(dt) >= kMaxRowBytes) return DFA_ERR_TOO_LARGE;
     for (const void* x : {out, dout, static_cast<const void*>(dq), static_cast<const void*>(dk), static_cast<const void*>(dv), static_cast<const void*>(workspace)})
         if (!aligned(x, 16)) return DFA_ERR_ALIGN;
     if (!aligned(lse, 4)) return DFA_ERR_ALIGN;
