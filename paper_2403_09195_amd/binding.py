@@ -1150,8 +1150,12 @@ def rms_norm(x, weight, eps, residual=None, quantized=False, h=None):
     """(y, h) with h = x + residual (None without a residual) and y = h * rsqrt(mean(h^2) + eps) * weight over the last dimension, in fp32 up to one rounding each.
     x [..., C] bf16 or fp32; weight [C] (fp32 for fp32 rows, either for bf16; None: ones).  quantized: y is a QuantizedMatrix of its rows in blocks of 1 x 128,
     what quantized_product takes; "both": y is (y, QuantizedMatrix).  h: a tensor for the sum, which may be x or residual itself."""
+    both = isinstance(quantized, str)
+    if both and quantized != "both":
+        raise ValueError(f'quantized must be true, false or "both", not "{quantized}"')
+    plain, quantized = both or not quantized, bool(quantized)
     if h is None:
-        res = _native_call("rms_norm", x, weight, eps, residual, quantized is not True, bool(quantized))
+        res = _native_call("rms_norm", x, weight, eps, residual, plain, quantized)
         if res is not None:
             y, h, values, scales = res
             if values is not None:
@@ -1163,14 +1167,14 @@ def rms_norm(x, weight, eps, residual=None, quantized=False, h=None):
     dev = _device(*given)
     if _elsewhere(dev):
         with torch.cuda.device(dev):
-            return rms_norm(x, weight, eps, residual, quantized, h)
+            return rms_norm(x, weight, eps, residual, "both" if both else quantized, h)
     _same_shape(x, ("residual", residual), ("h", h))
     code, (M, ldx), C = _dtype_code(x), _rows_of(x, "x"), x.shape[-1]
     w, w_code = _norm_weight(weight, C, code)
     ldr = _rows_of(residual, "residual")[1] if residual is not None else 0
     if h is None and residual is not None:
         h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    y = None if quantized is True else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if plain else None
     q = _empty_quantized(M, C, x) if quantized else None
     _check(lib().dfa_rms_norm(x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr, w, w_code, code, eps, None if h is None else h.data_ptr(),
                               0 if h is None else _rows_of(h, "h")[1], None if y is None else y.data_ptr(), C, ctypes.byref(_quantized(q, "q")) if q else None,

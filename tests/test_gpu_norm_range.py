@@ -125,3 +125,19 @@ def test_more_rows_than_a_grid_has_places_for_one_each(B):
     u = x.double() / torch.sqrt(x.double().square().mean(1, keepdim=True) + 1e-6)
     products = dy.double() * u
     _close(dw, products.sum(0), (1025 + 3 + 16 + 8 + 2) * ref.E * products.abs().sum(0) + ref.NORM_OFF * products.abs().sum(0), "dw")
+
+
+@pytest.mark.parametrize("given", [None, "h"])
+def test_whatever_counts_as_true(B, given):
+    """quantized=1 and numpy's True are True: y in 8 bits alone, in native code and in Python."""
+    import numpy as np
+    import torch
+    x = _rows(1, 5, 200, "bf16")
+    h = None if given is None else torch.empty_like(x)
+    want, _ = B.rms_norm(x, None, 1e-6, quantized=True, h=h)
+    for yes in (1, np.True_, torch.tensor(True)):
+        q, _ = B.rms_norm(x, None, 1e-6, quantized=yes, h=h)
+        assert isinstance(q, B.QuantizedMatrix) and torch.equal(q.values.view(torch.uint8), want.values.view(torch.uint8))
+    for no in (0, np.False_, None):
+        y, _ = B.rms_norm(x, None, 1e-6, quantized=no, h=h)
+        assert isinstance(y, torch.Tensor)

@@ -34,3 +34,12 @@ def test_rows_of_its_gradients(B, C):
     for M in (2 ** 22 - 1, 2 ** 22, 2 ** 26, 2 ** 31 + 1):
         assert rc(M) == -5 and size(M, C) == size(2 ** 21, C) > 0
     assert rc(2 ** 48 // C + 1) == rc(2 ** 63 - 1) == -7 and size(2 ** 48 // C + 1, C) == size(2 ** 63 - 1, C) == 0
+
+
+def test_what_quantized_may_be(B):
+    """A word other than "both" is no answer to whether y is wanted in 8 bits."""
+    import torch
+    x = torch.zeros((2, 64))
+    for word in ("yes", "true", "BOTH", ""):
+        with pytest.raises(ValueError, match="quantized"):
+            B.rms_norm(x, None, 1e-6, quantized=word)
