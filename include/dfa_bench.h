@@ -101,6 +101,14 @@ int dfa_cache_attention_describe(int32_t B, int32_t M, int32_t H, int32_t heads,
                                  dfa_cache_attention_form_t *form);
 
 /*
+ * The same of dfa_prompt_attention: tiles of `rows` rows, whose walk along the keys `groups` groups of waves share out.
+ */
+typedef struct {
+    int32_t rows, groups;
+} dfa_prompt_attention_form_t;
+int dfa_prompt_attention_describe(int32_t T, int32_t H, int32_t Hkv, int32_t D, dfa_dtype_t dt, int32_t B, int32_t causal, dfa_prompt_attention_form_t *form);
+
+/*
  * Measurement aid (no part of the operator): what the matrix cores sustain on their own, the
  * ceiling that the kernels' MFMA rooflines are also quoted against.  Runs a loop of
  * independent v_mfma_f32_32x32x16_bf16 on the whole chip (two waves per SIMD, no memory

@@ -30,7 +30,7 @@ EXPORTS = [
     "dfa_rms_norm", "dfa_rms_norm_backward", "dfa_rms_norm_backward_workspace_bytes", "dfa_cache_reserve", "dfa_cache_release", "dfa_cache_append_packed",
 ]
 BENCH_EXPORTS = ["dfa_launch_describe", "dfa_launch_image", "dfa_forward_timed", "dfa_mfma_peak", "dfa_dense_unfused", "dfa_dense_unfused_workspace_bytes",
-                 "dfa_quantized_describe", "dfa_cache_attention_describe"]
+                 "dfa_quantized_describe", "dfa_cache_attention_describe", "dfa_prompt_attention_describe"]
 
 
 class Branch(ctypes.Structure):
@@ -61,6 +61,10 @@ class QuantizedForm(ctypes.Structure):
 
 class CacheAttentionForm(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("tile_rows", "row_tiles", "splits", "split_tokens")]
+
+
+class PromptAttentionForm(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "groups")]
 
 
 class Launch(ctypes.Structure):
@@ -151,6 +155,7 @@ def lib():
         L.dfa_cache_attention.argtypes = [vp, Strides, ctypes.c_int, i32, i32, i32, Cache, vp, i32, i64, vp, vp, i32, f32, i64, vp, vp, vp, st, vp]
         L.dfa_quantized_describe.argtypes = [i32, ctypes.c_int, i64, i64, i64, ctypes.POINTER(QuantizedForm)]
         L.dfa_cache_attention_describe.argtypes = [i32, i32, i32, i32, i32, ctypes.c_int, i64, ctypes.POINTER(CacheAttentionForm)]
+        L.dfa_prompt_attention_describe.argtypes = [i32, i32, i32, i32, ctypes.c_int, i32, i32, ctypes.POINTER(PromptAttentionForm)]
         L.dfa_prompt_attention.argtypes = [vp, vp, vp, Strides, Strides, Strides, ctypes.c_int, i32, i32, i32, i32, vp, i32, i32, f32, vp, vp, vp]
         L.dfa_prompt_attention_backward_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
         L.dfa_prompt_attention_backward.argtypes = [vp, vp, vp, Strides, Strides, Strides, vp, vp, vp, ctypes.c_int, i32, i32, i32, i32, vp, i32, i32, f32,
@@ -957,6 +962,13 @@ def describe_cache_attention(B, M, H, heads, D, dtype_code, max_length):
     """CacheAttentionForm that a call of this size takes (no GPU needed)."""
     form = CacheAttentionForm()
     _check(lib().dfa_cache_attention_describe(B, M, H, heads, D, dtype_code, max_length, ctypes.byref(form)), "dfa_cache_attention_describe")
+    return form
+
+
+def describe_prompt_attention(T, H, Hkv, D, dtype_code, B, causal=True):
+    """Form that dfa_prompt_attention takes for these sizes (include/dfa_bench.h): .rows of a tile, .groups of waves that share its walk out."""
+    form = PromptAttentionForm()
+    _check(lib().dfa_prompt_attention_describe(T, H, Hkv, D, dtype_code, B, int(bool(causal)), ctypes.byref(form)), "dfa_prompt_attention_describe")
     return form
 
 

@@ -6,6 +6,7 @@
 #include <new>
 
 #include "../../include/dfa.h"
+#include "../../include/dfa_bench.h"
 #include "dfa_cache.h"
 #include "dfa_norm.h"
 #include "dfa_prompt.h"
@@ -255,6 +256,18 @@ int dfa_cache_append_packed(const void* k, const void* v, dfa_strides_t sk, dfa_
                         table, ld_table, width, lengths, nullptr};
     p.B = B, p.T = T, p.page_blocks = (int32_t)blocks, p.starts = starts;
     return status(launch_cache_append(p, dt == DFA_F32, cache.D, static_cast<hipStream_t>(stream)));
+}
+
+// ---- which form a call takes (dfa_bench.h) ----
+
+int dfa_prompt_attention_describe(int32_t T, int32_t H, int32_t Hkv, int32_t D, dfa_dtype_t dt, int32_t B, int32_t causal, dfa_prompt_attention_form_t* form) {
+    if (!form) return DFA_ERR_NULL;
+    if (!known(dt)) return DFA_ERR_DTYPE;
+    const int rc = check_prompt_sizes(T, H, Hkv, D, B);
+    if (rc != DFA_OK) return rc;
+    const PromptForm f = prompt_fwd_form(T, B, H, D, dt == DFA_F32, causal != 0, chip_or_default());
+    *form = dfa_prompt_attention_form_t{f.rows, f.groups};
+    return DFA_OK;
 }
 
 }  // extern "C"

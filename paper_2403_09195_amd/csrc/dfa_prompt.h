@@ -25,6 +25,12 @@ struct PromptParams {
     float* parts;                           // [shares][2][T][Hkv][D] workspace: dk and dv of a share of the group's heads
     int32_t shares;
 };
+// A forward launch: rows of a tile, and groups of waves that share a tile's walk out.
+struct PromptForm {
+    int32_t rows, groups;
+};
+PromptForm prompt_fwd_form(int32_t T, int32_t B, int32_t H, int32_t D, bool f32, bool causal, const ChipShape& chip);
+PromptForm prompt_fwd_form_f32(int32_t T, int32_t B, int32_t H, int32_t D, const ChipShape& chip);
 hipError_t launch_prompt_fwd(const PromptParams& p, bool f32, int32_t D, const ChipShape& chip, hipStream_t st);
 // Workgroups that share the query heads of a key head out in the launch of dk and dv.
 int32_t prompt_bwd_shares(int32_t T, int32_t B, int32_t H, int32_t Hkv, const ChipShape& chip);

@@ -565,17 +565,21 @@ void launch_both(const PromptParams& p, hipStream_t st) {
 // Forms by what is known of the lengths, their mean, and by how many workgroups there are.
 namespace {
 // Workgroups of R-row tiles, about.
-int64_t tiles(const PromptParams& p, int32_t R, int32_t heads) { return std::max<int64_t>((p.T + R - 1) / R, std::min(p.T, p.B)) * heads; }
+int64_t tiles(int32_t T, int32_t B, int32_t R, int32_t heads) { return std::max<int64_t>(((int64_t)T + R - 1) / R, std::min(T, B)) * heads; }
+int64_t tiles(const PromptParams& p, int32_t R, int32_t heads) { return tiles(p.T, p.B, R, heads); }
 }  // namespace
 
 // Large launches: 128 rows, one walk.  Others, 64 rows: four groups of waves to a walk (two of D = 128) where a workgroup has its compute unit to itself; two groups of D = 64, two workgroups
 // to a compute unit, where there are more than that holds at once, and one's products fill the time in which the other splits its operands (12 heads of 64, us with four groups / two:
 // forward 1 x 1000 34.3 / 43.8, 4 x 512 27.6 / 27.5, 8 x 512 48.2 / 39.3, 1 x 4000 232 / 214, 64 x <= 60 28.4 / 17.7).
+PromptForm prompt_fwd_form_f32(int32_t T, int32_t B, int32_t H, int32_t D, const ChipShape& chip) {
+    if (!prompt_small(T, B, H, chip)) return PromptForm{128, 1};
+    return PromptForm{64, D == 128 || tiles(T, B, 64, H) > 2 * chip.cus ? 2 : 4};
+}
 hipError_t launch_prompt_fwd_f32(const PromptParams& p, int32_t D, const ChipShape& chip, hipStream_t st) {
-    const bool small = prompt_small(p.T, p.B, p.H, chip);
-    if (D == 128) return small ? launch_fwd<128, 2, 2, false, 1>(p, st) : launch_fwd<128, 4, 1, true, 1>(p, st);
-    if (!small) return launch_fwd<64, 4, 1, true, 2>(p, st);
-    return tiles(p, 64, p.H) > 2 * chip.cus ? launch_fwd<64, 2, 2, false, 2>(p, st) : launch_fwd<64, 2, 4, false, 2>(p, st);
+    const PromptForm form = prompt_fwd_form_f32(p.T, p.B, p.H, D, chip);
+    if (D == 128) return form.groups == 2 ? launch_fwd<128, 2, 2, false, 1>(p, st) : launch_fwd<128, 4, 1, true, 1>(p, st);
+    return form.groups == 1 ? launch_fwd<64, 4, 1, true, 2>(p, st) : form.groups == 2 ? launch_fwd<64, 2, 2, false, 2>(p, st) : launch_fwd<64, 2, 4, false, 2>(p, st);
 }
 
 // As the forward's, by the workgroups of both parts; small launches work them side by side (us of the whole call, one launch after the other / side by side: 12 heads of 64, 1 x 77 tokens 23 / 15,

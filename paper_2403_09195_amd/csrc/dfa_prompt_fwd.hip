@@ -415,19 +415,29 @@ hipError_t launch(const PromptParams& p, hipStream_t st) {
 
 }  // namespace
 
-hipError_t launch_prompt_fwd(const PromptParams& p, bool f32, int32_t D, const ChipShape& chip, hipStream_t st) {
-    if (f32) return launch_prompt_fwd_f32(p, D, chip, st);
+PromptForm prompt_fwd_form(int32_t T, int32_t B, int32_t H, int32_t D, bool f32, bool causal, const ChipShape& chip) {
+    if (f32) return prompt_fwd_form_f32(T, B, H, D, chip);
     // What is known of the lengths is their mean.  Two groups of waves to a walk where the workgroups of half the rows are resident at once (two to a compute unit, one of
-    // D = 128), or where walks are so long that half as many more do (us with one group / two: 12 heads of 64, 1000 tokens 19.0 / 14.1, 2 x 2000 33.7 / 29.2, 3000 45 / 33, 4 x 512 12.3 / 11.6,
-    // 8 x 512 14.6 / 19.2, 32 heads, 2000 tokens 36.5 / 40.1; 16 heads of 128, 300 tokens 10.9 / 11.3, 1000 24.0 / 19.2, 2000 42.2 / 39.2, 4000 88 / 123).
-    const int64_t mean = p.T / p.B, halves = std::max<int64_t>((p.T + 63) / 64, std::min(p.T, p.B)) * p.H, resident = (D == 64 ? 2 : 1) * (int64_t)chip.cus;
-    if (mean >= 384 && (halves <= resident || (mean >= 1536 && 2 * halves <= 3 * resident))) return D == 64 ? launch<64, 1, 2>(p, st) : launch<128, 1, 2>(p, st);
-    if (D == 128) return launch<128, 1, 1>(p, st);
+    // D = 128: us with one group / two, 16 heads of 128, 300 tokens 10.9 / 11.3, 1000 24.1 / 19.6; 12 heads of 64, 1000 tokens 18.6 / 13.9, 4 x 512 12.3 / 11.6, 8 x 512 14.6 / 19.2).  Beyond
+    // that where walks are long and causal: longest first, the workgroups of a second round are the short ones.  D = 128, two rounds (16 heads, 2000 tokens 42.1 / 39.1, 2500 52.7 / 61.5,
+    // 4000 88 / 123; 8 heads, 4000 75.5 / 63.8, not causal 79.3 / 108; 32 heads, 1000 24.9 / 27.6); of 64, one and a half (12 heads, 4000 tokens 59.1 / 43.8, 2 x 2000 32.8 / 28.5, not
+    // causal 41.8 / 45.9; two rounds: 16 heads, 4000 59.7 / 57.8, 32 heads, 2000 33.4 / 35.2).
+    const int64_t mean = T / B, halves = std::max<int64_t>((T + 63) / 64, std::min(T, B)) * H, resident = (D == 64 ? 2 : 1) * (int64_t)chip.cus;
+    const int64_t most = causal && mean >= 1536 ? (D == 64 ? resident * 3 / 2 : resident * 2) : resident;
+    if (mean >= 384 && halves <= most) return PromptForm{64, 2};
+    if (D == 128) return PromptForm{128, 1};
     // 64 rows to a wave (a fragment read feeds two products, but two waves to a SIMD) where that leaves enough workgroups, and walks are long enough for the products to decide
     // (us with 32 rows / 64: 8 x 512 tokens, 12 heads 14.4 / 23.1, 32 x 512 36.1 / 40.1, 24 of up to 2048, 32 heads 260 / 263, 8 x 4096, 12 heads 254 / 251, not causal 432 / 392, 16384 tokens, 32 heads
     // 1107 / 1023).
-    const bool enough = ((int64_t)p.T / 128 + std::min(p.T, p.B)) * p.H >= 4 * chip.cus;
-    return enough && (p.causal ? mean / 2 : mean) >= 1024 ? launch<64, 2, 1>(p, st) : launch<64, 1, 1>(p, st);
+    const bool enough = ((int64_t)T / 128 + std::min(T, B)) * H >= 4 * chip.cus;
+    return PromptForm{enough && (causal ? mean / 2 : mean) >= 1024 ? 256 : 128, 1};
+}
+
+hipError_t launch_prompt_fwd(const PromptParams& p, bool f32, int32_t D, const ChipShape& chip, hipStream_t st) {
+    if (f32) return launch_prompt_fwd_f32(p, D, chip, st);
+    const PromptForm form = prompt_fwd_form(p.T, p.B, p.H, D, false, p.causal, chip);
+    if (D == 128) return form.groups == 2 ? launch<128, 1, 2>(p, st) : launch<128, 1, 1>(p, st);
+    return form.groups == 2 ? launch<64, 1, 2>(p, st) : form.rows == 256 ? launch<64, 2, 1>(p, st) : launch<64, 1, 1>(p, st);
 }
 
 }  // namespace dfa
