@@ -604,7 +604,7 @@ hipError_t launch_prompt_bwd_f32(const PromptParams& p, int32_t D, const ChipSha
             launch_dkdv<Form<128, 4, 1, true>, 1>(p, st);
         }
     } else if (small) {
-        if (2 * tiles(p, 32, units) <= 3 * chip.cus) launch_both<Short, 1>(p, st);
+        if (2 * tiles(p, 32, units) <= 3 * chip.cus) launch_both<Short, 2>(p, st);
         else if (tiles(p, 64, units) > 2 * chip.cus) launch_both<Pairs, 2>(p, st);
         else launch_both<Fours, 2>(p, st);
     } else {

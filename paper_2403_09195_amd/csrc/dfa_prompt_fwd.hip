@@ -180,8 +180,8 @@ template <int QB> constexpr int kValueRing = 4 * QB;
 
 // KG: groups of waves that take every KG-th block of 32 keys (a "block" of the walk is KG of them then) and merge their results at the end.  For launches of
 // fewer workgroups than fit the chip, where the longest walk decides: half the rows, half the walk (1000 tokens, 16 heads of 128: 19.2 us, 24.0 with KG = 1).
-// Waves of a SIMD: 32 rows of D = 64 leave room for three (16 x 512 tokens, 12 heads: 22.6 us, 26.1 with two); two groups of D = 128 have LDS for one.
-template <int D, int QB, int KG> constexpr int kWaves = D == 64 && QB == 1 && KG == 1 ? 3 : D == 128 && KG == 2 ? 1 : 2;
+// Waves of a SIMD: 32 rows of D = 64 leave room for three (16 x 512 tokens, 12 heads: 22.6 us, 26.1 with two).
+template <int D, int QB, int KG> constexpr int kWaves = D == 64 && QB == 1 && KG == 1 ? 3 : 2;
 template <int D, int QB, int KG>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kWaves<D, QB, KG>, kWaves<D, QB, KG>))) void prompt_fwd_kernel(const PromptParams p, int32_t slots) {
     constexpr int kRowGroups = 4 / KG, R = 32 * QB * kRowGroups, kBlock = 32 * D;    // rows; elements of 32 keys or values
