@@ -1076,7 +1076,8 @@ def _cache_append_packed(k, v, cache, table, lengths, counts, starts):
 
 class Reserved(NamedTuple):
     """What cache_reserve leaves of a step: int32 lengths [B] and n_free [1] after it; starts [B + 1] of its packed rows; slots int64 [rows] (page * page size +
-    place in the page) and positions int32 [rows] of every row, -1 behind the last; refused int32 [1], 0 where the step fits (include/dfa.h)."""
+    place in the page) and positions int32 [rows] of every row, -1 behind the last; refused int32 [1], 0 where the step fits (include/dfa.h).
+    All of one allocation: whoever keeps one of them for long keeps 12 bytes a row with it (clone() it then)."""
     lengths: "torch.Tensor"
     n_free: "torch.Tensor"
     starts: "torch.Tensor"

@@ -4,8 +4,10 @@
 //   g = dy w,  u = h r,  dx = r (g - u mean(g u)) + dh,  dw = sum over the rows of dy u
 // In fp32 from the operands to the one rounding of each result: y comes of h before it is rounded.
 //
-// Bound: memory (16384 x 4096 with the residual to 8 bits 81.6 us, 5.8 TB/s; gradients of 32768 x 768 34.3 us, 5.9 TB/s, and 4.3 for the sum of dw); every operand is read once and every result written once.  A row is held in registers by kThreads threads, pieces of
-// eight elements kThreads pieces apart, so that every wave-wide load is of whole lines and a block of 128 elements is 16 neighbouring lanes'.
+// Bound: memory (16384 x 4096 with the residual to 8 bits 81.6 us, 5.8 TB/s; gradients of 32768 x 768 34.3 us, 5.9 TB/s, and 4.3 for the sum of dw); every operand is read once and every
+// result written once.  A row is held in registers by kThreads threads, pieces of eight elements kThreads pieces apart, so that every wave-wide load is of whole lines and a block of 128
+// elements is 16 neighbouring lanes'.  Rows of 64 and 128 columns leave most of their wave's lanes without data: a million rows of 128 282 us (1.8 TB/s), gradients 427 (1.8); 262144 of 64
+// 63 (1.1), gradients 97 (1.0).
 #include <algorithm>
 
 #include "dfa_norm.h"

@@ -3,7 +3,9 @@
 // Products as in dfa_mfma_f32.h: a number is the sum of three bf16 parts, six of the nine partial products are taken, at six times a bf16
 // product's time.  The walked rows are split once, by the workgroup, on their way into LDS, where the three parts of a block lie as
 // blocks of the bf16 kernels (dfa_prompt.h): 32 rows go memory -> registers a block ahead, and registers -> LDS, split, while the other of
-// two buffers is being read.  Bound: six products for one at long walks (24 sequences of up to 2048 tokens, 12 heads of 64: 466 us), splitting and barriers at short ones.  The softmax weights are split in registers.  Small launches of the backward work dq and dk and dv side by side, behind one that leaves the rows' delta.
+// two buffers is being read.  Bound: six products for one, and beside them the splitting of every tile's walked rows and a barrier a step (24 sequences of up to 2048 tokens, 12 heads of
+// 64: 466 us, 64 % of what the products alone take); at short walks these and the start.  The softmax weights are split in registers.  Small launches of the backward work dq and dk and dv
+// side by side, behind one that leaves the rows' delta.
 #include <algorithm>
 
 #include "dfa_mfma_f32.h"

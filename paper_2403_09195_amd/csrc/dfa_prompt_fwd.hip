@@ -7,6 +7,8 @@
 // sequence's keys in blocks of 32, which go global -> LDS several stages ahead (global_load_lds).  Per block S^T = K Q^T and O^T +=
 // V^T P^T on v_mfma_f32_32x32x16_bf16; the registers of S^T, rounded, are the operand P^T as they stand.  Work is in beats: the
 // products of the next block's scores and of the block before, and between them, slot by slot, the exponentials of the block in hand.
+// P in bf16 is what the products take: error against 64 bits 0.0020 of the result, 0.0015 with P in 32 bits (the rounding of the result alone), where a second part of
+// P would be half as many products again.  The row's sum is of the numerators before they are rounded.
 //
 // Bound: the power limit and a fragment from LDS for every product where walks are long (16384 tokens, 32 heads of 128 in 8: 1.91-2.00 ms, 1.10-1.15 PFLOP/s; on zeros 1.41 ms), the ends of workgroups where they
 // are short (24 prompts of up to 2048 tokens: 445-471 us).  32 rows a wave of D = 128: 64 take 512 registers, one wave to a SIMD, and 2.25 ms instead of 1.99.
@@ -179,8 +181,9 @@ constexpr int kRing = 4;
 template <int QB> constexpr int kValueRing = 4 * QB;
 
 // KG: groups of waves that take every KG-th block of 32 keys (a "block" of the walk is KG of them then) and merge their results at the end.  For launches of
-// fewer workgroups than fit the chip, where the longest walk decides: half the rows, half the walk (1000 tokens, 16 heads of 128: 19.2 us, 24.0 with KG = 1).
-// Waves of a SIMD: 32 rows of D = 64 leave room for three (16 x 512 tokens, 12 heads: 22.6 us, 26.1 with two).
+// fewer workgroups than fit the chip, where the longest walk decides: half the rows, half the walk (1000 tokens, 16 heads of 128: 19.3 us, 24.1 with KG = 1).
+// Waves of a SIMD: 32 rows of D = 64 leave room for three (16 x 512 tokens, 12 heads: 22.6 us, 26.1 with two).  (Two groups of D = 128 have LDS for one; told so, the
+// compiler is 1 % slower: 2000 tokens, 16 heads 39.1 us, 38.8 this way.)
 template <int D, int QB, int KG> constexpr int kWaves = D == 64 && QB == 1 && KG == 1 ? 3 : 2;
 template <int D, int QB, int KG>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kWaves<D, QB, KG>, kWaves<D, QB, KG>))) void prompt_fwd_kernel(const PromptParams p, int32_t slots) {
@@ -419,7 +422,7 @@ PromptForm prompt_fwd_form(int32_t T, int32_t B, int32_t H, int32_t D, bool f32,
     if (f32) return prompt_fwd_form_f32(T, B, H, D, chip);
     // What is known of the lengths is their mean.  Two groups of waves to a walk where the workgroups of half the rows are resident at once (two to a compute unit, one of
     // D = 128: us with one group / two, 16 heads of 128, 300 tokens 10.9 / 11.3, 1000 24.1 / 19.6; 12 heads of 64, 1000 tokens 18.6 / 13.9, 4 x 512 12.3 / 11.6, 8 x 512 14.6 / 19.2).  Beyond
-    // that where walks are long and causal: longest first, the workgroups of a second round are the short ones.  D = 128, two rounds (16 heads, 2000 tokens 42.1 / 39.1, 2500 52.7 / 61.5,
+    // that where walks are long and causal: longest first, the workgroups of a second round are the short ones.  D = 128, two rounds (16 heads, 2000 tokens 42.1 / 38.8, 2500 52.7 / 61.5,
     // 4000 88 / 123; 8 heads, 4000 75.5 / 63.8, not causal 79.3 / 108; 32 heads, 1000 24.9 / 27.6); of 64, one and a half (12 heads, 4000 tokens 59.1 / 43.8, 2 x 2000 32.8 / 28.5, not
     // causal 41.8 / 45.9; two rounds: 16 heads, 4000 59.7 / 57.8, 32 heads, 2000 33.4 / 35.2).
     const int64_t mean = T / B, halves = std::max<int64_t>((T + 63) / 64, std::min(T, B)) * H, resident = (D == 64 ? 2 : 1) * (int64_t)chip.cus;
