@@ -505,7 +505,7 @@ int dfa_rms_norm(const void *x, int64_t ldx, const void *residual, int64_t ldr, 
  *   workspace   device, 16-byte aligned, ..._workspace_bytes(M, C) (0 = none, NULL allowed; not used without dw): partial sums of dw.  Written and read by this
  *               call only: calls that may overlap, captured ones among them, need one each.
  * Rows of h of any size, as above, and any number of them; g h may overflow (where it falls below 2^-126 it loses bits); a dx that fp32 does not hold is
- * infinite or NaN.  Sums are in a fixed order: equal calls give equal results.  Asynchronous on `stream`; allocates nothing.
+ * infinite or NaN, and may leave dw so.  Sums are in a fixed order: equal calls give equal results.  Asynchronous on `stream`; allocates nothing.
  */
 size_t dfa_rms_norm_backward_workspace_bytes(int64_t M, int64_t C);
 int dfa_rms_norm_backward(const void *dy, int64_t lddy, const void *h, int64_t ldh, const void *weight, dfa_dtype_t weight_dt, dfa_dtype_t dt, float eps,

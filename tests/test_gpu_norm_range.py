@@ -141,3 +141,19 @@ def test_whatever_counts_as_true(B, given):
     for no in (0, np.False_, None):
         y, _ = B.rms_norm(x, None, 1e-6, quantized=no, h=h)
         assert isinstance(y, torch.Tensor)
+
+
+@pytest.mark.parametrize("C", [96, 500, 4097, 20001])
+def test_sums_of_such_rows_in_place(B, C):
+    """h over x or over the residual, among ordinary rows; what is stored is the sum itself, not what it was scaled to."""
+    import torch
+    x, res = _rows(1, 6, C, "fp32"), _rows(2, 6, C, "fp32")
+    for row, size in ((1, 2.0 ** -135), (2, 2.0 ** 120), (4, 2.0 ** -145), (5, 2.0 ** 124)):
+        x[row], res[row] = _rows(10 + row, 1, C, "fp32", size)[0], _rows(20 + row, 1, C, "fp32", size)[0]
+    want, _ = ref.norm(x, None, 0.0, res)
+    sums = x + res
+    for place in (None, 0, 1):
+        a, b = x.clone(), res.clone()
+        y, h = B.rms_norm(a, None, 0.0, residual=b, h=None if place is None else (a, b)[place])
+        assert torch.equal(h, sums)
+        _close(y, want, want.abs() * (2 * ref.E + ref.NORM_OFF), "y")         # (the sum's rounding and y's)
